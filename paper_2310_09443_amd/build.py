@@ -1,13 +1,15 @@
 """Builds the HIP library for gfx950 into paper_2310_09443_amd/libg10.so."""
 import os
 import subprocess
-import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = [os.path.join(HERE, "csrc", f) for f in ("g10_api.hip", "g10_mem.hip", "g10_vitality.hip", "g10_plan.hip", "g10_loop.hip", "g10_prefetch.hip", "g10_replay.hip")]
-DEPS = SRC + [os.path.join(HERE, "csrc", "g10_internal.h"), os.path.join(HERE, "csrc", "g10_plan_defs.h"),
-              os.path.join(ROOT, "include", "g10.h")]
+SRC = [os.path.join(HERE, "csrc", f) for f in ("g10_api.hip", "g10_mem.hip", "g10_vitality.hip", "g10_plan.hip", "g10_loop.hip", "g10_prefetch.hip", "g10_replay.hip",
+                                               "g10_rope.hip", "g10_attn.hip", "g10_attn_back.hip", "g10_adamw.hip")]
+DEPS = SRC + [os.path.join(HERE, "csrc", "g10_internal.h"), os.path.join(HERE, "csrc", "g10_plan_defs.h"), os.path.join(HERE, "csrc", "g10_attn.h"),
+              os.path.join(ROOT, "include", "g10.h"), os.path.join(ROOT, "include", "g10_ops.h")]
 LIB = os.path.join(HERE, "libg10.so")
 
 
@@ -18,11 +20,13 @@ def up_to_date() -> bool:
 def build(force: bool = True) -> str:
     if not force and up_to_date():
         return LIB
-    cmd = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"),
-           "-Wall", "-Wno-unused-function"] + SRC + ["-o", LIB]
-    subprocess.run(cmd, check=True)
+    flags = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc"), "-Wall", "-Wno-unused-function"]
+    with tempfile.TemporaryDirectory() as tmp:                       # one compiler a source, side by side
+        objs = [os.path.join(tmp, os.path.basename(f) + ".o") for f in SRC]
+        with ThreadPoolExecutor(max_workers=4) as ex:
+            list(ex.map(lambda so: subprocess.run(["hipcc"] + flags + ["-c", so[0], "-o", so[1]], check=True), zip(SRC, objs)))
+        subprocess.run(["hipcc", "--offload-arch=gfx950", "-fPIC", "-shared"] + objs + ["-o", LIB], check=True)
     return LIB
 
 

@@ -1,0 +1,285 @@
+// What the attention kernels share: which keys a query sees, tiles of keys or queries in LDS, fragments
+// of the matrix instructions.
+#pragma once
+
+#include <math.h>
+
+#include "g10_internal.h"
+#include "g10_ops.h"
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+typedef u32 u32x4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Vec;
+template <> struct Vec<__bf16> {
+  typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 x4 __attribute__((ext_vector_type(4)));
+  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ x4 read_tr(const __bf16* p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4*)p);
+  }
+};
+template <> struct Vec<_Float16> {
+  typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 x4 __attribute__((ext_vector_type(4)));
+  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ x4 read_tr(const _Float16* p) {
+    typedef __fp16 h4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4*)p));
+  }
+};
+
+struct AttnArgs {
+  const void *q, *k, *v;
+  void *o, *dq, *dk, *dv;
+  const void* d_o;
+  float* lse;
+  const float* delta;              // backward: sum of do * o per query
+  const u32* amax;                 // backward: bits of the largest |do|
+  float *part, *part_ml;           // split over the keys: unfinished outputs and their maxima and sums
+  int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];   // batch, token, head
+  const int *q_start, *k_start, *k_len;
+  u32 batch, heads, kv_heads, group, dim;
+  u32 seq_q, seq_k, max_q, max_k;
+  u32 causal, window, sinks;
+  u32 tiles;                       // of queries (or of keys) per sequence and head in the grid
+  u32 splits;
+  float scale, scale2;             // scale2 = scale * log2(e)
+};
+
+// One sequence's place.  Numbers of a packed batch that point outside the tensors are moved to their border.
+struct Seq {
+  int64_t q0, k0;                  // first row in the tensors, in rows behind the batch's own
+  int nq, nk;
+};
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+__device__ __forceinline__ Seq seq_of(const AttnArgs& a, u32 b) {
+  Seq s;
+  if (a.q_start) {
+    const int q0 = clampi(a.q_start[b], 0, (int)a.seq_q), q1 = clampi(a.q_start[b + 1], q0, (int)a.seq_q);
+    const int k0 = clampi(a.k_start[b], 0, (int)a.seq_k), k1 = clampi(a.k_start[b + 1], k0, (int)a.seq_k);
+    s.q0 = q0; s.k0 = k0; s.nq = q1 - q0; s.nk = k1 - k0;
+  } else {
+    s.q0 = s.k0 = 0; s.nq = (int)a.seq_q;
+    s.nk = a.k_len ? clampi(a.k_len[b], 0, (int)a.seq_k) : (int)a.seq_k;
+  }
+  return s;
+}
+__device__ __forceinline__ int64_t batch_off(const AttnArgs& a, u32 b, int64_t stride) { return a.q_start ? 0 : (int64_t)b * stride; }
+// the place of (sequence, head, first query) in lse and delta
+__device__ __forceinline__ int64_t row_off(const AttnArgs& a, u32 b, u32 h, const Seq& s) {
+  return a.q_start ? (int64_t)h * a.seq_q + s.q0 : ((int64_t)b * a.heads + h) * a.seq_q;
+}
+
+// The keys that the query at position p sees: lo .. lo + span - 1, and those below `first`.
+struct Seen {
+  int lo, first;
+  u32 span;
+  __device__ __forceinline__ bool key(int j) const { return (u32)(j - lo) < span || j < first; }
+};
+__device__ __forceinline__ Seen keys_of(const AttnArgs& a, int p, int nk) {
+  const int w = (int)a.window, last = nk - 1;
+  int hi = last;
+  if (a.causal) hi = p < last ? p : last;
+  else if (w && p < last - w + 1) hi = p + w - 1;
+  Seen s;
+  s.lo = w && p - w + 1 > 0 ? p - w + 1 : 0;
+  s.span = hi >= s.lo ? (u32)(hi - s.lo + 1) : 0u;
+  s.first = 0;
+  if (w) {
+    const int end = a.causal ? (p < last ? p : last) + 1 : nk;
+    s.first = (int)a.sinks < end ? (int)a.sinks : end;
+  }
+  return s;
+}
+// Whether all positions p0..p1 see all keys j0..j1.
+__device__ __forceinline__ bool all_see(const AttnArgs& a, int p0, int p1, int j0, int j1, int nk) {
+  const int w = (int)a.window;
+  if (j1 >= nk || (a.causal && j1 > p0)) return false;
+  return w == 0 || j1 < (int)a.sinks || (p1 - j0 < w && (a.causal || j1 - p0 < w));
+}
+
+// The keys that any of the positions p0..p1 sees, as tiles of TILE keys: first `head` tiles from 0 on (the sinks), then
+// the tiles lo.. of the window, `count` in all.
+struct Tiles {
+  int head, lo, count;
+  __device__ __forceinline__ int at(int i) const { return i < head ? i : lo + i - head; }
+};
+template <int TILE>
+__device__ __forceinline__ Tiles key_tiles(const AttnArgs& a, int p0, int p1, int nk) {
+  const int w = (int)a.window;
+  int64_t hi = (int64_t)nk - 1;
+  if (a.causal) hi = p1 < hi ? p1 : hi;
+  else if (w && (int64_t)p1 + w - 1 < hi) hi = (int64_t)p1 + w - 1;
+  const int lo = w && p0 - w + 1 > 0 ? p0 - w + 1 : 0;
+  int first = (int)a.sinks < nk ? (int)a.sinks : nk;                 // sinks that any of them sees
+  if (a.causal && first > p1 + 1) first = p1 + 1 > 0 ? p1 + 1 : 0;
+  if (!w) first = 0;
+  Tiles t;
+  t.head = (first + TILE - 1) / TILE;
+  if (hi < lo) { t.lo = 0; t.count = t.head; return t; }
+  t.lo = lo / TILE;
+  if (t.head > t.lo) t.head = t.lo;
+  t.count = t.head + (int)(hi / TILE) - t.lo + 1;
+  return t;
+}
+
+// The queries (indices 0..nq-1) that see any key of j0..j1: lo..hi (empty: hi < lo).
+__device__ __forceinline__ void query_range(const AttnArgs& a, int j0, int j1, const Seq& s, int& lo, int& hi) {
+  const int off = s.nk - s.nq, w = (int)a.window;                    // p = i + off
+  lo = 0; hi = s.nq - 1;
+  if (a.causal && j0 - off > lo) lo = j0 - off;
+  if (w && !(j0 < (int)a.sinks)) {
+    if (!a.causal && j0 - w + 1 - off > lo) lo = j0 - w + 1 - off;
+    if ((int64_t)j1 + w - 1 - off < hi) hi = j1 + w - 1 - off;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Tiles in LDS.  A row holds DP values (DP * 2 bytes), in pieces of 16 bytes; piece c of row r lies at place
+// c ^ swz(r), so that the reads below touch every bank: a fragment read takes one piece of 8 rows running (the low three
+// bits of swz differ over any aligned 8 rows), a transposing read takes two neighbouring pieces of 4 rows running (bits
+// 1 and 2 differ over any aligned 4 rows).
+// ---------------------------------------------------------------------------------------------------------------------
+template <int DP>
+__device__ __forceinline__ int swz(int r) {
+  const int f = ((r & 3) << 1) | ((r >> 2) & 1) | (r & 8);
+  return DP == 64 ? f & 7 : f;
+}
+
+// 64 pieces straight from memory to LDS, lane i's to the place i behind lds (which is the same in every lane).
+// The address is that of the lane's piece: base (the same in every lane) + off bytes.
+// The instruction has no output register and its address is read when it is issued; who reads the tile waits for it first
+// (loads_done) and then meets the others at a barrier.
+__device__ __forceinline__ void load_piece(const void* base, u32 off, u32 lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void loads_done() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);                              // vmcnt 0 (as a builtin: the compiler then knows its own loads done too)
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ u32 lds_addr(const void* p) { return (u32)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// ROWS rows by NT threads (t = 0..NT-1) from row `row0` of a sequence of n > 0 rows; rows past its end repeat the last one
+// (no query sees them), pieces past the head's values repeat the first (they meet zeros, or go nowhere).
+template <int DP, int ROWS, int NT>
+struct Stage {
+  static constexpr int CPR = DP / 8, IT = ROWS * CPR / NT;
+  static_assert(ROWS * CPR % NT == 0, "whole rounds");
+  u32 off[IT];
+  int row[IT];
+  __device__ __forceinline__ void init(u32 t, u32 dim, int64_t stride) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int idx = i * NT + (int)t, r = idx / CPR;
+      int c = (idx % CPR) ^ swz<DP>(r);
+      if (c >= (int)(dim / 8)) c = 0;
+      row[i] = r;
+      off[i] = (u32)(r * (int)stride + c * 8) * 2;
+    }
+  }
+  // lds: LDS address of the tile + this wavefront's first piece (wave * 1024)
+  __device__ __forceinline__ void load(const void* seq_base, int64_t stride, int row0, int n, u32 lds) const {
+    const char* base = (const char*)seq_base + (int64_t)row0 * stride * 2;
+    if (row0 + ROWS <= n) {
+#pragma unroll
+      for (int i = 0; i < IT; ++i) load_piece(base, off[i], lds + (u32)(i * NT * 16));
+    } else {
+      const int last = n - 1 - row0;
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const u32 back = row[i] > last ? (u32)((row[i] - last) * (int)stride) * 2 : 0u;
+        load_piece(base, off[i] - back, lds + (u32)(i * NT * 16));
+      }
+    }
+  }
+};
+
+// Fragment of rows r0..r0+31, values 16 ks.. of a tile: lane l holds row l % 32, values 16 ks + 8 (l / 32) + 0..7.
+template <class T, int DP>
+__device__ __forceinline__ typename Vec<T>::x8 frag_rows(const T* tile, int r0, int ks) {
+  const int l = (int)lane_id(), r = r0 + (l & 31);
+  return *(const typename Vec<T>::x8*)(tile + r * DP + (((2 * ks + (l >> 5)) ^ swz<DP>(r & 15)) << 3));
+}
+// Fragment of the transposed tile: lane l holds value 32 db + l % 32 of the rows k0 + 4 (l / 32) + 0..3 and the same + 8:
+// the order of rows in which the results of a product lie (one register group each), so that these feed the next product
+// as they are.
+template <class T, int DP>
+__device__ __forceinline__ typename Vec<T>::x8 frag_tr(const T* tile, int k0, int db) {
+  const int l = (int)lane_id(), h = l >> 5, r = (l & 15) >> 2;
+  const int c = 4 * db + 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
+  const int row = k0 + 4 * h + r;
+  const T* p0 = tile + row * DP + ((c ^ swz<DP>(row & 15)) << 3) + (l & 1) * 4;
+  const T* p1 = tile + (row + 8) * DP + ((c ^ swz<DP>((row + 8) & 15)) << 3) + (l & 1) * 4;
+  const typename Vec<T>::x4 a = Vec<T>::read_tr(p0), b = Vec<T>::read_tr(p1);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// The row of a result's register r (0..15) in lane l.
+__device__ __forceinline__ int res_row(int r) { return 8 * (r >> 2) + 4 * (int)(lane_id() >> 5) + (r & 3); }
+
+// Fragments of 32 rows straight from memory (rows past `last` repeat it, values past dim are zeros).
+template <class T, int DP>
+__device__ __forceinline__ void frags_global(typename Vec<T>::x8 (&f)[DP / 16], const T* base, int64_t stride, int row, int last, u32 dim) {
+  const int l = (int)lane_id();
+  const T* p = base + (int64_t)(row < last ? row : last) * stride;
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) {
+    const u32 d = 16 * ks + 8 * (l >> 5);
+    typename Vec<T>::x8 z = {};
+    f[ks] = d < dim ? *(const typename Vec<T>::x8*)(p + d) : z;
+  }
+}
+
+// What the two halves of a wavefront hold of one row, joined.
+__device__ __forceinline__ float both_max(float x) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float x) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <class T>
+__device__ __forceinline__ typename Vec<T>::x8 pack8(const f32x16& x, int s) {
+  typename Vec<T>::x8 r;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const f32x2 two = {x[8 * s + j], x[8 * s + j + 1]};
+    const typename Vec<T>::x2 p = __builtin_convertvector(two, typename Vec<T>::x2);
+    r[j] = p[0]; r[j + 1] = p[1];
+  }
+  return r;
+}
+
+#define G10_NEG_INF (-__builtin_inff())
+#define G10_LOG2E 1.4426950408889634f
+#define G10_LN2 0.6931471805599453f
+
+// A workgroup's place among units (a sequence's key head) of `per` workgroups each.  Workgroups go round the 8 XCDs by
+// their number: a unit's keys and values stay in one L2 where there are enough units for all of them.
+__device__ __forceinline__ bool unit_of(u32 units, u32 per, u32& unit, u32& at) {
+  const u32 id = blockIdx.x;
+  if (units % 8 == 0 || units >= 64) {
+    const u32 slot = id / 8;
+    unit = id % 8 + 8 * (slot / per);
+    at = slot % per;
+    return unit < units;
+  }
+  unit = id / per; at = id % per;
+  return unit < units;
+}
+static inline u32 unit_grid(u32 units, u32 per) {
+  return units % 8 == 0 || units >= 64 ? 8 * ((units + 7) / 8) * per : units * per;
+}
+
+int attn_forward_split(const AttnArgs& a, u32 type, hipStream_t s);

@@ -1,0 +1,192 @@
+// Attention, forward.
+#include "g10_attn.h"
+
+#define BM 128                     // queries of a workgroup, 32 to a wavefront
+#define BN 64                      // keys of a tile
+
+// Forward pass.  A wavefront holds 32 queries in registers and walks over the keys they see, 64 at a time, with the running
+// maximum m and sum l of the softmax:  S = K Q^T,  P = 2^(S - m),  O^T = O^T 2^(m' - m) + V^T P.  S comes out transposed
+// (a lane holds one query's scores), so the row's maximum and sum are sums over registers and one exchange of the two halves,
+// and P feeds the second product as it lies in the registers.
+template <class T, int DP>
+__global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) T lds[2][2][BN * DP];
+  typedef typename Vec<T>::x8 x8;
+  u32 unit, at;
+  if (!unit_of(a.batch * a.kv_heads, a.group * a.tiles, unit, at)) return;
+  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + at / a.tiles;
+  const Seq s = seq_of(a, b);
+  const int off = s.nk - s.nq;
+  const u32 wave = uniform(wave_id()), lane = lane_id();
+  const T* Q = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2];
+  const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
+  const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
+  T* O = (T*)a.o + batch_off(a, b, a.os[0]) + s.q0 * a.os[1] + (int64_t)h * a.os[2];
+  float* L = a.lse + row_off(a, b, h, s);
+  Stage<DP, BN, 256> sk, sv;
+  sk.init(threadIdx.x, a.dim, a.ks[1]);
+  sv.init(threadIdx.x, a.dim, a.vs[1]);
+  const u32 lk[2] = {lds_addr(lds[0][0]) + wave * 1024, lds_addr(lds[1][0]) + wave * 1024};
+  const u32 lv[2] = {lds_addr(lds[0][1]) + wave * 1024, lds_addr(lds[1][1]) + wave * 1024};
+  // (the last tiles of a causal sequence are the longest: first)
+  for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BM < s.nq; qt += (int)a.tiles) {
+    const int i0 = qt * BM + (int)wave * 32, i = i0 + (int)(lane & 31);
+    const Seen seen = keys_of(a, i + off, s.nk);
+    const int wp0 = i0 + off, wp1 = (i0 + 31 < s.nq ? i0 + 31 : s.nq - 1) + off;       // the wavefront's positions
+    const int e1 = (qt + 1) * BM - 1 < s.nq ? (qt + 1) * BM - 1 : s.nq - 1;
+    const Tiles tiles = key_tiles<BN>(a, qt * BM + off, e1 + off, s.nk);
+    x8 q[DP / 16];
+    frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
+    f32x16 o[DP / 32] = {};
+    float m = G10_NEG_INF, l = 0.0f;
+    if (tiles.count) {
+      __syncthreads();                                             // (the tiles before are read)
+      sk.load(K, a.ks[1], tiles.at(0) * BN, s.nk, lk[0]);
+      sv.load(V, a.vs[1], tiles.at(0) * BN, s.nk, lv[0]);
+    }
+    for (int t = 0; t < tiles.count; ++t) {
+      const int j0 = tiles.at(t) * BN, buf = t & 1;
+      loads_done();
+      __syncthreads();
+      if (t + 1 < tiles.count) {
+        sk.load(K, a.ks[1], tiles.at(t + 1) * BN, s.nk, lk[buf ^ 1]);
+        sv.load(V, a.vs[1], tiles.at(t + 1) * BN, s.nk, lv[buf ^ 1]);
+      }
+      const T *tk = lds[buf][0], *tv = lds[buf][1];
+      f32x16 sc[2] = {};
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ++ks) sc[n] = Vec<T>::mfma(frag_rows<T, DP>(tk, 32 * n, ks), q[ks], sc[n]);
+      if (!all_see(a, wp0, wp1, j0, j0 + BN - 1, s.nk)) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[n][r] = seen.key(j0 + 32 * n + res_row(r)) ? sc[n][r] : G10_NEG_INF;
+      }
+      float top = sc[0][0];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[n][r]);
+      top = fmaxf(m, both_max(top));
+      const float base = top == G10_NEG_INF ? 0.0f : top * a.scale2;
+      const float fade = exp2_fast(m * a.scale2 - base);
+      m = top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sc[n][r] = exp2_fast(sc[n][r] * a.scale2 - base);
+          sum += sc[n][r];
+        }
+      l = l * fade + both_sum(sum);
+#pragma unroll
+      for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= fade;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const x8 pf = pack8<T>(sc[n], k);
+#pragma unroll
+          for (int db = 0; db < DP / 32; ++db) o[db] = Vec<T>::mfma(frag_tr<T, DP>(tv, 32 * n + 16 * k, db), pf, o[db]);
+        }
+    }
+    if (i < s.nq) {
+      const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // (l is NaN where a score is)
+      T* out = O + (int64_t)i * a.os[1];
+#pragma unroll
+      for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int d = 32 * db + 8 * g + 4 * (int)(lane >> 5);
+          if (d < (int)a.dim) {
+            typename Vec<T>::x4 w;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[r] = (T)(o[db][4 * g + r] * inv);
+            *(typename Vec<T>::x4*)(out + d) = w;
+          }
+        }
+      if (lane < 32) L[i] = l > 0.0f ? (m * a.scale2 + __log2f(l)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------------
+static bool aligned(const void* p, const int64_t* st, bool batch) {
+  if (!p || ((uintptr_t)p & 15)) return false;
+  for (int i = batch ? 0 : 1; i < 3; ++i)
+    if (st[i] & 7) return false;
+  return st[1] >= 0 && st[1] <= (1 << 22);
+}
+
+static int args_of(const g10_attention_args* g, bool back, AttnArgs& a) {
+  if (!g) return G10_EINVAL;
+  if (g->type != G10_F16 && g->type != G10_BF16) return G10_EINVAL;
+  if (!g->dim || g->dim % 8 || g->dim > 128) return G10_EINVAL;
+  if (!g->kv_heads || !g->heads || g->heads % g->kv_heads || g->heads > 65536) return G10_EINVAL;
+  if ((g->q_start == nullptr) != (g->k_start == nullptr) || (g->q_start && g->k_len)) return G10_EINVAL;
+  if (!(g->scale > 0.0f) || !(g->scale < 3e38f)) return G10_EINVAL;
+  if (g->causal > 1 || g->seq_q >= (1u << 30) || g->seq_k >= (1u << 30) || g->window >= (1u << 30) || g->sinks >= (1u << 30)) return G10_EINVAL;
+  if (g->max_q >= (1u << 30) || g->max_k >= (1u << 30)) return G10_EINVAL;
+  if ((uint64_t)g->batch * g->heads >= (1u << 24)) return G10_EINVAL;
+  const bool packed = g->q_start != nullptr;
+  a = AttnArgs{};
+  a.q = g->q; a.k = g->k; a.v = g->v; a.o = g->o; a.lse = g->lse; a.d_o = g->d_o; a.dq = g->dq; a.dk = g->dk; a.dv = g->dv;
+  for (int i = 0; i < 3; ++i) {
+    a.qs[i] = g->q_stride[i]; a.ks[i] = g->k_stride[i]; a.vs[i] = g->v_stride[i]; a.os[i] = g->o_stride[i];
+    a.dos[i] = g->do_stride[i]; a.dqs[i] = g->dq_stride[i]; a.dks[i] = g->dk_stride[i]; a.dvs[i] = g->dv_stride[i];
+  }
+  a.q_start = g->q_start; a.k_start = g->k_start; a.k_len = g->k_len;
+  a.batch = g->batch; a.heads = g->heads; a.kv_heads = g->kv_heads; a.group = g->heads / g->kv_heads; a.dim = g->dim;
+  a.seq_q = g->seq_q; a.seq_k = g->seq_k;
+  a.max_q = packed ? (g->max_q < g->seq_q ? g->max_q : g->seq_q) : g->seq_q;
+  a.max_k = packed ? (g->max_k < g->seq_k ? g->max_k : g->seq_k) : g->seq_k;
+  if (packed && g->seq_q && !a.max_q) a.max_q = 1;
+  if (packed && g->seq_k && !a.max_k) a.max_k = 1;
+  a.causal = g->causal; a.window = g->window; a.sinks = g->sinks;
+  a.scale = g->scale; a.scale2 = g->scale * G10_LOG2E;
+  const bool some_q = g->batch && g->seq_q, some_k = g->batch && g->seq_k;
+  if (some_q && (!aligned(g->q, g->q_stride, !packed) || !aligned(g->o, g->o_stride, !packed) || !g->lse)) return G10_EINVAL;
+  if (some_k && (!aligned(g->k, g->k_stride, !packed) || !aligned(g->v, g->v_stride, !packed))) return G10_EINVAL;
+  if (back) {
+    if (some_q && (!aligned(g->d_o, g->do_stride, !packed) || !aligned(g->dq, g->dq_stride, !packed))) return G10_EINVAL;
+    if (some_k && (!aligned(g->dk, g->dk_stride, !packed) || !aligned(g->dv, g->dv_stride, !packed))) return G10_EINVAL;
+  }
+  return G10_OK;
+}
+int attn_args(const g10_attention_args* g, bool back, AttnArgs& a) { return args_of(g, back, a); }
+
+extern "C" int g10_attention_workspace(const g10_attention_args* g, uint64_t* bytes) {
+  if (!bytes) return G10_EINVAL;
+  AttnArgs a;
+  G10_TRY(args_of(g, false, a));
+  *bytes = 0;
+  return G10_OK;
+}
+
+extern "C" int g10_attention(const g10_attention_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  AttnArgs a;
+  G10_TRY(args_of(g, false, a));
+  (void)workspace; (void)workspace_bytes;
+  if (!a.batch || !a.seq_q) return G10_OK;
+  hipStream_t s = (hipStream_t)hip_stream;
+  a.tiles = (a.max_q + BM - 1) / BM;
+  const uint64_t per = (uint64_t)a.group * a.tiles, units = (uint64_t)a.batch * a.kv_heads;
+  if ((units + 7) * per >= (1ull << 31)) return G10_EINVAL;
+  const dim3 grid(unit_grid((u32)units, (u32)per));
+  if (g->type == G10_BF16) {
+    if (a.dim <= 64) k_attn_fwd<__bf16, 64><<<grid, 256, 0, s>>>(a);
+    else k_attn_fwd<__bf16, 128><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (a.dim <= 64) k_attn_fwd<_Float16, 64><<<grid, 256, 0, s>>>(a);
+    else k_attn_fwd<_Float16, 128><<<grid, 256, 0, s>>>(a);
+  }
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}
