@@ -1,9 +1,10 @@
 // The norms of queries and keys with the rotation by position, one pass over both; forward and backward.
 //
 // Bound by memory: a value is read once and written once (backward: read with its gradient, written once), some 20
-// operations between them.  A row (token, head) lies in the registers of a group of 8, 16 or 32 lanes, 8 values to a lane; its sums
-// are DPP steps inside the group, pairs of the rotation are values of one lane or of two lanes of the group.  A group keeps the
-// cosines and sines of its token for several heads (the table's values are four times a 16-bit head's).
+// operations between them.  A row (token, head) lies in the registers of a group of 8, 16 or 32 lanes, 8 values to a lane, which
+// are four pairs: neighbours lie side by side, halves as 4 values of the lower and the same 4 of the upper half, so that no value
+// has to change lanes for its rotation.  Sums are DPP steps inside the group.  A group keeps the cosines and sines of its token for
+// several heads (the table's values are four times a 16-bit head's) and has the next four heads on their way while it works.
 #include "g10_internal.h"
 #include "g10_ops.h"
 
@@ -19,43 +20,47 @@ struct RopeArgs {
   const float* table;
   const void* positions;
   float eps;
-  u32 w32, pos64, chunks, per;      // per heads to a task, chunks tasks to a token
+  u32 w32, pos64, per;              // heads to a task
+  u32 chunks[2], all_chunks;        // tasks to a token: of queries, of keys
   float* partial;                   // backward: [workgroups][2][dim]
 };
 
 template <class T> __device__ __forceinline__ float to_f(T x) { return (float)x; }
 
+// Eight values as they come from memory: two runs of four.
 template <class T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-    typedef T x8 __attribute__((ext_vector_type(8)));
-    const x8 a = *(const x8*)p;
+struct Raw {
+  typedef T x4 __attribute__((ext_vector_type(4)));
+  x4 a, b;
+  __device__ __forceinline__ void load(const T* p, u32 d0, u32 d1) { a = *(const x4*)(p + d0); b = *(const x4*)(p + d1); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+    for (int i = 0; i < 4; ++i) { v[i] = (float)a[i]; v[4 + i] = (float)b[i]; }
   }
-}
+};
 template <class T>
-__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
-  if constexpr (sizeof(T) == 4) {
-    *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
-    *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-  } else {
-    typedef T x8 __attribute__((ext_vector_type(8)));
-    x8 a;
+__device__ __forceinline__ void store8(T* p, u32 d0, u32 d1, const float (&v)[8]) {
+  typedef T x4 __attribute__((ext_vector_type(4)));
+  x4 a, b;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = (T)v[i];
-    *(x8*)p = a;
-  }
+  for (int i = 0; i < 4; ++i) { a[i] = (T)v[i]; b[i] = (T)v[4 + i]; }
+  *(x4*)(p + d0) = a;
+  *(x4*)(p + d1) = b;
 }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
 // sum over an aligned group of G lanes, in each of them
 template <int G>
 __device__ __forceinline__ float group_sum(float x) {
-#pragma unroll
-  for (int d = 1; d < G; d *= 2) x += __shfl_xor(x, d, 64);
+  x = dpp_add<0xb1>(x);                                             // lanes 1, 0, 3, 2 of a quad
+  x = dpp_add<0x4e>(x);                                             // lanes 2, 3, 0, 1
+  x = dpp_add<0x141>(x);                                            // eight lanes mirrored
+  if (G >= 16) x = dpp_add<0x140>(x);                               // sixteen lanes mirrored
+  if (G >= 32) x += __shfl_xor(x, 16, 64);
+  if (G >= 64) x += __shfl_xor(x, 32, 64);
   return x;
 }
 
@@ -68,121 +73,127 @@ __device__ __forceinline__ float weight(const RopeArgs& a, int part, u32 d) {
   return a.w32 ? ((const float*)a.w[part])[d] : to_f(((const T*)a.w[part])[d]);
 }
 
-// The cosines and sines that a lane's values 8 lane .. + 7 meet.  Values past `rot` meet 1 and 0.
-template <bool PAIRS>
-__device__ __forceinline__ void angles(const RopeArgs& a, int64_t pos, u32 d0, float (&c)[8], float (&s)[8]) {
-  const bool in = d0 < a.rot;
-  const float* t = a.table + pos * a.rot;
-  if constexpr (PAIRS) {
-    const u32 i = in ? d0 / 2 : 0u;
+// A lane's four pairs turned by their angles; BACK: by the angles' opposites.
+template <bool PAIRS, bool BACK>
+__device__ __forceinline__ void turn(float (&v)[8], const float4& c4, const float4& s4) {
+  const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float x = in ? t[i + k] : 1.0f, y = in ? t[a.rot / 2 + i + k] : 0.0f;
-      c[2 * k] = c[2 * k + 1] = x; s[2 * k] = s[2 * k + 1] = y;
-    }
-  } else {
-    const u32 i = in ? d0 % (a.rot / 2) : 0u;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      c[k] = in ? t[i + k] : 1.0f;
-      s[k] = in ? t[a.rot / 2 + i + k] : 0.0f;
-    }
+  for (int k = 0; k < 4; ++k) {
+    const int i = PAIRS ? 2 * k : k, j = PAIRS ? 2 * k + 1 : k + 4;
+    const float x = v[i], y = v[j], t = BACK ? -s[k] : s[k];
+    v[i] = x * c[k] - y * t;
+    v[j] = y * c[k] + x * t;
   }
 }
-// Values turned by their angles; `back`: by the angles' opposites.  Lane l's values are 8 (l % G) .. + 7 of the row.
-template <bool PAIRS, bool BACK>
-__device__ __forceinline__ void turn(const RopeArgs& a, u32 d0, float (&v)[8], const float (&c)[8], const float (&s)[8]) {
-  if constexpr (PAIRS) {
-#pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-      const float x = v[k], y = v[k + 1], t = BACK ? -s[k] : s[k];
-      v[k] = x * c[k] - y * t;
-      v[k + 1] = y * c[k] + x * t;
-    }
-  } else {
-    const u32 half = a.rot / 16;                                    // lanes between the two values of a pair
-    const bool low = d0 < a.rot / 2, in = d0 < a.rot;
-    const int other = (int)lane_id() + (in ? (low ? (int)half : -(int)half) : 0);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float y = __shfl(v[k], other, 64);
-      const float t = low != BACK ? -s[k] : s[k];
-      v[k] = v[k] * c[k] + y * t;
-    }
-  }
+
+// Where a task's rows lie: token, and up to `per` heads of the queries or the keys.
+struct Task {
+  u64 tok;
+  int64_t b, i;
+  u32 h0, n;                        // first head, heads (0: no task)
+  int part;
+};
+__device__ __forceinline__ Task task_of(const RopeArgs& a, u64 task, u64 tasks) {
+  Task t;
+  const bool real = task < tasks;
+  t.tok = real ? task / a.all_chunks : 0;
+  u32 c = real ? (u32)(task % a.all_chunks) : 0u;
+  t.part = c >= a.chunks[0];
+  if (t.part) c -= a.chunks[0];
+  t.h0 = c * a.per;
+  const u32 left = a.heads[t.part] - t.h0;
+  t.n = real ? (left < a.per ? left : a.per) : 0u;
+  t.b = (int64_t)(t.tok / a.seq);
+  t.i = (int64_t)(t.tok % a.seq);
+  return t;
 }
 
 template <class T, int G, bool PAIRS, bool BACK>
 __global__ __launch_bounds__(256) void k_rope(const RopeArgs a) {
-  const u32 l = lane_id() % G, d0 = 8 * l;
-  const bool has = d0 < a.dim;
+  const u32 l = lane_id() % G, half = a.rot / 2;
+  const bool has = 8 * l < a.dim, in = 8 * l < a.rot;
+  const u32 dl = has ? 8 * l : 0u;                                  // (lanes without values read the first ones, and write nothing)
+  const u32 d0 = !PAIRS && in ? 4 * l : dl, d1 = !PAIRS && in ? half + 4 * l : dl + 4;
+  const u32 at = in ? 4 * l : 0u;                                   // its angles
   const float inv_dim = 1.0f / (float)a.dim;
   float w[2][8], dw[2][8] = {};
 #pragma unroll
   for (int part = 0; part < 2; ++part)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[part][k] = has ? weight<T>(a, part, d0 + k) : 0.0f;
-  const u64 tasks = a.tokens * a.chunks, step = (u64)gridDim.x * (256 / G);
+    for (int k = 0; k < 8; ++k) w[part][k] = has ? weight<T>(a, part, (k < 4 ? d0 + k : d1 + k - 4)) : 0.0f;
+  const u64 tasks = a.tokens * a.all_chunks, step = (u64)gridDim.x * (256 / G);
   // (whole wavefronts stay in the loop: the sums below go over lanes)
   for (u64 first = (u64)blockIdx.x * (256 / G) + wave_id() * (64 / G); first < tasks; first += step) {
-    const u64 task = first + lane_id() / G;
-    const bool real = task < tasks;
-    const u64 tok = real ? task / a.chunks : 0;
-    const u32 h0 = real ? (u32)(task % a.chunks) * a.per : 0u;
-    const u32 h1 = real ? (h0 + a.per < a.all_heads ? h0 + a.per : a.all_heads) : 0u;
-    const int64_t pos = position(a, tok), b = (int64_t)(tok / a.seq), i = (int64_t)(tok % a.seq);
+    const Task t = task_of(a, first + lane_id() / G, tasks);
+    const int p = t.part;
+    const int64_t pos = position(a, t.tok);
+    const int64_t xh = p ? a.xs[1][2] : a.xs[0][2], yh = p ? a.dys[1][2] : a.dys[0][2], oh = p ? a.os[1][2] : a.os[0][2];
+    const T* x = (const T*)(p ? a.x[1] : a.x[0]) + t.b * (p ? a.xs[1][0] : a.xs[0][0]) + t.i * (p ? a.xs[1][1] : a.xs[0][1]) + t.h0 * xh;
+    const T* y = nullptr;
+    if (BACK) y = (const T*)(p ? a.dy[1] : a.dy[0]) + t.b * (p ? a.dys[1][0] : a.dys[0][0]) + t.i * (p ? a.dys[1][1] : a.dys[0][1]) + t.h0 * yh;
+    T* out = (T*)(p ? a.out[1] : a.out[0]) + t.b * (p ? a.os[1][0] : a.os[0][0]) + t.i * (p ? a.os[1][1] : a.os[0][1]) + t.h0 * oh;
+    const u32 last = t.n ? t.n - 1 : 0u;                            // (heads past the task's repeat its last)
+    Raw<T> rx[4], ry[4];
+#pragma unroll
+    for (u32 u = 0; u < 4; ++u) {
+      const u32 h = u < last ? u : last;
+      rx[u].load(x + h * xh, d0, d1);
+      if (BACK) ry[u].load(y + h * yh, d0, d1);
+    }
     const bool fine = pos >= 0 && pos < (int64_t)a.n_pos;
-    float c[8], s[8];
-    angles<PAIRS>(a, fine ? pos : 0, d0, c, s);
+    const float* tab = a.table + (fine ? pos : 0) * a.rot;
+    float4 c = make_float4(1.0f, 1.0f, 1.0f, 1.0f), s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (in) { c = *(const float4*)(tab + at); s = *(const float4*)(tab + half + at); }
+    float sw[8], sdw[8] = {};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sw[k] = p ? w[1][k] : w[0][k];
     for (u32 q = 0; q < a.per; q += 4) {
-      float x[4][8], dy[4][8];
+      Raw<T> nx[4], ny[4];
+      if (q + 4 < a.per) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const u32 h = h0 + q + u;
-        const bool on = h < h1 && q + u < a.per && has;
-        const int part = h >= a.heads[0];
-        const u32 hh = part ? h - a.heads[0] : h;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) { x[u][k] = 0.0f; if (BACK) dy[u][k] = 0.0f; }
-        if (on) {
-          load8((const T*)a.x[part] + b * a.xs[part][0] + i * a.xs[part][1] + hh * a.xs[part][2] + d0, x[u]);
-          if (BACK) load8((const T*)a.dy[part] + b * a.dys[part][0] + i * a.dys[part][1] + hh * a.dys[part][2] + d0, dy[u]);
+        for (u32 u = 0; u < 4; ++u) {
+          const u32 h = q + 4 + u < last ? q + 4 + u : last;
+          nx[u].load(x + h * xh, d0, d1);
+          if (BACK) ny[u].load(y + h * yh, d0, d1);
         }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const u32 h = h0 + q + u;
+      for (u32 u = 0; u < 4; ++u) {
         if (q + u >= a.per) break;                                  // (the same in every lane)
-        const bool on = h < h1 && has;
-        const int part = h >= a.heads[0];
-        const u32 hh = part ? h - a.heads[0] : h;
-        float sum = 0.0f;
+        const bool on = q + u < t.n && has;
+        float v[8], sum = 0.0f;
+        rx[u].get(v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum += x[u][k] * x[u][k];
-        sum = group_sum<G>(sum);
+        for (int k = 0; k < 8; ++k) sum += v[k] * v[k];
+        sum = group_sum<G>(has ? sum : 0.0f);
         const float r = fine ? 1.0f / sqrtf(sum * inv_dim + a.eps) : __builtin_nanf("");
-        float v[8];
         if constexpr (!BACK) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = x[u][k] * r * (part ? w[1][k] : w[0][k]);
-          turn<PAIRS, false>(a, d0, v, c, s);
+          for (int k = 0; k < 8; ++k) v[k] = v[k] * r * sw[k];
+          turn<PAIRS, false>(v, c, s);
         } else {
-          float dot = 0.0f;
-          turn<PAIRS, true>(a, d0, dy[u], c, s);
+          float g[8], dot = 0.0f;
+          ry[u].get(g);
+          turn<PAIRS, true>(g, c, s);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float n = x[u][k] * r, g = dy[u][k];
-            x[u][k] = n;
-            v[k] = g * (part ? w[1][k] : w[0][k]);
-            dot += v[k] * n;
-            if (on) { if (part) dw[1][k] += g * n; else dw[0][k] += g * n; }
+            v[k] *= r;
+            sdw[k] += on ? g[k] * v[k] : 0.0f;
+            g[k] *= sw[k];
+            dot += g[k] * v[k];
           }
-          dot = group_sum<G>(dot) * inv_dim;
+          dot = group_sum<G>(has ? dot : 0.0f) * inv_dim;
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = r * (v[k] - x[u][k] * dot);
+          for (int k = 0; k < 8; ++k) v[k] = r * (g[k] - v[k] * dot);
         }
-        if (on) store8((T*)a.out[part] + b * a.os[part][0] + i * a.os[part][1] + hh * a.os[part][2] + d0, v);
+        if (on) store8(out + (q + u) * oh, d0, d1, v);
       }
+#pragma unroll
+      for (u32 u = 0; u < 4; ++u) { rx[u] = nx[u]; ry[u] = ny[u]; }
+    }
+    if (BACK) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) { dw[0][k] += p ? 0.0f : sdw[k]; dw[1][k] += p ? sdw[k] : 0.0f; }
     }
   }
   if constexpr (BACK) {
@@ -195,7 +206,7 @@ __global__ __launch_bounds__(256) void k_rope(const RopeArgs a) {
         float t = dw[part][k];
 #pragma unroll
         for (int d = G; d < 64; d *= 2) t += __shfl_xor(t, d, 64);
-        if (lane_id() < G) sums[wave_id()][part][d0 + k] = t;
+        if (lane_id() < G && has) sums[wave_id()][part][k < 4 ? d0 + k : d1 + k - 4] = t;
       }
     __syncthreads();
     for (u32 e = threadIdx.x; e < 2 * a.dim; e += 256) {
@@ -283,18 +294,20 @@ __global__ __launch_bounds__(256) void k_rope_any(const RopeArgs a, u32 pairs) {
   }
 }
 
-// Gradients of the weights: the workgroups' sums, 32 values to a workgroup, in one order and 64 bits.
+// Gradients of the weights: the workgroups' sums, 16 values to a workgroup, in one order and 64 bits.
 template <class T>
-__global__ __launch_bounds__(256) void k_rope_weights(const RopeArgs a, u32 n) {
-  __shared__ double sums[8][32];
-  const u32 e = blockIdx.x * 32 + threadIdx.x % 32, w = threadIdx.x / 32;
+__global__ __launch_bounds__(1024) void k_rope_weights(const RopeArgs a, u32 n) {
+  __shared__ double sums[64][16];
+  const u32 e = blockIdx.x * 16 + threadIdx.x % 16, w = threadIdx.x / 16;
   double t = 0.0;
-  if (e < 2 * a.dim)
-    for (u32 i = w; i < n; i += 8) t += (double)a.partial[(u64)i * 2 * a.dim + e];
-  sums[w][threadIdx.x % 32] = t;
+  if (e < 2 * a.dim) {
+#pragma unroll 8
+    for (u32 i = w; i < n; i += 64) t += (double)a.partial[(u64)i * 2 * a.dim + e];
+  }
+  sums[w][threadIdx.x % 16] = t;
   __syncthreads();
   if (w || e >= 2 * a.dim) return;
-  for (u32 i = 1; i < 8; ++i) t += sums[i][threadIdx.x];
+  for (u32 i = 1; i < 64; ++i) t += sums[i][threadIdx.x];
   const u32 part = e / a.dim, d = e % a.dim;
   if (!a.dw[part]) return;
   if (a.w32) ((float*)a.dw[part])[d] = (float)t;
@@ -304,7 +317,7 @@ __global__ __launch_bounds__(256) void k_rope_weights(const RopeArgs a, u32 n) {
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-#define ROPE_GROUPS 2048           // workgroups of a backward pass: 8 on each of 256 compute units
+#define ROPE_GROUPS 1024           // workgroups of a backward pass: 4 on each of 256 compute units
 
 struct RopePlan { u32 grid, lanes; bool any, weights; };
 
@@ -322,7 +335,7 @@ static int rope_args(const g10_rope_args* g, bool back, RopeArgs& a, RopePlan& p
   const bool pairs = g->flags & G10_ROPE_INTERLEAVED;
   const u32 e = g->type == G10_F32 ? 4 : 2, step = 16 / e;          // elements of 16 bytes
   p.weights = false;
-  p.any = g->dim % 8 || (pairs ? g->rot % 8 : g->rot % 16) || ((uintptr_t)g->table & 15);
+  p.any = g->dim % 8 || g->rot % 8 || ((uintptr_t)g->table & 15);
   for (int k = 0; k < 2; ++k) {
     const g10_rope_part& s = g->part[k];
     a.heads[k] = s.heads;
@@ -347,8 +360,9 @@ static int rope_args(const g10_rope_args* g, bool back, RopeArgs& a, RopePlan& p
   // A task takes 8 heads where that still fills the chip, else one: with few tokens a row's way from memory and back is all there is.
   const u64 rows = a.tokens * heads;
   a.per = rows / 8 * p.lanes >= 256ull * 8 * 64 ? 8 : 1;
-  a.chunks = some ? (u32)((heads + a.per - 1) / a.per) : 0;
-  const u64 groups = p.any ? (rows + 3) / 4 : (a.tokens * a.chunks + 256 / p.lanes - 1) / (256 / p.lanes);
+  for (int k = 0; k < 2; ++k) a.chunks[k] = some ? (a.heads[k] + a.per - 1) / a.per : 0;
+  a.all_chunks = a.chunks[0] + a.chunks[1];
+  const u64 groups = p.any ? (rows + 3) / 4 : (a.tokens * a.all_chunks + 256 / p.lanes - 1) / (256 / p.lanes);
   p.grid = (u32)(back ? (groups < ROPE_GROUPS ? groups : ROPE_GROUPS) : (groups < (1u << 30) ? groups : (1u << 30)));
   return G10_OK;
 }
@@ -402,10 +416,10 @@ extern "C" int g10_norm_rope_backward(const g10_rope_args* g, void* workspace, u
     else rope_launch<__bf16, true>(a, p, pairs, s);
   }
   if (p.weights) {                                                   // (without tokens: zeros)
-    const u32 grid = (2 * a.dim + 31) / 32;
-    if (g->type == G10_F32) k_rope_weights<float><<<grid, 256, 0, s>>>(a, p.grid);
-    else if (g->type == G10_F16) k_rope_weights<_Float16><<<grid, 256, 0, s>>>(a, p.grid);
-    else k_rope_weights<__bf16><<<grid, 256, 0, s>>>(a, p.grid);
+    const u32 grid = (2 * a.dim + 15) / 16;
+    if (g->type == G10_F32) k_rope_weights<float><<<grid, 1024, 0, s>>>(a, p.grid);
+    else if (g->type == G10_F16) k_rope_weights<_Float16><<<grid, 1024, 0, s>>>(a, p.grid);
+    else k_rope_weights<__bf16><<<grid, 1024, 0, s>>>(a, p.grid);
   }
   G10_HIP(hipGetLastError());
   return G10_OK;
