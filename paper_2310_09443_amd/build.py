@@ -7,7 +7,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = [os.path.join(HERE, "csrc", f) for f in ("g10_api.hip", "g10_mem.hip", "g10_vitality.hip", "g10_plan.hip", "g10_loop.hip", "g10_prefetch.hip", "g10_replay.hip",
-                                               "g10_rope.hip", "g10_attn.hip", "g10_attn_back.hip", "g10_adamw.hip")]
+                                               "g10_rope.hip", "g10_attn.hip", "g10_attn_split.hip", "g10_attn_back.hip", "g10_adamw.hip")]
 DEPS = SRC + [os.path.join(HERE, "csrc", "g10_internal.h"), os.path.join(HERE, "csrc", "g10_plan_defs.h"), os.path.join(HERE, "csrc", "g10_attn.h"),
               os.path.join(ROOT, "include", "g10.h"), os.path.join(ROOT, "include", "g10_ops.h")]
 LIB = os.path.join(HERE, "libg10.so")

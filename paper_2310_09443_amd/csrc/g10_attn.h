@@ -282,4 +282,7 @@ static inline u32 unit_grid(u32 units, u32 per) {
   return units % 8 == 0 || units >= 64 ? 8 * ((units + 7) / 8) * per : units * per;
 }
 
-int attn_forward_split(const AttnArgs& a, u32 type, hipStream_t s);
+int attn_args(const g10_attention_args* g, bool back, AttnArgs& a);
+u32 attn_splits(const AttnArgs& a);
+u64 attn_split_bytes(const AttnArgs& a, u32 splits);
+int attn_forward_split(AttnArgs a, u32 splits, void* workspace, u32 type, hipStream_t s);

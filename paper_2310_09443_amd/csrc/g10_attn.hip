@@ -125,7 +125,7 @@ static bool aligned(const void* p, const int64_t* st, bool batch) {
   return st[1] >= 0 && st[1] <= (1 << 22);
 }
 
-static int args_of(const g10_attention_args* g, bool back, AttnArgs& a) {
+int attn_args(const g10_attention_args* g, bool back, AttnArgs& a) {
   if (!g) return G10_EINVAL;
   if (g->type != G10_F16 && g->type != G10_BF16) return G10_EINVAL;
   if (!g->dim || g->dim % 8 || g->dim > 128) return G10_EINVAL;
@@ -160,22 +160,25 @@ static int args_of(const g10_attention_args* g, bool back, AttnArgs& a) {
   }
   return G10_OK;
 }
-int attn_args(const g10_attention_args* g, bool back, AttnArgs& a) { return args_of(g, back, a); }
 
 extern "C" int g10_attention_workspace(const g10_attention_args* g, uint64_t* bytes) {
   if (!bytes) return G10_EINVAL;
   AttnArgs a;
-  G10_TRY(args_of(g, false, a));
-  *bytes = 0;
+  G10_TRY(attn_args(g, false, a));
+  *bytes = a.batch && a.seq_q ? attn_split_bytes(a, attn_splits(a)) : 0;
   return G10_OK;
 }
 
 extern "C" int g10_attention(const g10_attention_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
   AttnArgs a;
-  G10_TRY(args_of(g, false, a));
-  (void)workspace; (void)workspace_bytes;
+  G10_TRY(attn_args(g, false, a));
   if (!a.batch || !a.seq_q) return G10_OK;
   hipStream_t s = (hipStream_t)hip_stream;
+  if (const u32 splits = attn_splits(a)) {
+    const u64 need = attn_split_bytes(a, splits);
+    if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return G10_EINVAL;
+    return attn_forward_split(a, splits, workspace, g->type, s);
+  }
   a.tiles = (a.max_q + BM - 1) / BM;
   const uint64_t per = (uint64_t)a.group * a.tiles, units = (uint64_t)a.batch * a.kv_heads;
   if ((units + 7) * per >= (1ull << 31)) return G10_EINVAL;

@@ -4,8 +4,6 @@
 // no atomics, and nothing of the size of the scores in memory.
 #include "g10_attn.h"
 
-int attn_args(const g10_attention_args* g, bool back, AttnArgs& a);
-
 #define BT 64                      // rows of a staged tile
 #define BW 128                     // rows of a workgroup, 32 to a wavefront
 
