@@ -19,8 +19,8 @@ template <> struct Vec<__bf16> {
   typedef __bf16 x4 __attribute__((ext_vector_type(4)));
   typedef __bf16 x2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ x4 read_tr(const __bf16* p) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4*)p);
+  static __device__ __forceinline__ x4 read_tr(u32 at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) x4*)(uintptr_t)at);
   }
 };
 template <> struct Vec<_Float16> {
@@ -28,11 +28,21 @@ template <> struct Vec<_Float16> {
   typedef _Float16 x4 __attribute__((ext_vector_type(4)));
   typedef _Float16 x2 __attribute__((ext_vector_type(2)));
   static __device__ __forceinline__ f32x16 mfma(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-  static __device__ __forceinline__ x4 read_tr(const _Float16* p) {
+  static __device__ __forceinline__ x4 read_tr(u32 at) {
     typedef __fp16 h4 __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4*)p));
+    return __builtin_bit_cast(x4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) h4*)(uintptr_t)at));
   }
 };
+
+// f(0), f(1), ... f(N - 1) with constant arguments, whatever the size of what f does (the compiler stops unrolling long loops).
+template <int N> struct Const { static constexpr int value = N; };
+template <int I, int N, class F>
+__device__ __forceinline__ void each_of(F&& f) {
+  if constexpr (I < N) {
+    f(Const<I>{});
+    each_of<I + 1, N>(f);
+  }
+}
 
 struct AttnArgs {
   const void *q, *k, *v;
@@ -40,6 +50,7 @@ struct AttnArgs {
   const void* d_o;
   float* lse;
   const float* delta;              // backward: sum of do * o per query
+  const float* lse2;               // backward: lse in powers of two, less the lift of P
   const u32* amax;                 // backward: bits of the largest |do|
   float *part, *part_ml;           // split over the keys: unfinished outputs and their maxima and sums
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];   // batch, token, head
@@ -48,7 +59,8 @@ struct AttnArgs {
   u32 seq_q, seq_k, max_q, max_k;
   u32 causal, window, sinks;
   u32 tiles;                       // of queries (or of keys) per sequence and head in the grid
-  u32 splits;
+  u32 splits;                      // forward: workgroups that share a row's keys; backward: that share a tile of sinks' queries
+  u32 sink_tiles;                  // backward: key tiles whose queries are shared
   float scale, scale2;             // scale2 = scale * log2(e)
 };
 
@@ -141,17 +153,25 @@ __device__ __forceinline__ void query_range(const AttnArgs& a, int j0, int j1, c
     if ((int64_t)j1 + w - 1 - off < hi) hi = j1 + w - 1 - off;
   }
 }
+// The queries that see all of them.
+__device__ __forceinline__ void full_range(const AttnArgs& a, int j0, int j1, const Seq& s, int& lo, int& hi) {
+  const int off = s.nk - s.nq, w = (int)a.window;
+  lo = 0; hi = j1 < s.nk ? s.nq - 1 : -1;
+  if (a.causal && j1 - off > lo) lo = j1 - off;
+  if (w && j1 >= (int)a.sinks) {
+    if (!a.causal && j1 - w + 1 - off > lo) lo = j1 - w + 1 - off;
+    if ((int64_t)j0 + w - 1 - off < hi) hi = j0 + w - 1 - off;
+  }
+}
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Tiles in LDS.  A row holds DP values (DP * 2 bytes), in pieces of 16 bytes; piece c of row r lies at place
-// c ^ swz(r), so that the reads below touch every bank: a fragment read takes one piece of 8 rows running (the low three
-// bits of swz differ over any aligned 8 rows), a transposing read takes two neighbouring pieces of 4 rows running (bits
-// 1 and 2 differ over any aligned 4 rows).
+// Tiles in LDS.  A row holds DP values (DP * 2 bytes), in pieces of 16 bytes; piece c of row r lies at place c ^ swz(r), so that
+// the reads below take each of the 64 banks once a cycle: a fragment read takes one piece of 16 rows running (their places
+// in a line of 256 bytes all differ), a transposing read takes four neighbouring pieces of 4 rows running, 64 bytes of each.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DP>
 __device__ __forceinline__ int swz(int r) {
-  const int f = ((r & 3) << 1) | ((r >> 2) & 1) | (r & 8);
-  return DP == 64 ? f & 7 : f;
+  return DP == 64 ? ((r & 2) << 1) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
 }
 
 // 64 pieces straight from memory to LDS, lane i's to the place i behind lds (which is the same in every lane).
@@ -166,23 +186,35 @@ __device__ __forceinline__ void loads_done() {
   __builtin_amdgcn_s_waitcnt(0x0f70);                              // vmcnt 0 (as a builtin: the compiler then knows its own loads done too)
   asm volatile("" ::: "memory");
 }
+// All but the wavefront's last N of them.
+template <int N>
+__device__ __forceinline__ void loads_done_but() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+// 64 words, lane i's from its own address to the place i behind lds.
+__device__ __forceinline__ void load_words(const void* p, u32 lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+}
 __device__ __forceinline__ u32 lds_addr(const void* p) { return (u32)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
 // ROWS rows by NT threads (t = 0..NT-1) from row `row0` of a sequence of n > 0 rows; rows past its end repeat the last one
 // (no query sees them), pieces past the head's values repeat the first (they meet zeros, or go nowhere).
 template <int DP, int ROWS, int NT>
 struct Stage {
-  static constexpr int CPR = DP / 8, IT = ROWS * CPR / NT;
-  static_assert(ROWS * CPR % NT == 0, "whole rounds");
-  u32 off[IT];
-  int row[IT];
+  static constexpr int CPR = DP / 8, IT = ROWS * CPR / NT, STEP = NT / CPR;       // rows of a round
+  static constexpr bool EVEN = STEP % 16 == 0;                                    // every round's pieces lie alike
+  static_assert(ROWS * CPR % NT == 0 && NT % CPR == 0, "whole rounds of whole rows");
+  u32 off[EVEN ? 1 : IT];
+  int row;
   __device__ __forceinline__ void init(u32 t, u32 dim, int64_t stride) {
+    row = (int)t / CPR;
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      const int idx = i * NT + (int)t, r = idx / CPR;
-      int c = (idx % CPR) ^ swz<DP>(r);
+    for (int i = 0; i < (EVEN ? 1 : IT); ++i) {
+      const int r = i * STEP + row;
+      int c = ((int)t % CPR) ^ swz<DP>(r);
       if (c >= (int)(dim / 8)) c = 0;
-      row[i] = r;
       off[i] = (u32)(r * (int)stride + c * 8) * 2;
     }
   }
@@ -191,35 +223,71 @@ struct Stage {
     const char* base = (const char*)seq_base + (int64_t)row0 * stride * 2;
     if (row0 + ROWS <= n) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i) load_piece(base, off[i], lds + (u32)(i * NT * 16));
+      for (int i = 0; i < IT; ++i) {
+        if constexpr (EVEN) load_piece(base + (int64_t)(i * STEP) * stride * 2, off[0], lds + (u32)(i * NT * 16));
+        else load_piece(base, off[i], lds + (u32)(i * NT * 16));
+      }
     } else {
       const int last = n - 1 - row0;
 #pragma unroll
       for (int i = 0; i < IT; ++i) {
-        const u32 back = row[i] > last ? (u32)((row[i] - last) * (int)stride) * 2 : 0u;
-        load_piece(base, off[i] - back, lds + (u32)(i * NT * 16));
+        const int r = i * STEP + row, over = r > last ? r - last : 0;
+        const u32 at = EVEN ? off[0] + (u32)(i * STEP * (int)stride) * 2 : off[EVEN ? 0 : i];
+        load_piece(base, at - (u32)(over * (int)stride) * 2, lds + (u32)(i * NT * 16));
       }
     }
   }
 };
 
-// Fragment of rows r0..r0+31, values 16 ks.. of a tile: lane l holds row l % 32, values 16 ks + 8 (l / 32) + 0..7.
-template <class T, int DP>
-__device__ __forceinline__ typename Vec<T>::x8 frag_rows(const T* tile, int r0, int ks) {
-  const int l = (int)lane_id(), r = r0 + (l & 31);
-  return *(const typename Vec<T>::x8*)(tile + r * DP + (((2 * ks + (l >> 5)) ^ swz<DP>(r & 15)) << 3));
+// The same for a walk over tiles one behind the other, with nothing to multiply on the way: `at` is the next tile's place.
+template <int DP, int ROWS, int NT>
+struct Walk {
+  Stage<DP, ROWS, NT> st;
+  const char* at;
+  int64_t step;                    // bytes of a round's rows
+  static_assert(Stage<DP, ROWS, NT>::EVEN, "rounds of 16 rows");
+  __device__ __forceinline__ void init(u32 t, u32 dim, int64_t stride) { st.init(t, dim, stride); step = (int64_t)st.STEP * stride * 2; }
+  __device__ __forceinline__ void from(const void* seq_base, int64_t stride, int row0) { at = (const char*)seq_base + (int64_t)row0 * stride * 2; }
+  // n: rows from the tile's first to the sequence's end
+  __device__ __forceinline__ void load(int n, int64_t stride, u32 lds) {
+    if (n >= ROWS) {
+#pragma unroll
+      for (int i = 0; i < st.IT; ++i) { load_piece(at, st.off[0], lds + (u32)(i * NT * 16)); at += step; }
+    } else {
+#pragma unroll
+      for (int i = 0; i < st.IT; ++i) {
+        const int r = i * st.STEP + st.row, over = r > n - 1 ? r - (n - 1) : 0;
+        load_piece(at, st.off[0] + (u32)((i * st.STEP - over) * (int)stride) * 2, lds + (u32)(i * NT * 16));
+      }
+      at += st.IT * step;
+    }
+  }
+};
+
+// LDS addresses (of tiles that begin at a multiple of 256 bytes) as the places' exclusive or makes them: a base for all
+// fragments of a tile, and one operation for each.
+//   fragment of rows r0..r0+31, values 16 ks..: lane l holds row l % 32, values 16 ks + 8 (l / 32) + 0..7
+template <int DP>
+__device__ __forceinline__ u32 rows_base(u32 tile) {
+  const u32 l = lane_id();
+  return tile + (l & 31) * (DP * 2) + (((l >> 5) ^ (u32)swz<DP>((int)(l & 15))) << 4);
 }
-// Fragment of the transposed tile: lane l holds value 32 db + l % 32 of the rows k0 + 4 (l / 32) + 0..3 and the same + 8:
-// the order of rows in which the results of a product lie (one register group each), so that these feed the next product
-// as they are.
 template <class T, int DP>
-__device__ __forceinline__ typename Vec<T>::x8 frag_tr(const T* tile, int k0, int db) {
-  const int l = (int)lane_id(), h = l >> 5, r = (l & 15) >> 2;
-  const int c = 4 * db + 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
-  const int row = k0 + 4 * h + r;
-  const T* p0 = tile + row * DP + ((c ^ swz<DP>(row & 15)) << 3) + (l & 1) * 4;
-  const T* p1 = tile + (row + 8) * DP + ((c ^ swz<DP>((row + 8) & 15)) << 3) + (l & 1) * 4;
-  const typename Vec<T>::x4 a = Vec<T>::read_tr(p0), b = Vec<T>::read_tr(p1);
+__device__ __forceinline__ typename Vec<T>::x8 frag_rows(u32 base, int r0, int ks) {
+  typedef typename Vec<T>::x8 x8;
+  return *(__attribute__((address_space(3))) const x8*)(uintptr_t)((base ^ (u32)(ks << 5)) + (u32)(r0 * DP * 2));
+}
+//   fragment of the transposed tile: lane l holds value 32 db + l % 32 of the rows k0 + 4 (l / 32) + 0..3 and the same + 8: the
+//   order of rows in which the results of a product lie (one register group each), so that these feed the next product as they are
+template <int DP>
+__device__ __forceinline__ u32 cols_base(u32 tile) {
+  const u32 l = lane_id(), row = 4 * (l >> 5) + ((l & 15) >> 2), c = 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
+  return tile + row * (DP * 2) + ((c ^ (u32)swz<DP>((int)row)) << 4) + (l & 1) * 8;
+}
+template <class T, int DP>
+__device__ __forceinline__ typename Vec<T>::x8 frag_tr(u32 base, int k0, int db) {
+  const u32 at = base ^ (u32)(db << 6);
+  const typename Vec<T>::x4 a = Vec<T>::read_tr(at + (u32)(k0 * DP * 2)), b = Vec<T>::read_tr((at ^ 32) + (u32)((k0 + 8) * DP * 2));
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 // The row of a result's register r (0..15) in lane l.
@@ -260,6 +328,10 @@ __device__ __forceinline__ typename Vec<T>::x8 pack8(const f32x16& x, int s) {
   }
   return r;
 }
+
+// Products in groups of four with the fragments of the next group on their way from LDS.  The compiler left to itself puts each read right
+// before its product and has the wavefront wait for LDS every time; nothing moves over a line drawn by hold().
+__device__ __forceinline__ void hold() { __builtin_amdgcn_sched_barrier(0); }
 
 #define G10_NEG_INF (-__builtin_inff())
 #define G10_LOG2E 1.4426950408889634f

@@ -1,16 +1,65 @@
 // Attention, forward.
 #include "g10_attn.h"
 
-#define BM 128                     // queries of a workgroup, 32 to a wavefront
 #define BN 64                      // keys of a tile
 
-// Forward pass.  A wavefront holds 32 queries in registers and walks over the keys they see, 64 at a time, with the running
+// Forward pass.  A wavefront holds 32 queries in registers and walks over the keys they see, 64 at a time, with a running
 // maximum m and sum l of the softmax:  S = K Q^T,  P = 2^(S - m),  O^T = O^T 2^(m' - m) + V^T P.  S comes out transposed
 // (a lane holds one query's scores), so the row's maximum and sum are sums over registers and one exchange of the two halves,
 // and P feeds the second product as it lies in the registers.
-template <class T, int DP>
-__global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
-  __shared__ __attribute__((aligned(16))) T lds[2][2][BN * DP];
+// A tile's exponentials take the vector unit as long as its products take the matrix unit, so each wavefront works on both at
+// once: the scores of the next tile and the outputs of this one, product by product, with the exponentials of this tile
+// strewn between and the fragments of the products four ahead on their way from LDS.  hold() keeps the compiler from putting
+// these apart again.
+
+// The products of a tile, in order: NS of the next tile's scores (none if !NEXT), NV of this tile's outputs.
+template <class T, int DP, bool NEXT>
+__device__ __forceinline__ void tile_step(u32 tk, u32 tv, const typename Vec<T>::x8 (&q)[DP / 16], f32x16 (&sc)[2], f32x16 (&sn)[2],
+                                          f32x16 (&o)[DP / 32], float scale2, float base, float& l) {
+  typedef typename Vec<T>::x8 x8;
+  constexpr int NS = NEXT ? 2 * DP / 16 : 0, NV = 4 * DP / 32, N = NS + NV, KS = DP / 16, DB = DP / 32, AHEAD = 4, RING = 5;
+  // exponentials of the first 32 keys before the first output's product, of the others before the second half's
+  constexpr int EARLY = NEXT ? 20 : 16;
+  x8 f[RING], pf[4];
+  float sum[4] = {};
+  auto read = [&](int e) -> x8 {
+    return e < NS ? frag_rows<T, DP>(tk, e % 2 * 32, e / 2) : frag_tr<T, DP>(tv, (e - NS) / DB * 16, (e - NS) % DB);
+  };
+  auto exps = [&](int from, int to) {
+#pragma unroll
+    for (int x = from; x < to; ++x) {
+      const int n = x / 16, r = x % 16;
+      sc[n][r] = exp2_fast(sc[n][r] * scale2 - base);
+      sum[r & 3] += sc[n][r];
+      if (r % 8 == 7) pf[x / 8] = pack8<T>(sc[n], r / 8);
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < AHEAD; ++e) f[e % RING] = read(e);
+  hold();
+  if (!NEXT) { exps(0, EARLY); hold(); }
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if (e + AHEAD < N) f[(e + AHEAD) % RING] = read(e + AHEAD);
+    if (e < NS) {
+      if (e < 2) sn[e] = f32x16{};
+      sn[e % 2] = Vec<T>::mfma(f[e % RING], q[e / 2], sn[e % 2]);
+      exps(EARLY * e / (NS ? NS : 1), EARLY * (e + 1) / (NS ? NS : 1));
+    } else {
+      const int v = e - NS;
+      o[v % DB] = Vec<T>::mfma(f[e % RING], pf[v / DB], o[v % DB]);
+      if (v < NV / 2) exps(EARLY + (32 - EARLY) * v / (NV / 2), EARLY + (32 - EARLY) * (v + 1) / (NV / 2));
+    }
+    hold();
+  }
+  l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// NW wavefronts to a workgroup, 32 queries each.
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnArgs a) {
+  constexpr int BM = 32 * NW;
+  __shared__ __attribute__((aligned(256))) T lds[2][2][BN * DP];      // keys, values; even and odd tiles
   typedef typename Vec<T>::x8 x8;
   u32 unit, at;
   if (!unit_of(a.batch * a.kv_heads, a.group * a.tiles, unit, at)) return;
@@ -21,13 +70,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
   const T* Q = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2];
   const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
   const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
-  T* O = (T*)a.o + batch_off(a, b, a.os[0]) + s.q0 * a.os[1] + (int64_t)h * a.os[2];
-  float* L = a.lse + row_off(a, b, h, s);
-  Stage<DP, BN, 256> sk, sv;
+  Stage<DP, BN, 64 * NW> sk, sv;
   sk.init(threadIdx.x, a.dim, a.ks[1]);
   sv.init(threadIdx.x, a.dim, a.vs[1]);
-  const u32 lk[2] = {lds_addr(lds[0][0]) + wave * 1024, lds_addr(lds[1][0]) + wave * 1024};
-  const u32 lv[2] = {lds_addr(lds[0][1]) + wave * 1024, lds_addr(lds[1][1]) + wave * 1024};
+  const u32 lk = lds_addr(lds[0][0]) + wave * 1024, lv = lds_addr(lds[1][0]) + wave * 1024;
+  constexpr u32 odd = BN * DP * 2;
+  const u32 tk = rows_base<DP>(lds_addr(lds[0][0])), tv = cols_base<DP>(lds_addr(lds[1][0]));
   // (the last tiles of a causal sequence are the longest: first)
   for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BM < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BM + (int)wave * 32, i = i0 + (int)(lane & 31);
@@ -35,69 +83,81 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
     const int wp0 = i0 + off, wp1 = (i0 + 31 < s.nq ? i0 + 31 : s.nq - 1) + off;       // the wavefront's positions
     const int e1 = (qt + 1) * BM - 1 < s.nq ? (qt + 1) * BM - 1 : s.nq - 1;
     const Tiles tiles = key_tiles<BN>(a, qt * BM + off, e1 + off, s.nk);
-    x8 q[DP / 16];
-    frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
     f32x16 o[DP / 32] = {};
-    float m = G10_NEG_INF, l = 0.0f;
+    float m = G10_NEG_INF, l = 0.0f;                                 // m in powers of two
     if (tiles.count) {
-      __syncthreads();                                             // (the tiles before are read)
-      sk.load(K, a.ks[1], tiles.at(0) * BN, s.nk, lk[0]);
-      sv.load(V, a.vs[1], tiles.at(0) * BN, s.nk, lv[0]);
-    }
-    for (int t = 0; t < tiles.count; ++t) {
-      const int j0 = tiles.at(t) * BN, buf = t & 1;
+      x8 q[DP / 16];
+      frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
       loads_done();
-      __syncthreads();
-      if (t + 1 < tiles.count) {
-        sk.load(K, a.ks[1], tiles.at(t + 1) * BN, s.nk, lk[buf ^ 1]);
-        sv.load(V, a.vs[1], tiles.at(t + 1) * BN, s.nk, lv[buf ^ 1]);
-      }
-      const T *tk = lds[buf][0], *tv = lds[buf][1];
-      f32x16 sc[2] = {};
+      __syncthreads();                                               // (the tiles of the queries before are read)
+      sk.load(K, a.ks[1], tiles.at(0) * BN, s.nk, lk);
+      sv.load(V, a.vs[1], tiles.at(0) * BN, s.nk, lv);
+      f32x16 sa[2], sb[2];
+      // scores of a tile that are not seen leave; the maximum
+      auto settle = [&](f32x16(&sc)[2], int t) {
+        const int j0 = tiles.at(t) * BN;
+        if (!all_see(a, wp0, wp1, j0, j0 + BN - 1, s.nk)) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) sc[n] = Vec<T>::mfma(frag_rows<T, DP>(tk, 32 * n, ks), q[ks], sc[n]);
-      if (!all_see(a, wp0, wp1, j0, j0 + BN - 1, s.nk)) {
+            for (int r = 0; r < 16; ++r) sc[n][r] = seen.key(j0 + 32 * n + res_row(r)) ? sc[n][r] : G10_NEG_INF;
+        }
+        float top = sc[0][0];
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sc[n][r] = seen.key(j0 + 32 * n + res_row(r)) ? sc[n][r] : G10_NEG_INF;
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[n][r]);
+        top = both_max(top) * a.scale2;
+        // The sums stay relative to an older maximum until it is passed by more than 2^8: what is added then is below 2^8, far from
+        // any type's end, and most tiles leave the outputs as they are.
+        if (ballot(top > m + 8.0f)) {
+          const float now = fmaxf(m, top), fade = exp2_fast(m - (now == G10_NEG_INF ? 0.0f : now));
+          m = now;
+          l *= fade;
+#pragma unroll
+          for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[db][r] *= fade;
+        }
+      };
+      loads_done();
+      __syncthreads();
+      if (tiles.count > 1) sk.load(K, a.ks[1], tiles.at(1) * BN, s.nk, lk + odd);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        sa[n] = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ++ks) sa[n] = Vec<T>::mfma(frag_rows<T, DP>(tk, 32 * n, ks), q[ks], sa[n]);
       }
-      float top = sc[0][0];
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[n][r]);
-      top = fmaxf(m, both_max(top));
-      const float base = top == G10_NEG_INF ? 0.0f : top * a.scale2;
-      const float fade = exp2_fast(m * a.scale2 - base);
-      m = top;
-      float sum = 0.0f;
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          sc[n][r] = exp2_fast(sc[n][r] * a.scale2 - base);
-          sum += sc[n][r];
-        }
-      l = l * fade + both_sum(sum);
-#pragma unroll
-      for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[db][r] *= fade;
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const x8 pf = pack8<T>(sc[n], k);
-#pragma unroll
-          for (int db = 0; db < DP / 32; ++db) o[db] = Vec<T>::mfma(frag_tr<T, DP>(tv, 32 * n + 16 * k, db), pf, o[db]);
-        }
+      settle(sa, 0);
+      // tile t: its scores lie in sc; the next tile's keys and this one's values are in LDS, the ones behind them on their way
+      auto turn = [&](f32x16(&sc)[2], f32x16(&sn)[2], int t, u32 even, u32 other) {
+        loads_done();
+        __syncthreads();
+        if (t + 2 < tiles.count) sk.load(K, a.ks[1], tiles.at(t + 2) * BN, s.nk, lk + even);
+        sv.load(V, a.vs[1], tiles.at(t + 1) * BN, s.nk, lv + other);
+        tile_step<T, DP, true>(tk + other, tv + even, q, sc, sn, o, a.scale2, m == G10_NEG_INF ? 0.0f : m, l);
+        settle(sn, t + 1);
+      };
+      int t = 0;
+      for (; t + 2 < tiles.count; t += 2) {
+        turn(sa, sb, t, 0, odd);
+        turn(sb, sa, t + 1, odd, 0);
+      }
+      if (t + 1 < tiles.count) {
+        turn(sa, sb, t, 0, odd);
+        sa[0] = sb[0];
+        sa[1] = sb[1];
+        ++t;
+      }
+      loads_done();
+      __syncthreads();
+      tile_step<T, DP, false>(0, tv + (t & 1 ? odd : 0), q, sa, sb, o, a.scale2, m == G10_NEG_INF ? 0.0f : m, l);
     }
+    l = both_sum(l);
     if (i < s.nq) {
+      T* out = (T*)a.o + batch_off(a, b, a.os[0]) + (s.q0 + i) * a.os[1] + (int64_t)h * a.os[2];
       const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;  // (l is NaN where a score is)
-      T* out = O + (int64_t)i * a.os[1];
 #pragma unroll
       for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
@@ -110,7 +170,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(const AttnArgs a) {
             *(typename Vec<T>::x4*)(out + d) = w;
           }
         }
-      if (lane < 32) L[i] = l > 0.0f ? (m * a.scale2 + __log2f(l)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
+      if (lane < 32) (a.lse + row_off(a, b, h, s))[i] = l > 0.0f ? (m + __log2f(l)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
     }
   }
 }
@@ -179,16 +239,20 @@ extern "C" int g10_attention(const g10_attention_args* g, void* workspace, uint6
     if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return G10_EINVAL;
     return attn_forward_split(a, splits, workspace, g->type, s);
   }
-  a.tiles = (a.max_q + BM - 1) / BM;
+#ifndef NWX
+#define NWX 4
+#endif
+  const u32 nw = NWX;
+  a.tiles = (a.max_q + 32 * nw - 1) / (32 * nw);
   const uint64_t per = (uint64_t)a.group * a.tiles, units = (uint64_t)a.batch * a.kv_heads;
   if ((units + 7) * per >= (1ull << 31)) return G10_EINVAL;
   const dim3 grid(unit_grid((u32)units, (u32)per));
   if (g->type == G10_BF16) {
-    if (a.dim <= 64) k_attn_fwd<__bf16, 64><<<grid, 256, 0, s>>>(a);
-    else k_attn_fwd<__bf16, 128><<<grid, 256, 0, s>>>(a);
+    if (a.dim <= 64) k_attn_fwd<__bf16, 64, NWX><<<grid, 64 * nw, 0, s>>>(a);
+    else k_attn_fwd<__bf16, 128, NWX><<<grid, 64 * nw, 0, s>>>(a);
   } else {
-    if (a.dim <= 64) k_attn_fwd<_Float16, 64><<<grid, 256, 0, s>>>(a);
-    else k_attn_fwd<_Float16, 128><<<grid, 256, 0, s>>>(a);
+    if (a.dim <= 64) k_attn_fwd<_Float16, 64, NWX><<<grid, 64 * nw, 0, s>>>(a);
+    else k_attn_fwd<_Float16, 128, NWX><<<grid, 64 * nw, 0, s>>>(a);
   }
   G10_HIP(hipGetLastError());
   return G10_OK;

@@ -4,7 +4,7 @@
 // no atomics, and nothing of the size of the scores in memory.
 #include "g10_attn.h"
 
-#define BT 64                      // rows of a staged tile
+#define BT 64                      // rows of a tile in LDS
 #define BW 128                     // rows of a workgroup, 32 to a wavefront
 
 // In 16-bit floats with a short exponent, P and dS of long rows would fall below the smallest number.  P is held times
@@ -49,129 +49,263 @@ __global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a, u64 rows, 
   }
 #pragma unroll
   for (int d = 8; d; d /= 2) sum += __shfl_xor(sum, d, 16);
-  if (row < rows && !c) ((float*)a.delta)[at] = sum;
+  if (row < rows && !c) {
+    ((float*)a.delta)[at] = sum;
+    const float l = a.lse[at];                                       // (a query that sees no key: its probabilities are to be 0)
+    ((float*)a.lse2)[at] = l == G10_NEG_INF ? -l : l * G10_LOG2E - Lift<T>::p2;
+  }
   if (amax) {
     const u32 top = wave_max(__float_as_uint(big));
     if (!lane_id() && top > __hip_atomic_load(amax, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(amax, top);
   }
 }
 
+// A workgroup's unit, first tile of keys and part of the queries: the parts of the sinks' tiles first, of all units, then a
+// unit's other tiles together.
+__device__ __forceinline__ bool tile_of(const AttnArgs& a, u32& unit, u32& kt, u32& part) {
+  const u32 units = a.batch * a.kv_heads, ahead = a.sink_tiles * a.splits, rest = a.tiles - a.sink_tiles;
+  const bool round = units % 8 == 0 || units >= 64;                  // (as in unit_of)
+  const u32 slot = round ? blockIdx.x / 8 : blockIdx.x, mine = round ? (units + 7) / 8 : units;
+  u32 u, at;
+  if (slot < mine * ahead) {
+    u = slot % mine;
+    at = slot / mine;
+    kt = at / a.splits;
+    part = at % a.splits;
+  } else {
+    u = (slot - mine * ahead) / rest;
+    kt = a.sink_tiles + (slot - mine * ahead) % rest;
+    part = 0;
+  }
+  unit = round ? blockIdx.x % 8 + 8 * u : u;
+  return unit < units;
+}
+
 // Gradients of 128 keys and values, 32 to a wavefront, which holds their rows and sums in registers and walks over the
-// queries that see them, of all heads of the group:  S = Q K^T,  dP = dO V^T  come out with a key to a lane;
-// dV^T += dO^T P,  dK^T += Q^T dS  read the tiles of queries once more, transposed.
+// queries that see them, of all heads of the group, 32 at a time:
+//   S = Q K^T,  P = 2^(S - lse),  dP = dO V^T,  dS = P (dP - delta),  dV^T += dO^T P,  dK^T += Q^T dS
+// The first products come out with a key to a lane and feed the second ones as they lie.  A wavefront has a SIMD's registers to
+// itself (in heads of 64 values: half of them), so nobody else's work fills its waits: it works on the next 32 queries' first
+// products and these ones' second ones, product by product, with these ones' exponentials strewn between and the fragments four
+// ahead on their way from LDS.  Tiles of 64 queries: this one, the next, and the one on its way from memory.
+// A tile with sinks is seen by all later queries, the others by those of a window: the sinks' are worked on by several workgroups,
+// the first ones to start, whose sums meet in k_attn_sinks.
+struct Half { u32 rows, cols, stats; };                              // LDS addresses of 32 queries of a tile: rows_base and cols_base of Q, with dO a tile behind it; lse2 and delta
+
+// In: the tile's scores and dP in sc and dp.  Out: the next tile's.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_dkdv(const AttnArgs a) {
-  __shared__ __attribute__((aligned(16))) T lds[2][2][BT * DP];
-  __shared__ float row_lse[2][BT], row_delta[2][BT];
+__device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const typename Vec<T>::x8 (&kf)[DP / 16], const typename Vec<T>::x8 (&vf)[DP / 16],
+                                          f32x16& sc, f32x16& dp, f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], float scale2, float lift_ds) {
   typedef typename Vec<T>::x8 x8;
-  u32 unit, at;
-  if (!unit_of(a.batch * a.kv_heads, a.tiles, unit, at)) return;
+  constexpr int KS = DP / 16, DB = DP / 32, N = 2 * KS + 4 * DB, AHEAD = 4, RING = 5;
+  x8 f[RING], pf[2], df[2];
+  auto read = [&](int e) -> x8 {
+    if (e < 2 * KS) return frag_rows<T, DP>(nx.rows, e % 2 * BT, e / 2);
+    e -= 2 * KS;
+    return frag_tr<T, DP>(cu.cols, (e < 2 * DB ? BT : -32) + e / DB * 16, e % DB);
+  };
+  // four queries' lse2 (k = 0..3) or delta (k = 4..7), read one group ahead
+  f32x4 row[2];
+  auto row_read = [&](int k) { row[k & 1] = *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(cu.stats + (u32)(k / 4 * (BT * 4) + k % 4 * 32)); };
+  auto exps = [&](int from, int to) {
+#pragma unroll
+    for (int r = from; r < to; ++r) {
+      if (r % 4 == 0) row_read(r / 4 + 1);
+      sc[r] = exp2_fast(sc[r] * scale2 - row[r / 4 & 1][r % 4]);
+      if (r % 8 == 7) pf[r / 8] = pack8<T>(sc, r / 8);
+    }
+  };
+  auto grads = [&](int from, int to) {
+#pragma unroll
+    for (int r = from; r < to; ++r) {
+      if (r % 4 == 0 && r < 12) row_read(r / 4 + 5);
+      dp[r] = sc[r] * ((dp[r] - row[r / 4 & 1][r % 4]) * lift_ds);
+      if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
+    }
+  };
+  row_read(0);
+#pragma unroll
+  for (int e = 0; e < AHEAD; ++e) f[e % RING] = read(e);
+  f32x16 sn = {}, dn = {};
+  hold();
+  each_of<0, N>([&](auto step) __attribute__((always_inline)) {
+    constexpr int e = decltype(step)::value;
+    if constexpr (e + AHEAD < N) f[(e + AHEAD) % RING] = read(e + AHEAD);
+    if constexpr (e < 2 * KS) {                                      // (in turn: a product on the sums of the one before would wait for it)
+      if constexpr (e % 2 == 0) sn = Vec<T>::mfma(f[e % RING], kf[e / 2], sn);
+      else dn = Vec<T>::mfma(f[e % RING], vf[e / 2], dn);
+      if constexpr (e < KS) exps(16 * e / KS, 16 * (e + 1) / KS);
+      else grads(16 * (e - KS) / KS, 16 * (e - KS + 1) / KS);
+    } else {
+      constexpr int v = e - 2 * KS;
+      if constexpr (v < 2 * DB) dv[v % DB] = Vec<T>::mfma(f[e % RING], pf[v / DB], dv[v % DB]);
+      else dk[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB - 2], dk[v % DB]);
+#pragma unroll
+      for (int r = 16 * v / (4 * DB); r < 16 * (v + 1) / (4 * DB); ++r) { sc[r] = sn[r]; dp[r] = dn[r]; }
+    }
+    hold();
+  });
+}
+
+template <class T, int DP>
+__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnArgs a) {
+  __shared__ __attribute__((aligned(256))) T lds[3][2][BT * DP];
+  __shared__ __attribute__((aligned(16))) float rows[3][2][BT];      // lse2, delta of a tile's queries
+  typedef typename Vec<T>::x8 x8;
+  u32 unit, kt0, part;
+  if (!tile_of(a, unit, kt0, part)) return;
   const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads;
   const Seq s = seq_of(a, b);
-  const int off = s.nk - s.nq;
   const u32 wave = uniform(wave_id()), lane = lane_id();
-  const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
-  const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
-  T* dK = (T*)a.dk + batch_off(a, b, a.dks[0]) + s.k0 * a.dks[1] + (int64_t)hk * a.dks[2];
-  T* dV = (T*)a.dv + batch_off(a, b, a.dvs[0]) + s.k0 * a.dvs[1] + (int64_t)hk * a.dvs[2];
+  const T* Q0 = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)hk * a.group * a.qs[2];
+  const T* D0 = (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)hk * a.group * a.dos[2];
   const int nk_all = a.q_start ? s.nk : (int)a.seq_k;                // rows of dk and dv to be written
-  Stage<DP, BT, 256> sq, sd;
+  Walk<DP, BT, 256> sq, sd;
   sq.init(threadIdx.x, a.dim, a.qs[1]);
   sd.init(threadIdx.x, a.dim, a.dos[1]);
-  const u32 lq[2] = {lds_addr(lds[0][0]) + wave * 1024, lds_addr(lds[1][0]) + wave * 1024};
-  const u32 ld[2] = {lds_addr(lds[0][1]) + wave * 1024, lds_addr(lds[1][1]) + wave * 1024};
+  const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024, rows0 = lds_addr(rows[0]);
   const float lift = Lift<T>::ds(a.amax), lift_ds = lift / Lift<T>::p;
-  for (int kt = (int)(at % a.tiles); kt * BW < nk_all; kt += (int)a.tiles) {
+  for (int kt = (int)kt0; kt * BW < nk_all; kt += (int)a.tiles) {
+    const bool shared = (u32)kt < a.sink_tiles;
+    if (!shared && part) break;
     const int j0 = kt * BW + (int)wave * 32, j = j0 + (int)(lane & 31);
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
     int lo = 0, hi = -1;                                             // queries that see any key of the workgroup
     const int e1 = (kt + 1) * BW < s.nk ? (kt + 1) * BW - 1 : s.nk - 1;
     if (kt * BW < s.nk) query_range(a, kt * BW, e1, s, lo, hi);
-    if (hi >= lo) {
+    const int first = lo / 32 * 32, each = hi >= lo ? (hi - first) / BT + 1 : 0;      // tiles of queries ...
+    int from = 0, all = each * (int)a.group;                         // ... of all heads one after the other
+    if (shared) {
+      from = (int)((int64_t)all * part / a.splits);
+      all = (int)((int64_t)all * (part + 1) / a.splits) - from;
+    }
+    if (all > 0) {
       const int wj1 = j0 + 31 < s.nk ? j0 + 31 : s.nk - 1;
-      int wlo = 0, whi = -1, ilo = 0, ihi = -1;                      // ... of the wavefront, of the lane
+      int wlo = 0, whi = -1, ilo = 0, ihi = -1, flo, fhi;            // ... of the wavefront, of the lane; that see all of the wavefront's keys
       if (j0 < s.nk) query_range(a, j0, wj1, s, wlo, whi);
       if (j < s.nk) query_range(a, j, j, s, ilo, ihi);
+      full_range(a, j0, j0 + 31, s, flo, fhi);
       const u32 span = ihi >= ilo ? (u32)(ihi - ilo + 1) : 0u;
-      x8 kf[DP / 16], vf[DP / 16];
-      frags_global<T, DP>(kf, K, a.ks[1], j, s.nk - 1, a.dim);
-      frags_global<T, DP>(vf, V, a.vs[1], j, s.nk - 1, a.dim);
-      const int t0 = lo / BT, nt = hi / BT - t0 + 1, all = nt * (int)a.group;
-      float mine = 0.0f;
-      // what the thread brings of a tile's lse and delta
-      auto fetch = [&](int t) {
-        const u32 h = hk * a.group + (u32)(t / nt);
-        const int i0 = (t0 + t % nt) * BT;
-        const T* Q = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2];
-        const T* D = (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)h * a.dos[2];
-        sq.load(Q, a.qs[1], i0, s.nq, lq[t & 1]);
-        sd.load(D, a.dos[1], i0, s.nq, ld[t & 1]);
-        if (threadIdx.x < 2 * BT) {
-          const int i = i0 + (int)(threadIdx.x % BT), c = i < s.nq ? i : s.nq - 1;
-          const int64_t r = row_off(a, b, h, s) + c;
-          mine = threadIdx.x < BT ? a.lse[r] : a.delta[r];
+      const int head = from / each;
+      int fi = first + from % each * BT, cur = fi;                   // first query of the tile to be fetched, of this tile
+      const T *Q = Q0 + head * a.qs[2], *D = D0 + head * a.dos[2];   // of the head to be fetched
+      const float* L = (wave == 0 ? a.lse2 : a.delta) + row_off(a, b, hk * a.group + (u32)head, s) + lane;
+      sq.from(Q, a.qs[1], fi);
+      sd.from(D, a.dos[1], fi);
+      u32 to = 0;                                                    // buffer of the next tile to be fetched
+      auto fetch = [&]() {
+        const u32 at = tile0 + to * (2 * BT * DP * 2);
+        sq.load(s.nq - fi, a.qs[1], at);
+        sd.load(s.nq - fi, a.dos[1], at + BT * DP * 2);
+        if (wave < 2) load_words(L + (fi + (int)lane < s.nq ? fi : s.nq - 1 - (int)lane), rows0 + (2 * to + wave) * (BT * 4));
+        to = to == 2 ? 0 : to + 1;
+        fi += BT;
+        if (fi > hi) {                                               // the next head of the group
+          fi = first;
+          Q += a.qs[2];
+          D += a.dos[2];
+          L += a.seq_q;
+          sq.from(Q, a.qs[1], first);
+          sd.from(D, a.dos[1], first);
         }
       };
+      x8 kf[DP / 16], vf[DP / 16];
+      frags_global<T, DP>(kf, (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2], a.ks[1], j, s.nk - 1, a.dim);
+      frags_global<T, DP>(vf, (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2], a.vs[1], j, s.nk - 1, a.dim);
+      loads_done();
       __syncthreads();
-      fetch(0);
-      for (int t = 0; t < all; ++t) {
-        const int i0 = (t0 + t % nt) * BT, buf = t & 1;
-        loads_done();
-        if (threadIdx.x < BT) row_lse[buf][threadIdx.x] = mine * G10_LOG2E - Lift<T>::p2;
-        else if (threadIdx.x < 2 * BT) row_delta[buf][threadIdx.x - BT] = mine;
-        __syncthreads();
-        if (t + 1 < all) fetch(t + 1);
-        if (whi < i0 || wlo >= i0 + BT) continue;
-        const T *tq = lds[buf][0], *td = lds[buf][1];
+      fetch();
+      if (all > 1) fetch();
+      const u32 rb = rows_base<DP>(lds_addr(lds[0][0])), cb = cols_base<DP>(lds_addr(lds[0][0])), lb = rows0 + 16 * (lane >> 5);
+      auto half = [&](u32 buf, u32 n) {
+        return Half{rb + buf * (2 * BT * DP * 2) + n * (32 * DP * 2), cb + buf * (2 * BT * DP * 2) + n * (32 * DP * 2), lb + buf * (2 * BT * 4) + n * 128};
+      };
+      f32x16 sc = {}, dp = {};
+      loads_done();
+      __syncthreads();
 #pragma unroll
-        for (int n = 0; n < BT / 32; ++n) {
-          f32x16 sc = {}, dp = {};
+      for (int ks = 0; ks < DP / 16; ++ks) sc = Vec<T>::mfma(frag_rows<T, DP>(rb, 0, ks), kf[ks], sc);
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) sc = Vec<T>::mfma(frag_rows<T, DP>(tq, 32 * n, ks), kf[ks], sc);
+      for (int ks = 0; ks < DP / 16; ++ks) dp = Vec<T>::mfma(frag_rows<T, DP>(rb, BT, ks), vf[ks], dp);
+      u32 buf = 0, n = 0;                                            // this tile's buffer; its half
+      int t = 0;
+#pragma nounroll
+      while (t < all) {
+        if (!n) {                                                    // this tile and the next are there; the one behind them goes where the one before lay
+          loads_done();
+          __syncthreads();
+          if (t + 2 < all) fetch();
+        }
+        if (!(cur >= flo && cur + 31 <= fhi)) {                      // not all queries see all keys
+          const int at = cur + 4 * (int)(lane >> 5) - ilo;
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) dp = Vec<T>::mfma(frag_rows<T, DP>(td, 32 * n, ks), vf[ks], dp);
-          const bool full = j0 + 31 < s.nk && i0 + 32 * n + 31 < s.nq &&
-                            all_see(a, i0 + 32 * n + off, i0 + 32 * n + 31 + off, j0, j0 + 31, s.nk);
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const f32x4 le = *(const f32x4*)&row_lse[buf][32 * n + 8 * g + 4 * (lane >> 5)];
-            const f32x4 de = *(const f32x4*)&row_delta[buf][32 * n + 8 * g + 4 * (lane >> 5)];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              float p = exp2_fast(sc[4 * g + r] * a.scale2 - le[r]);
-              if (!full) p = (u32)(i0 + 32 * n + 8 * g + 4 * (int)(lane >> 5) + r - ilo) < span ? p : 0.0f;
-              sc[4 * g + r] = p;
-              dp[4 * g + r] = full || p != 0.0f ? p * (dp[4 * g + r] - de[r]) * lift_ds : 0.0f;
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const x8 pf = pack8<T>(sc, k), df = pack8<T>(dp, k);
-#pragma unroll
-            for (int db = 0; db < DP / 32; ++db) {
-              dv[db] = Vec<T>::mfma(frag_tr<T, DP>(td, 32 * n + 16 * k, db), pf, dv[db]);
-              dk[db] = Vec<T>::mfma(frag_tr<T, DP>(tq, 32 * n + 16 * k, db), df, dk[db]);
-            }
+          for (int r = 0; r < 16; ++r) {
+            const bool seen = (u32)(at + 8 * (r / 4) + r % 4) < span;
+            sc[r] = seen ? sc[r] : G10_NEG_INF;
+            dp[r] = seen ? dp[r] : 0.0f;                             // (what no query sees may hold anything)
           }
         }
+        const Half here = half(buf, n);
+        cur += 32;
+        if (n || cur > hi) {                                         // the tile's last
+          n = 0;
+          ++t;
+          buf = buf == 2 ? 0 : buf + 1;
+          if (cur > hi) cur = first;
+        } else n = 1;
+        back_step<T, DP>(here, half(buf, n), kf, vf, sc, dp, dk, dv, a.scale2, lift_ds);
       }
     }
-    if (j < nk_all) {
-      const float fk = a.scale / lift, fv = 1.0f / Lift<T>::p;
+    const float fk = a.scale / lift, fv = 1.0f / Lift<T>::p;
+    if (shared) {
+      float* to = a.part + (((u64)unit * a.sink_tiles + (u32)kt) * a.splits + part) * (2 * BW * DP) + ((int)wave * 32 + (int)(lane & 31)) * DP;
 #pragma unroll
-      for (int db = 0; db < DP / 32; ++db)
+      for (int x = 0; x < DP / 32; ++x)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const int d = 32 * db + 8 * g + 4 * (int)(lane >> 5);
-          if (d < (int)a.dim) {
-            typename Vec<T>::x4 x, y;
+          const int d = 32 * x + 8 * g + 4 * (int)(lane >> 5);
+          *(f32x4*)(to + d) = f32x4{dv[x][4 * g], dv[x][4 * g + 1], dv[x][4 * g + 2], dv[x][4 * g + 3]} * fv;
+          *(f32x4*)(to + BW * DP + d) = f32x4{dk[x][4 * g], dk[x][4 * g + 1], dk[x][4 * g + 2], dk[x][4 * g + 3]} * fk;
+        }
+    } else if (j < nk_all) {
+      T* dK = (T*)a.dk + batch_off(a, b, a.dks[0]) + (s.k0 + j) * a.dks[1] + (int64_t)hk * a.dks[2];
+      T* dV = (T*)a.dv + batch_off(a, b, a.dvs[0]) + (s.k0 + j) * a.dvs[1] + (int64_t)hk * a.dvs[2];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) { x[r] = (T)(dk[db][4 * g + r] * fk); y[r] = (T)(dv[db][4 * g + r] * fv); }
-            *(typename Vec<T>::x4*)(dK + (int64_t)j * a.dks[1] + d) = x;
-            *(typename Vec<T>::x4*)(dV + (int64_t)j * a.dvs[1] + d) = y;
+      for (int x = 0; x < DP / 32; ++x)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int d = 32 * x + 8 * g + 4 * (int)(lane >> 5);
+          if (d < (int)a.dim) {
+            typename Vec<T>::x4 y, z;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { y[r] = (T)(dk[x][4 * g + r] * fk); z[r] = (T)(dv[x][4 * g + r] * fv); }
+            *(typename Vec<T>::x4*)(dK + d) = y;
+            *(typename Vec<T>::x4*)(dV + d) = z;
           }
         }
     }
+  }
+}
+
+// The sums of a tile of sinks' workgroups, joined in their order.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
+  const u32 unit = blockIdx.x / a.sink_tiles, kt = blockIdx.x % a.sink_tiles, b = unit / a.kv_heads, hk = unit % a.kv_heads;
+  const bool key = blockIdx.y & 1;
+  const Seq s = seq_of(a, b);
+  const int nk_all = a.q_start ? s.nk : (int)a.seq_k;
+  const float* from = a.part + (((u64)unit * a.sink_tiles + kt) * a.splits * 2 + key) * (BW * DP);
+  T* out = key ? (T*)a.dk + batch_off(a, b, a.dks[0]) + s.k0 * a.dks[1] + (int64_t)hk * a.dks[2]
+               : (T*)a.dv + batch_off(a, b, a.dvs[0]) + s.k0 * a.dvs[1] + (int64_t)hk * a.dvs[2];
+  for (u32 e = blockIdx.y / 2 * 256 + threadIdx.x; e < BW * DP / 4; e += 4 * 256) {
+    const int j = (int)(kt * BW + e / (DP / 4)), d = (int)(e % (DP / 4)) * 4;
+    if (j >= nk_all || d >= (int)a.dim) continue;
+    f32x4 x = *(const f32x4*)(from + 4 * e);
+    for (u32 k = 1; k < a.splits; ++k) x += *(const f32x4*)(from + (u64)k * 2 * BW * DP + 4 * e);
+    typename Vec<T>::x4 y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = (T)x[r];
+    *(typename Vec<T>::x4*)(out + (int64_t)j * (key ? a.dks[1] : a.dvs[1]) + d) = y;
   }
 }
 
@@ -179,7 +313,7 @@ __global__ __launch_bounds__(256) void k_attn_dkdv(const AttnArgs a) {
 // to a lane;  dQ^T += K^T dS^T.
 template <class T, int DP>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
-  __shared__ __attribute__((aligned(16))) T lds[2][2][BT * DP];
+  __shared__ __attribute__((aligned(256))) T lds[2][2][BT * DP];
   typedef typename Vec<T>::x8 x8;
   u32 unit, at;
   if (!unit_of(a.batch * a.kv_heads, a.group * a.tiles, unit, at)) return;
@@ -208,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
     frags_global<T, DP>(dout, D, a.dos[1], i, s.nq - 1, a.dim);
     const int64_t r0 = row_off(a, b, h, s) + (i < s.nq ? i : s.nq - 1);
-    const float le = a.lse[r0] * G10_LOG2E, de = a.delta[r0];
+    const float le = a.lse2[r0] + Lift<T>::p2, de = a.delta[r0];
     f32x16 dq[DP / 32] = {};
     if (tiles.count) {
       __syncthreads();
@@ -223,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         sk.load(K, a.ks[1], tiles.at(t + 1) * BT, s.nk, lk[buf ^ 1]);
         sv.load(V, a.vs[1], tiles.at(t + 1) * BT, s.nk, lv[buf ^ 1]);
       }
-      const T *tk = lds[buf][0], *tv = lds[buf][1];
+      const u32 tk = rows_base<DP>(lds_addr(lds[buf][0])), tv = rows_base<DP>(lds_addr(lds[buf][1])), tc = cols_base<DP>(lds_addr(lds[buf][0]));
       const bool full = all_see(a, wp0, wp1, j0, j0 + BT - 1, s.nk);
 #pragma unroll
       for (int n = 0; n < BT / 32; ++n) {
@@ -242,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         for (int k = 0; k < 2; ++k) {
           const x8 df = pack8<T>(dp, k);
 #pragma unroll
-          for (int db = 0; db < DP / 32; ++db) dq[db] = Vec<T>::mfma(frag_tr<T, DP>(tk, 32 * n + 16 * k, db), df, dq[db]);
+          for (int db = 0; db < DP / 32; ++db) dq[db] = Vec<T>::mfma(frag_tr<T, DP>(tc, 32 * n + 16 * k, db), df, dq[db]);
         }
       }
     }
@@ -269,11 +403,36 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
 // ---------------------------------------------------------------------------------------------------------------------
 static uint64_t rows_of(const AttnArgs& a) { return (uint64_t)(a.q_start ? 1 : a.batch) * a.heads * a.seq_q; }
 
+static uint64_t pad256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+// How the queries of a sinks' tile are shared: so many workgroups that each has about as many queries as a tile of the window.
+// (Packed sequences go by twice their mean length, which is known here; max_q only cuts the grid.)  At most 256 MB of sums.
+static void share_sinks(AttnArgs& a) {
+  a.sink_tiles = 0;
+  a.splits = 1;
+  if (!a.window || !a.sinks || !a.seq_q || !a.seq_k || !a.batch) return;
+  const uint64_t nq = a.q_start ? 2 * (((uint64_t)a.seq_q + a.batch - 1) / a.batch) : a.seq_q;
+  const uint64_t near = (uint64_t)a.window * (a.causal ? 1 : 2) + BW;
+  const uint64_t tiles = ((a.q_start ? a.seq_k : a.max_k) + BW - 1) / BW, units = (uint64_t)a.batch * a.kv_heads;
+  uint64_t n = (nq + near - 1) / near, sink_tiles = ((uint64_t)a.sinks + BW - 1) / BW;
+  if (n > 16) n = 16;
+  if (sink_tiles > tiles) sink_tiles = tiles;
+  const uint64_t each = units * sink_tiles * 2 * BW * (a.dim <= 64 ? 64 : 128) * 4, most = (256ull << 20) / each;
+  if (n > most) n = most;
+  if (n < 2) return;
+  a.sink_tiles = (u32)sink_tiles;
+  a.splits = (u32)n;
+}
+static uint64_t sink_bytes(const AttnArgs& a) {
+  return a.sink_tiles ? (uint64_t)a.batch * a.kv_heads * a.sink_tiles * a.splits * 2 * BW * (a.dim <= 64 ? 64 : 128) * 4 : 0;
+}
+
 extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uint64_t* bytes) {
   if (!bytes) return G10_EINVAL;
   AttnArgs a;
   G10_TRY(attn_args(g, true, a));
-  *bytes = rows_of(a) * 4 + 256;                                     // delta, the largest |do|
+  share_sinks(a);
+  *bytes = 256 + pad256(rows_of(a) * 8) + sink_bytes(a);             // the largest |do|; delta, lse2; sums of the sinks' tiles
   return G10_OK;
 }
 
@@ -282,12 +441,15 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   G10_TRY(attn_args(g, true, a));
   if (!a.batch) return G10_OK;
   const uint64_t rows = rows_of(a), units = (uint64_t)a.batch * a.kv_heads;
-  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < rows * 4 + 256) return G10_EINVAL;
-  const uint64_t qt = (a.max_q + BW - 1) / BW, kt = (a.max_k + BW - 1) / BW;
-  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * kt >= (1ull << 31) || rows / 16 >= (1ull << 31) - 1) return G10_EINVAL;
+  share_sinks(a);
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < 256 + pad256(rows * 8) + sink_bytes(a)) return G10_EINVAL;
+  const uint64_t qt = (a.max_q + BW - 1) / BW, kt0 = (a.max_k + BW - 1) / BW, kt = kt0 > a.sink_tiles ? kt0 : a.sink_tiles;
+  const uint64_t per = kt + (uint64_t)a.sink_tiles * (a.splits - 1);
+  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * per >= (1ull << 31) || rows / 16 >= (1ull << 31) - 1) return G10_EINVAL;
   hipStream_t s = (hipStream_t)hip_stream;
   a.amax = (const u32*)workspace;
   a.delta = (const float*)((char*)workspace + 256);
+  a.lse2 = a.delta + rows;
   u32* const amax = g->type == G10_F16 ? (u32*)workspace : nullptr;
   if (amax) k_attn_clear<<<1, 1, 0, s>>>(amax);
   if (rows) {
@@ -298,11 +460,19 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
   if (kt) {
     a.tiles = (u32)kt;
-    const dim3 grid(unit_grid((u32)units, a.tiles));
+    a.part = (float*)((char*)workspace + 256 + pad256(rows * 8));
+    const dim3 grid(unit_grid((u32)units, (u32)per));
     if (bf && narrow) k_attn_dkdv<__bf16, 64><<<grid, 256, 0, s>>>(a);
     else if (bf) k_attn_dkdv<__bf16, 128><<<grid, 256, 0, s>>>(a);
     else if (narrow) k_attn_dkdv<_Float16, 64><<<grid, 256, 0, s>>>(a);
     else k_attn_dkdv<_Float16, 128><<<grid, 256, 0, s>>>(a);
+  }
+  if (kt && a.sink_tiles) {
+    const dim3 grid((u32)units * a.sink_tiles, 8);
+    if (bf && narrow) k_attn_sinks<__bf16, 64><<<grid, 256, 0, s>>>(a);
+    else if (bf) k_attn_sinks<__bf16, 128><<<grid, 256, 0, s>>>(a);
+    else if (narrow) k_attn_sinks<_Float16, 64><<<grid, 256, 0, s>>>(a);
+    else k_attn_sinks<_Float16, 128><<<grid, 256, 0, s>>>(a);
   }
   if (qt) {
     a.tiles = (u32)qt;

@@ -22,7 +22,7 @@ __device__ __forceinline__ Piece piece_of(const AttnArgs& a, u32 b, const Seq& s
 template <class T, int DP>
 __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
   // [wavefront][buffer][keys, values]; afterwards the wavefronts' outputs
-  __shared__ __attribute__((aligned(16))) T lds[SW][2][2][ST * DP];
+  __shared__ __attribute__((aligned(256))) T lds[SW][2][2][ST * DP];
   __shared__ float ms[SW][32], ls[SW][32];
   typedef typename Vec<T>::x8 x8;
   const u32 wave = uniform(wave_id()), lane = lane_id();
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
         sk.load(K, a.ks[1], tiles.at(t + SW) * ST, s.nk, lk[buf ^ 1]);
         sv.load(V, a.vs[1], tiles.at(t + SW) * ST, s.nk, lv[buf ^ 1]);
       }
-      const T *tk = lds[wave][buf][0], *tv = lds[wave][buf][1];
+      const u32 tk = rows_base<DP>(lk[buf]), tv = cols_base<DP>(lv[buf]);
       f32x16 sc = {};
 #pragma unroll
       for (int ks = 0; ks < DP / 16; ++ks) sc = Vec<T>::mfma(frag_rows<T, DP>(tk, 0, ks), q[ks], sc);

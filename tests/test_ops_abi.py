@@ -102,7 +102,7 @@ def attention_args(**kw):
 def test_attention_refuses(bad):
     lib, n = ops._load(), C.c_uint64()
     assert lib.g10_attention_workspace(C.byref(attention_args()), C.byref(n)) == 0
-    assert lib.g10_attention_backward_workspace(C.byref(attention_args()), C.byref(n)) == 0 and n.value == 2 * 4 * 8 * 4 + 256
+    assert lib.g10_attention_backward_workspace(C.byref(attention_args()), C.byref(n)) == 0 and n.value == 2 * 4 * 8 * 8 + 256
     assert lib.g10_attention(C.byref(attention_args(**bad)), 4096, 1 << 40, None) == binding.EINVAL
     assert lib.g10_attention_backward(C.byref(attention_args(**bad)), 4096, 1 << 40, None) == binding.EINVAL
 
