@@ -51,7 +51,7 @@ struct AttnArgs {
   float* lse;
   const float* delta;              // backward: sum of do * o per query
   const float* lse2;               // backward: lse in powers of two, less the lift of P
-  const u32* amax;                 // backward: bits of the largest |do|
+  const u32* amax;                 // backward: bits of the largest |do| of each sequence and head
   float *part, *part_ml;           // split over the keys: unfinished outputs and their maxima and sums
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];   // batch, token, head
   const int *q_start, *k_start, *k_len;

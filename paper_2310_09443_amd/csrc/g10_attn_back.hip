@@ -1,5 +1,4 @@
-// Attention, backward:  delta = sum(do * o) per query, then one kernel for the gradients of keys and values and one for the
-// queries'.  Both work P = 2^(S - lse) and dS = P (do V^T - delta) out again from q, k, v and the forward pass's lse.  Two
+// Attention, backward: a kernel for the gradients of the queries and one for those of keys and values.  Both work P = 2^(S - lse) and dS = P (do V^T - delta) out again from q, k, v and the forward pass's lse.  Two
 // kernels make seven products of the five that are needed; in return every gradient is summed by one wavefront in one order:
 // no atomics, and nothing of the size of the scores in memory.
 #include "g10_attn.h"
@@ -8,56 +7,22 @@
 #define BW 128                     // rows of a workgroup, 32 to a wavefront
 
 // In 16-bit floats with a short exponent, P and dS of long rows would fall below the smallest number.  P is held times
-// 2^12 (it is at most 1), dS times 8 over the power of two at the largest |do|: both leave by exact powers of two at the end.
+// 2^12 (it is at most 1), dS times 8 over the power of two at the largest |do| of what it is summed over: of the query for dQ, of the
+// group's heads for dK.  Both leave by exact powers of two at the end.
 template <class T> struct Lift;
 template <> struct Lift<__bf16> {
   static constexpr float p2 = 0.0f, p = 1.0f;
-  static __device__ __forceinline__ float ds(const u32*) { return 1.0f; }
+  static constexpr bool ds = false;
 };
 template <> struct Lift<_Float16> {
   static constexpr float p2 = 12.0f, p = 4096.0f;
-  static __device__ __forceinline__ float ds(const u32* amax) {
-    const int e = clampi((int)(*amax >> 23) - 127, -60, 60);
-    return __uint_as_float((u32)(127 + 3 - e) << 23);
-  }
+  static constexpr bool ds = true;
 };
+__device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)(127 + 3 - clampi((int)(top >> 23) - 127, -60, 60)) << 23); }
 
-__global__ void k_attn_clear(u32* x) { *x = 0; }
-
-// delta, 16 lanes to a row; one read of do and o.
-template <class T>
-__global__ __launch_bounds__(256) void k_attn_delta(const AttnArgs a, u64 rows, u32* amax) {
-  typedef typename Vec<T>::x8 x8;
-  const u64 row = (u64)blockIdx.x * 16 + threadIdx.x / 16;
-  const u32 c = threadIdx.x % 16;
-  float sum = 0.0f, big = 0.0f;
-  u64 at = 0;
-  if (row < rows) {
-    const u32 h = (u32)(row % a.heads);
-    const u64 tok = row / a.heads;
-    const u64 b = a.q_start ? 0 : tok / a.seq_q, i = a.q_start ? tok : tok % a.seq_q;
-    at = (b * a.heads + h) * a.seq_q + i;
-    if (c * 8 < a.dim) {
-      const x8 x = *(const x8*)((const T*)a.d_o + (int64_t)b * a.dos[0] + (int64_t)i * a.dos[1] + (int64_t)h * a.dos[2] + c * 8);
-      const x8 y = *(const x8*)((const T*)a.o + (int64_t)b * a.os[0] + (int64_t)i * a.os[1] + (int64_t)h * a.os[2] + c * 8);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sum += (float)x[j] * (float)y[j];
-        big = fmaxf(big, fabsf((float)x[j]));
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 8; d; d /= 2) sum += __shfl_xor(sum, d, 16);
-  if (row < rows && !c) {
-    ((float*)a.delta)[at] = sum;
-    const float l = a.lse[at];                                       // (a query that sees no key: its probabilities are to be 0)
-    ((float*)a.lse2)[at] = l == G10_NEG_INF ? -l : l * G10_LOG2E - Lift<T>::p2;
-  }
-  if (amax) {
-    const u32 top = wave_max(__float_as_uint(big));
-    if (!lane_id() && top > __hip_atomic_load(amax, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(amax, top);
-  }
+__global__ __launch_bounds__(256) void k_attn_clear(u32* x, u32 n) {
+  const u32 i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) x[i] = 0;
 }
 
 // A workgroup's unit, first tile of keys and part of the queries: the parts of the sinks' tiles first, of all units, then a
@@ -119,7 +84,7 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
 #pragma unroll
     for (int r = from; r < to; ++r) {
       if (r % 4 == 0 && r < 12) row_read(r / 4 + 5);
-      dp[r] = sc[r] * ((dp[r] - row[r / 4 & 1][r % 4]) * lift_ds);
+      dp[r] = sc[r] * (Lift<T>::ds ? (dp[r] - row[r / 4 & 1][r % 4]) * lift_ds : dp[r] - row[r / 4 & 1][r % 4]);
       if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
     }
   };
@@ -164,7 +129,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
   sq.init(threadIdx.x, a.dim, a.qs[1]);
   sd.init(threadIdx.x, a.dim, a.dos[1]);
   const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024, rows0 = lds_addr(rows[0]);
-  const float lift = Lift<T>::ds(a.amax), lift_ds = lift / Lift<T>::p;
+  float lift = 1.0f;
+  if (Lift<T>::ds) {
+    u32 top = 0;
+    for (u32 g = 0; g < a.group; ++g) top = max(top, a.amax[b * a.heads + hk * a.group + g]);
+    lift = lift_of(top);
+  }
+  const float lift_ds = lift / Lift<T>::p;
   for (int kt = (int)kt0; kt * BW < nk_all; kt += (int)a.tiles) {
     const bool shared = (u32)kt < a.sink_tiles;
     if (!shared && part) break;
@@ -309,11 +280,51 @@ __global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
   }
 }
 
-// Gradients of 128 queries, 32 to a wavefront, as in the forward pass:  S^T = K Q^T,  dP^T = V dO^T  come out with a query
-// to a lane;  dQ^T += K^T dS^T.
+// Gradients of 128 queries, 32 to a wavefront, which walks over the keys they see, 32 at a time:
+//   S^T = K Q^T,  dP^T = V dO^T  come out with a query to a lane,  dQ^T += K^T dS^T;   first, delta = sum(do * o) of each query, which
+// the keys' kernel takes from here.  The same pipeline as there, two wavefronts to a SIMD.
+// In: these keys' scores and dP in sc and dp.  Out: the next ones'.  LDS: rows_base of the next keys, with their values behind them,
+// cols_base of these keys.
+template <class T, int DP>
+__device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Vec<T>::x8 (&q)[DP / 16], const typename Vec<T>::x8 (&dout)[DP / 16],
+                                           f32x16& sc, f32x16& dp, f32x16 (&dq)[DP / 32], float scale2, float le, float de, float lift) {
+  typedef typename Vec<T>::x8 x8;
+  constexpr int KS = DP / 16, DB = DP / 32, N = 2 * KS + 2 * DB, AHEAD = 4, RING = 5;
+  x8 f[RING], df[2];
+  auto read = [&](int e) -> x8 {
+    if (e < 2 * KS) return frag_rows<T, DP>(rows, e % 2 * 32, e / 2);
+    return frag_tr<T, DP>(cols, (e - 2 * KS) / DB * 16, (e - 2 * KS) % DB);
+  };
+#pragma unroll
+  for (int e = 0; e < AHEAD; ++e) f[e % RING] = read(e);
+  f32x16 sn = {}, dn = {};
+  hold();
+  each_of<0, N>([&](auto step) __attribute__((always_inline)) {
+    constexpr int e = decltype(step)::value;
+    if constexpr (e + AHEAD < N) f[(e + AHEAD) % RING] = read(e + AHEAD);
+    if constexpr (e < 2 * KS) {
+      if constexpr (e % 2 == 0) sn = Vec<T>::mfma(f[e % RING], q[e / 2], sn);
+      else dn = Vec<T>::mfma(f[e % RING], dout[e / 2], dn);
+#pragma unroll
+      for (int r = 16 * e / (2 * KS); r < 16 * (e + 1) / (2 * KS); ++r) {
+        const float p = exp2_fast(sc[r] * scale2 - le);
+        dp[r] = p * (Lift<T>::ds ? (dp[r] - de) * lift : dp[r] - de);
+        if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
+      }
+    } else {
+      constexpr int v = e - 2 * KS;
+      dq[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB], dq[v % DB]);
+#pragma unroll
+      for (int r = 16 * v / (2 * DB); r < 16 * (v + 1) / (2 * DB); ++r) { sc[r] = sn[r]; dp[r] = dn[r]; }
+    }
+    hold();
+  });
+}
+
 template <class T, int DP>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
-  __shared__ __attribute__((aligned(256))) T lds[2][2][BT * DP];
+  constexpr int KT = 32, NB = 4;                                     // keys of a tile; these, the next, two on their way
+  __shared__ __attribute__((aligned(256))) T lds[NB][2][KT * DP];
   typedef typename Vec<T>::x8 x8;
   u32 unit, at;
   if (!unit_of(a.batch * a.kv_heads, a.group * a.tiles, unit, at)) return;
@@ -321,66 +332,104 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   const Seq s = seq_of(a, b);
   const int off = s.nk - s.nq;
   const u32 wave = uniform(wave_id()), lane = lane_id();
-  const T* Q = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2];
-  const T* D = (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)h * a.dos[2];
   const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
   const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
-  T* dQ = (T*)a.dq + batch_off(a, b, a.dqs[0]) + s.q0 * a.dqs[1] + (int64_t)h * a.dqs[2];
-  Stage<DP, BT, 256> sk, sv;
+  Walk<DP, KT, 256> sk, sv;
   sk.init(threadIdx.x, a.dim, a.ks[1]);
   sv.init(threadIdx.x, a.dim, a.vs[1]);
-  const u32 lk[2] = {lds_addr(lds[0][0]) + wave * 1024, lds_addr(lds[1][0]) + wave * 1024};
-  const u32 lv[2] = {lds_addr(lds[0][1]) + wave * 1024, lds_addr(lds[1][1]) + wave * 1024};
-  const float lift = Lift<T>::ds(a.amax), lift_ds = lift;
+  const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024;
+  const u32 rb = rows_base<DP>(lds_addr(lds[0][0])), cb = cols_base<DP>(lds_addr(lds[0][0]));
   for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BW < s.nq; qt += (int)a.tiles) {
-    const int i0 = qt * BW + (int)wave * 32, i = i0 + (int)(lane & 31);
+    const int i0 = qt * BW + (int)wave * 32, i = i0 + (int)(lane & 31), c = i < s.nq ? i : s.nq - 1;
     const Seen seen = keys_of(a, i + off, s.nk);
     const int wp0 = i0 + off, wp1 = (i0 + 31 < s.nq ? i0 + 31 : s.nq - 1) + off;
     const int e1 = (qt + 1) * BW - 1 < s.nq ? (qt + 1) * BW - 1 : s.nq - 1;
-    const Tiles tiles = key_tiles<BT>(a, qt * BW + off, e1 + off, s.nk);
+    const Tiles tiles = key_tiles<KT>(a, qt * BW + off, e1 + off, s.nk);
+    // keys that all of the wavefront's queries see: flo..fhi, and the sinks up to fhi
+    const int w = (int)a.window;
+    int flo = w ? wp1 - w + 1 : 0, fhi = s.nk - 1;
+    if (a.causal && wp0 < fhi) fhi = wp0;
+    if (!a.causal && w && wp0 + w - 1 < fhi) fhi = wp0 + w - 1;
+    const int ftop = a.causal ? fhi : s.nk - 1;
+
     x8 q[DP / 16], dout[DP / 16];
-    frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
-    frags_global<T, DP>(dout, D, a.dos[1], i, s.nq - 1, a.dim);
-    const int64_t r0 = row_off(a, b, h, s) + (i < s.nq ? i : s.nq - 1);
-    const float le = a.lse2[r0] + Lift<T>::p2, de = a.delta[r0];
+    frags_global<T, DP>(q, (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2], a.qs[1], i, s.nq - 1, a.dim);
+    frags_global<T, DP>(dout, (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)h * a.dos[2], a.dos[1], i, s.nq - 1, a.dim);
+    float de = 0.0f, big = 0.0f, le;
+    {
+      x8 o[DP / 16];
+      frags_global<T, DP>(o, (const T*)a.o + batch_off(a, b, a.os[0]) + s.q0 * a.os[1] + (int64_t)h * a.os[2], a.os[1], i, s.nq - 1, a.dim);
+      const int64_t r0 = row_off(a, b, h, s) + c;
+      le = a.lse[r0];
+      le = le == G10_NEG_INF ? -le : le * G10_LOG2E;                 // (a query that sees no key: its probabilities are to be 0)
+#pragma unroll
+      for (int ks = 0; ks < DP / 16; ++ks)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          de += (float)dout[ks][x] * (float)o[ks][x];
+          if (Lift<T>::ds) big = fmaxf(big, fabsf((float)dout[ks][x]));
+        }
+      de = both_sum(de);
+      if (lane < 32 && i < s.nq) {
+        ((float*)a.delta)[r0] = de;
+        ((float*)a.lse2)[r0] = le - Lift<T>::p2;
+      }
+    }
+    float lift = 1.0f;
+    if (Lift<T>::ds) {
+      big = both_max(big);
+      lift = lift_of(__float_as_uint(big));
+      const u32 top = wave_max(__float_as_uint(big));
+      if (!lane) atomicMax((u32*)a.amax + b * a.heads + h, top);
+    }
     f32x16 dq[DP / 32] = {};
     if (tiles.count) {
+      u32 to = 0;
+      int ft = 0;                                                    // next tile to be fetched
+      auto fetch = [&]() {
+        if (ft == 0 || ft == tiles.head) { sk.from(K, a.ks[1], tiles.at(ft) * KT); sv.from(V, a.vs[1], tiles.at(ft) * KT); }
+        const u32 to_at = tile0 + to * (2 * KT * DP * 2);
+        const int left = s.nk - tiles.at(ft) * KT;
+        sk.load(left, a.ks[1], to_at);
+        sv.load(left, a.vs[1], to_at + KT * DP * 2);
+        to = (to + 1) % NB;
+        ++ft;
+      };
+      loads_done();                                                  // (the compiler knows of no other loads: none of these may be in doubt below)
       __syncthreads();
-      sk.load(K, a.ks[1], tiles.at(0) * BT, s.nk, lk[0]);
-      sv.load(V, a.vs[1], tiles.at(0) * BT, s.nk, lv[0]);
-    }
-    for (int t = 0; t < tiles.count; ++t) {
-      const int j0 = tiles.at(t) * BT, buf = t & 1;
-      loads_done();
+      for (int t = 0; t < 3 && t < tiles.count; ++t) fetch();
+      f32x16 sc = {}, dp = {};
+      if (tiles.count > 2) loads_done_but<Stage<DP, KT, 256>::IT * 2>();
+      else loads_done();
       __syncthreads();
-      if (t + 1 < tiles.count) {
-        sk.load(K, a.ks[1], tiles.at(t + 1) * BT, s.nk, lk[buf ^ 1]);
-        sv.load(V, a.vs[1], tiles.at(t + 1) * BT, s.nk, lv[buf ^ 1]);
+#pragma unroll
+      for (int ks = 0; ks < DP / 16; ++ks) {
+        sc = Vec<T>::mfma(frag_rows<T, DP>(rb, 0, ks), q[ks], sc);
+        dp = Vec<T>::mfma(frag_rows<T, DP>(rb, KT, ks), dout[ks], dp);
       }
-      const u32 tk = rows_base<DP>(lds_addr(lds[buf][0])), tv = rows_base<DP>(lds_addr(lds[buf][1])), tc = cols_base<DP>(lds_addr(lds[buf][0]));
-      const bool full = all_see(a, wp0, wp1, j0, j0 + BT - 1, s.nk);
+      u32 buf = 0;
+#pragma nounroll
+      for (int t = 0; t < tiles.count; ++t) {
+        if (t + 2 < tiles.count) loads_done_but<Stage<DP, KT, 256>::IT * 2>();       // the next tile is there, the one behind it may be on its way
+        else loads_done();
+        __syncthreads();
+        if (ft < tiles.count) fetch();
+        const int j0 = tiles.at(t) * KT, j1 = j0 + KT - 1;
+        if (!((j0 >= flo && j1 <= fhi) || (j1 < (int)a.sinks && j1 <= ftop))) {
 #pragma unroll
-      for (int n = 0; n < BT / 32; ++n) {
-        f32x16 sc = {}, dp = {};
-#pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) sc = Vec<T>::mfma(frag_rows<T, DP>(tk, 32 * n, ks), q[ks], sc);
-#pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) dp = Vec<T>::mfma(frag_rows<T, DP>(tv, 32 * n, ks), dout[ks], dp);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float p = exp2_fast(sc[r] * a.scale2 - le);
-          if (!full) p = seen.key(j0 + 32 * n + res_row(r)) ? p : 0.0f;
-          dp[r] = full || p != 0.0f ? p * (dp[r] - de) * lift_ds : 0.0f;
+          for (int r = 0; r < 16; ++r) {
+            const bool on = seen.key(j0 + res_row(r));
+            sc[r] = on ? sc[r] : G10_NEG_INF;
+            dp[r] = on ? dp[r] : 0.0f;                               // (what the query does not see may hold anything)
+          }
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const x8 df = pack8<T>(dp, k);
-#pragma unroll
-          for (int db = 0; db < DP / 32; ++db) dq[db] = Vec<T>::mfma(frag_tr<T, DP>(tc, 32 * n + 16 * k, db), df, dq[db]);
-        }
+        const u32 next = (buf + 1) % NB;
+        query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, dq, a.scale2, le, de, lift);
+        buf = next;
       }
     }
     if (i < s.nq) {
+      T* dQ = (T*)a.dq + batch_off(a, b, a.dqs[0]) + (s.q0 + i) * a.dqs[1] + (int64_t)h * a.dqs[2];
       const float f = a.scale / lift;
 #pragma unroll
       for (int db = 0; db < DP / 32; ++db)
@@ -388,10 +437,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         for (int g = 0; g < 4; ++g) {
           const int d = 32 * db + 8 * g + 4 * (int)(lane >> 5);
           if (d < (int)a.dim) {
-            typename Vec<T>::x4 w;
+            typename Vec<T>::x4 x;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) w[r] = (T)(dq[db][4 * g + r] * f);
-            *(typename Vec<T>::x4*)(dQ + (int64_t)i * a.dqs[1] + d) = w;
+            for (int r = 0; r < 4; ++r) x[r] = (T)(dq[db][4 * g + r] * f);
+            *(typename Vec<T>::x4*)(dQ + d) = x;
           }
         }
     }
@@ -432,7 +481,7 @@ extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uin
   AttnArgs a;
   G10_TRY(attn_args(g, true, a));
   share_sinks(a);
-  *bytes = 256 + pad256(rows_of(a) * 8) + sink_bytes(a);             // the largest |do|; delta, lse2; sums of the sinks' tiles
+  *bytes = pad256((uint64_t)a.batch * a.heads * 4) + pad256(rows_of(a) * 8) + sink_bytes(a);      // the largest |do| of each head; delta, lse2; sums of the sinks' tiles
   return G10_OK;
 }
 
@@ -442,25 +491,27 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   if (!a.batch) return G10_OK;
   const uint64_t rows = rows_of(a), units = (uint64_t)a.batch * a.kv_heads;
   share_sinks(a);
-  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < 256 + pad256(rows * 8) + sink_bytes(a)) return G10_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < pad256((uint64_t)a.batch * a.heads * 4) + pad256(rows * 8) + sink_bytes(a)) return G10_EINVAL;
   const uint64_t qt = (a.max_q + BW - 1) / BW, kt0 = (a.max_k + BW - 1) / BW, kt = kt0 > a.sink_tiles ? kt0 : a.sink_tiles;
   const uint64_t per = kt + (uint64_t)a.sink_tiles * (a.splits - 1);
-  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * per >= (1ull << 31) || rows / 16 >= (1ull << 31) - 1) return G10_EINVAL;
+  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * per >= (1ull << 31)) return G10_EINVAL;
   hipStream_t s = (hipStream_t)hip_stream;
   a.amax = (const u32*)workspace;
-  a.delta = (const float*)((char*)workspace + 256);
+  a.delta = (const float*)((char*)workspace + pad256((uint64_t)a.batch * a.heads * 4));
   a.lse2 = a.delta + rows;
-  u32* const amax = g->type == G10_F16 ? (u32*)workspace : nullptr;
-  if (amax) k_attn_clear<<<1, 1, 0, s>>>(amax);
-  if (rows) {
-    const dim3 grid((u32)((rows + 15) / 16));
-    if (g->type == G10_BF16) k_attn_delta<__bf16><<<grid, 256, 0, s>>>(a, rows, amax);
-    else k_attn_delta<_Float16><<<grid, 256, 0, s>>>(a, rows, amax);
-  }
+  a.part = (float*)((char*)a.delta + pad256(rows * 8));
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
+  if (qt) {
+    if (!bf) k_attn_clear<<<(a.batch * a.heads + 255) / 256, 256, 0, s>>>((u32*)workspace, a.batch * a.heads);
+    a.tiles = (u32)qt;
+    const dim3 grid(unit_grid((u32)units, a.group * a.tiles));
+    if (bf && narrow) k_attn_dq<__bf16, 64><<<grid, 256, 0, s>>>(a);
+    else if (bf) k_attn_dq<__bf16, 128><<<grid, 256, 0, s>>>(a);
+    else if (narrow) k_attn_dq<_Float16, 64><<<grid, 256, 0, s>>>(a);
+    else k_attn_dq<_Float16, 128><<<grid, 256, 0, s>>>(a);
+  }
   if (kt) {
     a.tiles = (u32)kt;
-    a.part = (float*)((char*)workspace + 256 + pad256(rows * 8));
     const dim3 grid(unit_grid((u32)units, (u32)per));
     if (bf && narrow) k_attn_dkdv<__bf16, 64><<<grid, 256, 0, s>>>(a);
     else if (bf) k_attn_dkdv<__bf16, 128><<<grid, 256, 0, s>>>(a);
@@ -473,14 +524,6 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
     else if (bf) k_attn_sinks<__bf16, 128><<<grid, 256, 0, s>>>(a);
     else if (narrow) k_attn_sinks<_Float16, 64><<<grid, 256, 0, s>>>(a);
     else k_attn_sinks<_Float16, 128><<<grid, 256, 0, s>>>(a);
-  }
-  if (qt) {
-    a.tiles = (u32)qt;
-    const dim3 grid(unit_grid((u32)units, a.group * a.tiles));
-    if (bf && narrow) k_attn_dq<__bf16, 64><<<grid, 256, 0, s>>>(a);
-    else if (bf) k_attn_dq<__bf16, 128><<<grid, 256, 0, s>>>(a);
-    else if (narrow) k_attn_dq<_Float16, 64><<<grid, 256, 0, s>>>(a);
-    else k_attn_dq<_Float16, 128><<<grid, 256, 0, s>>>(a);
   }
   G10_HIP(hipGetLastError());
   return G10_OK;
