@@ -57,7 +57,7 @@ __device__ __forceinline__ void tile_step(u32 tk, u32 tv, const typename Vec<T>:
 
 // NW wavefronts to a workgroup, 32 queries each.
 template <class T, int DP, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnArgs a) {
+__global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const AttnArgs a) {
   constexpr int BM = 32 * NW;
   __shared__ __attribute__((aligned(256))) T lds[2][2][BN * DP];      // keys, values; even and odd tiles
   typedef typename Vec<T>::x8 x8;
@@ -76,6 +76,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnArgs a) {
   const u32 lk = lds_addr(lds[0][0]) + wave * 1024, lv = lds_addr(lds[1][0]) + wave * 1024;
   constexpr u32 odd = BN * DP * 2;
   const u32 tk = rows_base<DP>(lds_addr(lds[0][0])), tv = cols_base<DP>(lds_addr(lds[1][0]));
+  bool again = false;
   // (the last tiles of a causal sequence are the longest: first)
   for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BM < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BM + (int)wave * 32, i = i0 + (int)(lane & 31);
@@ -86,12 +87,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_fwd(const AttnArgs a) {
     f32x16 o[DP / 32] = {};
     float m = G10_NEG_INF, l = 0.0f;                                 // m in powers of two
     if (tiles.count) {
-      x8 q[DP / 16];
-      frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
-      loads_done();
-      __syncthreads();                                               // (the tiles of the queries before are read)
+      if (again) __syncthreads();                                    // (the tiles of the queries before are read)
+      again = true;
       sk.load(K, a.ks[1], tiles.at(0) * BN, s.nk, lk);
       sv.load(V, a.vs[1], tiles.at(0) * BN, s.nk, lv);
+      x8 q[DP / 16];
+      frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
       f32x16 sa[2], sb[2];
       // scores of a tile that are not seen leave; the maximum
       auto settle = [&](f32x16(&sc)[2], int t) {

@@ -136,6 +136,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
     lift = lift_of(top);
   }
   const float lift_ds = lift / Lift<T>::p;
+  bool again = false;
   for (int kt = (int)kt0; kt * BW < nk_all; kt += (int)a.tiles) {
     const bool shared = (u32)kt < a.sink_tiles;
     if (!shared && part) break;
@@ -180,13 +181,13 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
           sd.from(D, a.dos[1], first);
         }
       };
+      if (again) __syncthreads();                                    // (the tiles of the keys before are read)
+      again = true;
+      fetch();
+      if (all > 1) fetch();
       x8 kf[DP / 16], vf[DP / 16];
       frags_global<T, DP>(kf, (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2], a.ks[1], j, s.nk - 1, a.dim);
       frags_global<T, DP>(vf, (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2], a.vs[1], j, s.nk - 1, a.dim);
-      loads_done();
-      __syncthreads();
-      fetch();
-      if (all > 1) fetch();
       const u32 rb = rows_base<DP>(lds_addr(lds[0][0])), cb = cols_base<DP>(lds_addr(lds[0][0])), lb = rows0 + 16 * (lane >> 5);
       auto half = [&](u32 buf, u32 n) {
         return Half{rb + buf * (2 * BT * DP * 2) + n * (32 * DP * 2), cb + buf * (2 * BT * DP * 2) + n * (32 * DP * 2), lb + buf * (2 * BT * 4) + n * 128};
@@ -283,11 +284,11 @@ __global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
 // Gradients of 128 queries, 32 to a wavefront, which walks over the keys they see, 32 at a time:
 //   S^T = K Q^T,  dP^T = V dO^T  come out with a query to a lane,  dQ^T += K^T dS^T;   first, delta = sum(do * o) of each query, which
 // the keys' kernel takes from here.  The same pipeline as there, two wavefronts to a SIMD.
-// In: these keys' scores and dP in sc and dp.  Out: the next ones'.  LDS: rows_base of the next keys, with their values behind them,
+// These keys' scores and dP are in sc and dp, the next ones' go to sn and dn.  LDS: rows_base of the next keys, with their values behind them,
 // cols_base of these keys.
 template <class T, int DP>
 __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Vec<T>::x8 (&q)[DP / 16], const typename Vec<T>::x8 (&dout)[DP / 16],
-                                           f32x16& sc, f32x16& dp, f32x16 (&dq)[DP / 32], float scale2, float le, float de, float lift) {
+                                           f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn, f32x16 (&dq)[DP / 32], float scale2, float le, float de, float lift) {
   typedef typename Vec<T>::x8 x8;
   constexpr int KS = DP / 16, DB = DP / 32, N = 2 * KS + 2 * DB, AHEAD = 4, RING = 5;
   x8 f[RING], df[2];
@@ -297,7 +298,7 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
   };
 #pragma unroll
   for (int e = 0; e < AHEAD; ++e) f[e % RING] = read(e);
-  f32x16 sn = {}, dn = {};
+  sn = dn = f32x16{};
   hold();
   each_of<0, N>([&](auto step) __attribute__((always_inline)) {
     constexpr int e = decltype(step)::value;
@@ -314,8 +315,6 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
     } else {
       constexpr int v = e - 2 * KS;
       dq[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB], dq[v % DB]);
-#pragma unroll
-      for (int r = 16 * v / (2 * DB); r < 16 * (v + 1) / (2 * DB); ++r) { sc[r] = sn[r]; dp[r] = dn[r]; }
     }
     hold();
   });
@@ -339,6 +338,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   sv.init(threadIdx.x, a.dim, a.vs[1]);
   const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024;
   const u32 rb = rows_base<DP>(lds_addr(lds[0][0])), cb = cols_base<DP>(lds_addr(lds[0][0]));
+  bool again = false;
   for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BW < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BW + (int)wave * 32, i = i0 + (int)(lane & 31), c = i < s.nq ? i : s.nq - 1;
     const Seen seen = keys_of(a, i + off, s.nk);
@@ -352,6 +352,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     if (!a.causal && w && wp0 + w - 1 < fhi) fhi = wp0 + w - 1;
     const int ftop = a.causal ? fhi : s.nk - 1;
 
+    u32 to = 0;
+    int ft = 0;                                                      // next tile to be fetched
+    auto fetch = [&]() {
+      if (ft == 0 || ft == tiles.head) { sk.from(K, a.ks[1], tiles.at(ft) * KT); sv.from(V, a.vs[1], tiles.at(ft) * KT); }
+      const u32 to_at = tile0 + to * (2 * KT * DP * 2);
+      const int left = s.nk - tiles.at(ft) * KT;
+      sk.load(left, a.ks[1], to_at);
+      sv.load(left, a.vs[1], to_at + KT * DP * 2);
+      to = (to + 1) % NB;
+      ++ft;
+    };
+    if (again) __syncthreads();                                      // (the tiles of the queries before are read)
+    again = true;
+    for (int t = 0; t < 3 && t < tiles.count; ++t) fetch();
     x8 q[DP / 16], dout[DP / 16];
     frags_global<T, DP>(q, (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2], a.qs[1], i, s.nq - 1, a.dim);
     frags_global<T, DP>(dout, (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)h * a.dos[2], a.dos[1], i, s.nq - 1, a.dim);
@@ -383,33 +397,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
       if (!lane) atomicMax((u32*)a.amax + b * a.heads + h, top);
     }
     f32x16 dq[DP / 32] = {};
+    loads_done();
     if (tiles.count) {
-      u32 to = 0;
-      int ft = 0;                                                    // next tile to be fetched
-      auto fetch = [&]() {
-        if (ft == 0 || ft == tiles.head) { sk.from(K, a.ks[1], tiles.at(ft) * KT); sv.from(V, a.vs[1], tiles.at(ft) * KT); }
-        const u32 to_at = tile0 + to * (2 * KT * DP * 2);
-        const int left = s.nk - tiles.at(ft) * KT;
-        sk.load(left, a.ks[1], to_at);
-        sv.load(left, a.vs[1], to_at + KT * DP * 2);
-        to = (to + 1) % NB;
-        ++ft;
-      };
-      loads_done();                                                  // (the compiler knows of no other loads: none of these may be in doubt below)
-      __syncthreads();
-      for (int t = 0; t < 3 && t < tiles.count; ++t) fetch();
-      f32x16 sc = {}, dp = {};
-      if (tiles.count > 2) loads_done_but<Stage<DP, KT, 256>::IT * 2>();
-      else loads_done();
+      f32x16 sa = {}, da = {}, sb, db;
       __syncthreads();
 #pragma unroll
       for (int ks = 0; ks < DP / 16; ++ks) {
-        sc = Vec<T>::mfma(frag_rows<T, DP>(rb, 0, ks), q[ks], sc);
-        dp = Vec<T>::mfma(frag_rows<T, DP>(rb, KT, ks), dout[ks], dp);
+        sa = Vec<T>::mfma(frag_rows<T, DP>(rb, 0, ks), q[ks], sa);
+        da = Vec<T>::mfma(frag_rows<T, DP>(rb, KT, ks), dout[ks], da);
       }
       u32 buf = 0;
-#pragma nounroll
-      for (int t = 0; t < tiles.count; ++t) {
+      auto turn = [&](int t, f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
         if (t + 2 < tiles.count) loads_done_but<Stage<DP, KT, 256>::IT * 2>();       // the next tile is there, the one behind it may be on its way
         else loads_done();
         __syncthreads();
@@ -424,9 +422,16 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
           }
         }
         const u32 next = (buf + 1) % NB;
-        query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, dq, a.scale2, le, de, lift);
+        query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, de, lift);
         buf = next;
+      };
+      int t = 0;
+#pragma nounroll
+      for (; t + 1 < tiles.count; t += 2) {
+        turn(t, sa, da, sb, db);
+        turn(t + 1, sb, db, sa, da);
       }
+      if (t < tiles.count) turn(t, sa, da, sb, db);
     }
     if (i < s.nq) {
       T* dQ = (T*)a.dq + batch_off(a, b, a.dqs[0]) + (s.q0 + i) * a.dqs[1] + (int64_t)h * a.dqs[2];
