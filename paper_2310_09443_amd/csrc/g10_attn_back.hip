@@ -20,6 +20,9 @@ template <> struct Lift<_Float16> {
 };
 __device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)(127 + 3 - clampi((int)(top >> 23) - 127, -60, 60)) << 23); }
 
+// A product that is 0 where p is, whatever x is: behind a probability of 0 may lie a pair that does not see each other, and anything in it.
+__device__ __forceinline__ float times(float p, float x) { return __builtin_amdgcn_fmul_legacy(p, x); }
+
 __global__ __launch_bounds__(256) void k_attn_clear(u32* x, u32 n) {
   const u32 i = blockIdx.x * 256 + threadIdx.x;
   if (i < n) x[i] = 0;
@@ -84,7 +87,7 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
 #pragma unroll
     for (int r = from; r < to; ++r) {
       if (r % 4 == 0 && r < 12) row_read(r / 4 + 5);
-      dp[r] = sc[r] * (Lift<T>::ds ? (dp[r] - row[r / 4 & 1][r % 4]) * lift_ds : dp[r] - row[r / 4 & 1][r % 4]);
+      dp[r] = times(sc[r], Lift<T>::ds ? (dp[r] - row[r / 4 & 1][r % 4]) * lift_ds : dp[r] - row[r / 4 & 1][r % 4]);
       if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
     }
   };
@@ -214,7 +217,6 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
           for (int r = 0; r < 16; ++r) {
             const bool seen = (u32)(at + 8 * (r / 4) + r % 4) < span;
             sc[r] = seen ? sc[r] : G10_NEG_INF;
-            dp[r] = seen ? dp[r] : 0.0f;                             // (what no query sees may hold anything)
           }
         }
         const Half here = half(buf, n);
@@ -309,7 +311,7 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
 #pragma unroll
       for (int r = 16 * e / (2 * KS); r < 16 * (e + 1) / (2 * KS); ++r) {
         const float p = exp2_fast(sc[r] * scale2 - le);
-        dp[r] = p * (Lift<T>::ds ? (dp[r] - de) * lift : dp[r] - de);
+        dp[r] = times(p, Lift<T>::ds ? (dp[r] - de) * lift : dp[r] - de);
         if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
       }
     } else {
@@ -415,11 +417,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         const int j0 = tiles.at(t) * KT, j1 = j0 + KT - 1;
         if (!((j0 >= flo && j1 <= fhi) || (j1 < (int)a.sinks && j1 <= ftop))) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const bool on = seen.key(j0 + res_row(r));
-            sc[r] = on ? sc[r] : G10_NEG_INF;
-            dp[r] = on ? dp[r] : 0.0f;                               // (what the query does not see may hold anything)
-          }
+          for (int r = 0; r < 16; ++r) sc[r] = seen.key(j0 + res_row(r)) ? sc[r] : G10_NEG_INF;
         }
         const u32 next = (buf + 1) % NB;
         query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, de, lift);
