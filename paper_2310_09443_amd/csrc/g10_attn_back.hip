@@ -21,7 +21,8 @@ template <> struct Lift<_Float16> {
 __device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)(127 + 3 - clampi((int)(top >> 23) - 127, -60, 60)) << 23); }
 
 // A product that is 0 where p is, whatever x is: behind a probability of 0 may lie a pair that does not see each other, and anything in it.
-__device__ __forceinline__ float times(float p, float x) { return __builtin_amdgcn_fmul_legacy(p, x); }
+// (v_mul_legacy_f32, which the compiler knows by this name only)
+extern "C" __device__ float times(float p, float x) __asm("llvm.amdgcn.fmul.legacy");
 
 __global__ __launch_bounds__(256) void k_attn_clear(u32* x, u32 n) {
   const u32 i = blockIdx.x * 256 + threadIdx.x;
