@@ -164,6 +164,24 @@ __device__ __forceinline__ void full_range(const AttnArgs& a, int j0, int j1, co
   }
 }
 
+// Rows of a sequence that nobody sees: lo..hi-1.  Whatever they hold, nothing comes of it: a probability of 0 times NaN would be NaN, so a tile
+// holds one of its other rows in their place.
+struct Unseen { int lo, hi; };
+// Keys between the sinks and the first query's window.
+__device__ __forceinline__ Unseen unseen_keys(const AttnArgs& a, const Seq& s) {
+  const int64_t first = (int64_t)s.nk - s.nq - a.window + 1;
+  Unseen u;
+  u.hi = a.window && first > 0 ? (int)first : 0;
+  u.lo = (int)a.sinks < u.hi ? (int)a.sinks : u.hi;
+  return u;
+}
+// Queries before the first key (s.nk > 0).
+__device__ __forceinline__ Unseen unseen_queries(const AttnArgs& a, const Seq& s) {
+  int64_t before = (int64_t)s.nq - s.nk;
+  if (!a.causal) before = a.window && !a.sinks ? before - a.window + 1 : 0;
+  return Unseen{0, before > 0 ? (int)before : 0};
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
 // Tiles in LDS.  A row holds DP values (DP * 2 bytes), in pieces of 16 bytes; piece c of row r lies at place c ^ swz(r), so that
 // the reads below take each of the 64 banks once a cycle: a fragment read takes one piece of 16 rows running (their places
@@ -199,6 +217,12 @@ __device__ __forceinline__ void load_words(const void* p, u32 lds) {
 }
 __device__ __forceinline__ u32 lds_addr(const void* p) { return (u32)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
+// What row r of a tile is taken from, of n rows in the sequence and those unseen, all counted from the tile's first row; some row of the tile is seen.
+__device__ __forceinline__ int row_for(int r, int n, int lo, int hi) {
+  r = r < n ? r : n - 1;
+  return r < lo || r >= hi ? r : lo > 0 ? lo - 1 : hi;
+}
+
 // ROWS rows by NT threads (t = 0..NT-1) from row `row0` of a sequence of n > 0 rows; rows past its end repeat the last one
 // (no query sees them), pieces past the head's values repeat the first (they meet zeros, or go nowhere).
 template <int DP, int ROWS, int NT>
@@ -219,19 +243,18 @@ struct Stage {
     }
   }
   // lds: LDS address of the tile + this wavefront's first piece (wave * 1024)
-  __device__ __forceinline__ void load(const void* seq_base, int64_t stride, int row0, int n, u32 lds) const {
+  __device__ __forceinline__ void load(const void* seq_base, int64_t stride, int row0, int n, const Unseen& u, u32 lds) const {
     const char* base = (const char*)seq_base + (int64_t)row0 * stride * 2;
-    if (row0 + ROWS <= n) {
+    if (row0 + ROWS <= n && row0 >= u.hi) {
 #pragma unroll
       for (int i = 0; i < IT; ++i) {
         if constexpr (EVEN) load_piece(base + (int64_t)(i * STEP) * stride * 2, off[0], lds + (u32)(i * NT * 16));
         else load_piece(base, off[i], lds + (u32)(i * NT * 16));
       }
     } else {
-      const int last = n - 1 - row0;
 #pragma unroll
       for (int i = 0; i < IT; ++i) {
-        const int r = i * STEP + row, over = r > last ? r - last : 0;
+        const int r = i * STEP + row, over = r - row_for(r, n - row0, u.lo - row0, u.hi - row0);
         const u32 at = EVEN ? off[0] + (u32)(i * STEP * (int)stride) * 2 : off[EVEN ? 0 : i];
         load_piece(base, at - (u32)(over * (int)stride) * 2, lds + (u32)(i * NT * 16));
       }
@@ -248,15 +271,14 @@ struct Walk {
   static_assert(Stage<DP, ROWS, NT>::EVEN, "rounds of 16 rows");
   __device__ __forceinline__ void init(u32 t, u32 dim, int64_t stride) { st.init(t, dim, stride); step = (int64_t)st.STEP * stride * 2; }
   __device__ __forceinline__ void from(const void* seq_base, int64_t stride, int row0) { at = (const char*)seq_base + (int64_t)row0 * stride * 2; }
-  // n: rows from the tile's first to the sequence's end
-  __device__ __forceinline__ void load(int n, int64_t stride, u32 lds) {
-    if (n >= ROWS) {
+  __device__ __forceinline__ void load(int row0, int n, const Unseen& u, int64_t stride, u32 lds) {
+    if (row0 + ROWS <= n && row0 >= u.hi) {
 #pragma unroll
       for (int i = 0; i < st.IT; ++i) { load_piece(at, st.off[0], lds + (u32)(i * NT * 16)); at += step; }
     } else {
 #pragma unroll
       for (int i = 0; i < st.IT; ++i) {
-        const int r = i * st.STEP + st.row, over = r > n - 1 ? r - (n - 1) : 0;
+        const int r = i * st.STEP + st.row, over = r - row_for(r, n - row0, u.lo - row0, u.hi - row0);
         load_piece(at, st.off[0] + (u32)((i * st.STEP - over) * (int)stride) * 2, lds + (u32)(i * NT * 16));
       }
       at += st.IT * step;
@@ -315,6 +337,8 @@ __device__ __forceinline__ float both_sum(float x) {
   const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// A product that is 0 where p is, whatever x is (v_mul_legacy_f32, which the compiler knows by this name only).
+extern "C" __device__ float times(float p, float x) __asm("llvm.amdgcn.fmul.legacy");
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <class T>

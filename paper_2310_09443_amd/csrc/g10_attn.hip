@@ -17,7 +17,7 @@ template <class T, int DP, bool NEXT>
 __device__ __forceinline__ void tile_step(u32 tk, u32 tv, const typename Vec<T>::x8 (&q)[DP / 16], f32x16 (&sc)[2], f32x16 (&sn)[2],
                                           f32x16 (&o)[DP / 32], float scale2, float base, float& l) {
   typedef typename Vec<T>::x8 x8;
-  constexpr int NS = NEXT ? 2 * DP / 16 : 0, NV = 4 * DP / 32, N = NS + NV, KS = DP / 16, DB = DP / 32, AHEAD = 4, RING = 5;
+  constexpr int NS = NEXT ? 2 * DP / 16 : 0, NV = 4 * DP / 32, N = NS + NV, DB = DP / 32, AHEAD = 4, RING = 5;
   // exponentials of the first 32 keys before the first output's product, of the others before the second half's
   constexpr int EARLY = NEXT ? 20 : 16;
   x8 f[RING], pf[4];
@@ -66,6 +66,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
   const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + at / a.tiles;
   const Seq s = seq_of(a, b);
   const int off = s.nk - s.nq;
+  const Unseen unseen = unseen_keys(a, s);
   const u32 wave = uniform(wave_id()), lane = lane_id();
   const T* Q = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2];
   const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
@@ -89,8 +90,8 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
     if (tiles.count) {
       if (again) __syncthreads();                                    // (the tiles of the queries before are read)
       again = true;
-      sk.load(K, a.ks[1], tiles.at(0) * BN, s.nk, lk);
-      sv.load(V, a.vs[1], tiles.at(0) * BN, s.nk, lv);
+      sk.load(K, a.ks[1], tiles.at(0) * BN, s.nk, unseen, lk);
+      sv.load(V, a.vs[1], tiles.at(0) * BN, s.nk, unseen, lv);
       x8 q[DP / 16];
       frags_global<T, DP>(q, Q, a.qs[1], i, s.nq - 1, a.dim);
       f32x16 sa[2], sb[2];
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
       };
       loads_done();
       __syncthreads();
-      if (tiles.count > 1) sk.load(K, a.ks[1], tiles.at(1) * BN, s.nk, lk + odd);
+      if (tiles.count > 1) sk.load(K, a.ks[1], tiles.at(1) * BN, s.nk, unseen, lk + odd);
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         sa[n] = f32x16{};
@@ -135,8 +136,8 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
       auto turn = [&](f32x16(&sc)[2], f32x16(&sn)[2], int t, u32 even, u32 other) {
         loads_done();
         __syncthreads();
-        if (t + 2 < tiles.count) sk.load(K, a.ks[1], tiles.at(t + 2) * BN, s.nk, lk + even);
-        sv.load(V, a.vs[1], tiles.at(t + 1) * BN, s.nk, lv + other);
+        if (t + 2 < tiles.count) sk.load(K, a.ks[1], tiles.at(t + 2) * BN, s.nk, unseen, lk + even);
+        sv.load(V, a.vs[1], tiles.at(t + 1) * BN, s.nk, unseen, lv + other);
         tile_step<T, DP, true>(tk + other, tv + even, q, sc, sn, o, a.scale2, m == G10_NEG_INF ? 0.0f : m, l);
         settle(sn, t + 1);
       };
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
           if (d < (int)a.dim) {
             typename Vec<T>::x4 w;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) w[r] = (T)(o[db][4 * g + r] * inv);
+            for (int r = 0; r < 4; ++r) w[r] = (T)times(inv, o[db][4 * g + r]);
             *(typename Vec<T>::x4*)(out + d) = w;
           }
         }
@@ -240,20 +241,17 @@ extern "C" int g10_attention(const g10_attention_args* g, void* workspace, uint6
     if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return G10_EINVAL;
     return attn_forward_split(a, splits, workspace, g->type, s);
   }
-#ifndef NWX
-#define NWX 4
-#endif
-  const u32 nw = NWX;
+  constexpr int nw = 4;
   a.tiles = (a.max_q + 32 * nw - 1) / (32 * nw);
   const uint64_t per = (uint64_t)a.group * a.tiles, units = (uint64_t)a.batch * a.kv_heads;
   if ((units + 7) * per >= (1ull << 31)) return G10_EINVAL;
   const dim3 grid(unit_grid((u32)units, (u32)per));
   if (g->type == G10_BF16) {
-    if (a.dim <= 64) k_attn_fwd<__bf16, 64, NWX><<<grid, 64 * nw, 0, s>>>(a);
-    else k_attn_fwd<__bf16, 128, NWX><<<grid, 64 * nw, 0, s>>>(a);
+    if (a.dim <= 64) k_attn_fwd<__bf16, 64, nw><<<grid, 64 * nw, 0, s>>>(a);
+    else k_attn_fwd<__bf16, 128, nw><<<grid, 64 * nw, 0, s>>>(a);
   } else {
-    if (a.dim <= 64) k_attn_fwd<_Float16, 64, NWX><<<grid, 64 * nw, 0, s>>>(a);
-    else k_attn_fwd<_Float16, 128, NWX><<<grid, 64 * nw, 0, s>>>(a);
+    if (a.dim <= 64) k_attn_fwd<_Float16, 64, nw><<<grid, 64 * nw, 0, s>>>(a);
+    else k_attn_fwd<_Float16, 128, nw><<<grid, 64 * nw, 0, s>>>(a);
   }
   G10_HIP(hipGetLastError());
   return G10_OK;

@@ -20,10 +20,6 @@ template <> struct Lift<_Float16> {
 };
 __device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)(127 + 3 - clampi((int)(top >> 23) - 127, -60, 60)) << 23); }
 
-// A product that is 0 where p is, whatever x is: behind a probability of 0 may lie a pair that does not see each other, and anything in it.
-// (v_mul_legacy_f32, which the compiler knows by this name only)
-extern "C" __device__ float times(float p, float x) __asm("llvm.amdgcn.fmul.legacy");
-
 __global__ __launch_bounds__(256) void k_attn_clear(u32* x, u32 n) {
   const u32 i = blockIdx.x * 256 + threadIdx.x;
   if (i < n) x[i] = 0;
@@ -140,6 +136,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
     lift = lift_of(top);
   }
   const float lift_ds = lift / Lift<T>::p;
+  const Unseen unseen = unseen_queries(a, s);
   bool again = false;
   for (int kt = (int)kt0; kt * BW < nk_all; kt += (int)a.tiles) {
     const bool shared = (u32)kt < a.sink_tiles;
@@ -171,8 +168,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
       u32 to = 0;                                                    // buffer of the next tile to be fetched
       auto fetch = [&]() {
         const u32 at = tile0 + to * (2 * BT * DP * 2);
-        sq.load(s.nq - fi, a.qs[1], at);
-        sd.load(s.nq - fi, a.dos[1], at + BT * DP * 2);
+        sq.load(fi, s.nq, unseen, a.qs[1], at);
+        sd.load(fi, s.nq, unseen, a.dos[1], at + BT * DP * 2);
         if (wave < 2) load_words(L + (fi + (int)lane < s.nq ? fi : s.nq - 1 - (int)lane), rows0 + (2 * to + wave) * (BT * 4));
         to = to == 2 ? 0 : to + 1;
         fi += BT;
@@ -341,6 +338,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   sv.init(threadIdx.x, a.dim, a.vs[1]);
   const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024;
   const u32 rb = rows_base<DP>(lds_addr(lds[0][0])), cb = cols_base<DP>(lds_addr(lds[0][0]));
+  const Unseen unseen = unseen_keys(a, s);
   bool again = false;
   for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BW < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BW + (int)wave * 32, i = i0 + (int)(lane & 31), c = i < s.nq ? i : s.nq - 1;
@@ -360,9 +358,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     auto fetch = [&]() {
       if (ft == 0 || ft == tiles.head) { sk.from(K, a.ks[1], tiles.at(ft) * KT); sv.from(V, a.vs[1], tiles.at(ft) * KT); }
       const u32 to_at = tile0 + to * (2 * KT * DP * 2);
-      const int left = s.nk - tiles.at(ft) * KT;
-      sk.load(left, a.ks[1], to_at);
-      sv.load(left, a.vs[1], to_at + KT * DP * 2);
+      const int row0 = tiles.at(ft) * KT;
+      sk.load(row0, s.nk, unseen, a.ks[1], to_at);
+      sv.load(row0, s.nk, unseen, a.vs[1], to_at + KT * DP * 2);
       to = (to + 1) % NB;
       ++ft;
     };
@@ -394,7 +392,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     }
     float lift = 1.0f;
     if (Lift<T>::ds) {
-      big = both_max(big);
+      big = le == -G10_NEG_INF ? 0.0f : both_max(big);              // (a query that sees no key has no part in the gradients)
       lift = lift_of(__float_as_uint(big));
       const u32 top = wave_max(__float_as_uint(big));
       if (!lane) atomicMax((u32*)a.amax + b * a.heads + h, top);
@@ -434,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     }
     if (i < s.nq) {
       T* dQ = (T*)a.dq + batch_off(a, b, a.dqs[0]) + (s.q0 + i) * a.dqs[1] + (int64_t)h * a.dqs[2];
-      const float f = a.scale / lift;
+      const float f = le == -G10_NEG_INF ? 0.0f : a.scale / lift;
 #pragma unroll
       for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
@@ -443,7 +441,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
           if (d < (int)a.dim) {
             typename Vec<T>::x4 x;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = (T)(dq[db][4 * g + r] * f);
+            for (int r = 0; r < 4; ++r) x[r] = (T)times(f, dq[db][4 * g + r]);
             *(typename Vec<T>::x4*)(dQ + d) = x;
           }
         }

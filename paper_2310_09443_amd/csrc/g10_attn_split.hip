@@ -31,6 +31,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
   const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, split = at % a.splits;
   const Seq s = seq_of(a, b);
   const int off = s.nk - s.nq, rows = s.nq * (int)a.group;
+  const Unseen unseen = unseen_keys(a, s);
   const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
   const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
   Stage<DP, ST, 64> sk, sv;
@@ -54,15 +55,15 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
     float m = G10_NEG_INF, l = 0.0f;
     int t = t0 + (int)wave;
     if (t < t1) {
-      sk.load(K, a.ks[1], tiles.at(t) * ST, s.nk, lk[0]);
-      sv.load(V, a.vs[1], tiles.at(t) * ST, s.nk, lv[0]);
+      sk.load(K, a.ks[1], tiles.at(t) * ST, s.nk, unseen, lk[0]);
+      sv.load(V, a.vs[1], tiles.at(t) * ST, s.nk, unseen, lv[0]);
     }
     for (int buf = 0; t < t1; t += SW, buf ^= 1) {
       const int j0 = tiles.at(t) * ST;
       loads_done();
       if (t + SW < t1) {
-        sk.load(K, a.ks[1], tiles.at(t + SW) * ST, s.nk, lk[buf ^ 1]);
-        sv.load(V, a.vs[1], tiles.at(t + SW) * ST, s.nk, lv[buf ^ 1]);
+        sk.load(K, a.ks[1], tiles.at(t + SW) * ST, s.nk, unseen, lk[buf ^ 1]);
+        sv.load(V, a.vs[1], tiles.at(t + SW) * ST, s.nk, unseen, lv[buf ^ 1]);
       }
       const u32 tk = rows_base<DP>(lk[buf]), tv = cols_base<DP>(lv[buf]);
       f32x16 sc = {};
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
         const int d = 8 * db + 2 * g + (int)(lane >> 5);            // in fours
         f32x4 x;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = o[db][4 * g + r] * mine;
+        for (int r = 0; r < 4; ++r) x[r] = times(mine, o[db][4 * g + r]);
         *(f32x4*)(part + (lane & 31) * DP + ((d ^ (int)(lane & 7)) << 2)) = x;
       }
     __syncthreads();
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
         if (a.splits > 1) *(f32x4*)(piece.o + 4 * d) = x;
         else {
           typename Vec<T>::x4 y;
-          for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
+          for (int r = 0; r < 4; ++r) y[r] = (T)times(inv, x[r]);
           *(typename Vec<T>::x4*)(out + 4 * d) = y;
         }
       }
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
     const float inv = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     if (has) {
       typename Vec<T>::x2 y;
-      y[0] = (T)(x0 * inv); y[1] = (T)(x1 * inv);
+      y[0] = (T)times(inv, x0); y[1] = (T)times(inv, x1);
       *(typename Vec<T>::x2*)((T*)a.o + batch_off(a, b, a.os[0]) + (s.q0 + i) * a.os[1] + (int64_t)h * a.os[2] + 2 * lane) = y;
     }
     if (!lane) (a.lse + row_off(a, b, h, s))[i] = l > 0.0f ? (big + __log2f(l)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;

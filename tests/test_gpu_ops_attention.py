@@ -242,3 +242,29 @@ def test_same_every_time_other_streams_and_graphs(ops):
         eager = work()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(inside, eager)), n
+
+
+@pytest.mark.parametrize("dim, dtype", [(64, torch.float16), (128, torch.bfloat16)])
+@pytest.mark.parametrize("nq, nk, causal, window, sinks", [
+    (1, 500, True, 100, 4), (1, 500, True, 100, 0), (1, 70, False, 9, 40), (40, 500, True, 30, 5), (40, 500, True, 1, 0), (40, 130, False, 20, 70),
+    (130, 500, True, 64, 33), (130, 500, False, 1, 0), (300, 70, True, 0, 0), (300, 70, True, 20, 3), (300, 70, False, 33, 0), (140, 1, True, 1, 0)])
+def test_what_nobody_sees_may_hold_anything(ops, dim, dtype, nq, nk, causal, window, sinks):
+    """Keys between the sinks and the first window, as a cache that is written round and round leaves them, and queries before the first key."""
+    q, k, v, do = make((2, nq), (2, nk), 4, 2, dim, dtype, seed=nq + nk)
+    args = dict(causal=causal, window=window, sinks=sinks)
+    seen = O.visible(nq, nk, causal, window, sinks)
+    blind, unseen = ~seen.any(1), ~seen.any(0)
+    assert blind.any() or unseen.any()
+
+    def run(q, k, v, do):
+        o, lse = ops.g10_attention(q, k, v, **args)
+        return (o, lse, *ops.g10_attention_backward(do, q, k, v, o, lse, **args))
+
+    want = run(q, k, v, do)
+    for value in (float("nan"), float("inf"), -torch.finfo(dtype).max):
+        for t in (k, v):
+            t[:, unseen.cuda()] = value
+        for t in (q, do):
+            t[:, blind.cuda()] = value
+        for x, y in zip(run(q, k, v, do), want):
+            assert torch.equal(x, y)
