@@ -143,6 +143,20 @@ __device__ __forceinline__ Tiles key_tiles(const AttnArgs& a, int p0, int p1, in
   return t;
 }
 
+// Those of a workgroup's tiles in which the positions p0..p1 (none: p1 < p0) among its own see any key: 0..head-1 and from..end-1.
+struct Runs { int head, from, end; };
+template <int TILE>
+__device__ __forceinline__ Runs runs_of(const AttnArgs& a, const Tiles& t, int p0, int p1, int nk) {
+  Runs r = {0, t.count, t.count};
+  if (p1 < p0) return r;
+  const Tiles mine = key_tiles<TILE>(a, p0, p1, nk);
+  const int rest = mine.count - mine.head;
+  r.head = mine.head;                                                // (more than t.head only where t's tiles are all in a row)
+  if (rest > 0) { r.from = mine.lo - t.lo + t.head; r.end = r.from + rest; }
+  if (r.from == r.head) r.head = r.from = 0;
+  return r;
+}
+
 // The queries (indices 0..nq-1) that see any key of j0..j1: lo..hi (empty: hi < lo).
 __device__ __forceinline__ void query_range(const AttnArgs& a, int j0, int j1, const Seq& s, int& lo, int& hi) {
   const int off = s.nk - s.nq, w = (int)a.window;                    // p = i + off

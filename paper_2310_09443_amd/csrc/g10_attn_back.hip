@@ -153,9 +153,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
       all = (int)((int64_t)all * (part + 1) / a.splits) - from;
     }
     if (all > 0) {
-      const int wj1 = j0 + 31 < s.nk ? j0 + 31 : s.nk - 1;
-      int wlo = 0, whi = -1, ilo = 0, ihi = -1, flo, fhi;            // ... of the wavefront, of the lane; that see all of the wavefront's keys
-      if (j0 < s.nk) query_range(a, j0, wj1, s, wlo, whi);
+      int ilo = 0, ihi = -1, flo, fhi;                               // ... of the lane; that see all of the wavefront's keys
       if (j < s.nk) query_range(a, j, j, s, ilo, ihi);
       full_range(a, j0, j0 + 31, s, flo, fhi);
       const u32 span = ihi >= ilo ? (u32)(ihi - ilo + 1) : 0u;
@@ -400,19 +398,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     f32x16 dq[DP / 32] = {};
     loads_done();
     if (tiles.count) {
-      f32x16 sa = {}, da = {}, sb, db;
-      __syncthreads();
-#pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) {
-        sa = Vec<T>::mfma(frag_rows<T, DP>(rb, 0, ks), q[ks], sa);
-        da = Vec<T>::mfma(frag_rows<T, DP>(rb, KT, ks), dout[ks], da);
-      }
+      f32x16 sa, da, sb, db;
       u32 buf = 0;
-      auto turn = [&](int t, f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
+      int t = 0;
+      auto arrive = [&]() __attribute__((always_inline)) {
         if (t + 2 < tiles.count) loads_done_but<Stage<DP, KT, 256>::IT * 2>();       // the next tile is there, the one behind it may be on its way
         else loads_done();
         __syncthreads();
         if (ft < tiles.count) fetch();
+      };
+      auto turn = [&](f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
+        arrive();
         const int j0 = tiles.at(t) * KT, j1 = j0 + KT - 1;
         if (!((j0 >= flo && j1 <= fhi) || (j1 < (int)a.sinks && j1 <= ftop))) {
 #pragma unroll
@@ -421,14 +417,34 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         const u32 next = (buf + 1) % NB;
         query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, de, lift);
         buf = next;
+        ++t;
       };
-      int t = 0;
+      const Runs runs = runs_of<KT>(a, tiles, wp0, wp1, s.nk);
+      __syncthreads();
+      // two runs of tiles with something to do; between them only what the other wavefronts' tiles need
 #pragma nounroll
-      for (; t + 1 < tiles.count; t += 2) {
-        turn(t, sa, da, sb, db);
-        turn(t + 1, sb, db, sa, da);
+      for (int run = 0; run < 3; ++run) {
+        const int from = run == 0 ? 0 : run == 1 ? runs.from : tiles.count, end = run == 0 ? runs.head : run == 1 ? runs.end : 0;
+#pragma nounroll
+        for (; t < from; ++t) {
+          arrive();
+          buf = (buf + 1) % NB;
+        }
+        if (t >= end) continue;
+        const u32 rows = rb + buf * (2 * KT * DP * 2);
+        sa = da = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ++ks) {
+          sa = Vec<T>::mfma(frag_rows<T, DP>(rows, 0, ks), q[ks], sa);
+          da = Vec<T>::mfma(frag_rows<T, DP>(rows, KT, ks), dout[ks], da);
+        }
+#pragma nounroll
+        while (t + 1 < end) {
+          turn(sa, da, sb, db);
+          turn(sb, db, sa, da);
+        }
+        if (t < end) turn(sa, da, sb, db);
       }
-      if (t < tiles.count) turn(t, sa, da, sb, db);
     }
     if (i < s.nq) {
       T* dQ = (T*)a.dq + batch_off(a, b, a.dqs[0]) + (s.q0 + i) * a.dqs[1] + (int64_t)h * a.dqs[2];
