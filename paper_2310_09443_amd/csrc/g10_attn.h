@@ -49,7 +49,7 @@ struct AttnArgs {
   void *o, *dq, *dk, *dv;
   const void* d_o;
   float* lse;
-  const float* delta;              // backward: sum of do * o per query
+  const float* delta;              // backward: - sum of do * o per query
   const float* lse2;               // backward: lse in powers of two, less the lift of P
   const u32* amax;                 // backward: bits of the largest |do| of each sequence and head
   float *part, *part_ml;           // split over the keys: unfinished outputs and their maxima and sums

@@ -57,7 +57,19 @@ __device__ __forceinline__ bool tile_of(const AttnArgs& a, u32& unit, u32& kt, u
 // the first ones to start, whose sums meet in k_attn_sinks.
 struct Half { u32 rows, cols, stats; };                              // LDS addresses of 32 queries of a tile: rows_base and cols_base of Q, with dO a tile behind it; lse2 and delta
 
-// In: the tile's scores and dP in sc and dp.  Out: the next tile's.
+// The sums of dP begin with what is taken from them.
+__device__ __forceinline__ f32x16 minus_delta(const Half& x) {
+  f32x16 d;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x4 four = *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(x.stats + (u32)(BT * 4 + k * 32));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) d[4 * k + r] = four[r];
+  }
+  return d;
+}
+
+// In: the tile's scores and dP - delta in sc and dp.  Out: the next tile's.
 template <class T, int DP>
 __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const typename Vec<T>::x8 (&kf)[DP / 16], const typename Vec<T>::x8 (&vf)[DP / 16],
                                           f32x16& sc, f32x16& dp, f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], float scale2, float lift_ds) {
@@ -69,13 +81,13 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
     e -= 2 * KS;
     return frag_tr<T, DP>(cu.cols, (e < 2 * DB ? BT : -32) + e / DB * 16, e % DB);
   };
-  // four queries' lse2 (k = 0..3) or delta (k = 4..7), read one group ahead
+  // four queries' lse2, read one group ahead
   f32x4 row[2];
-  auto row_read = [&](int k) { row[k & 1] = *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(cu.stats + (u32)(k / 4 * (BT * 4) + k % 4 * 32)); };
+  auto row_read = [&](int k) { row[k & 1] = *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(cu.stats + (u32)(k * 32)); };
   auto exps = [&](int from, int to) {
 #pragma unroll
     for (int r = from; r < to; ++r) {
-      if (r % 4 == 0) row_read(r / 4 + 1);
+      if (r % 4 == 0 && r < 12) row_read(r / 4 + 1);
       sc[r] = exp2_fast(sc[r] * scale2 - row[r / 4 & 1][r % 4]);
       if (r % 8 == 7) pf[r / 8] = pack8<T>(sc, r / 8);
     }
@@ -83,15 +95,14 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
   auto grads = [&](int from, int to) {
 #pragma unroll
     for (int r = from; r < to; ++r) {
-      if (r % 4 == 0 && r < 12) row_read(r / 4 + 5);
-      dp[r] = times(sc[r], Lift<T>::ds ? (dp[r] - row[r / 4 & 1][r % 4]) * lift_ds : dp[r] - row[r / 4 & 1][r % 4]);
+      dp[r] = times(sc[r], Lift<T>::ds ? dp[r] * lift_ds : dp[r]);
       if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
     }
   };
   row_read(0);
 #pragma unroll
   for (int e = 0; e < AHEAD; ++e) f[e % RING] = read(e);
-  f32x16 sn = {}, dn = {};
+  f32x16 sn = {}, dn = minus_delta(nx);
   hold();
   each_of<0, N>([&](auto step) __attribute__((always_inline)) {
     constexpr int e = decltype(step)::value;
@@ -191,9 +202,9 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
       auto half = [&](u32 buf, u32 n) {
         return Half{rb + buf * (2 * BT * DP * 2) + n * (32 * DP * 2), cb + buf * (2 * BT * DP * 2) + n * (32 * DP * 2), lb + buf * (2 * BT * 4) + n * 128};
       };
-      f32x16 sc = {}, dp = {};
       loads_done();
       __syncthreads();
+      f32x16 sc = {}, dp = minus_delta(half(0, 0));
 #pragma unroll
       for (int ks = 0; ks < DP / 16; ++ks) sc = Vec<T>::mfma(frag_rows<T, DP>(rb, 0, ks), kf[ks], sc);
 #pragma unroll
@@ -384,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         }
       de = both_sum(de);
       if (lane < 32 && i < s.nq) {
-        ((float*)a.delta)[r0] = de;
+        ((float*)a.delta)[r0] = -de;
         ((float*)a.lse2)[r0] = le - Lift<T>::p2;
       }
     }
