@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
 // cols_base of these keys.
 template <class T, int DP>
 __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Vec<T>::x8 (&q)[DP / 16], const typename Vec<T>::x8 (&dout)[DP / 16],
-                                           f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn, f32x16 (&dq)[DP / 32], float scale2, float le, float de, float lift) {
+                                           f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn, f32x16 (&dq)[DP / 32], float scale2, float le, const f32x16& less, float lift) {
   typedef typename Vec<T>::x8 x8;
   constexpr int KS = DP / 16, DB = DP / 32, N = 2 * KS + 2 * DB, AHEAD = 4, RING = 5;
   x8 f[RING], df[2];
@@ -307,7 +307,8 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
   };
 #pragma unroll
   for (int e = 0; e < AHEAD; ++e) f[e % RING] = read(e);
-  sn = dn = f32x16{};
+  sn = f32x16{};
+  dn = less;
   hold();
   each_of<0, N>([&](auto step) __attribute__((always_inline)) {
     constexpr int e = decltype(step)::value;
@@ -315,11 +316,12 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
     if constexpr (e < 2 * KS) {
       if constexpr (e % 2 == 0) sn = Vec<T>::mfma(f[e % RING], q[e / 2], sn);
       else dn = Vec<T>::mfma(f[e % RING], dout[e / 2], dn);
+      // (a value's product one behind its exponential, which takes its time)
 #pragma unroll
-      for (int r = 16 * e / (2 * KS); r < 16 * (e + 1) / (2 * KS); ++r) {
-        const float p = exp2_fast(sc[r] * scale2 - le);
-        dp[r] = times(p, Lift<T>::ds ? (dp[r] - de) * lift : dp[r] - de);
-        if (r % 8 == 7) df[r / 8] = pack8<T>(dp, r / 8);
+      for (int r = 16 * e / (2 * KS); r < 16 * (e + 1) / (2 * KS) + (e == 2 * KS - 1); ++r) {
+        if (r < 16) sc[r] = exp2_fast(sc[r] * scale2 - le);
+        if (r) dp[r - 1] = times(sc[r - 1], Lift<T>::ds ? dp[r - 1] * lift : dp[r - 1]);
+        if (r == 8 || r == 16) df[r / 8 - 1] = pack8<T>(dp, r / 8 - 1);
       }
     } else {
       constexpr int v = e - 2 * KS;
@@ -409,7 +411,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     f32x16 dq[DP / 32] = {};
     loads_done();
     if (tiles.count) {
-      f32x16 sa, da, sb, db;
+      f32x16 sa, da, sb, db, less;                                   // (the sums of dP begin with minus delta)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) less[r] = -de;
       u32 buf = 0;
       int t = 0;
       auto arrive = [&]() __attribute__((always_inline)) {
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
           for (int r = 0; r < 16; ++r) sc[r] = seen.key(j0 + res_row(r)) ? sc[r] : G10_NEG_INF;
         }
         const u32 next = (buf + 1) % NB;
-        query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, de, lift);
+        query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, less, lift);
         buf = next;
         ++t;
       };
@@ -443,7 +447,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         }
         if (t >= end) continue;
         const u32 rows = rb + buf * (2 * KT * DP * 2);
-        sa = da = f32x16{};
+        sa = f32x16{};
+        da = less;
 #pragma unroll
         for (int ks = 0; ks < DP / 16; ++ks) {
           sa = Vec<T>::mfma(frag_rows<T, DP>(rows, 0, ks), q[ks], sa);
