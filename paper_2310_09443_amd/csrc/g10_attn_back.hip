@@ -20,11 +20,6 @@ template <> struct Lift<_Float16> {
 };
 __device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)(127 + 3 - clampi((int)(top >> 23) - 127, -60, 60)) << 23); }
 
-__global__ __launch_bounds__(256) void k_attn_clear(u32* x, u32 n) {
-  const u32 i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) x[i] = 0;
-}
-
 // A workgroup's unit, first tile of keys and part of the queries: the parts of the sinks' tiles first, of all units, then a
 // unit's other tiles together.
 __device__ __forceinline__ bool tile_of(const AttnArgs& a, u32& unit, u32& kt, u32& part) {
@@ -142,8 +137,11 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
   const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024, rows0 = lds_addr(rows[0]);
   float lift = 1.0f;
   if (Lift<T>::ds) {
+    const u32 n = a.group * a.q_tiles * 4;
+    const u32* all = a.amax + (u64)unit * n;
     u32 top = 0;
-    for (u32 g = 0; g < a.group; ++g) top = max(top, a.amax[b * a.heads + hk * a.group + g]);
+    for (u32 x = lane; x < n; x += 64) top = max(top, all[x]);
+    top = wave_max(top);
     lift = lift_of(top);
   }
   const float lift_ds = lift / Lift<T>::p;
@@ -351,6 +349,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   const u32 rb = rows_base<DP>(lds_addr(lds[0][0])), cb = cols_base<DP>(lds_addr(lds[0][0]));
   const Unseen unseen = unseen_keys(a, s);
   bool again = false;
+  u32 most = 0;
   for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BW < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BW + (int)wave * 32, i = i0 + (int)(lane & 31), c = i < s.nq ? i : s.nq - 1;
     const Seen seen = keys_of(a, i + off, s.nk);
@@ -405,8 +404,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     if (Lift<T>::ds) {
       big = le == -G10_NEG_INF ? 0.0f : both_max(big);              // (a query that sees no key has no part in the gradients)
       lift = lift_of(__float_as_uint(big));
-      const u32 top = wave_max(__float_as_uint(big));
-      if (!lane) atomicMax((u32*)a.amax + b * a.heads + h, top);
+      most = max(most, wave_max(__float_as_uint(big)));
     }
     f32x16 dq[DP / 32] = {};
     loads_done();
@@ -479,6 +477,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         }
     }
   }
+  if (Lift<T>::ds && !lane) ((u32*)a.amax)[((u64)unit * a.group * a.tiles + at) * 4 + wave] = most;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -487,6 +486,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
 static uint64_t rows_of(const AttnArgs& a) { return (uint64_t)(a.q_start ? 1 : a.batch) * a.heads * a.seq_q; }
 
 static uint64_t pad256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+// The workspace: the largest |do| of each wavefront of the queries' kernel; delta and lse2; sums of the sinks' tiles.
+static uint64_t top_bytes(const AttnArgs& a) { return pad256((uint64_t)a.batch * a.heads * ((a.max_q + BW - 1) / BW) * 16); }
 
 // How the queries of a sinks' tile are shared: so many workgroups that each has about as many queries as a tile of the window.
 // (Packed sequences go by twice their mean length, which is known here; max_q only cuts the grid.)  At most 256 MB of sums.
@@ -515,7 +517,7 @@ extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uin
   AttnArgs a;
   G10_TRY(attn_args(g, true, a));
   share_sinks(a);
-  *bytes = pad256((uint64_t)a.batch * a.heads * 4) + pad256(rows_of(a) * 8) + sink_bytes(a);      // the largest |do| of each head; delta, lse2; sums of the sinks' tiles
+  *bytes = top_bytes(a) + pad256(rows_of(a) * 8) + sink_bytes(a);
   return G10_OK;
 }
 
@@ -525,18 +527,18 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   if (!a.batch) return G10_OK;
   const uint64_t rows = rows_of(a), units = (uint64_t)a.batch * a.kv_heads;
   share_sinks(a);
-  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < pad256((uint64_t)a.batch * a.heads * 4) + pad256(rows * 8) + sink_bytes(a)) return G10_EINVAL;
-  const uint64_t qt = (a.max_q + BW - 1) / BW, kt0 = (a.max_k + BW - 1) / BW, kt = kt0 > a.sink_tiles ? kt0 : a.sink_tiles;
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < top_bytes(a) + pad256(rows * 8) + sink_bytes(a)) return G10_EINVAL;
+  a.q_tiles = (a.max_q + BW - 1) / BW;
+  const uint64_t qt = a.q_tiles, kt0 = (a.max_k + BW - 1) / BW, kt = kt0 > a.sink_tiles ? kt0 : a.sink_tiles;
   const uint64_t per = kt + (uint64_t)a.sink_tiles * (a.splits - 1);
   if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * per >= (1ull << 31)) return G10_EINVAL;
   hipStream_t s = (hipStream_t)hip_stream;
   a.amax = (const u32*)workspace;
-  a.delta = (const float*)((char*)workspace + pad256((uint64_t)a.batch * a.heads * 4));
+  a.delta = (const float*)((char*)workspace + top_bytes(a));
   a.lse2 = a.delta + rows;
   a.part = (float*)((char*)a.delta + pad256(rows * 8));
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
   if (qt) {
-    if (!bf) k_attn_clear<<<(a.batch * a.heads + 255) / 256, 256, 0, s>>>((u32*)workspace, a.batch * a.heads);
     a.tiles = (u32)qt;
     const dim3 grid(unit_grid((u32)units, a.group * a.tiles));
     if (bf && narrow) k_attn_dq<__bf16, 64><<<grid, 256, 0, s>>>(a);
