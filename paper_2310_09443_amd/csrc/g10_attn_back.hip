@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
 }
 
 // Gradients of 128 queries, 32 to a wavefront, which walks over the keys they see, 32 at a time:
-//   S^T = K Q^T,  dP^T = V dO^T  come out with a query to a lane,  dQ^T += K^T dS^T;   first, delta = sum(do * o) of each query, which
+//   S^T = K Q^T,  dP^T = V dO^T  come out with a query to a lane,  dQ^T += K^T dS^T;   first, delta = sum(do o) of each query, which
 // the keys' kernel takes from here.  The same pipeline as there, two wavefronts to a SIMD.
 // These keys' scores and dP are in sc and dp, the next ones' go to sn and dn.  LDS: rows_base of the next keys, with their values behind them,
 // cols_base of these keys.
@@ -331,7 +331,7 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
 
 template <class T, int DP>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
-  constexpr int KT = 32, NB = 4;                                     // keys of a tile; these, the next, two on their way
+  constexpr int KT = 32, NB = 4, FEW = 12;                           // keys of a tile; these, the next, two on their way
   __shared__ __attribute__((aligned(256))) T lds[NB][2][KT * DP];
   typedef typename Vec<T>::x8 x8;
   u32 unit, at;
@@ -363,8 +363,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     if (!a.causal && w && wp0 + w - 1 < fhi) fhi = wp0 + w - 1;
     const int ftop = a.causal ? fhi : s.nk - 1;
 
+    // delta is sum(P dP) as well as sum(do o).  The second costs a reading of o, but o is rounded, and where few keys are seen that
+    // error is large beside dq and dk: against a result that is only rounded once, theirs is 1.4 times as large with the first and with
+    // the second 2.3 times for 4 keys, 1.6 for 128, 1.5 for 400.  So the first up to 384 keys of the workgroup's, for one more walk over them
+    // (two of a step's three products).
+    const bool few = tiles.count <= FEW;
     u32 to = 0;
-    int ft = 0;                                                      // next tile to be fetched
+    int ft = 0, rest = few ? 2 * tiles.count : tiles.count;          // next tile to be fetched; how many there are to be
     auto fetch = [&]() {
       if (ft == 0 || ft == tiles.head) { sk.from(K, a.ks[1], tiles.at(ft) * KT); sv.from(V, a.vs[1], tiles.at(ft) * KT); }
       const u32 to_at = tile0 + to * (2 * KT * DP * 2);
@@ -372,54 +377,81 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
       sk.load(row0, s.nk, unseen, a.ks[1], to_at);
       sv.load(row0, s.nk, unseen, a.vs[1], to_at + KT * DP * 2);
       to = (to + 1) % NB;
-      ++ft;
+      if (++ft == tiles.count) ft = 0;
+      --rest;
     };
     if (again) __syncthreads();                                      // (the tiles of the queries before are read)
     again = true;
-    for (int t = 0; t < 3 && t < tiles.count; ++t) fetch();
+    for (int t = 0; t < 3 && rest; ++t) fetch();
     x8 q[DP / 16], dout[DP / 16];
     frags_global<T, DP>(q, (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)h * a.qs[2], a.qs[1], i, s.nq - 1, a.dim);
     frags_global<T, DP>(dout, (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)h * a.dos[2], a.dos[1], i, s.nq - 1, a.dim);
     float de = 0.0f, big = 0.0f, le;
-    {
+    const int64_t r0 = row_off(a, b, h, s) + c;
+    le = a.lse[r0];
+    le = le == G10_NEG_INF ? -le : le * G10_LOG2E;                   // (a query that sees no key: its probabilities are to be 0)
+    if (!few) {
       x8 o[DP / 16];
       frags_global<T, DP>(o, (const T*)a.o + batch_off(a, b, a.os[0]) + s.q0 * a.os[1] + (int64_t)h * a.os[2], a.os[1], i, s.nq - 1, a.dim);
-      const int64_t r0 = row_off(a, b, h, s) + c;
-      le = a.lse[r0];
-      le = le == G10_NEG_INF ? -le : le * G10_LOG2E;                 // (a query that sees no key: its probabilities are to be 0)
 #pragma unroll
       for (int ks = 0; ks < DP / 16; ++ks)
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          de += (float)dout[ks][x] * (float)o[ks][x];
-          if (Lift<T>::ds) big = fmaxf(big, fabsf((float)dout[ks][x]));
-        }
-      de = both_sum(de);
-      if (lane < 32 && i < s.nq) {
-        ((float*)a.delta)[r0] = -de;
-        ((float*)a.lse2)[r0] = le - Lift<T>::p2;
-      }
+        for (int x = 0; x < 8; ++x) de += (float)dout[ks][x] * (float)o[ks][x];
     }
     float lift = 1.0f;
     if (Lift<T>::ds) {
-      big = le == -G10_NEG_INF ? 0.0f : both_max(big);              // (a query that sees no key has no part in the gradients)
+#pragma unroll
+      for (int ks = 0; ks < DP / 16; ++ks)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) big = fmaxf(big, fabsf((float)dout[ks][x]));
+      big = le == -G10_NEG_INF ? 0.0f : both_max(big);               // (a query that sees no key has no part in the gradients)
       lift = lift_of(__float_as_uint(big));
       most = max(most, wave_max(__float_as_uint(big)));
     }
     f32x16 dq[DP / 32] = {};
     loads_done();
+    __syncthreads();
+    u32 buf = 0;
+    auto arrive = [&]() __attribute__((always_inline)) {
+      if (rest) loads_done_but<Stage<DP, KT, 256>::IT * 2>();        // the next tile is there, the one behind it may be on its way
+      else loads_done();
+      __syncthreads();
+      if (rest) fetch();
+    };
+    f32x16 sa, da;
+    auto scores = [&](u32 rows, const f32x16& from) __attribute__((always_inline)) {
+      sa = f32x16{};
+      da = from;
+#pragma unroll
+      for (int ks = 0; ks < DP / 16; ++ks) {
+        sa = Vec<T>::mfma(frag_rows<T, DP>(rows, 0, ks), q[ks], sa);
+        da = Vec<T>::mfma(frag_rows<T, DP>(rows, KT, ks), dout[ks], da);
+      }
+    };
+    if (few) {                                                       // (without a pipeline: it is short)
+#pragma nounroll
+      for (int t = 0; t < tiles.count; ++t) {
+        arrive();
+        scores(rb + buf * (2 * KT * DP * 2), f32x16{});
+        const int j0 = tiles.at(t) * KT;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = exp2_fast((seen.key(j0 + res_row(r)) ? sa[r] : G10_NEG_INF) * a.scale2 - le);
+          de += times(p, da[r]);
+        }
+        buf = (buf + 1) % NB;
+      }
+    }
+    de = both_sum(de);
+    if (lane < 32 && i < s.nq) {
+      ((float*)a.delta)[r0] = -de;
+      ((float*)a.lse2)[r0] = le - Lift<T>::p2;
+    }
     if (tiles.count) {
-      f32x16 sa, da, sb, db, less;                                   // (the sums of dP begin with minus delta)
+      f32x16 sb, db, less;                                           // (the sums of dP begin with minus delta)
 #pragma unroll
       for (int r = 0; r < 16; ++r) less[r] = -de;
-      u32 buf = 0;
       int t = 0;
-      auto arrive = [&]() __attribute__((always_inline)) {
-        if (t + 2 < tiles.count) loads_done_but<Stage<DP, KT, 256>::IT * 2>();       // the next tile is there, the one behind it may be on its way
-        else loads_done();
-        __syncthreads();
-        if (ft < tiles.count) fetch();
-      };
       auto turn = [&](f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
         arrive();
         const int j0 = tiles.at(t) * KT, j1 = j0 + KT - 1;
@@ -433,7 +465,6 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         ++t;
       };
       const Runs runs = runs_of<KT>(a, tiles, wp0, wp1, s.nk);
-      __syncthreads();
       // two runs of tiles with something to do; between them only what the other wavefronts' tiles need
 #pragma nounroll
       for (int run = 0; run < 3; ++run) {
@@ -444,14 +475,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
           buf = (buf + 1) % NB;
         }
         if (t >= end) continue;
-        const u32 rows = rb + buf * (2 * KT * DP * 2);
-        sa = f32x16{};
-        da = less;
-#pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) {
-          sa = Vec<T>::mfma(frag_rows<T, DP>(rows, 0, ks), q[ks], sa);
-          da = Vec<T>::mfma(frag_rows<T, DP>(rows, KT, ks), dout[ks], da);
-        }
+        scores(rb + buf * (2 * KT * DP * 2), less);
 #pragma nounroll
         while (t + 1 < end) {
           turn(sa, da, sb, db);
