@@ -9,38 +9,116 @@
 #define ST 32                      // keys of a tile
 #define SW 4                       // wavefronts of a workgroup
 #define JOIN 8                     // parts of a row on their way at once
+#define BATCH (64 * SW)            // sequences whose work is cut into equal shares
+#define LEAST 8                    // tiles of a share: two for each wavefront
 
-struct Piece { float *o, *ml; };   // unfinished output of a row and a split: [dim] and {maximum, sum}
+// The work of all sequences' key heads and blocks of 32 columns in one row, in tiles of keys, cut into equal shares: sequences of unlike
+// lengths keep all compute units busy to the end.  A cut goes through a block wherever it falls; the pieces of a
+// block meet in k_attn_join.  At most BATCH sequences; a sequence to a thread.
+struct Shares {
+  u32 each, total;                 // tiles of a share, of all
+  const u32* end;                  // in LDS: tiles up to and with sequence b
+};
+struct Row { u32 blocks, tiles; };                                   // of a sequence: blocks of columns, tiles of keys to each
+__device__ __forceinline__ Row row_of(const AttnArgs& a, const Seq& s) {
+  const Tiles t = key_tiles<ST>(a, s.nk - s.nq, s.nk - 1, s.nk);
+  return Row{((u32)s.nq * a.group + 31) / 32, s.nq ? (u32)t.count : 0u};
+}
+__device__ __forceinline__ Shares shares_of(const AttnArgs& a, u32* end, u32* tmp) {
+  u32 n = 0, most = 0;
+  if (threadIdx.x < a.batch) {
+    const Row w = row_of(a, seq_of(a, threadIdx.x));
+    n = w.blocks * w.tiles * a.kv_heads;
+    most = w.tiles;
+  }
+  const u32 sum = wave_scan_incl(n), top = wave_max(most);
+  if (lane_id() == 63) { tmp[wave_id()] = sum; tmp[SW + wave_id()] = top; }
+  __syncthreads();
+  u32 before = 0, longest = 0;
+  Shares x = {0, 0, end};
+  for (u32 w = 0; w < SW; ++w) {
+    if (w < wave_id()) before += tmp[w];
+    x.total += tmp[w];
+    longest = max(longest, tmp[SW + w]);
+  }
+  end[threadIdx.x] = before + sum;
+  __syncthreads();
+  // no more pieces to a block than there is room for, and a piece is worth its joining
+  x.each = max(max((x.total + a.shares - 1) / a.shares, (longest + a.splits - 2) / (a.splits - 1)), (u32)LEAST);
+  return x;
+}
+
+struct Piece { float *o, *ml; u32* n; };                             // unfinished output of a row and a piece: [dim] and {maximum, sum}; the row's pieces
 
 __device__ __forceinline__ Piece piece_of(const AttnArgs& a, u32 b, const Seq& s, int i, u32 h, u32 split) {
   const u64 row = ((a.q_start ? (u64)s.q0 : (u64)b * a.seq_q) + (u64)i) * a.heads + h;
   Piece p;
   p.o = a.part + (row * a.splits + split) * a.dim;
   p.ml = a.part_ml + (row * a.splits + split) * 2;
+  p.n = a.part_n + row;
   return p;
 }
 
-template <class T, int DP>
+// SHARED: a workgroup to a share, pieces of blocks to the workspace.  Otherwise a workgroup to a block.
+template <class T, int DP, bool SHARED>
 __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
   // [wavefront][buffer][keys, values]; afterwards the wavefronts' outputs
   __shared__ __attribute__((aligned(256))) T lds[SW][2][2][ST * DP];
   __shared__ float ms[SW][32], ls[SW][32];
+  __shared__ u32 ends[BATCH], tmp[2 * SW];
   typedef typename Vec<T>::x8 x8;
   const u32 wave = uniform(wave_id()), lane = lane_id();
-  u32 unit, at;
-  if (!unit_of(a.batch * a.kv_heads, a.tiles * a.splits, unit, at)) return;
-  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, split = at % a.splits;
-  const Seq s = seq_of(a, b);
-  const int off = s.nk - s.nq, rows = s.nq * (int)a.group;
-  const Unseen unseen = unseen_keys(a, s);
-  const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
-  const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
+  u32 lk[2], lv[2];
+  for (int i = 0; i < 2; ++i) { lk[i] = lds_addr(lds[wave][i][0]); lv[i] = lds_addr(lds[wave][i][1]); }
   Stage<DP, ST, 64> sk, sv;
   sk.init(lane, a.dim, a.ks[1]);
   sv.init(lane, a.dim, a.vs[1]);
-  u32 lk[2], lv[2];
-  for (int i = 0; i < 2; ++i) { lk[i] = lds_addr(lds[wave][i][0]); lv[i] = lds_addr(lds[wave][i][1]); }
-  for (int rb = (int)(at / a.splits); rb * 32 < rows; rb += (int)a.tiles) {
+  u32 unit = 0, at = 0, mine = 0, place = 0, stop = 0;
+  Shares sh = {};
+  if constexpr (SHARED) {
+    sh = shares_of(a, ends, tmp);
+    mine = blockIdx.x % a.tiles * (a.shares / a.tiles) + blockIdx.x / a.tiles;
+    if ((u64)mine * sh.each >= sh.total) return;
+    place = mine * sh.each;
+    stop = min(place + sh.each, sh.total);
+  } else {
+    if (!unit_of(a.batch * a.kv_heads, a.tiles, unit, at)) return;
+  }
+  while (true) {
+    u32 b, hk, piece = 0, pieces = 1, from = 0, take = 1, whole = 1;             // tiles from / whole .. (from + take) / whole of the block's
+    int rb;
+    Seq s;
+    if constexpr (SHARED) {
+      u32 lo = 0, hi = a.batch - 1;
+      while (lo < hi) {
+        const u32 mid = (lo + hi) / 2;
+        if (uniform(sh.end[mid]) > place) hi = mid;
+        else lo = mid + 1;
+      }
+      b = lo;
+      s = seq_of(a, b);
+      const Row w = row_of(a, s);
+      const u32 in = place - (b ? uniform(sh.end[b - 1]) : 0);
+      hk = in / w.tiles / w.blocks;
+      rb = (int)(in / w.tiles % w.blocks);
+      whole = w.tiles;
+      from = in % w.tiles;
+      take = min(whole - from, stop - place);
+      const u32 first = place - from;                                // of the block
+      piece = mine - first / sh.each;
+      pieces = (first + whole - 1) / sh.each - first / sh.each + 1;
+      place += take;
+    } else {
+      b = unit / a.kv_heads;
+      hk = unit % a.kv_heads;
+      s = seq_of(a, b);
+      rb = (int)at;
+    }
+    const int off = s.nk - s.nq, rows = s.nq * (int)a.group;
+    const Unseen unseen = unseen_keys(a, s);
+    const T* K = (const T*)a.k + batch_off(a, b, a.ks[0]) + s.k0 * a.ks[1] + (int64_t)hk * a.ks[2];
+    const T* V = (const T*)a.v + batch_off(a, b, a.vs[0]) + s.k0 * a.vs[1] + (int64_t)hk * a.vs[2];
+    if (!SHARED && rb * 32 >= rows) break;
     const int r0 = rb * 32, r1 = r0 + 31 < rows ? r0 + 31 : rows - 1;
     const int row = r0 + (int)(lane & 31), c = row < rows ? row : rows - 1;
     const int i = c / (int)a.group;
@@ -48,7 +126,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
     const Seen seen = keys_of(a, i + off, s.nk);
     const int p0 = r0 / (int)a.group + off, p1 = r1 / (int)a.group + off;
     const Tiles tiles = key_tiles<ST>(a, p0, p1, s.nk);
-    const int t0 = (int)((int64_t)tiles.count * split / a.splits), t1 = (int)((int64_t)tiles.count * (split + 1) / a.splits);
+    const int t0 = (int)((int64_t)tiles.count * from / whole), t1 = (int)((int64_t)tiles.count * (from + take) / whole);
     x8 q[DP / 16];
     const T* Q = (const T*)a.q + batch_off(a, b, a.qs[0]) + (s.q0 + i) * a.qs[1] + (int64_t)h * a.qs[2];
     frags_global<T, DP>(q, Q, 0, 0, 0, a.dim);
@@ -129,13 +207,13 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
       const int oi = orow / (int)a.group;
       const u32 oh = hk * a.group + (u32)(orow % (int)a.group);
       const float inv = cl > 0.0f ? 1.0f / cl : cl == 0.0f ? 0.0f : cl;
-      const Piece piece = piece_of(a, b, s, oi, oh, split);
+      const Piece to = piece_of(a, b, s, oi, oh, piece);
       T* out = (T*)a.o + batch_off(a, b, a.os[0]) + (s.q0 + oi) * a.os[1] + (int64_t)oh * a.os[2];
       for (int d = (int)threadIdx.x % 8; d < (int)a.dim / 4; d += 8) {
         const float* src = (const float*)&lds[0][0][0][0] + col * DP + ((d ^ (col & 7)) << 2);
         f32x4 x = *(const f32x4*)src;
         for (int w = 1; w < SW; ++w) x += *(const f32x4*)(src + w * 32 * DP);
-        if (a.splits > 1) *(f32x4*)(piece.o + 4 * d) = x;
+        if (SHARED) *(f32x4*)(to.o + 4 * d) = x;
         else {
           typename Vec<T>::x4 y;
           for (int r = 0; r < 4; ++r) y[r] = (T)times(inv, x[r]);
@@ -143,33 +221,44 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
         }
       }
       if (threadIdx.x % 8 == 0) {
-        if (a.splits > 1) { piece.ml[0] = cm; piece.ml[1] = cl; }
-        else (a.lse + row_off(a, b, oh, s))[oi] = cl > 0.0f ? (cm + __log2f(cl)) * G10_LN2 : cl == 0.0f ? G10_NEG_INF : cl;
+        if (SHARED) {
+          to.ml[0] = cm;
+          to.ml[1] = cl;
+          if (!piece) *to.n = pieces;
+        }
+        if (!SHARED) (a.lse + row_off(a, b, oh, s))[oi] = cl > 0.0f ? (cm + __log2f(cl)) * G10_LN2 : cl == 0.0f ? G10_NEG_INF : cl;
       }
     }
-    __syncthreads();                                                // (the next rows' tiles go where the parts lie)
+    __syncthreads();                                                // (the next block's tiles go where the parts lie)
+    if constexpr (SHARED) {
+      if (place >= stop) break;
+    } else {
+      at += a.tiles;
+    }
   }
 }
 
-// A row's splits joined, a wavefront to a row, eight parts on their way at once: bound by the memory's latency (splits of
-// 8 sequences of 32768 keys, 16 to a row: XX us; part by part it was 17).
+// A row's pieces joined, a wavefront to a row, eight pieces on their way at once.  Bound by the memory's latency: 5 us for 8 sequences of
+// up to 32768 keys, one piece after the other 17.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
+__global__ __launch_bounds__(64 * SW) void k_attn_join(const AttnArgs a) {
   const u32 unit = blockIdx.x / a.tiles, b = unit / a.kv_heads, hk = unit % a.kv_heads, lane = lane_id();
   const Seq s = seq_of(a, b);
+  const Row w = row_of(a, s);
   const int rows = s.nq * (int)a.group;
-  for (int r = (int)((blockIdx.x % a.tiles) * 4 + wave_id()); r < rows; r += (int)a.tiles * 4) {
+  for (int r = (int)((blockIdx.x % a.tiles) * SW + wave_id()); r < rows; r += (int)a.tiles * SW) {
     const int i = r / (int)a.group;
     const u32 h = hk * a.group + (u32)(r % (int)a.group);
     const Piece p = piece_of(a, b, s, i, h, 0);
+    const u32 splits = w.tiles ? uniform(*p.n) : 0u;                 // (no key, no piece)
     float big = G10_NEG_INF;
-    for (u32 k = lane; k < a.splits; k += 64) big = fmaxf(big, p.ml[2 * k]);
+    for (u32 k = lane; k < splits; k += 64) big = fmaxf(big, p.ml[2 * k]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) big = fmaxf(big, __shfl_xor(big, d, 64));
     float x0 = 0.0f, x1 = 0.0f, l = 0.0f;
     const bool has = 2 * lane < a.dim;
-    for (u32 k0 = 0; k0 < a.splits; k0 += 64) {                      // a lane to a split for the weights, then a lane to two values
-      const u32 n = a.splits - k0 < 64 ? a.splits - k0 : 64;
+    for (u32 k0 = 0; k0 < splits; k0 += 64) {                      // a lane to a split for the weights, then a lane to two values
+      const u32 n = splits - k0 < 64 ? splits - k0 : 64;
       const float m = lane < n ? p.ml[2 * (k0 + lane)] : G10_NEG_INF, w = m == G10_NEG_INF ? 0.0f : exp2_fast(m - big);
       if (lane < n) l += m == G10_NEG_INF ? p.ml[2 * (k0 + lane) + 1] : p.ml[2 * (k0 + lane) + 1] * w;
       const float* from = p.o + (u64)k0 * a.dim + (has ? 2 * lane : 0);
@@ -202,51 +291,72 @@ __global__ __launch_bounds__(256) void k_attn_join(const AttnArgs a) {
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-// How many workgroups share a row's keys; 0: the work is not for these kernels.
-//   - Up to 64 columns (a row's heads times its queries) half or more of a query tile of k_attn_fwd would be empty.
-//   - The workgroups hold 128 KB of LDS each, one to a compute unit: four rounds of 256 even out sequences of unlike lengths.
-//   - A split has 256 keys or more, two tiles for each wavefront: less does not pay for the joining.
-// (Packed sequences go by their mean lengths, which are known here; max_q and max_k only cut the grid.)
-u32 attn_splits(const AttnArgs& a) {
+#define CUS 256                    // compute units
+
+static u32 attn_shares(const AttnArgs& a) { return a.dim <= 64 ? 2 * CUS : CUS; }
+
+// Whether few queries meet so many keys that these kernels are faster than k_attn_fwd, whose workgroups take 128 queries of a head each.  Times
+// in nanoseconds, measured: k_attn_fwd takes 16 for a workgroup's key (20 where two share a compute unit), these kernels 12 for a
+// block's key on a compute unit, and 9000 for the joining.  32 queries of 32 heads (8 of keys) on 32768 keys: 516 us there,
+// 54 here; 256 queries: 519 and 340; 512 queries: 520 and 688.  (Packed sequences go by their mean lengths, which are known here; max_q and max_k only cut the grid.)
+static bool few_queries(const AttnArgs& a, u64& blocks, u64& keys) {
   const u64 nq = a.q_start ? ((u64)a.seq_q + a.batch - 1) / a.batch : a.seq_q, nk = a.q_start ? ((u64)a.seq_k + a.batch - 1) / a.batch : a.seq_k;
-  const u64 cols = nq * a.group;
-  if (cols > 64) return 0;
-  u64 keys = nk;
+  blocks = (u64)a.batch * a.kv_heads * ((nq * a.group + 31) / 32);
+  keys = nk;
   if (a.window) {
     const u64 near = (u64)a.window * (a.causal ? 1 : 2) + nq + a.sinks;
     if (near < keys) keys = near;
   }
-  const u64 units = (u64)a.batch * a.kv_heads * ((cols + 31) / 32);
-  u64 n = (1024 + units - 1) / units;
-  const u64 most = (keys + 255) / 256;
-  if (n > most) n = most;
-  if (n > 512) n = 512;
-  return n ? (u32)n : 1u;
+  if (nq * a.group <= 32) return true;                               // (three of four wavefronts there would have no query)
+  const u64 there = (u64)a.batch * a.heads * ((nq + 127) / 128), rounds = there <= CUS ? CUS : there * 5 / 4;
+  return 12 * keys * blocks / CUS + 9000 < 16 * keys * rounds / CUS;
+}
+// The pieces of a block that there is room for; 0: the work is not for these kernels; 1: nothing is cut.  A compute unit holds one workgroup
+// (heads of up to 64 values: two), each gets a share: with four times as many shares one sequence of 32768 keys takes 52 us in
+// place of 32, with twice as many 40.  Cutting costs a second launch and a workgroup's search for its share: 512 keys of
+// one sequence take 13.0 us cut and 10.8 whole, 1024 keys 13.3 and 16.2; where there is a block for every compute unit, 1024 keys
+// of 32 sequences 30 us and 25, 2048 of 64 109 and 105 - more keys are cut all the same, for sequences of unlike lengths.
+u32 attn_splits(const AttnArgs& a) {
+  u64 blocks, keys;
+  if (!few_queries(a, blocks, keys)) return 0;
+  if (a.batch > BATCH || keys <= 768 || blocks >= 4 * CUS || (blocks >= CUS && keys <= 2048)) return 1;
+  const u64 most = ((u64)a.seq_q * a.group / 32 + 1) * (a.q_start ? 1 : a.batch) + a.batch;
+  if (most * a.kv_heads * (a.seq_k / ST + 2) >= 1ull << 31) return 1;                  // (tiles are counted in 32 bits)
+  const u64 n = (u64)a.batch * a.kv_heads;                           // (blocks of one key head lie in a row: the more, the fewer pieces)
+  return (u32)(2 * ((attn_shares(a) + n - 1) / n) + 2);
 }
 u64 attn_split_bytes(const AttnArgs& a, u32 splits) {
   if (splits <= 1) return 0;
   const u64 rows = (u64)(a.q_start ? 1 : a.batch) * a.seq_q * a.heads;
-  return rows * splits * (a.dim + 2) * 4;
+  return rows * (splits * (a.dim + 2) + 1) * 4;
 }
 
 template <class T>
 static void launch(AttnArgs a, hipStream_t s) {
   const u32 units = a.batch * a.kv_heads;
-  a.tiles = (u32)(((u64)a.max_q * a.group + 31) / 32);
-  const dim3 grid(unit_grid(units, a.tiles * a.splits));
-  if (a.dim <= 64) k_attn_split<T, 64><<<grid, 64 * SW, 0, s>>>(a);
-  else k_attn_split<T, 128><<<grid, 64 * SW, 0, s>>>(a);
   if (a.splits > 1) {
-    a.tiles = (u32)(((u64)a.max_q * a.group + 3) / 4);
-    k_attn_join<T><<<units * a.tiles, 256, 0, s>>>(a);
+    // with several blocks to a key head an XCD's shares lie in a row, so that blocks of the same keys meet in its L2 (64 queries of 4 x 8192
+    // keys: 168 -> 101 us); with one they do not (8 x 32768 keys: 188 us, in a row 204)
+    a.tiles = a.max_q * a.group > 32 ? 8 : 1;
+    if (a.dim <= 64) k_attn_split<T, 64, true><<<a.shares, 64 * SW, 0, s>>>(a);
+    else k_attn_split<T, 128, true><<<a.shares, 64 * SW, 0, s>>>(a);
+    a.tiles = (u32)(((u64)a.max_q * a.group + SW - 1) / SW);
+    k_attn_join<T><<<units * a.tiles, 64 * SW, 0, s>>>(a);
+  } else {
+    a.tiles = (u32)(((u64)a.max_q * a.group + 31) / 32);
+    const dim3 grid(unit_grid(units, a.tiles));
+    if (a.dim <= 64) k_attn_split<T, 64, false><<<grid, 64 * SW, 0, s>>>(a);
+    else k_attn_split<T, 128, false><<<grid, 64 * SW, 0, s>>>(a);
   }
 }
 
 int attn_forward_split(AttnArgs a, u32 splits, void* workspace, u32 type, hipStream_t s) {
   a.splits = splits;
+  a.shares = attn_shares(a);
   const u64 rows = (u64)(a.q_start ? 1 : a.batch) * a.seq_q * a.heads;
   a.part = (float*)workspace;
   a.part_ml = splits > 1 ? a.part + rows * splits * a.dim : nullptr;
+  a.part_n = splits > 1 ? (u32*)(a.part_ml + rows * splits * 2) : nullptr;
   if (type == G10_BF16) launch<__bf16>(a, s);
   else launch<_Float16>(a, s);
   G10_HIP(hipGetLastError());

@@ -268,3 +268,34 @@ def test_what_nobody_sees_may_hold_anything(ops, dim, dtype, nq, nk, causal, win
             t[:, blind.cuda()] = value
         for x, y in zip(run(q, k, v, do), want):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("heads, kv, dim, dtype", [(8, 2, 128, torch.bfloat16), (4, 4, 64, torch.float16), (32, 1, 40, torch.bfloat16)])
+@pytest.mark.parametrize("nq, nk, window, sinks", [(9, 2000, 0, 0), (17, 1100, 0, 0), (70, 3000, 0, 0), (70, 3000, 1200, 5), (130, 2500, 900, 0), (33, 2600, 40, 4)])
+def test_few_queries_and_many_keys(ops, nq, nk, window, sinks, heads, kv, dim, dtype):
+    """Blocks of queries and heads whose keys are cut into shares: sequences of unlike lengths, one without a key, one shorter than the queries."""
+    q, k, v, _ = make((5, nq), (5, nk), heads, kv, dim, dtype, seed=nq + nk)
+    k_len = torch.tensor([nk, 0, max(1, nq // 2), nk - 33, 700], dtype=torch.int32).cuda()
+    for b, n in enumerate(k_len.tolist()):
+        k[b, n:] = float("nan")
+        v[b, n:] = float("inf")
+    check(ops, q, k, v, window=window, sinks=sinks, k_len=k_len)
+    check(ops, q[:1], k[:1], v[:1], window=window, sinks=sinks, causal=False)
+
+
+def test_few_packed_queries_and_many_keys(ops):
+    nq, nk = [20, 0, 1, 64, 3], [3000, 900, 1500, 64, 0]
+    at = [torch.tensor([0] + n).cumsum(0).to(torch.int32).cuda() for n in (nq, nk)]
+    q, k, v, _ = make((sum(nq),), (sum(nk),), 8, 2, 64, torch.bfloat16)
+    first = check(ops, q, k, v, q_start=at[0], k_start=at[1], max_q=64, max_k=3000)
+    for most in (1, 30, None):
+        o, lse = ops.g10_attention(q, k, v, q_start=at[0], k_start=at[1], max_q=most, max_k=most)
+        assert torch.equal(o, first["o"]) and torch.equal(lse, first["lse"])
+
+
+def test_more_sequences_than_are_cut(ops):
+    """300 sequences: whole blocks; 200: shares, most of them shorter than a share."""
+    for n in (300, 200):
+        q, k, v, _ = make((n, 1), (n, 900), 4, 1, 64, torch.bfloat16, seed=n)
+        k_len = (torch.arange(n, dtype=torch.int32) * 37 % 901).cuda()
+        check(ops, q, k, v, k_len=k_len)
