@@ -5,6 +5,9 @@
 
 #define BT 64                      // rows of a tile in LDS
 #define BW 128                     // rows of a workgroup, 32 to a wavefront
+#define FEW 12                     // tiles of 32 keys up to which delta comes from P and dP; keys up to which dS keeps its lower half for dq, and
+#define SOME 768                   // P and dS theirs for dk and dv
+#define FEWEST 128
 
 // In 16-bit floats with a short exponent, P and dS of long rows would fall below the smallest number.  P is held times
 // 2^12 (it is at most 1), dS times 8 over the power of two at the largest |do| of what it is summed over: of the query for dQ, of the
@@ -64,13 +67,21 @@ __device__ __forceinline__ f32x16 minus_delta(const Half& x) {
   return d;
 }
 
-// In: the tile's scores and dP - delta in sc and dp.  Out: the next tile's.
-template <class T, int DP>
+// What rounding eight values of x left of them.
+template <class T>
+__device__ __forceinline__ typename Vec<T>::x8 left8(f32x16& x, const typename Vec<T>::x8& got, int s) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[8 * s + k] -= (float)got[k];
+  return pack8<T>(x, s);
+}
+
+// In: the tile's scores and dP - delta in sc and dp.  Out: the next tile's.  FINE: P and dS meet dO and Q as their rounding and what that left.
+template <class T, int DP, bool FINE>
 __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const typename Vec<T>::x8 (&kf)[DP / 16], const typename Vec<T>::x8 (&vf)[DP / 16],
                                           f32x16& sc, f32x16& dp, f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], float scale2, float lift_ds) {
   typedef typename Vec<T>::x8 x8;
   constexpr int KS = DP / 16, DB = DP / 32, N = 2 * KS + 4 * DB, AHEAD = 4, RING = 5;
-  x8 f[RING], pf[2], df[2];
+  x8 f[RING], pf[2], df[2], pl[2], dl[2];
   auto read = [&](int e) -> x8 {
     if (e < 2 * KS) return frag_rows<T, DP>(nx.rows, e % 2 * BT, e / 2);
     e -= 2 * KS;
@@ -107,10 +118,16 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
       else dn = Vec<T>::mfma(f[e % RING], vf[e / 2], dn);
       if constexpr (e < KS) exps(16 * e / KS, 16 * (e + 1) / KS);
       else grads(16 * (e - KS) / KS, 16 * (e - KS + 1) / KS);
+      if constexpr (FINE && e == 2 * KS - 1) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) { pl[k] = left8<T>(sc, pf[k], k); dl[k] = left8<T>(dp, df[k], k); }
+      }
     } else {
       constexpr int v = e - 2 * KS;
       if constexpr (v < 2 * DB) dv[v % DB] = Vec<T>::mfma(f[e % RING], pf[v / DB], dv[v % DB]);
       else dk[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB - 2], dk[v % DB]);
+      if constexpr (FINE && v < 2 * DB) dv[v % DB] = Vec<T>::mfma(f[e % RING], pl[v / DB], dv[v % DB]);
+      if constexpr (FINE && v >= 2 * DB) dk[v % DB] = Vec<T>::mfma(f[e % RING], dl[v / DB - 2], dk[v % DB]);
 #pragma unroll
       for (int r = 16 * v / (4 * DB); r < 16 * (v + 1) / (4 * DB); ++r) { sc[r] = sn[r]; dp[r] = dn[r]; }
     }
@@ -118,7 +135,7 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
   });
 }
 
-template <class T, int DP>
+template <class T, int DP, bool FINE>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnArgs a) {
   __shared__ __attribute__((aligned(256))) T lds[3][2][BT * DP];
   __shared__ __attribute__((aligned(16))) float rows[3][2][BT];      // lse2, delta of a tile's queries
@@ -232,7 +249,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
           buf = buf == 2 ? 0 : buf + 1;
           if (cur > hi) cur = first;
         } else n = 1;
-        back_step<T, DP>(here, half(buf, n), kf, vf, sc, dp, dk, dv, a.scale2, lift_ds);
+        back_step<T, DP, FINE>(here, half(buf, n), kf, vf, sc, dp, dk, dv, a.scale2, lift_ds);
       }
     }
     const float fk = a.scale / lift, fv = 1.0f / Lift<T>::p;
@@ -292,13 +309,13 @@ __global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
 //   S^T = K Q^T,  dP^T = V dO^T  come out with a query to a lane,  dQ^T += K^T dS^T;   first, delta = sum(do o) of each query, which
 // the keys' kernel takes from here.  The same pipeline as there, two wavefronts to a SIMD.
 // These keys' scores and dP are in sc and dp, the next ones' go to sn and dn.  LDS: rows_base of the next keys, with their values behind them,
-// cols_base of these keys.
-template <class T, int DP>
+// cols_base of these keys.  FINE: dS meets the keys as its rounding and what that left, in two products.
+template <class T, int DP, bool FINE>
 __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Vec<T>::x8 (&q)[DP / 16], const typename Vec<T>::x8 (&dout)[DP / 16],
                                            f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn, f32x16 (&dq)[DP / 32], float scale2, float le, const f32x16& less, float lift) {
   typedef typename Vec<T>::x8 x8;
   constexpr int KS = DP / 16, DB = DP / 32, N = 2 * KS + 2 * DB, AHEAD = 4, RING = 5;
-  x8 f[RING], df[2];
+  x8 f[RING], df[2], left[2];
   auto read = [&](int e) -> x8 {
     if (e < 2 * KS) return frag_rows<T, DP>(rows, e % 2 * 32, e / 2);
     return frag_tr<T, DP>(cols, (e - 2 * KS) / DB * 16, (e - 2 * KS) % DB);
@@ -324,14 +341,18 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
     } else {
       constexpr int v = e - 2 * KS;
       dq[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB], dq[v % DB]);
+      if constexpr (FINE) {
+        if constexpr (v % DB == 0) left[v / DB] = left8<T>(dp, df[v / DB], v / DB);
+        dq[v % DB] = Vec<T>::mfma(f[e % RING], left[v / DB], dq[v % DB]);
+      }
     }
     hold();
   });
 }
 
-template <class T, int DP>
+template <class T, int DP, bool FINE>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
-  constexpr int KT = 32, NB = 4, FEW = 12;                           // keys of a tile; these, the next, two on their way
+  constexpr int KT = 32, NB = 4;                                     // keys of a tile; these, the next, two on their way
   __shared__ __attribute__((aligned(256))) T lds[NB][2][KT * DP];
   typedef typename Vec<T>::x8 x8;
   u32 unit, at;
@@ -366,7 +387,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     // delta is sum(P dP) as well as sum(do o).  The second costs a reading of o, but o is rounded, and where few keys are seen that
     // error is large beside dq and dk: against a result that is only rounded once, theirs is 1.4 times as large with the first and with
     // the second 2.3 times for 4 keys, 1.6 for 128, 1.5 for 400.  So the first up to 384 keys of the workgroup's, for one more walk over them
-    // (two of a step's three products).
+    // (two of a step's three products).  (See keys_seen for more of them.)
     const bool few = tiles.count <= FEW;
     u32 to = 0;
     int ft = 0, rest = few ? 2 * tiles.count : tiles.count;          // next tile to be fetched; how many there are to be
@@ -460,7 +481,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
           for (int r = 0; r < 16; ++r) sc[r] = seen.key(j0 + res_row(r)) ? sc[r] : G10_NEG_INF;
         }
         const u32 next = (buf + 1) % NB;
-        query_step<T, DP>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, less, lift);
+        query_step<T, DP, FINE>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, less, lift);
         buf = next;
         ++t;
       };
@@ -536,6 +557,29 @@ static uint64_t sink_bytes(const AttnArgs& a) {
   return a.sink_tiles ? (uint64_t)a.batch * a.kv_heads * a.sink_tiles * a.splits * 2 * BW * (a.dim <= 64 ? 64 : 128) * 4 : 0;
 }
 
+// How many keys a query sees at most, or in a packed sequence of mean length, which is known here: it decides where P and dS keep their lower halves.
+// As 16-bit numbers they add about as much error to the gradients as those' own rounding, 1.41 times that in all; o's rounding in delta brings dq to 1.5
+// times where few keys are seen, and with very few of them a single factor's rounding may rule a row.  Up to 768 keys dq has both halves of
+// dS (1.05 to 1.08 times its rounding, for one product of three more: 32 x 512 tokens of 12 heads of 64, 198 -> 204 us forward and backward; delta from
+// P and dP up to there: 245), up to 128 dk and dv have those of dS and P too.
+static uint64_t keys_seen(const AttnArgs& a) {
+  const uint64_t keys = a.q_start ? ((uint64_t)a.seq_k + a.batch - 1) / a.batch : a.seq_k;
+  const uint64_t near = a.window ? (uint64_t)a.window * (a.causal ? 1 : 2) + a.sinks : keys;
+  return near < keys ? near : keys;
+}
+
+template <class T, int DP>
+static void launch_dq(const AttnArgs& a, bool fine, dim3 grid, hipStream_t s) {
+  if (fine) k_attn_dq<T, DP, true><<<grid, 256, 0, s>>>(a);
+  else k_attn_dq<T, DP, false><<<grid, 256, 0, s>>>(a);
+}
+
+template <class T, int DP>
+static void launch_dkdv(const AttnArgs& a, bool fine, dim3 grid, hipStream_t s) {
+  if (fine) k_attn_dkdv<T, DP, true><<<grid, 256, 0, s>>>(a);
+  else k_attn_dkdv<T, DP, false><<<grid, 256, 0, s>>>(a);
+}
+
 extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uint64_t* bytes) {
   if (!bytes) return G10_EINVAL;
   AttnArgs a;
@@ -557,26 +601,29 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   const uint64_t per = kt + (uint64_t)a.sink_tiles * (a.splits - 1);
   if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * per >= (1ull << 31)) return G10_EINVAL;
   hipStream_t s = (hipStream_t)hip_stream;
+  const uint64_t seen = keys_seen(a);
   a.amax = (const u32*)workspace;
   a.delta = (const float*)((char*)workspace + top_bytes(a));
   a.lse2 = a.delta + rows;
   a.part = (float*)((char*)a.delta + pad256(rows * 8));
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
   if (qt) {
+    const bool fine = seen <= SOME;
     a.tiles = (u32)qt;
     const dim3 grid(unit_grid((u32)units, a.group * a.tiles));
-    if (bf && narrow) k_attn_dq<__bf16, 64><<<grid, 256, 0, s>>>(a);
-    else if (bf) k_attn_dq<__bf16, 128><<<grid, 256, 0, s>>>(a);
-    else if (narrow) k_attn_dq<_Float16, 64><<<grid, 256, 0, s>>>(a);
-    else k_attn_dq<_Float16, 128><<<grid, 256, 0, s>>>(a);
+    if (bf && narrow) launch_dq<__bf16, 64>(a, fine, grid, s);
+    else if (bf) launch_dq<__bf16, 128>(a, fine, grid, s);
+    else if (narrow) launch_dq<_Float16, 64>(a, fine, grid, s);
+    else launch_dq<_Float16, 128>(a, fine, grid, s);
   }
   if (kt) {
+    const bool fine = seen <= FEWEST;
     a.tiles = (u32)kt;
     const dim3 grid(unit_grid((u32)units, (u32)per));
-    if (bf && narrow) k_attn_dkdv<__bf16, 64><<<grid, 256, 0, s>>>(a);
-    else if (bf) k_attn_dkdv<__bf16, 128><<<grid, 256, 0, s>>>(a);
-    else if (narrow) k_attn_dkdv<_Float16, 64><<<grid, 256, 0, s>>>(a);
-    else k_attn_dkdv<_Float16, 128><<<grid, 256, 0, s>>>(a);
+    if (bf && narrow) launch_dkdv<__bf16, 64>(a, fine, grid, s);
+    else if (bf) launch_dkdv<__bf16, 128>(a, fine, grid, s);
+    else if (narrow) launch_dkdv<_Float16, 64>(a, fine, grid, s);
+    else launch_dkdv<_Float16, 128>(a, fine, grid, s);
   }
   if (kt && a.sink_tiles) {
     const dim3 grid((u32)units * a.sink_tiles, 8);

@@ -299,3 +299,16 @@ def test_more_sequences_than_are_cut(ops):
         q, k, v, _ = make((n, 1), (n, 900), 4, 1, 64, torch.bfloat16, seed=n)
         k_len = (torch.arange(n, dtype=torch.int32) * 37 % 901).cuda()
         check(ops, q, k, v, k_len=k_len)
+
+
+@pytest.mark.parametrize("dim, dtype", [(64, torch.float16), (128, torch.bfloat16)])
+@pytest.mark.parametrize("n, causal, window", [(7, True, 0), (60, True, 0), (380, False, 0), (512, False, 0), (760, False, 0), (1200, True, 500)])
+def test_gradients_are_off_by_little_more_than_their_rounding(ops, n, causal, window, dim, dtype):
+    """Their own rounding, once more as much from the 16-bit factors of their products, a quarter of it from delta: 1.5 times one rounding in all."""
+    q, k, v, do = make((2, n), (2, n), 4, 2, dim, dtype, seed=n)
+    want = O.attention(q.cpu(), k.cpu(), v.cpu(), do.cpu(), causal, window, 0)
+    o, lse = ops.g10_attention(q, k, v, causal=causal, window=window)
+    for name, x in zip(("dq", "dk", "dv"), ops.g10_attention_backward(do, q, k, v, o, lse, causal=causal, window=window)):
+        exact = want[name][0]
+        once = (exact.to(dtype).double() - exact).norm()
+        assert (O.d(x) - exact).norm() <= 1.5 * once, name
