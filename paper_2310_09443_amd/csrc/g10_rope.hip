@@ -38,14 +38,16 @@ struct Raw {
     for (int i = 0; i < 4; ++i) { v[i] = (float)a[i]; v[4 + i] = (float)b[i]; }
   }
 };
+// (Past the L2, which would write them back when the kernel ends: 32768 tokens of 64 heads of 128 218 -> 210 us, 5001 of 20 heads of 80 in 32 bits,
+// forward and backward, 55 -> 48.)
 template <class T>
 __device__ __forceinline__ void store8(T* p, u32 d0, u32 d1, const float (&v)[8]) {
   typedef T x4 __attribute__((ext_vector_type(4)));
   x4 a, b;
 #pragma unroll
   for (int i = 0; i < 4; ++i) { a[i] = (T)v[i]; b[i] = (T)v[4 + i]; }
-  *(x4*)(p + d0) = a;
-  *(x4*)(p + d1) = b;
+  __builtin_nontemporal_store(a, (x4*)(p + d0));
+  __builtin_nontemporal_store(b, (x4*)(p + d1));
 }
 
 template <int CTRL>
