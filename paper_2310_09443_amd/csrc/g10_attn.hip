@@ -61,9 +61,9 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
   constexpr int BM = 32 * NW;
   __shared__ __attribute__((aligned(256))) T lds[2][2][BN * DP];      // keys, values; even and odd tiles
   typedef typename Vec<T>::x8 x8;
-  u32 unit, at;
-  if (!unit_of(a.batch * a.kv_heads, a.group * a.tiles, unit, at)) return;
-  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + at / a.tiles;
+  u32 unit, head, last;
+  if (!block_of(a.batch * a.kv_heads, a.group, a.tiles, unit, head, last)) return;
+  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + head;
   const Seq s = seq_of(a, b);
   const int off = s.nk - s.nq;
   const Unseen unseen = unseen_keys(a, s);
@@ -78,8 +78,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
   constexpr u32 odd = BN * DP * 2;
   const u32 tk = rows_base<DP>(lds_addr(lds[0][0])), tv = cols_base<DP>(lds_addr(lds[1][0]));
   bool again = false;
-  // (the last tiles of a causal sequence are the longest: first)
-  for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BM < s.nq; qt += (int)a.tiles) {
+  for (int qt = (int)last; qt * BM < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BM + (int)wave * 32, i = i0 + (int)(lane & 31);
     const Seen seen = keys_of(a, i + off, s.nk);
     const int wp0 = i0 + off, wp1 = (i0 + 31 < s.nq ? i0 + 31 : s.nq - 1) + off;       // the wavefront's positions

@@ -355,9 +355,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   constexpr int KT = 32, NB = 4;                                     // keys of a tile; these, the next, two on their way
   __shared__ __attribute__((aligned(256))) T lds[NB][2][KT * DP];
   typedef typename Vec<T>::x8 x8;
-  u32 unit, at;
-  if (!unit_of(a.batch * a.kv_heads, a.group * a.tiles, unit, at)) return;
-  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + at / a.tiles;
+  u32 unit, head, first;
+  if (!block_of(a.batch * a.kv_heads, a.group, a.tiles, unit, head, first)) return;
+  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + head;
   const Seq s = seq_of(a, b);
   const int off = s.nk - s.nq;
   const u32 wave = uniform(wave_id()), lane = lane_id();
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   const Unseen unseen = unseen_keys(a, s);
   bool again = false;
   u32 most = 0;
-  for (int qt = (int)(a.tiles - 1 - at % a.tiles); qt * BW < s.nq; qt += (int)a.tiles) {
+  for (int qt = (int)first; qt * BW < s.nq; qt += (int)a.tiles) {
     const int i0 = qt * BW + (int)wave * 32, i = i0 + (int)(lane & 31), c = i < s.nq ? i : s.nq - 1;
     const Seen seen = keys_of(a, i + off, s.nk);
     const int wp0 = i0 + off, wp1 = (i0 + 31 < s.nq ? i0 + 31 : s.nq - 1) + off;
@@ -522,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
         }
     }
   }
-  if (Lift<T>::ds && !lane) ((u32*)a.amax)[((u64)unit * a.group * a.tiles + at) * 4 + wave] = most;
+  if (Lift<T>::ds && !lane) ((u32*)a.amax)[(((u64)unit * a.group + head) * a.tiles + first) * 4 + wave] = most;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
