@@ -44,6 +44,8 @@ __device__ __forceinline__ void each_of(F&& f) {
   }
 }
 
+struct Cut { u32 b, hk, kt, more; };   // backward: a tile of keys that begins in a share and goes on in `more` others
+
 struct AttnArgs {
   const void *q, *k, *v;
   void *o, *dq, *dk, *dv;
@@ -52,18 +54,18 @@ struct AttnArgs {
   const float* delta;              // backward: - sum of do * o per query
   const float* lse2;               // backward: lse in powers of two, less the lift of P
   const u32* amax;                 // backward: bits of the largest |do| of each wavefront of k_attn_dq
-  float *part, *part_ml;           // split over the keys: unfinished outputs and their maxima and sums; how many to a row
+  float *part, *part_ml;           // split over the keys: unfinished outputs and their maxima and sums; how many to a row.  Backward: unfinished dv and dk
   u32* part_n;
+  Cut* cuts;                       // backward: a share's
   int64_t qs[3], ks[3], vs[3], os[3], dos[3], dqs[3], dks[3], dvs[3];   // batch, token, head
   const int *q_start, *k_start, *k_len;
   u32 batch, heads, kv_heads, group, dim;
   u32 seq_q, seq_k, max_q, max_k;
   u32 causal, window, sinks;
   u32 tiles;                       // of queries (or of keys) per sequence and head in the grid
-  u32 splits;                      // forward: pieces of a block that there is room for; backward: workgroups that share a tile of sinks' queries
-  u32 shares;                      // forward: that the work is cut into
+  u32 splits;                      // forward: pieces of a block that there is room for
+  u32 shares;                      // that the work is cut into; backward: 0: it is not
   u32 q_tiles;                     // backward: of queries per sequence and head in k_attn_dq's grid
-  u32 sink_tiles;                  // backward: key tiles whose queries are shared
   float scale, scale2;             // scale2 = scale * log2(e)
 };
 

@@ -23,25 +23,81 @@ template <> struct Lift<_Float16> {
 };
 __device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)(127 + 3 - clampi((int)(top >> 23) - 127, -60, 60)) << 23); }
 
-// A workgroup's unit, first tile of keys and part of the queries: the parts of the sinks' tiles first, of all units, then a
-// unit's other tiles together.
-__device__ __forceinline__ bool tile_of(const AttnArgs& a, u32& unit, u32& kt, u32& part) {
-  const u32 units = a.batch * a.kv_heads, ahead = a.sink_tiles * a.splits, rest = a.tiles - a.sink_tiles;
-  const bool round = units % 8 == 0 || units >= 64;                  // (as in unit_of)
-  const u32 slot = round ? blockIdx.x / 8 : blockIdx.x, mine = round ? (units + 7) / 8 : units;
-  u32 u, at;
-  if (slot < mine * ahead) {
-    u = slot % mine;
-    at = slot / mine;
-    kt = at / a.splits;
-    part = at % a.splits;
-  } else {
-    u = (slot - mine * ahead) / rest;
-    kt = a.sink_tiles + (slot - mine * ahead) % rest;
-    part = 0;
+// The work of k_attn_dkdv, all sequences' key heads and tiles of 128 keys in one row, in steps of 64 queries and ENTRY more a tile, cut
+// into equal shares: a tile with sinks is seen by all later queries and one at the end of a causal sequence by few, and
+// few tiles, or a few more than there are compute units, leave units idle.  A cut goes through a tile wherever it falls; its pieces
+// meet in k_attn_cuts.
+#define ENTRY 2u                   // steps that a tile's begin and end take
+#define JOIN 8                     // pieces of a tile on their way at once where they are joined
+#define SHARE 8                    // steps of a share at least: its pieces are worth their joining
+struct Steps { int first, hi, each; u32 all; };                      // first and last query, tiles of 64 queries to a head, steps
+__device__ __forceinline__ Steps steps_of(const AttnArgs& a, const Seq& s, int kt) {
+  int lo = 0;                                                        // queries that see any key of the tile
+  const int e1 = (kt + 1) * BW < s.nk ? (kt + 1) * BW - 1 : s.nk - 1;
+  Steps x;
+  x.hi = -1;
+  if (kt * BW < s.nk) query_range(a, kt * BW, e1, s, lo, x.hi);
+  x.first = lo / 32 * 32;
+  x.each = x.hi >= lo ? (x.hi - x.first) / BT + 1 : 0;
+  x.all = ENTRY + (u32)x.each * a.group;
+  return x;
+}
+__device__ __forceinline__ int key_rows(const AttnArgs& a, const Seq& s) { return a.q_start ? s.nk : (int)a.seq_k; }   // of dk and dv to be written
+__device__ __forceinline__ u64 head_steps(const AttnArgs& a, u32 b) {
+  const Seq s = seq_of(a, b);
+  u64 n = 0;
+  for (int kt = 0; kt * BW < key_rows(a, s); ++kt) n += steps_of(a, s, kt).all;
+  return n;
+}
+struct Place {
+  u32 b, hk;
+  int kt;
+  u32 in;                          // steps of the tile before it
+};
+struct Row {
+  u64 each, total;                 // steps of a share, of all
+  const u64* end;                  // in LDS: steps up to and with a thread's sequences
+  u32 seqs;                        // sequences to a thread
+  __device__ __forceinline__ Place at(const AttnArgs& a, u64 place) const {
+    u32 lo = 0, hi = 255;
+    while (lo < hi) {
+      const u32 mid = (lo + hi) / 2;
+      if (uniform(end[mid]) > place) hi = mid;
+      else lo = mid + 1;
+    }
+    const u64 before = lo ? uniform(end[lo - 1]) : 0;
+    u64 in = place - before, head;
+    Place p = {lo * seqs, 0, 0, 0};
+    while (true) {
+      head = seqs == 1 ? (uniform(end[lo]) - before) / a.kv_heads : head_steps(a, p.b);
+      if (in < head * a.kv_heads) break;
+      in -= head * a.kv_heads;
+      ++p.b;
+    }
+    p.hk = (u32)(in / head);
+    in %= head;
+    const Seq s = seq_of(a, p.b);
+    for (u32 n; in >= (n = steps_of(a, s, p.kt).all); ++p.kt) in -= n;
+    p.in = (u32)in;
+    return p;
   }
-  unit = round ? blockIdx.x % 8 + 8 * u : u;
-  return unit < units;
+};
+__device__ __forceinline__ Row row_of(const AttnArgs& a, u64* end) {
+  Row r = {0, 0, end, (a.batch + 255) / 256};
+  u64 n = 0;
+  for (u32 b = threadIdx.x * r.seqs; b < (threadIdx.x + 1) * r.seqs && b < a.batch; ++b) n += head_steps(a, b) * a.kv_heads;
+  end[threadIdx.x] = n;
+  __syncthreads();
+  for (u32 d = 1; d < 256; d *= 2) {
+    const u64 x = threadIdx.x >= d ? end[threadIdx.x - d] : 0;
+    __syncthreads();
+    end[threadIdx.x] += x;
+    __syncthreads();
+  }
+  r.total = uniform(end[255]);
+  r.each = (r.total + a.shares - 1) / a.shares;
+  if (r.each < SHARE) r.each = SHARE;
+  return r;
 }
 
 // Gradients of 128 keys and values, 32 to a wavefront, which holds their rows and sums in registers and walks over the
@@ -51,8 +107,7 @@ __device__ __forceinline__ bool tile_of(const AttnArgs& a, u32& unit, u32& kt, u
 // itself (in heads of 64 values: half of them), so nobody else's work fills its waits: it works on the next 32 queries' first
 // products and these ones' second ones, product by product, with these ones' exponentials strewn between and the fragments four
 // ahead on their way from LDS.  Tiles of 64 queries: this one, the next, and the one on its way from memory.
-// A tile with sinks is seen by all later queries, the others by those of a window: the sinks' are worked on by several workgroups,
-// the first ones to start, whose sums meet in k_attn_sinks.
+// SHARED: a workgroup to a share.  Otherwise one to a tile.
 struct Half { u32 rows, cols, stats; };                              // LDS addresses of 32 queries of a tile: rows_base and cols_base of Q, with dO a tile behind it; lse2 and delta
 
 // The sums of dP begin with what is taken from them.
@@ -135,49 +190,68 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
   });
 }
 
-template <class T, int DP, bool FINE>
+template <class T, int DP, bool FINE, bool SHARED>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnArgs a) {
   __shared__ __attribute__((aligned(256))) T lds[3][2][BT * DP];
   __shared__ __attribute__((aligned(16))) float rows[3][2][BT];      // lse2, delta of a tile's queries
+  __shared__ u64 ends[SHARED ? 256 : 1];
   typedef typename Vec<T>::x8 x8;
-  u32 unit, kt0, part;
-  if (!tile_of(a, unit, kt0, part)) return;
-  const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads;
-  const Seq s = seq_of(a, b);
+  Place at = {};
+  u64 place = 0, stop = 0;
+  Row row = {};
+  u32 mine = 0;
+  if constexpr (SHARED) {
+    row = row_of(a, ends);
+    mine = blockIdx.x % 8 * (a.shares / 8) + blockIdx.x / 8;         // (an XCD's shares lie in a row)
+    if (!threadIdx.x) a.cuts[mine] = Cut{};
+    place = mine * row.each;
+    if (place >= row.total) return;
+    stop = place + row.each < row.total ? place + row.each : row.total;
+    at = row.at(a, place);
+  } else {
+    u32 unit, kt;
+    if (!unit_of(a.batch * a.kv_heads, a.tiles, unit, kt)) return;
+    at.b = unit / a.kv_heads;
+    at.hk = unit % a.kv_heads;
+    at.kt = (int)kt;
+  }
   const u32 wave = uniform(wave_id()), lane = lane_id();
-  const T* Q0 = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)hk * a.group * a.qs[2];
-  const T* D0 = (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)hk * a.group * a.dos[2];
-  const int nk_all = a.q_start ? s.nk : (int)a.seq_k;                // rows of dk and dv to be written
   Walk<DP, BT, 256> sq, sd;
   sq.init(threadIdx.x, a.dim, a.qs[1]);
   sd.init(threadIdx.x, a.dim, a.dos[1]);
   const u32 tile0 = lds_addr(lds[0][0]) + wave * 1024, rows0 = lds_addr(rows[0]);
-  float lift = 1.0f;
-  if (Lift<T>::ds) {
-    const u32 n = a.group * a.q_tiles * 4;
-    const u32* all = a.amax + (u64)unit * n;
-    u32 top = 0;
-    for (u32 x = lane; x < n; x += 64) top = max(top, all[x]);
-    top = wave_max(top);
-    lift = lift_of(top);
-  }
-  const float lift_ds = lift / Lift<T>::p;
-  const Unseen unseen = unseen_queries(a, s);
   bool again = false;
-  for (int kt = (int)kt0; kt * BW < nk_all; kt += (int)a.tiles) {
-    const bool shared = (u32)kt < a.sink_tiles;
-    if (!shared && part) break;
+  while (true) {
+    const u32 b = at.b, hk = at.hk;
+    const int kt = at.kt;
+    const Seq s = seq_of(a, b);
+    const int nk_all = key_rows(a, s);
+    if (!SHARED && kt * BW >= nk_all) break;
+    const T* Q0 = (const T*)a.q + batch_off(a, b, a.qs[0]) + s.q0 * a.qs[1] + (int64_t)hk * a.group * a.qs[2];
+    const T* D0 = (const T*)a.d_o + batch_off(a, b, a.dos[0]) + s.q0 * a.dos[1] + (int64_t)hk * a.group * a.dos[2];
+    float lift = 1.0f;
+    if (Lift<T>::ds) {
+      const u32 n = a.group * a.q_tiles * 4;
+      const u32* all = a.amax + ((u64)b * a.kv_heads + hk) * n;
+      u32 top = 0;
+      for (u32 x = lane; x < n; x += 64) top = max(top, all[x]);
+      top = wave_max(top);
+      lift = lift_of(top);
+    }
+    const float lift_ds = lift / Lift<T>::p;
+    const Unseen unseen = unseen_queries(a, s);
     const int j0 = kt * BW + (int)wave * 32, j = j0 + (int)(lane & 31);
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
-    int lo = 0, hi = -1;                                             // queries that see any key of the workgroup
-    const int e1 = (kt + 1) * BW < s.nk ? (kt + 1) * BW - 1 : s.nk - 1;
-    if (kt * BW < s.nk) query_range(a, kt * BW, e1, s, lo, hi);
-    const int first = lo / 32 * 32, each = hi >= lo ? (hi - first) / BT + 1 : 0;      // tiles of queries ...
-    int from = 0, all = each * (int)a.group;                         // ... of all heads one after the other
-    if (shared) {
-      from = (int)((int64_t)all * part / a.splits);
-      all = (int)((int64_t)all * (part + 1) / a.splits) - from;
+    const Steps steps = steps_of(a, s, kt);
+    const int first = steps.first, each = steps.each, hi = steps.hi;
+    int from = 0, all = each * (int)a.group;                         // tiles of queries of all heads one after the other
+    u32 take = steps.all;
+    if constexpr (SHARED) {
+      if ((u64)(take - at.in) > stop - place) take = at.in + (u32)(stop - place);
+      from = at.in > ENTRY ? (int)(at.in - ENTRY) : 0;
+      all = (take > ENTRY ? (int)(take - ENTRY) : 0) - from;
     }
+    const bool whole = !SHARED || (!at.in && take == steps.all);
     if (all > 0) {
       int ilo = 0, ihi = -1, flo, fhi;                               // ... of the lane; that see all of the wavefront's keys
       if (j < s.nk) query_range(a, j, j, s, ilo, ihi);
@@ -253,8 +327,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
       }
     }
     const float fk = a.scale / lift, fv = 1.0f / Lift<T>::p;
-    if (shared) {
-      float* to = a.part + (((u64)unit * a.sink_tiles + (u32)kt) * a.splits + part) * (2 * BW * DP) + ((int)wave * 32 + (int)(lane & 31)) * DP;
+    if (!whole) {
+      if (!at.in && !threadIdx.x) {                                  // the first piece
+        const u64 last = place + steps.all - 1;
+        a.cuts[mine] = Cut{b, hk, (u32)kt, (u32)(last / row.each) - mine};
+      }
+      float* to = a.part + ((u64)mine * 2 + !at.in) * (2 * BW * DP) + ((int)wave * 32 + (int)(lane & 31)) * DP;
 #pragma unroll
       for (int x = 0; x < DP / 32; ++x)
 #pragma unroll
@@ -280,24 +358,47 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
           }
         }
     }
+    if constexpr (SHARED) {
+      place += take - at.in;
+      if (place >= stop) break;
+      at.in = 0;
+      if (++at.kt * BW >= nk_all) {                                  // the next key head; the next sequence with keys
+        at.kt = 0;
+        if (++at.hk == a.kv_heads) {
+          at.hk = 0;
+          while (!key_rows(a, seq_of(a, ++at.b))) {}
+        }
+      }
+    } else {
+      at.kt += (int)a.tiles;
+    }
   }
 }
 
-// The sums of a tile of sinks' workgroups, joined in their order.
+// The pieces of a tile that is cut, joined in their order: the first lies in its share's second place, the others in the first ones
+// of the shares behind.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void k_attn_sinks(const AttnArgs a) {
-  const u32 unit = blockIdx.x / a.sink_tiles, kt = blockIdx.x % a.sink_tiles, b = unit / a.kv_heads, hk = unit % a.kv_heads;
+__global__ __launch_bounds__(256) void k_attn_cuts(const AttnArgs a) {
+  const Cut c = a.cuts[blockIdx.x];
+  if (!c.more) return;
+  const u32 b = c.b, hk = c.hk, kt = c.kt;
   const bool key = blockIdx.y & 1;
   const Seq s = seq_of(a, b);
-  const int nk_all = a.q_start ? s.nk : (int)a.seq_k;
-  const float* from = a.part + (((u64)unit * a.sink_tiles + kt) * a.splits * 2 + key) * (BW * DP);
+  const int nk_all = key_rows(a, s);
+  const float* from = a.part + ((u64)blockIdx.x * 4 + 2 + key) * (BW * DP);
   T* out = key ? (T*)a.dk + batch_off(a, b, a.dks[0]) + s.k0 * a.dks[1] + (int64_t)hk * a.dks[2]
                : (T*)a.dv + batch_off(a, b, a.dvs[0]) + s.k0 * a.dvs[1] + (int64_t)hk * a.dvs[2];
   for (u32 e = blockIdx.y / 2 * 256 + threadIdx.x; e < BW * DP / 4; e += 4 * 256) {
     const int j = (int)(kt * BW + e / (DP / 4)), d = (int)(e % (DP / 4)) * 4;
     if (j >= nk_all || d >= (int)a.dim) continue;
     f32x4 x = *(const f32x4*)(from + 4 * e);
-    for (u32 k = 1; k < a.splits; ++k) x += *(const f32x4*)(from + (u64)k * 2 * BW * DP + 4 * e);
+    for (u32 k = 1; k <= c.more; k += JOIN) {                        // (eight on their way at once)
+      f32x4 y[JOIN];
+#pragma unroll
+      for (u32 n = 0; n < JOIN; ++n) y[n] = *(const f32x4*)(from + ((u64)(k + n < c.more ? k + n : c.more) * 4 - 2) * (BW * DP) + 4 * e);
+#pragma unroll
+      for (u32 n = 0; n < JOIN; ++n) if (k + n <= c.more) x += y[n];
+    }
     typename Vec<T>::x4 y;
 #pragma unroll
     for (int r = 0; r < 4; ++r) y[r] = (T)x[r];
@@ -532,30 +633,27 @@ static uint64_t rows_of(const AttnArgs& a) { return (uint64_t)(a.q_start ? 1 : a
 
 static uint64_t pad256(uint64_t x) { return (x + 255) / 256 * 256; }
 
-// The workspace: the largest |do| of each wavefront of the queries' kernel; delta and lse2; sums of the sinks' tiles.
+// The workspace: the largest |do| of each wavefront of the queries' kernel; delta and lse2; a share's two pieces at most, what is cut.
 static uint64_t top_bytes(const AttnArgs& a) { return pad256((uint64_t)a.batch * a.heads * ((a.max_q + BW - 1) / BW) * 16); }
 
-// How the queries of a sinks' tile are shared: so many workgroups that each has about as many queries as a tile of the window.
-// (Packed sequences go by twice their mean length, which is known here; max_q only cuts the grid.)  At most 256 MB of sums.
-static void share_sinks(AttnArgs& a) {
-  a.sink_tiles = 0;
-  a.splits = 1;
-  if (!a.window || !a.sinks || !a.seq_q || !a.seq_k || !a.batch) return;
-  const uint64_t nq = a.q_start ? 2 * (((uint64_t)a.seq_q + a.batch - 1) / a.batch) : a.seq_q;
-  const uint64_t near = (uint64_t)a.window * (a.causal ? 1 : 2) + BW;
-  const uint64_t tiles = ((a.q_start ? a.seq_k : a.max_k) + BW - 1) / BW, units = (uint64_t)a.batch * a.kv_heads;
-  uint64_t n = (nq + near - 1) / near, sink_tiles = ((uint64_t)a.sinks + BW - 1) / BW;
-  if (n > 16) n = 16;
-  if (sink_tiles > tiles) sink_tiles = tiles;
-  const uint64_t each = units * sink_tiles * 2 * BW * (a.dim <= 64 ? 64 : 128) * 4, most = (256ull << 20) / each;
-  if (n > most) n = most;
-  if (n < 2) return;
-  a.sink_tiles = (u32)sink_tiles;
-  a.splits = (u32)n;
+// Shares for the keys' kernel, one to a place on a compute unit; 0: a workgroup to a tile. Cutting and joining cost 20 us, some 12 steps (of narrow heads
+// 20); what they save is the longest tile's steps beyond a share's where every tile has a place of its own, and else about half of the longest
+// tile's. Measured, forward and backward, a workgroup to a tile and shares: one sequence of 1000 tokens of 32 heads on 8 194 us and 119; 16 of 2048 of 32
+// heads 3311 and 3148; 14 of 1490 with a window of 1 and 4 sinks 479 and 405; but 3 of 700 of 12 heads of 64 62 and 76, 8 of 600 of 8 heads 119 and
+// 127. (Packed sequences go by their mean lengths, which are known here; max_q and max_k only cut the grid.)
+static u32 key_shares(const AttnArgs& a) {
+  const uint64_t nq = a.q_start ? ((uint64_t)a.seq_q + a.batch - 1) / a.batch : a.seq_q, nk = a.q_start ? ((uint64_t)a.seq_k + a.batch - 1) / a.batch : a.seq_k;
+  const uint64_t near = a.window ? (uint64_t)a.window * (a.causal ? 1 : 2) + BW : nq;
+  const uint64_t all = (nq + BT - 1) / BT * a.group, some = ((near < nq ? near : nq) + BT - 1) / BT * a.group;
+  const uint64_t longest = a.window && !a.sinks ? some : all, mean = a.causal && !a.window ? (all + 1) / 2 : some;
+  const uint64_t units = (uint64_t)a.batch * a.kv_heads, tiles = (nk + BW - 1) / BW, shares = a.dim <= 64 ? 512 : 256;
+  if (!longest || !nk) return 0;
+  const uint64_t each = units * (tiles * (mean + ENTRY) + longest - mean) / shares, share = each > SHARE ? each : SHARE;
+  const uint64_t saved = units * tiles > shares ? longest / 2 : longest > share ? longest - share : 0;
+  if (saved <= (a.dim <= 64 ? 20 : 12)) return 0;
+  return (u32)shares;
 }
-static uint64_t sink_bytes(const AttnArgs& a) {
-  return a.sink_tiles ? (uint64_t)a.batch * a.kv_heads * a.sink_tiles * a.splits * 2 * BW * (a.dim <= 64 ? 64 : 128) * 4 : 0;
-}
+static uint64_t share_bytes(const AttnArgs& a) { return (uint64_t)a.shares * (sizeof(Cut) + 4 * BW * (a.dim <= 64 ? 64 : 128) * 4); }
 
 // How many keys a query sees at most, or in a packed sequence of mean length, which is known here: it decides where P and dS keep their lower halves.
 // As 16-bit numbers they add about as much error to the gradients as those' own rounding, 1.41 times that in all; o's rounding in delta brings dq to 1.5
@@ -576,16 +674,18 @@ static void launch_dq(const AttnArgs& a, bool fine, dim3 grid, hipStream_t s) {
 
 template <class T, int DP>
 static void launch_dkdv(const AttnArgs& a, bool fine, dim3 grid, hipStream_t s) {
-  if (fine) k_attn_dkdv<T, DP, true><<<grid, 256, 0, s>>>(a);
-  else k_attn_dkdv<T, DP, false><<<grid, 256, 0, s>>>(a);
+  if (fine && a.shares) k_attn_dkdv<T, DP, true, true><<<grid, 256, 0, s>>>(a);
+  else if (fine) k_attn_dkdv<T, DP, true, false><<<grid, 256, 0, s>>>(a);
+  else if (a.shares) k_attn_dkdv<T, DP, false, true><<<grid, 256, 0, s>>>(a);
+  else k_attn_dkdv<T, DP, false, false><<<grid, 256, 0, s>>>(a);
 }
 
 extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uint64_t* bytes) {
   if (!bytes) return G10_EINVAL;
   AttnArgs a;
   G10_TRY(attn_args(g, true, a));
-  share_sinks(a);
-  *bytes = top_bytes(a) + pad256(rows_of(a) * 8) + sink_bytes(a);
+  a.shares = a.batch ? key_shares(a) : 0;
+  *bytes = top_bytes(a) + pad256(rows_of(a) * 8) + share_bytes(a);
   return G10_OK;
 }
 
@@ -594,18 +694,18 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   G10_TRY(attn_args(g, true, a));
   if (!a.batch) return G10_OK;
   const uint64_t rows = rows_of(a), units = (uint64_t)a.batch * a.kv_heads;
-  share_sinks(a);
-  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < top_bytes(a) + pad256(rows * 8) + sink_bytes(a)) return G10_EINVAL;
+  a.shares = key_shares(a);
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < top_bytes(a) + pad256(rows * 8) + share_bytes(a)) return G10_EINVAL;
   a.q_tiles = (a.max_q + BW - 1) / BW;
-  const uint64_t qt = a.q_tiles, kt0 = (a.max_k + BW - 1) / BW, kt = kt0 > a.sink_tiles ? kt0 : a.sink_tiles;
-  const uint64_t per = kt + (uint64_t)a.sink_tiles * (a.splits - 1);
-  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * per >= (1ull << 31)) return G10_EINVAL;
+  const uint64_t qt = a.q_tiles, kt = (a.max_k + BW - 1) / BW;
+  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * kt >= (1ull << 31)) return G10_EINVAL;
   hipStream_t s = (hipStream_t)hip_stream;
   const uint64_t seen = keys_seen(a);
   a.amax = (const u32*)workspace;
   a.delta = (const float*)((char*)workspace + top_bytes(a));
   a.lse2 = a.delta + rows;
   a.part = (float*)((char*)a.delta + pad256(rows * 8));
+  a.cuts = (Cut*)(a.part + (uint64_t)a.shares * 4 * BW * (a.dim <= 64 ? 64 : 128));
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
   if (qt) {
     const bool fine = seen <= SOME;
@@ -619,18 +719,18 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   if (kt) {
     const bool fine = seen <= FEWEST;
     a.tiles = (u32)kt;
-    const dim3 grid(unit_grid((u32)units, (u32)per));
+    const dim3 grid(a.shares ? a.shares : unit_grid((u32)units, a.tiles));
     if (bf && narrow) launch_dkdv<__bf16, 64>(a, fine, grid, s);
     else if (bf) launch_dkdv<__bf16, 128>(a, fine, grid, s);
     else if (narrow) launch_dkdv<_Float16, 64>(a, fine, grid, s);
     else launch_dkdv<_Float16, 128>(a, fine, grid, s);
   }
-  if (kt && a.sink_tiles) {
-    const dim3 grid((u32)units * a.sink_tiles, 8);
-    if (bf && narrow) k_attn_sinks<__bf16, 64><<<grid, 256, 0, s>>>(a);
-    else if (bf) k_attn_sinks<__bf16, 128><<<grid, 256, 0, s>>>(a);
-    else if (narrow) k_attn_sinks<_Float16, 64><<<grid, 256, 0, s>>>(a);
-    else k_attn_sinks<_Float16, 128><<<grid, 256, 0, s>>>(a);
+  if (kt && a.shares) {
+    const dim3 grid(a.shares, 8);
+    if (bf && narrow) k_attn_cuts<__bf16, 64><<<grid, 256, 0, s>>>(a);
+    else if (bf) k_attn_cuts<__bf16, 128><<<grid, 256, 0, s>>>(a);
+    else if (narrow) k_attn_cuts<_Float16, 64><<<grid, 256, 0, s>>>(a);
+    else k_attn_cuts<_Float16, 128><<<grid, 256, 0, s>>>(a);
   }
   G10_HIP(hipGetLastError());
   return G10_OK;

@@ -312,3 +312,24 @@ def test_gradients_are_off_by_little_more_than_their_rounding(ops, n, causal, wi
         exact = want[name][0]
         once = (exact.to(dtype).double() - exact).norm()
         assert (O.d(x) - exact).norm() <= 1.5 * once, name
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_gradients_of_keys_in_shares(ops, dtype):
+    """Few tiles of keys with many queries each: cut into shares, wherever the cuts fall."""
+    check(ops, *make((1, 1200), (1, 1200), 8, 1, 128, dtype, seed=1))
+    check(ops, *make((2, 640), (2, 640), 16, 1, 64, dtype, seed=2), causal=False, window=100)
+    q, k, v, do = make((3, 150), (3, 400), 12, 1, 128, dtype, seed=3)
+    got = check(ops, q, k, v, do, causal=False, k_len=torch.tensor([400, 0, 129], dtype=torch.int32).cuda())
+    assert not got["dk"][1].any() and not got["dv"][2, 129:].any()
+    nq, nk = [0, 500, 1, 0, 300, 640], [90, 500, 700, 0, 40, 640]        # rows that see few keys, sinks that all see
+    at = [torch.tensor([0] + n).cumsum(0).to(torch.int32).cuda() for n in (nq, nk)]
+    args = make((sum(nq),), (sum(nk),), 16, 2, 64, dtype, seed=4)
+    check(ops, *args, q_start=at[0], k_start=at[1], window=30, sinks=140)
+    check(ops, *args, q_start=at[0], k_start=at[1], window=30, sinks=5, max_q=640, max_k=700)
+
+
+def test_gradients_of_keys_in_shares_of_many_sequences(ops):
+    n = [(i * 37) % 80 if i % 7 else 0 for i in range(600)]
+    at = torch.tensor([0] + n).cumsum(0).to(torch.int32).cuda()
+    check(ops, *make((sum(n),), (sum(n),), 64, 1, 72, torch.bfloat16, seed=5), q_start=at, k_start=at, max_q=80, max_k=80)
