@@ -28,7 +28,7 @@ __device__ __forceinline__ float lift_of(u32 top) { return __uint_as_float((u32)
 // few tiles, or a few more than there are compute units, leave units idle.  A cut goes through a tile wherever it falls; its pieces
 // meet in k_attn_cuts.
 #define ENTRY 2u                   // steps that a tile's begin and end take
-#define JOIN 8                     // pieces of a tile on their way at once where they are joined
+#define JOIN 4                     // pieces of a tile on their way at once where they are joined
 #define SHARE 8                    // steps of a share at least: its pieces are worth their joining
 struct Steps { int first, hi, each; u32 all; };                      // first and last query, tiles of 64 queries to a head, steps
 __device__ __forceinline__ Steps steps_of(const AttnArgs& a, const Seq& s, int kt) {
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
 }
 
 // The pieces of a tile that is cut, joined in their order: the first lies in its share's second place, the others in the first ones
-// of the shares behind.
+// of the shares behind.  Bound by the memory that holds them: 256 shares of heads of 128 values 64 MB, 17 us.
 template <class T, int DP>
 __global__ __launch_bounds__(256) void k_attn_cuts(const AttnArgs a) {
   const Cut c = a.cuts[blockIdx.x];
@@ -392,13 +392,16 @@ __global__ __launch_bounds__(256) void k_attn_cuts(const AttnArgs a) {
     const int j = (int)(kt * BW + e / (DP / 4)), d = (int)(e % (DP / 4)) * 4;
     if (j >= nk_all || d >= (int)a.dim) continue;
     f32x4 x = *(const f32x4*)(from + 4 * e);
-    for (u32 k = 1; k <= c.more; k += JOIN) {                        // (eight on their way at once)
+    auto piece = [&](u32 k) { return *(const f32x4*)(from + ((u64)k * 4 - 2) * (BW * DP) + 4 * e); };
+    u32 k = 1;
+    for (; k + JOIN - 1 <= c.more; k += JOIN) {
       f32x4 y[JOIN];
 #pragma unroll
-      for (u32 n = 0; n < JOIN; ++n) y[n] = *(const f32x4*)(from + ((u64)(k + n < c.more ? k + n : c.more) * 4 - 2) * (BW * DP) + 4 * e);
+      for (u32 n = 0; n < JOIN; ++n) y[n] = piece(k + n);
 #pragma unroll
-      for (u32 n = 0; n < JOIN; ++n) if (k + n <= c.more) x += y[n];
+      for (u32 n = 0; n < JOIN; ++n) x += y[n];
     }
+    for (; k <= c.more; ++k) x += piece(k);
     typename Vec<T>::x4 y;
 #pragma unroll
     for (int r = 0; r < 4; ++r) y[r] = (T)x[r];
