@@ -11,7 +11,8 @@
 
 // In 16-bit floats with a short exponent, P and dS of long rows would fall below the smallest number.  P is held times
 // 2^12 (it is at most 1), dS times 8 over the power of two at the largest |do| of what it is summed over: of the query for dQ, of the
-// group's heads for dK.  Both leave by exact powers of two at the end.
+// group's heads for dK.  Both leave by exact powers of two at the end.  (dS passes the type's largest number only where sum |v - o| of a key and a
+// query is above 4000.)
 template <class T> struct Lift;
 template <> struct Lift<__bf16> {
   static constexpr float p2 = 0.0f, p = 1.0f;
