@@ -71,7 +71,8 @@ int g10_norm_rope_backward(const g10_rope_args *args, void *workspace, uint64_t 
  * head h reads key head h / (heads / kv_heads), whose gradient is the sum over them.
  * Sequences lie side by side ([batch][seq][head][dim]; q_start = k_start = NULL), k_len then says how many keys each
  * has; or packed one behind the other ([total][head][dim]): q_start and k_start hold where each begins, batch + 1
- * numbers.  Keys past a sequence's end are not read.  Numbers that point outside the tensors are moved to their border. */
+ * numbers, none below the one before it.  Keys past a sequence's end are not read.  Numbers that point outside the tensors are moved
+ * to their border.  Rows of packed tensors before the first sequence and behind the last one (padding) see nothing and are seen by none. */
 typedef struct {
   const void *q, *k, *v;
   void *o;                   /* forward: output; backward: the forward pass's                  */

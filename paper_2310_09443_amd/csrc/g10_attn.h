@@ -66,6 +66,7 @@ struct AttnArgs {
   u32 splits;                      // forward: pieces of a block that there is room for
   u32 shares;                      // that the work is cut into; backward: 0: it is not
   u32 q_tiles;                     // backward: of queries per sequence and head in k_attn_dq's grid
+  u32 work;                        // workgroups of the grid with work on sequences; the ones behind them clear rows of none
   float scale, scale2;             // scale2 = scale * log2(e)
 };
 
@@ -407,6 +408,48 @@ __device__ __forceinline__ bool block_of(u32 units, u32 group, u32 tiles, u32& u
 }
 static inline u32 unit_grid(u32 units, u32 per) {
   return units % 8 == 0 || units >= 64 ? 8 * ((units + 7) / 8) * per : units * per;
+}
+
+// Rows of a packed tensor that belong to no sequence, as padding behind the last one: below lo and from hi on. Their outputs and gradients are
+// zeros: the allocator's memory holds whatever it held. REST workgroups behind the grid's others clear them, so that it takes no
+// launch of its own. (Where the starts fall, which they must not, rows between may belong to none as well.)
+#define REST 64u
+struct Rest { int lo, hi, rows; u32 part; };                         // rows: how many; part: this workgroup's number
+__device__ __forceinline__ Rest rest_of(const int* start, u32 batch, u32 n, u32 part) {
+  __shared__ u32 tmp[G10_WAVES];
+  u32 lo = n, hi = 0;
+  for (u32 b = threadIdx.x; b <= batch; b += G10_BLOCK) {
+    const u32 x = (u32)clampi(start[b], 0, (int)n);
+    lo = min(lo, x);
+    hi = max(hi, x);
+  }
+  lo = n - block_max(n - lo, tmp);
+  hi = block_max(hi, tmp);
+  return Rest{(int)lo, (int)hi, (int)(lo + n - hi), part};
+}
+template <class F>
+__device__ __forceinline__ void each_rest(const Rest& r, u32 per, F&& f) {   // f(row, 0..per-1)
+  const u64 all = (u64)r.rows * per;
+  for (u64 e = (u64)r.part * G10_BLOCK + threadIdx.x; e < all; e += (u64)REST * G10_BLOCK) {
+    const int row = (int)(e / per);
+    f(row < r.lo ? row : r.hi + row - r.lo, (u32)(e % per));
+  }
+}
+template <class T>
+__device__ __forceinline__ void clear_rest(const Rest& r, void* p, const int64_t (&st)[3], u32 heads, u32 dim) {
+  const u32 pieces = dim / 8;
+  each_rest(r, heads * pieces, [&](int row, u32 e) { *(u32x4*)((T*)p + row * st[1] + (int64_t)(e / pieces) * st[2] + e % pieces * 8) = u32x4{}; });
+}
+// The forward kernels' outputs.
+template <class T>
+__device__ __forceinline__ void clear_outputs(const AttnArgs& a) {
+  const Rest r = rest_of(a.q_start, a.batch, a.seq_q, blockIdx.x - a.work);
+  clear_rest<T>(r, a.o, a.os, a.heads, a.dim);
+  each_rest(r, a.heads, [&](int row, u32 h) { a.lse[(int64_t)h * a.seq_q + row] = -__builtin_inff(); });
+}
+static inline u32 with_rest(AttnArgs& a, u32 grid) {
+  a.work = grid;
+  return a.q_start ? grid + REST : grid;
 }
 
 int attn_args(const g10_attention_args* g, bool back, AttnArgs& a);

@@ -61,6 +61,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
   constexpr int BM = 32 * NW;
   __shared__ __attribute__((aligned(256))) T lds[2][2][BN * DP];      // keys, values; even and odd tiles
   typedef typename Vec<T>::x8 x8;
+  if (blockIdx.x >= a.work) { clear_outputs<T>(a); return; }
   u32 unit, head, last;
   if (!block_of(a.batch * a.kv_heads, a.group, a.tiles, unit, head, last)) return;
   const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + head;
@@ -244,7 +245,7 @@ extern "C" int g10_attention(const g10_attention_args* g, void* workspace, uint6
   a.tiles = (a.max_q + 32 * nw - 1) / (32 * nw);
   const uint64_t per = (uint64_t)a.group * a.tiles, units = (uint64_t)a.batch * a.kv_heads;
   if ((units + 7) * per >= (1ull << 31)) return G10_EINVAL;
-  const dim3 grid(unit_grid((u32)units, (u32)per));
+  const dim3 grid(with_rest(a, unit_grid((u32)units, (u32)per)));
   if (g->type == G10_BF16) {
     if (a.dim <= 64) k_attn_fwd<__bf16, 64, nw><<<grid, 64 * nw, 0, s>>>(a);
     else k_attn_fwd<__bf16, 128, nw><<<grid, 64 * nw, 0, s>>>(a);

@@ -197,6 +197,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
   __shared__ __attribute__((aligned(16))) float rows[3][2][BT];      // lse2, delta of a tile's queries
   __shared__ u64 ends[SHARED ? 256 : 1];
   typedef typename Vec<T>::x8 x8;
+  if (blockIdx.x >= a.work) {
+    const Rest r = rest_of(a.k_start, a.batch, a.seq_k, blockIdx.x - a.work);
+    clear_rest<T>(r, a.dk, a.dks, a.kv_heads, a.dim);
+    clear_rest<T>(r, a.dv, a.dvs, a.kv_heads, a.dim);
+    return;
+  }
   Place at = {};
   u64 place = 0, stop = 0;
   Row row = {};
@@ -460,6 +466,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   constexpr int KT = 32, NB = 4;                                     // keys of a tile; these, the next, two on their way
   __shared__ __attribute__((aligned(256))) T lds[NB][2][KT * DP];
   typedef typename Vec<T>::x8 x8;
+  if (blockIdx.x >= a.work) {
+    clear_rest<T>(rest_of(a.q_start, a.batch, a.seq_q, blockIdx.x - a.work), a.dq, a.dqs, a.heads, a.dim);
+    return;
+  }
   u32 unit, head, first;
   if (!block_of(a.batch * a.kv_heads, a.group, a.tiles, unit, head, first)) return;
   const u32 b = unit / a.kv_heads, hk = unit % a.kv_heads, h = hk * a.group + head;
@@ -714,7 +724,7 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   if (qt) {
     const bool fine = seen <= SOME;
     a.tiles = (u32)qt;
-    const dim3 grid(unit_grid((u32)units, a.group * a.tiles));
+    const dim3 grid(with_rest(a, unit_grid((u32)units, a.group * a.tiles)));
     if (bf && narrow) launch_dq<__bf16, 64>(a, fine, grid, s);
     else if (bf) launch_dq<__bf16, 128>(a, fine, grid, s);
     else if (narrow) launch_dq<_Float16, 64>(a, fine, grid, s);
@@ -723,7 +733,7 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   if (kt) {
     const bool fine = seen <= FEWEST;
     a.tiles = (u32)kt;
-    const dim3 grid(a.shares ? a.shares : unit_grid((u32)units, a.tiles));
+    const dim3 grid(with_rest(a, a.shares ? a.shares : unit_grid((u32)units, a.tiles)));
     if (bf && narrow) launch_dkdv<__bf16, 64>(a, fine, grid, s);
     else if (bf) launch_dkdv<__bf16, 128>(a, fine, grid, s);
     else if (narrow) launch_dkdv<_Float16, 64>(a, fine, grid, s);

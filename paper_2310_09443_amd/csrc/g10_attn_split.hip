@@ -67,6 +67,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
   __shared__ float ms[SW][32], ls[SW][32];
   __shared__ u32 ends[BATCH], tmp[2 * SW];
   typedef typename Vec<T>::x8 x8;
+  if (blockIdx.x >= a.work) { clear_outputs<T>(a); return; }
   const u32 wave = uniform(wave_id()), lane = lane_id();
   u32 lk[2], lv[2];
   for (int i = 0; i < 2; ++i) { lk[i] = lds_addr(lds[wave][i][0]); lv[i] = lds_addr(lds[wave][i][1]); }
@@ -338,13 +339,14 @@ static void launch(AttnArgs a, hipStream_t s) {
     // with several blocks to a key head an XCD's shares lie in a row, so that blocks of the same keys meet in its L2 (64 queries of 4 x 8192
     // keys: 168 -> 101 us); with one they do not (8 x 32768 keys: 188 us, in a row 204)
     a.tiles = a.max_q * a.group > 32 ? 8 : 1;
-    if (a.dim <= 64) k_attn_split<T, 64, true><<<a.shares, 64 * SW, 0, s>>>(a);
-    else k_attn_split<T, 128, true><<<a.shares, 64 * SW, 0, s>>>(a);
+    const u32 grid = with_rest(a, a.shares);
+    if (a.dim <= 64) k_attn_split<T, 64, true><<<grid, 64 * SW, 0, s>>>(a);
+    else k_attn_split<T, 128, true><<<grid, 64 * SW, 0, s>>>(a);
     a.tiles = (u32)(((u64)a.max_q * a.group + SW - 1) / SW);
     k_attn_join<T><<<units * a.tiles, 64 * SW, 0, s>>>(a);
   } else {
     a.tiles = (u32)(((u64)a.max_q * a.group + 31) / 32);
-    const dim3 grid(unit_grid(units, a.tiles));
+    const dim3 grid(with_rest(a, unit_grid(units, a.tiles)));
     if (a.dim <= 64) k_attn_split<T, 64, false><<<grid, 64 * SW, 0, s>>>(a);
     else k_attn_split<T, 128, false><<<grid, 64 * SW, 0, s>>>(a);
   }

@@ -268,6 +268,7 @@ static py::tuple attention(const at::Tensor& q, const at::Tensor& k, const at::T
   at::Tensor o = at::empty(q.sizes(), opt.dtype(q.scalar_type()));
   at::Tensor lse = c.packed ? at::empty({a.heads, a.seq_q}, opt.dtype(at::kFloat)) : at::empty({a.batch, a.heads, a.seq_q}, opt.dtype(at::kFloat));
   if (!q.numel()) return py::make_tuple(o, lse);
+  if (!a.batch) return py::make_tuple(o.zero_(), lse.fill_(-INFINITY));                // (rows, and no sequence)
   put(a.o, a.o_stride, o);
   a.lse = lse.mutable_data_ptr<float>();
   const c10::DeviceGuard guard(c.dev);

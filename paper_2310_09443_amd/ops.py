@@ -157,16 +157,17 @@ def norm_rope(q, k, table, positions, q_weight=None, k_weight=None, eps=1e-6, in
 def g10_attention(q, k, v, causal=True, window=0, sinks=0, scale=None, q_start=None, k_start=None, k_len=None, max_q=None, max_k=None):
     """softmax(scale q k^T) v over the keys each query sees, which stand side by side: q [batch, token, head, dim], k and v
     [batch, token, kv_head, dim], with `k_len` (int32 [batch]) keys in use; or packed: [token, head, dim] with `q_start` and
-    `k_start` (int32 [batch + 1]), `max_q` and `max_k` the longest sequences' lengths (they steer how the work is cut).
+    `k_start` (int32 [batch + 1], not falling), `max_q` and `max_k` the longest sequences' lengths (they steer how the work is cut).
     The last query of a sequence stands at its last key.  causal: no key behind the query; window w > 0: only the last w keys up
     to the query's own (not causal: fewer than w places away), and the first `sinks` ones.  Returns (o, lse); a query that sees no key has
-    o = 0 and lse = -inf.  Rows of packed tensors that belong to no sequence are not written."""
+    o = 0 and lse = -inf, as do rows of packed tensors that belong to no sequence (padding before the first or behind the last one)."""
     return _calls().attention(q, k, v, causal, window or 0, sinks, scale, q_start, k_start, k_len, max_q, max_k)
 
 
 def g10_attention_backward(do, q, k, v, o, lse, causal=True, window=0, sinks=0, scale=None, q_start=None, k_start=None, k_len=None,
                            max_q=None, max_k=None):
-    """Gradients (dq, dk, dv) from that of o, with g10_attention's inputs and outputs.  Keys past k_len get zeros."""
+    """Gradients (dq, dk, dv) from that of o, with g10_attention's inputs and outputs.  Keys past k_len and rows that belong to no sequence
+    get zeros."""
     return _calls().attention_backward(do, q, k, v, o, lse, causal, window or 0, sinks, scale, q_start, k_start, k_len, max_q, max_k)
 
 
