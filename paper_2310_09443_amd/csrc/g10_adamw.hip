@@ -353,9 +353,13 @@ extern "C" int g10_adamw_step(g10_adamw_t* h, const void* const* grads, const g1
     if (!launch_of(h, k, grads, g, first, n)) continue;
     a.tensor0 = k * GRADS;
     const bool small = h->state_type == G10_E4M3;
-    if (h->type == G10_F32) step_launch<float>(h->grad_type, small, (u32)n, a, h->chunks + first, g, s);
-    else if (h->type == G10_F16) step_launch<_Float16>(h->grad_type, small, (u32)n, a, h->chunks + first, g, s);
-    else step_launch<__bf16>(h->grad_type, small, (u32)n, a, h->chunks + first, g, s);
+    for (u64 at = 0; at < n; at += G10_GROUPS_MOST) {
+      const u32 grid = n - at < G10_GROUPS_MOST ? (u32)(n - at) : G10_GROUPS_MOST;
+      const Chunk* chunks = h->chunks + first + at;
+      if (h->type == G10_F32) step_launch<float>(h->grad_type, small, grid, a, chunks, g, s);
+      else if (h->type == G10_F16) step_launch<_Float16>(h->grad_type, small, grid, a, chunks, g, s);
+      else step_launch<__bf16>(h->grad_type, small, grid, a, chunks, g, s);
+    }
   }
   G10_HIP(hipGetLastError());
   return G10_OK;

@@ -196,7 +196,7 @@ int attn_args(const g10_attention_args* g, bool back, AttnArgs& a) {
   if (!(g->scale > 0.0f) || !(g->scale < 3e38f)) return G10_EINVAL;
   if (g->causal > 1 || g->seq_q >= (1u << 30) || g->seq_k >= (1u << 30) || g->window >= (1u << 30) || g->sinks >= (1u << 30)) return G10_EINVAL;
   if (g->max_q >= (1u << 30) || g->max_k >= (1u << 30)) return G10_EINVAL;
-  if ((uint64_t)g->batch * g->heads >= (1u << 24)) return G10_EINVAL;
+  if (((uint64_t)g->batch * g->kv_heads + 7) / 8 * 8 * (g->heads / g->kv_heads) + REST > G10_GROUPS_MOST) return G10_EINVAL;   // (a workgroup for each head at least)
   const bool packed = g->q_start != nullptr;
   a = AttnArgs{};
   a.q = g->q; a.k = g->k; a.v = g->v; a.o = g->o; a.lse = g->lse; a.d_o = g->d_o; a.dq = g->dq; a.dk = g->dk; a.dv = g->dv;
@@ -242,10 +242,9 @@ extern "C" int g10_attention(const g10_attention_args* g, void* workspace, uint6
     return attn_forward_split(a, splits, workspace, g->type, s);
   }
   constexpr int nw = 4;
-  a.tiles = (a.max_q + 32 * nw - 1) / (32 * nw);
-  const uint64_t per = (uint64_t)a.group * a.tiles, units = (uint64_t)a.batch * a.kv_heads;
-  if ((units + 7) * per >= (1ull << 31)) return G10_EINVAL;
-  const dim3 grid(with_rest(a, unit_grid((u32)units, (u32)per)));
+  const u32 units = a.batch * a.kv_heads;
+  a.tiles = tiles_in(units, a.group, (a.max_q + 32 * nw - 1) / (32 * nw));
+  const dim3 grid(with_rest(a, unit_grid(units, a.group * a.tiles)));
   if (g->type == G10_BF16) {
     if (a.dim <= 64) k_attn_fwd<__bf16, 64, nw><<<grid, 64 * nw, 0, s>>>(a);
     else k_attn_fwd<__bf16, 128, nw><<<grid, 64 * nw, 0, s>>>(a);

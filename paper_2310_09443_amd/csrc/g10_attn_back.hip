@@ -648,7 +648,8 @@ static uint64_t rows_of(const AttnArgs& a) { return (uint64_t)(a.q_start ? 1 : a
 static uint64_t pad256(uint64_t x) { return (x + 255) / 256 * 256; }
 
 // The workspace: the largest |do| of each wavefront of the queries' kernel; delta and lse2; a share's two pieces at most, what is cut.
-static uint64_t top_bytes(const AttnArgs& a) { return pad256((uint64_t)a.batch * a.heads * ((a.max_q + BW - 1) / BW) * 16); }
+static u32 query_tiles(const AttnArgs& a) { return tiles_in(a.batch * a.kv_heads, a.group, (a.max_q + BW - 1) / BW); }
+static uint64_t top_bytes(const AttnArgs& a) { return pad256((uint64_t)a.batch * a.heads * query_tiles(a) * 16); }
 
 // Shares for the keys' kernel, one to a place on a compute unit; 0: a workgroup to a tile. Cutting and joining cost 20 us, some 12 steps (of narrow heads
 // 20); what they save is the longest tile's steps beyond a share's where every tile has a place of its own, and else about half of the longest
@@ -698,7 +699,8 @@ extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uin
   if (!bytes) return G10_EINVAL;
   AttnArgs a;
   G10_TRY(attn_args(g, true, a));
-  a.shares = a.batch ? key_shares(a) : 0;
+  if (!a.batch) { *bytes = 0; return G10_OK; }
+  a.shares = key_shares(a);
   *bytes = top_bytes(a) + pad256(rows_of(a) * 8) + share_bytes(a);
   return G10_OK;
 }
@@ -707,12 +709,11 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   AttnArgs a;
   G10_TRY(attn_args(g, true, a));
   if (!a.batch) return G10_OK;
-  const uint64_t rows = rows_of(a), units = (uint64_t)a.batch * a.kv_heads;
+  const uint64_t rows = rows_of(a);
+  const u32 units = a.batch * a.kv_heads;
   a.shares = key_shares(a);
   if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < top_bytes(a) + pad256(rows * 8) + share_bytes(a)) return G10_EINVAL;
-  a.q_tiles = (a.max_q + BW - 1) / BW;
-  const uint64_t qt = a.q_tiles, kt = (a.max_k + BW - 1) / BW;
-  if ((units + 7) * a.group * qt >= (1ull << 31) || (units + 7) * kt >= (1ull << 31)) return G10_EINVAL;
+  const u32 qt = a.q_tiles = query_tiles(a), kt = tiles_in(units, 1, (a.max_k + BW - 1) / BW);
   hipStream_t s = (hipStream_t)hip_stream;
   const uint64_t seen = keys_seen(a);
   a.amax = (const u32*)workspace;
@@ -723,8 +724,8 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
   if (qt) {
     const bool fine = seen <= SOME;
-    a.tiles = (u32)qt;
-    const dim3 grid(with_rest(a, unit_grid((u32)units, a.group * a.tiles)));
+    a.tiles = qt;
+    const dim3 grid(with_rest(a, unit_grid(units, a.group * a.tiles)));
     if (bf && narrow) launch_dq<__bf16, 64>(a, fine, grid, s);
     else if (bf) launch_dq<__bf16, 128>(a, fine, grid, s);
     else if (narrow) launch_dq<_Float16, 64>(a, fine, grid, s);
@@ -732,8 +733,8 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   }
   if (kt) {
     const bool fine = seen <= FEWEST;
-    a.tiles = (u32)kt;
-    const dim3 grid(with_rest(a, a.shares ? a.shares : unit_grid((u32)units, a.tiles)));
+    a.tiles = kt;
+    const dim3 grid(with_rest(a, a.shares ? a.shares : unit_grid(units, a.tiles)));
     if (bf && narrow) launch_dkdv<__bf16, 64>(a, fine, grid, s);
     else if (bf) launch_dkdv<__bf16, 128>(a, fine, grid, s);
     else if (narrow) launch_dkdv<_Float16, 64>(a, fine, grid, s);

@@ -342,10 +342,10 @@ static void launch(AttnArgs a, hipStream_t s) {
     const u32 grid = with_rest(a, a.shares);
     if (a.dim <= 64) k_attn_split<T, 64, true><<<grid, 64 * SW, 0, s>>>(a);
     else k_attn_split<T, 128, true><<<grid, 64 * SW, 0, s>>>(a);
-    a.tiles = (u32)(((u64)a.max_q * a.group + SW - 1) / SW);
+    a.tiles = tiles_in(units, 1, ((u64)a.max_q * a.group + SW - 1) / SW);
     k_attn_join<T><<<units * a.tiles, 64 * SW, 0, s>>>(a);
   } else {
-    a.tiles = (u32)(((u64)a.max_q * a.group + 31) / 32);
+    a.tiles = tiles_in(units, 1, ((u64)a.max_q * a.group + 31) / 32);
     const dim3 grid(with_rest(a, unit_grid(units, a.tiles)));
     if (a.dim <= 64) k_attn_split<T, 64, false><<<grid, 64 * SW, 0, s>>>(a);
     else k_attn_split<T, 128, false><<<grid, 64 * SW, 0, s>>>(a);

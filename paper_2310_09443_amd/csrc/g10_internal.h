@@ -20,6 +20,9 @@ typedef uint32_t u32;
     if (e_ != hipSuccess) return g10_hip_fail(e_, __FILE__, __LINE__); \
   } while (0)
 
+// A launch's work-items are counted in 32 bits: no more workgroups of 256 to a launch than this.
+#define G10_GROUPS_MOST ((1u << 24) - 1)
+
 int g10_hip_fail(hipError_t e, const char* file, int line);
 #define G10_TRY(x) do { int rc_ = (x); if (rc_) return rc_; } while (0)
 

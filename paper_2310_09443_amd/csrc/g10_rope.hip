@@ -346,7 +346,6 @@ static int rope_args(const g10_rope_args* g, bool back, RopeArgs& a, RopePlan& p
   if (heads > 65536 || a.tokens * (heads ? heads : 1) >= (1ull << 40)) return G10_EINVAL;
   const bool some = a.tokens && heads;
   if (some && (!g->positions || !g->n_positions || (g->rot && !g->table))) return G10_EINVAL;
-  const bool pairs = g->flags & G10_ROPE_INTERLEAVED;
   const u32 e = g->type == G10_F32 ? 4 : 2, step = 16 / e;          // elements of 16 bytes
   p.weights = false;
   p.any = g->dim % 8 || g->rot % 8 || ((uintptr_t)g->table & 15);
@@ -387,7 +386,7 @@ static int rope_args(const g10_rope_args* g, bool back, RopeArgs& a, RopePlan& p
   }
   a.all_chunks = a.chunks[0] + a.chunks[1];
   const u64 groups = p.any ? (rows + 3) / 4 : (a.tokens * a.all_chunks + 256 / p.lanes - 1) / (256 / p.lanes);
-  p.grid = (u32)(back ? (groups < ROPE_GROUPS ? groups : ROPE_GROUPS) : (groups < (1u << 30) ? groups : (1u << 30)));
+  p.grid = (u32)(back ? (groups < ROPE_GROUPS ? groups : ROPE_GROUPS) : (groups < G10_GROUPS_MOST ? groups : G10_GROUPS_MOST));
   return G10_OK;
 }
 

@@ -75,3 +75,23 @@ def test_a_projection_learns_from_its_sequences_only(ops):
         grads.append(weight.grad)
     # the library's products of 128 and of 90 rows may be summed in other orders: each is rounded to bfloat16, q, k and v as well
     assert (grads[0] - grads[1]).abs().max() <= 2.0 ** -6 * grads[1].abs().max()
+
+
+def test_many_sequences_whose_lengths_are_not_told(ops):
+    """One token each: the output is its value, the value's gradient the sum over its heads.  A grid for the longest possible sequence
+    would have 2^32 workgroups."""
+    n, heads, kv, dim = 65600, 32, 8, 8
+    g = torch.Generator().manual_seed(7)
+    q, do = (torch.randn(n, heads, dim, generator=g).bfloat16().cuda() for _ in range(2))
+    k, v = (torch.randn(n, kv, dim, generator=g).bfloat16().cuda() for _ in range(2))
+    at = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    dirty(q)
+    o, lse = ops.g10_attention(q, k, v, q_start=at, k_start=at)
+    assert torch.equal(o, v.repeat_interleave(heads // kv, 1))
+    score = (O.d(q) * O.d(k).repeat_interleave(heads // kv, 1))
+    O.assert_near(lse, score.sum(-1).t() * dim ** -0.5, ((dim + 12) * O.U32 * (score.abs().sum(-1).t() * dim ** -0.5 + 1)), "lse")
+    dirty(k)
+    dv = ops.g10_attention_backward(do, q, k, v, o, lse, q_start=at, k_start=at)[2]
+    want = O.d(do).view(n, kv, heads // kv, dim)
+    # P is 2^(score - lse), both in 32 bits
+    O.assert_near(dv, want.sum(2), O.rounding(want.sum(2), torch.bfloat16) + (2 * (dim + 12) * 8 + 8) * O.U32 * want.abs().sum(2), "dv")
