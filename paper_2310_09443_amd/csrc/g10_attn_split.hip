@@ -321,8 +321,10 @@ u32 attn_splits(const AttnArgs& a) {
   u64 blocks, keys;
   if (!few_queries(a, blocks, keys)) return 0;
   if (a.batch > BATCH || keys <= 768 || blocks >= 4 * CUS || (blocks >= CUS && keys <= 2048)) return 1;
-  const u64 most = ((u64)a.seq_q * a.group / 32 + 1) * (a.q_start ? 1 : a.batch) + a.batch;
-  if (most * a.kv_heads * (a.seq_k / ST + 2) >= 1ull << 31) return 1;                  // (tiles are counted in 32 bits)
+  // Tiles are counted in 32 bits. Starts of packed sequences must not fall, but they are numbers on the device: where they do, every second sequence may
+  // be as long as all rows, and a count that wraps would point outside the tensors.
+  const u64 most = ((u64)a.seq_q * a.group / 32 + 1) * (a.q_start ? (a.batch + 1) / 2 : a.batch) + 2 * a.batch;
+  if (most * a.kv_heads * (a.seq_k / ST + 2) >= 1ull << 31) return 1;
   const u64 n = (u64)a.batch * a.kv_heads;                           // (blocks of one key head lie in a row: the more, the fewer pieces)
   return (u32)(2 * ((attn_shares(a) + n - 1) / n) + 2);
 }

@@ -109,6 +109,15 @@ def test_small_grids_are_what_the_work_asks_for(launches):
     assert rc == 0 and [x[1:] for x in ran] == [[8 * 8 + 64, 256]]
 
 
+def test_starts_that_fall_do_not_make_counts_wrap(launches):
+    """Work is cut into shares by counts in 32 bits.  Starts such as 0, n, 0, n, ... make every second sequence as long as all rows:
+    where their tiles together could pass 2^31, nothing is cut, and the few-query kernel has nothing to count."""
+    calls = [packed(256, 1024, 8, 1, seq_k=1 << 22), packed(200, 1600, 8, 2, seq_k=1 << 24), packed(100, 100, 32, 8, seq_k=10_000_000), packed(8, 8, 32, 8, seq_k=8 * 32768)]
+    for kw, cut, (rc, ran, n) in zip(calls, (False, False, True, True), launches(*[("attention", kw) for kw in calls])):
+        tiles = (kw["batch"] + 1) // 2 * -(-kw["seq_q"] * kw["heads"] // kw["kv_heads"] // 32) * kw["kv_heads"] * (kw["seq_k"] // 32)
+        assert rc == 0 and (tiles < 1 << 31) == cut and any("k_attn_join" in x[0] for x in ran) == cut == (n > 0), (kw, ran)
+
+
 def test_more_heads_than_a_grid_has_workgroups_are_refused(launches):
     for kw in (dict(batch=1 << 22, heads=4), dict(batch=1 << 18, heads=64, kv_heads=64), dict(batch=1 << 24, heads=2, kv_heads=1)):
         for rc, ran, _ in launches(("attention", kw), ("backward", kw)):
