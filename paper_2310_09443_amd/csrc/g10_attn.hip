@@ -12,6 +12,14 @@
 // strewn between and the fragments of the products four ahead on their way from LDS.  hold() keeps the compiler from putting
 // these apart again.
 
+// P is rounded to 16 bits for the second product. A 16-bit float with a short exponent has its smallest normal number at 2^-14, so P is held times
+// 2^LIFT there, and the maximum that it is relative to may lag by LAG less: 2^(LAG + LIFT) is below the largest number, and a key keeps
+// all its bits down to 2^-26 of the row's largest (18 nats: a first token that takes nearly all of a row, and thousands of keys that share the
+// rest). l sums P as it is held; the lift leaves with 1 / l, and from lse.
+template <class T> struct Hold;
+template <> struct Hold<__bf16> { static constexpr float lift = 0.0f, drop = 1.0f, lag = 8.0f; };
+template <> struct Hold<_Float16> { static constexpr float lift = 12.0f, drop = 0x1p-12f, lag = 3.0f; };
+
 // The products of a tile, in order: NS of the next tile's scores (none if !NEXT), NV of this tile's outputs.
 template <class T, int DP, bool NEXT>
 __device__ __forceinline__ void tile_step(u32 tk, u32 tv, const typename Vec<T>::x8 (&q)[DP / 16], f32x16 (&sc)[2], f32x16 (&sn)[2],
@@ -110,9 +118,9 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
 #pragma unroll
           for (int r = 0; r < 16; ++r) top = fmaxf(top, sc[n][r]);
         top = both_max(top) * a.scale2;
-        // The sums stay relative to an older maximum until it is passed by more than 2^8: what is added then is below 2^8, far from
-        // any type's end, and most tiles leave the outputs as they are.
-        if (ballot(top > m + 8.0f)) {
+        // The sums stay relative to an older maximum until it is passed by more than 2^LAG: what is added then is below 2^(LAG + LIFT), far from
+        // the type's end, and most tiles leave the outputs as they are.
+        if (ballot(top > m + Hold<T>::lag)) {
           const float now = fmaxf(m, top), fade = exp2_fast(m - (now == G10_NEG_INF ? 0.0f : now));
           m = now;
           l *= fade;
@@ -138,7 +146,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
         __syncthreads();
         if (t + 2 < tiles.count) sk.load(K, a.ks[1], tiles.at(t + 2) * BN, s.nk, unseen, lk + even);
         sv.load(V, a.vs[1], tiles.at(t + 1) * BN, s.nk, unseen, lv + other);
-        tile_step<T, DP, true>(tk + other, tv + even, q, sc, sn, o, a.scale2, m == G10_NEG_INF ? 0.0f : m, l);
+        tile_step<T, DP, true>(tk + other, tv + even, q, sc, sn, o, a.scale2, (m == G10_NEG_INF ? 0.0f : m) - Hold<T>::lift, l);
         settle(sn, t + 1);
       };
       int t = 0;
@@ -154,7 +162,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
       }
       loads_done();
       __syncthreads();
-      tile_step<T, DP, false>(0, tv + (t & 1 ? odd : 0), q, sa, sb, o, a.scale2, m == G10_NEG_INF ? 0.0f : m, l);
+      tile_step<T, DP, false>(0, tv + (t & 1 ? odd : 0), q, sa, sb, o, a.scale2, (m == G10_NEG_INF ? 0.0f : m) - Hold<T>::lift, l);
     }
     l = both_sum(l);
     if (i < s.nq) {
@@ -172,7 +180,7 @@ __global__ __launch_bounds__(64 * NW, DP == 64 ? 3 : 2) void k_attn_fwd(const At
             *(typename Vec<T>::x4*)(out + d) = w;
           }
         }
-      if (lane < 32) (a.lse + row_off(a, b, h, s))[i] = l > 0.0f ? (m + __log2f(l)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
+      if (lane < 32) (a.lse + row_off(a, b, h, s))[i] = l > 0.0f ? (m + __log2f(l * Hold<T>::drop)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
     }
   }
 }

@@ -12,6 +12,13 @@
 #define BATCH (64 * SW)            // sequences whose work is cut into equal shares
 #define LEAST 8                    // tiles of a share: two for each wavefront
 
+// P is held times 2^LIFT where 16-bit floats have a short exponent: it is at most 1 here, so a key keeps all its bits down to 2^-29 of the largest
+// of its part. The parts' sums are lifted alike; the lift leaves with 1 / l, and from lse.
+template <class T> constexpr float LIFT = 0.0f;
+template <class T> constexpr float DROP = 1.0f;
+template <> constexpr float LIFT<_Float16> = 15.0f;
+template <> constexpr float DROP<_Float16> = 0x1p-15f;
+
 // The work of all sequences' key heads and blocks of 32 columns in one row, in tiles of keys, cut into equal shares: sequences of unlike
 // lengths keep all compute units busy to the end.  A cut goes through a block wherever it falls; the pieces of a
 // block meet in k_attn_join.  At most BATCH sequences; a sequence to a thread.
@@ -163,7 +170,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
       float sum = 0.0f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        sc[r] = exp2_fast(sc[r] * a.scale2 - base);
+        sc[r] = exp2_fast(sc[r] * a.scale2 - (base - LIFT<T>));
         sum += sc[r];
       }
       l = l * fade + both_sum(sum);
@@ -227,7 +234,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_split(const AttnArgs a) {
           to.ml[1] = cl;
           if (!piece) *to.n = pieces;
         }
-        if (!SHARED) (a.lse + row_off(a, b, oh, s))[oi] = cl > 0.0f ? (cm + __log2f(cl)) * G10_LN2 : cl == 0.0f ? G10_NEG_INF : cl;
+        if (!SHARED) (a.lse + row_off(a, b, oh, s))[oi] = cl > 0.0f ? (cm + __log2f(cl * DROP<T>)) * G10_LN2 : cl == 0.0f ? G10_NEG_INF : cl;
       }
     }
     __syncthreads();                                                // (the next block's tiles go where the parts lie)
@@ -285,7 +292,7 @@ __global__ __launch_bounds__(64 * SW) void k_attn_join(const AttnArgs a) {
       y[0] = (T)times(inv, x0); y[1] = (T)times(inv, x1);
       *(typename Vec<T>::x2*)((T*)a.o + batch_off(a, b, a.os[0]) + (s.q0 + i) * a.os[1] + (int64_t)h * a.os[2] + 2 * lane) = y;
     }
-    if (!lane) (a.lse + row_off(a, b, h, s))[i] = l > 0.0f ? (big + __log2f(l)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
+    if (!lane) (a.lse + row_off(a, b, h, s))[i] = l > 0.0f ? (big + __log2f(l * DROP<T>)) * G10_LN2 : l == 0.0f ? G10_NEG_INF : l;
   }
 }
 
