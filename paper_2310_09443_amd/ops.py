@@ -197,7 +197,8 @@ class AdamW:
 
     state_bits 32: moments `m` and `v` in float32.  8: `m` and the root of v in float8_e4m3fn, in blocks of 256 values with a float32
     scale each (`m_scale`, `v_scale`): a quarter of the memory.  They are flat tensors, every parameter's part beginning at a multiple
-    of 256 (`starts`); saving and loading them and `steps` is all a checkpoint needs.  `copies`: tensors of float16 or bfloat16, one for each
+    of 256 (`starts`); saving and loading them and `steps` is all a checkpoint needs.  8-bit moments are rounded to nearest in the first 16 steps
+    and then so that their mean over steps is right (to nearest, small changes would be lost in every step).  `copies`: tensors of float16 or bfloat16, one for each
     parameter or None, that receive the updated values in the same pass.  The parameters' memory stays in place until close()."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copies=None):
