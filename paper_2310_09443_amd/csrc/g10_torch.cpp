@@ -342,6 +342,13 @@ class AdamwCore {
       p.coefficient = norm.const_data_ptr<float>() + 1;
     }
     check(lib.adamw_step(h_, at_.data(), &p, stream_of(dev_)), "g10_adamw_step");
+    // (written past autograd: a graph made before that still needs the values of then has to notice)
+    auto written = [](const at::Tensor& t) { if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version(); };
+    for (size_t i = 0; i < params_.size(); ++i)
+      if (at_[i]) {
+        written(params_[i]);
+        if (copies_[i]) written(*copies_[i]);
+      }
     keep_.clear();
     return max_norm ? py::cast(norm.select(0, 0)) : py::object(py::none());
   }
