@@ -323,8 +323,8 @@ class AdamwCore {
     h_ = nullptr;
   }
 
-  // the norm before clipping, or None
-  py::object step(const py::object& grads, double lr, double beta1, double beta2, double eps, double decay, uint64_t number, std::optional<double> max_norm,
+  // whether there was a gradient; the norm before clipping, or None
+  py::tuple step(const py::object& grads, double lr, double beta1, double beta2, double eps, double decay, uint64_t number, std::optional<double> max_norm,
                   const Maybe& coefficient) {
     TORCH_CHECK_VALUE(!max_norm || *max_norm > 0, "max_norm must be above zero");
     TORCH_CHECK_VALUE(!max_norm || !coefficient, "max_norm or coefficient");
@@ -332,7 +332,7 @@ class AdamwCore {
       on_device(*coefficient, "coefficient", &dev_);
       TORCH_CHECK_VALUE(coefficient->scalar_type() == at::kFloat && coefficient->numel() == 1, "coefficient must be one float32 number");
     }
-    if (!gather(grads)) return py::none();
+    if (!gather(grads)) return py::make_tuple(false, max_norm ? py::cast(at::zeros({}, at::TensorOptions().dtype(at::kFloat).device(dev_))) : py::object(py::none()));
     const c10::DeviceGuard guard(dev_);
     handle();
     g10_adamw_params p{lr, beta1, beta2, eps, decay, number, coefficient ? coefficient->const_data_ptr<float>() : nullptr};
@@ -350,7 +350,7 @@ class AdamwCore {
         if (copies_[i]) written(*copies_[i]);
       }
     keep_.clear();
-    return max_norm ? py::cast(norm.select(0, 0)) : py::object(py::none());
+    return py::make_tuple(true, max_norm ? py::cast(norm.select(0, 0)) : py::object(py::none()));
   }
 
   py::object grad_norm(const py::object& grads, double max_norm) {

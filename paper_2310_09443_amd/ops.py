@@ -242,10 +242,14 @@ class AdamW:
     def step(self, grads=None, max_norm=None, coefficient=None):
         """One update; `grads`: one for each parameter (default: its .grad), None leaves a parameter and its moments as they are.
         max_norm: the gradients are scaled so that their norm together is at most this; returns the norm before (a device tensor, no
-        waiting), and a norm that is not finite leaves everything as it is.  coefficient: a float32 device tensor of one number
-        that multiplies the gradients instead (not finite: nothing changes)."""
-        norm = self._core.step(grads, self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.steps + 1, max_norm, coefficient)
-        self.steps += 1
+        waiting), and a norm that is not finite leaves parameters and moments as they are.  coefficient: a float32 device tensor of one number
+        that multiplies the gradients instead (not finite: the same).
+
+        `steps`, whose number the bias corrections go by, counts the calls with a gradient for any parameter.  It is one number for all: a parameter whose first
+        gradient comes late is corrected as if the ones before had been 0.  Whether a norm was finite is known on the device only, so such a call counts too; a
+        program that looks at the norm may take it back (`opt.steps -= 1`)."""
+        some, norm = self._core.step(grads, self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.steps + 1, max_norm, coefficient)
+        self.steps += some
         return norm
 
     def close(self):

@@ -34,3 +34,24 @@ def test_tensors_of_inference_mode(ops):
     opt.step([torch.ones(10, device="cuda")])
     assert float(w[0]) < 1
     opt.close()
+
+
+def test_what_counts_as_a_step(ops):
+    """A call without any gradient changes nothing, the number that the bias corrections go by either."""
+    g = [torch.randn(300, device="cuda"), torch.randn(7, 5, device="cuda")]
+    a, b = ([torch.ones_like(x) for x in g] for _ in range(2))
+    oa, ob = ops.AdamW(a), ops.AdamW(b)
+    for k in range(3):
+        for _ in range(k):
+            assert oa.step([None, None]) is None and oa.step([None, None], coefficient=torch.ones(1, device="cuda")) is None
+            assert float(oa.step([None, None], max_norm=1.0)) == 0.0
+            assert oa.step() is None                                  # no parameter has a .grad
+        oa.step(g)
+        ob.step(g)
+        assert oa.steps == ob.steps == k + 1
+    oa.step([None, g[1]])
+    assert oa.steps == 4
+    ob.step([None, g[1]])
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    oa.close()
+    ob.close()
