@@ -371,6 +371,7 @@ class AdamwCore {
   at::Device dev_;
   g10_adamw_t* h_ = nullptr;
   at::ScalarType made_for_ = at::kFloat;           // the gradients' type of the handle
+  std::vector<const void*> places_;                // where its tensors lay
   std::vector<const void*> at_;                    // of this call: the gradients' addresses, their type, copies that had to be made
   at::ScalarType type_ = at::kFloat;
   std::vector<at::Tensor> keep_;
@@ -416,9 +417,26 @@ class AdamwCore {
     return found;
   }
 
+  // what the library's tables point to
+  template <class F>
+  void each_place(F&& f) const {
+    for (size_t i = 0; i < params_.size(); ++i) {
+      f(params_[i], "params[", i);
+      if (copies_[i]) f(*copies_[i], "copies[", i);
+    }
+    const at::Tensor* state[4] = {&m_, &v_, ms_ ? &*ms_ : nullptr, vs_ ? &*vs_ : nullptr};
+    for (size_t i = 0; i < 4; ++i)
+      if (state[i]) f(*state[i], "state[", i);
+  }
+
   void handle() {
     if (h_) {
       TORCH_CHECK_VALUE(type_ == made_for_, "the gradients' type changed");
+      size_t k = 0;
+      each_place([&](const at::Tensor& t, const char* what, size_t i) {
+        TORCH_CHECK_VALUE(!t.numel() || t.const_data_ptr() == places_[k], what, i, "] has moved: its memory must stay in place until close()");
+        ++k;
+      });
       return;
     }
     std::vector<g10_adamw_tensor> ts(params_.size());
@@ -438,6 +456,8 @@ class AdamwCore {
     if (ms_ && m_.numel()) { d.m_scale = ms_->data_ptr<float>(); d.v_scale = vs_->data_ptr<float>(); }
     check(lib.adamw_create(&d, stream_of(dev_), &h_), "g10_adamw_create");
     made_for_ = type_;
+    places_.clear();
+    each_place([&](const at::Tensor& t, const char*, size_t) { places_.push_back(t.numel() ? t.const_data_ptr() : nullptr); });
   }
 };
 

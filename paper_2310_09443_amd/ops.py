@@ -199,7 +199,8 @@ class AdamW:
     scale each (`m_scale`, `v_scale`): a quarter of the memory.  They are flat tensors, every parameter's part beginning at a multiple
     of 256 (`starts`); saving and loading them and `steps` is all a checkpoint needs.  8-bit moments are rounded to nearest in the first 16 steps
     and then so that their mean over steps is right (to nearest, small changes would be lost in every step).  `copies`: tensors of float16 or bfloat16, one for each
-    parameter or None, that receive the updated values in the same pass.  The parameters' memory stays in place until close()."""
+    parameter or None, that receive the updated values in the same pass.  The parameters' memory stays in place until close(); a step that finds it
+    elsewhere raises ValueError.  Steps and norms of one object share a workspace: they must not overlap on two streams."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copies=None):
         params = list(params)
@@ -229,11 +230,16 @@ class AdamW:
             self.starts.append(at)
             at += -(-p.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
         st = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
-        self.m, self.v = (torch.zeros(at, dtype=torch.float32 if state_bits == 32 else torch.uint8, device=dev).view(st) for _ in range(2))
-        self.m_scale = self.v_scale = None
-        if state_bits == 8:
-            self.m_scale, self.v_scale = (torch.zeros(at // ADAMW_BLOCK, device=dev) for _ in range(2))
-        self._core = _calls().AdamwCore(params, copies, self.m, self.v, self.m_scale, self.v_scale)
+        m, v = (torch.zeros(at, dtype=torch.float32 if state_bits == 32 else torch.uint8, device=dev).view(st) for _ in range(2))
+        scales = [torch.zeros(at // ADAMW_BLOCK, device=dev) for _ in range(2)] if state_bits == 8 else [None, None]
+        self._state = m, v, *scales
+        self._core = _calls().AdamwCore(params, copies, *self._state)
+
+    # What the steps work on: copied into (`opt.m.copy_(saved)`), not replaced.
+    m = property(lambda self: self._state[0])
+    v = property(lambda self: self._state[1])
+    m_scale = property(lambda self: self._state[2])
+    v_scale = property(lambda self: self._state[3])
 
     def grad_norm(self, grads=None, max_norm=float("inf")):
         """The norm of all gradients together, summed in 64 bits: a tensor of one number on the device."""

@@ -55,3 +55,33 @@ def test_what_counts_as_a_step(ops):
     assert all(torch.equal(x, y) for x, y in zip(a, b))
     oa.close()
     ob.close()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_tensors_that_are_replaced_are_refused(ops, bits):
+    """The library's tables point to the memory of the first step: what is put in its place would be ignored, or worse."""
+    def make():
+        w = [torch.randn(300, device="cuda"), torch.randn(4, device="cuda"), torch.empty(0, device="cuda")]
+        half = [w[0].half(), None, None]
+        opt = ops.AdamW(w, state_bits=bits, copies=half)
+        opt.step([torch.ones_like(x) for x in w])
+        return w, half, opt
+
+    for change in (lambda w, half, opt: setattr(w[1], "data", w[1].data.clone()), lambda w, half, opt: setattr(half[0], "data", half[0].data.clone()),
+                   lambda w, half, opt: opt.m.set_(opt.m.clone())):
+        w, half, opt = make()
+        change(w, half, opt)
+        kept, grads = [x.clone() for x in w], [torch.ones_like(x) for x in w]
+        for call in (lambda: opt.step(grads), lambda: opt.step(grads, max_norm=1.0), lambda: opt.grad_norm(grads)):
+            with pytest.raises(ValueError, match="has moved"):
+                call()
+        assert opt.steps == 1 and all(torch.equal(x, y) for x, y in zip(w, kept))
+        opt.close()
+        opt.step(grads)                                                # after close() the tables are made anew, of what is there
+        assert opt.steps == 2 and not torch.equal(w[1], kept[1])
+        opt.close()
+    w, half, opt = make()
+    for name in ("m", "v", "m_scale", "v_scale"):
+        with pytest.raises(AttributeError):
+            setattr(opt, name, torch.zeros(5))
+    opt.close()
