@@ -41,6 +41,7 @@ static void bind(const std::vector<uintptr_t>& at) {
 
 static void check(int rc, const char* what) {
   if (!rc) return;
+  TORCH_CHECK_VALUE(rc != G10_EINVAL, what, " refuses these sizes or numbers");       // (what the checks here leave to the library's)
   py::object error = py::module_::import("paper_2310_09443_amd.binding").attr("G10Error");
   PyErr_SetObject(error.ptr(), error(rc, what).ptr());
   throw py::error_already_set();
