@@ -5,9 +5,13 @@
 
 #define BT 64                      // rows of a tile in LDS
 #define BW 128                     // rows of a workgroup, 32 to a wavefront
-#define FEW 12                     // tiles of 32 keys up to which delta comes from P and dP; keys up to which dS keeps its lower half for dq, and
-#define SOME 768                   // P and dS theirs for dk and dv
-#define FEWEST 128
+#define FEW 12                     // tiles of 32 keys up to which delta comes from P and dP
+#define SOME 768                   // keys that a query sees up to which dS keeps its lower half for dq
+#define FEWEST 128                 // and up to which P and dS keep theirs for dk and dv
+
+// Whether lower halves are kept: in no sequence, in all, or where a sequence's own lengths say so. The third kernels hold both walks, one behind
+// the other: both forms of a step in one loop would take 100 to 450 registers that there are not.
+enum { PLAIN, FINE, OWN };
 
 // In 16-bit floats with a short exponent, P and dS of long rows would fall below the smallest number.  P is held times
 // 2^12 (it is at most 1), dS times 8 over the power of two at the largest |do| of what it is summed over: of the query for dQ, of the
@@ -123,6 +127,23 @@ __device__ __forceinline__ f32x16 minus_delta(const Half& x) {
   return d;
 }
 
+// Keys that the query at position p sees.
+__device__ __forceinline__ int keys_at(const AttnArgs& a, int p, int nk) {
+  const Seen s = keys_of(a, p, nk);
+  const int first = s.first > 0 ? s.first : 0;
+  return !s.span || s.lo < first ? max(first, s.span ? s.lo + (int)s.span : 0) : first + (int)s.span;
+}
+// Whether any of the queries at p0..p1 sees some keys, and SOME at most. (It sees more the further it stands, or is nearer to the middle: one at an end sees fewest.)
+__device__ __forceinline__ bool some_see_few(const AttnArgs& a, int p0, int p1, int nk) {
+  if (a.causal && p0 < 0) p0 = 0;
+  return p0 <= p1 && min(keys_at(a, p0, nk), keys_at(a, p1, nk)) <= SOME;
+}
+// Whether none of a sequence's queries sees more than FEWEST.
+__device__ __forceinline__ bool all_see_few(const AttnArgs& a, int nk) {
+  const u64 near = a.window ? (u64)a.window * (a.causal ? 1 : 2) + a.sinks : (u64)nk;
+  return (u64)nk <= FEWEST || near <= FEWEST;
+}
+
 // What rounding eight values of x left of them.
 template <class T>
 __device__ __forceinline__ typename Vec<T>::x8 left8(f32x16& x, const typename Vec<T>::x8& got, int s) {
@@ -131,8 +152,8 @@ __device__ __forceinline__ typename Vec<T>::x8 left8(f32x16& x, const typename V
   return pack8<T>(x, s);
 }
 
-// In: the tile's scores and dP - delta in sc and dp.  Out: the next tile's.  FINE: P and dS meet dO and Q as their rounding and what that left.
-template <class T, int DP, bool FINE>
+// In: the tile's scores and dP - delta in sc and dp.  Out: the next tile's.  BOTH: P and dS meet dO and Q as their rounding and what that left.
+template <class T, int DP, bool BOTH>
 __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const typename Vec<T>::x8 (&kf)[DP / 16], const typename Vec<T>::x8 (&vf)[DP / 16],
                                           f32x16& sc, f32x16& dp, f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], float scale2, float lift_ds) {
   typedef typename Vec<T>::x8 x8;
@@ -174,7 +195,7 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
       else dn = Vec<T>::mfma(f[e % RING], vf[e / 2], dn);
       if constexpr (e < KS) exps(16 * e / KS, 16 * (e + 1) / KS);
       else grads(16 * (e - KS) / KS, 16 * (e - KS + 1) / KS);
-      if constexpr (FINE && e == 2 * KS - 1) {
+      if constexpr (BOTH && e == 2 * KS - 1) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) { pl[k] = left8<T>(sc, pf[k], k); dl[k] = left8<T>(dp, df[k], k); }
       }
@@ -182,8 +203,8 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
       constexpr int v = e - 2 * KS;
       if constexpr (v < 2 * DB) dv[v % DB] = Vec<T>::mfma(f[e % RING], pf[v / DB], dv[v % DB]);
       else dk[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB - 2], dk[v % DB]);
-      if constexpr (FINE && v < 2 * DB) dv[v % DB] = Vec<T>::mfma(f[e % RING], pl[v / DB], dv[v % DB]);
-      if constexpr (FINE && v >= 2 * DB) dk[v % DB] = Vec<T>::mfma(f[e % RING], dl[v / DB - 2], dk[v % DB]);
+      if constexpr (BOTH && v < 2 * DB) dv[v % DB] = Vec<T>::mfma(f[e % RING], pl[v / DB], dv[v % DB]);
+      if constexpr (BOTH && v >= 2 * DB) dk[v % DB] = Vec<T>::mfma(f[e % RING], dl[v / DB - 2], dk[v % DB]);
 #pragma unroll
       for (int r = 16 * v / (4 * DB); r < 16 * (v + 1) / (4 * DB); ++r) { sc[r] = sn[r]; dp[r] = dn[r]; }
     }
@@ -191,7 +212,7 @@ __device__ __forceinline__ void back_step(const Half& cu, const Half& nx, const 
   });
 }
 
-template <class T, int DP, bool FINE, bool SHARED>
+template <class T, int DP, int FORM, bool SHARED>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnArgs a) {
   __shared__ __attribute__((aligned(256))) T lds[3][2][BT * DP];
   __shared__ __attribute__((aligned(16))) float rows[3][2][BT];      // lse2, delta of a tile's queries
@@ -307,31 +328,36 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkdv(const AttnA
       for (int ks = 0; ks < DP / 16; ++ks) dp = Vec<T>::mfma(frag_rows<T, DP>(rb, BT, ks), vf[ks], dp);
       u32 buf = 0, n = 0;                                            // this tile's buffer; its half
       int t = 0;
+      auto walk = [&](auto both) __attribute__((always_inline)) {
 #pragma nounroll
-      while (t < all) {
-        if (!n) {                                                    // this tile and the next are there; the one behind them goes where the one before lay
-          loads_done();
-          __syncthreads();
-          if (t + 2 < all) fetch();
-        }
-        if (!(cur >= flo && cur + 31 <= fhi)) {                      // not all queries see all keys
-          const int at = cur + 4 * (int)(lane >> 5) - ilo;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const bool seen = (u32)(at + 8 * (r / 4) + r % 4) < span;
-            sc[r] = seen ? sc[r] : G10_NEG_INF;
+        while (t < all) {
+          if (!n) {                                                    // this tile and the next are there; the one behind them goes where the one before lay
+            loads_done();
+            __syncthreads();
+            if (t + 2 < all) fetch();
           }
+          if (!(cur >= flo && cur + 31 <= fhi)) {                      // not all queries see all keys
+            const int at = cur + 4 * (int)(lane >> 5) - ilo;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const bool seen = (u32)(at + 8 * (r / 4) + r % 4) < span;
+              sc[r] = seen ? sc[r] : G10_NEG_INF;
+            }
+          }
+          const Half here = half(buf, n);
+          cur += 32;
+          if (n || cur > hi) {                                         // the tile's last
+            n = 0;
+            ++t;
+            buf = buf == 2 ? 0 : buf + 1;
+            if (cur > hi) cur = first;
+          } else n = 1;
+          back_step<T, DP, decltype(both)::value != 0>(here, half(buf, n), kf, vf, sc, dp, dk, dv, a.scale2, lift_ds);
         }
-        const Half here = half(buf, n);
-        cur += 32;
-        if (n || cur > hi) {                                         // the tile's last
-          n = 0;
-          ++t;
-          buf = buf == 2 ? 0 : buf + 1;
-          if (cur > hi) cur = first;
-        } else n = 1;
-        back_step<T, DP, FINE>(here, half(buf, n), kf, vf, sc, dp, dk, dv, a.scale2, lift_ds);
-      }
+      };
+      if constexpr (FORM != OWN) walk(Const<FORM == FINE>{});
+      else if (all_see_few(a, s.nk)) walk(Const<1>{});
+      else walk(Const<0>{});
     }
     const float fk = a.scale / lift, fv = 1.0f / Lift<T>::p;
     if (!whole) {
@@ -420,8 +446,8 @@ __global__ __launch_bounds__(256) void k_attn_cuts(const AttnArgs a) {
 //   S^T = K Q^T,  dP^T = V dO^T  come out with a query to a lane,  dQ^T += K^T dS^T;   first, delta = sum(do o) of each query, which
 // the keys' kernel takes from here.  The same pipeline as there, two wavefronts to a SIMD.
 // These keys' scores and dP are in sc and dp, the next ones' go to sn and dn.  LDS: rows_base of the next keys, with their values behind them,
-// cols_base of these keys.  FINE: dS meets the keys as its rounding and what that left, in two products.
-template <class T, int DP, bool FINE>
+// cols_base of these keys.  BOTH: dS meets the keys as its rounding and what that left, in two products.
+template <class T, int DP, bool BOTH>
 __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Vec<T>::x8 (&q)[DP / 16], const typename Vec<T>::x8 (&dout)[DP / 16],
                                            f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn, f32x16 (&dq)[DP / 32], float scale2, float le, const f32x16& less, float lift) {
   typedef typename Vec<T>::x8 x8;
@@ -452,7 +478,7 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
     } else {
       constexpr int v = e - 2 * KS;
       dq[v % DB] = Vec<T>::mfma(f[e % RING], df[v / DB], dq[v % DB]);
-      if constexpr (FINE) {
+      if constexpr (BOTH) {
         if constexpr (v % DB == 0) left[v / DB] = left8<T>(dp, df[v / DB], v / DB);
         dq[v % DB] = Vec<T>::mfma(f[e % RING], left[v / DB], dq[v % DB]);
       }
@@ -461,7 +487,7 @@ __device__ __forceinline__ void query_step(u32 rows, u32 cols, const typename Ve
   });
 }
 
-template <class T, int DP, bool FINE>
+template <class T, int DP, int FORM>
 __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
   constexpr int KT = 32, NB = 4;                                     // keys of a tile; these, the next, two on their way
   __shared__ __attribute__((aligned(256))) T lds[NB][2][KT * DP];
@@ -502,7 +528,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
     // delta is sum(P dP) as well as sum(do o).  The second costs a reading of o, but o is rounded, and where few keys are seen that
     // error is large beside dq and dk: against a result that is only rounded once, theirs is 1.4 times as large with the first and with
     // the second 2.3 times for 4 keys, 1.6 for 128, 1.5 for 400.  So the first up to 384 keys of the workgroup's, for one more walk over them
-    // (two of a step's three products).  (See keys_seen for more of them.)
+    // (two of a step's three products).  (See form_dq for more of them.)
     const bool few = tiles.count <= FEW;
     u32 to = 0;
     int ft = 0, rest = few ? 2 * tiles.count : tiles.count;          // next tile to be fetched; how many there are to be
@@ -587,38 +613,43 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AttnArgs a) {
       f32x16 sb, db, less;                                           // (the sums of dP begin with minus delta)
 #pragma unroll
       for (int r = 0; r < 16; ++r) less[r] = -de;
-      int t = 0;
-      auto turn = [&](f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
-        arrive();
-        const int j0 = tiles.at(t) * KT, j1 = j0 + KT - 1;
-        if (!((j0 >= flo && j1 <= fhi) || (j1 < (int)a.sinks && j1 <= ftop))) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sc[r] = seen.key(j0 + res_row(r)) ? sc[r] : G10_NEG_INF;
-        }
-        const u32 next = (buf + 1) % NB;
-        query_step<T, DP, FINE>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, less, lift);
-        buf = next;
-        ++t;
-      };
-      const Runs runs = runs_of<KT>(a, tiles, wp0, wp1, s.nk);
-      // two runs of tiles with something to do; between them only what the other wavefronts' tiles need
-#pragma nounroll
-      for (int run = 0; run < 3; ++run) {
-        const int from = run == 0 ? 0 : run == 1 ? runs.from : tiles.count, end = run == 0 ? runs.head : run == 1 ? runs.end : 0;
-#pragma nounroll
-        for (; t < from; ++t) {
+      auto walk = [&](auto both) __attribute__((always_inline)) {
+        int t = 0;
+        auto turn = [&](f32x16& sc, f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
           arrive();
-          buf = (buf + 1) % NB;
-        }
-        if (t >= end) continue;
-        scores(rb + buf * (2 * KT * DP * 2), less);
+          const int j0 = tiles.at(t) * KT, j1 = j0 + KT - 1;
+          if (!((j0 >= flo && j1 <= fhi) || (j1 < (int)a.sinks && j1 <= ftop))) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = seen.key(j0 + res_row(r)) ? sc[r] : G10_NEG_INF;
+          }
+          const u32 next = (buf + 1) % NB;
+          query_step<T, DP, decltype(both)::value != 0>(rb + next * (2 * KT * DP * 2), cb + buf * (2 * KT * DP * 2), q, dout, sc, dp, sn, dn, dq, a.scale2, le, less, lift);
+          buf = next;
+          ++t;
+        };
+        const Runs runs = runs_of<KT>(a, tiles, wp0, wp1, s.nk);
+        // two runs of tiles with something to do; between them only what the other wavefronts' tiles need
 #pragma nounroll
-        while (t + 1 < end) {
-          turn(sa, da, sb, db);
-          turn(sb, db, sa, da);
+        for (int run = 0; run < 3; ++run) {
+          const int from = run == 0 ? 0 : run == 1 ? runs.from : tiles.count, end = run == 0 ? runs.head : run == 1 ? runs.end : 0;
+#pragma nounroll
+          for (; t < from; ++t) {
+            arrive();
+            buf = (buf + 1) % NB;
+          }
+          if (t >= end) continue;
+          scores(rb + buf * (2 * KT * DP * 2), less);
+#pragma nounroll
+          while (t + 1 < end) {
+            turn(sa, da, sb, db);
+            turn(sb, db, sa, da);
+          }
+          if (t < end) turn(sa, da, sb, db);
         }
-        if (t < end) turn(sa, da, sb, db);
-      }
+      };
+      if constexpr (FORM != OWN) walk(Const<FORM == FINE>{});
+      else if (some_see_few(a, qt * BW + off, e1 + off, s.nk)) walk(Const<1>{});
+      else walk(Const<0>{});
     }
     if (i < s.nq) {
       T* dQ = (T*)a.dq + batch_off(a, b, a.dqs[0]) + (s.q0 + i) * a.dqs[1] + (int64_t)h * a.dqs[2];
@@ -670,29 +701,40 @@ static u32 key_shares(const AttnArgs& a) {
 }
 static uint64_t share_bytes(const AttnArgs& a) { return (uint64_t)a.shares * (sizeof(Cut) + 4 * BW * (a.dim <= 64 ? 64 : 128) * 4); }
 
-// How many keys a query sees at most, or in a packed sequence of mean length, which is known here: it decides where P and dS keep their lower halves.
-// As 16-bit numbers they add about as much error to the gradients as those' own rounding, 1.41 times that in all; o's rounding in delta brings dq to 1.5
-// times where few keys are seen, and with very few of them a single factor's rounding may rule a row.  Up to 768 keys dq has both halves of
-// dS (1.05 to 1.08 times its rounding, for one product of three more: 32 x 512 tokens of 12 heads of 64, 198 -> 204 us forward and backward; delta from
-// P and dP up to there: 245), up to 128 dk and dv have those of dS and P too.
-static uint64_t keys_seen(const AttnArgs& a) {
-  const uint64_t keys = a.q_start ? ((uint64_t)a.seq_k + a.batch - 1) / a.batch : a.seq_k;
-  const uint64_t near = a.window ? (uint64_t)a.window * (a.causal ? 1 : 2) + a.sinks : keys;
-  return near < keys ? near : keys;
+// As 16-bit numbers P and dS add about as much error to the gradients as those' own rounding, 1.41 times that in all; o's rounding in delta brings dq to 1.5
+// times where few keys are seen, and with very few of them a single factor's rounding may rule a row.  So dq has both halves of dS in blocks of queries any of which sees up to 768
+// keys (1.05 to 1.08 times its rounding, for one product of three more: 32 x 512 tokens of 12 heads of 64, 198 -> 204 us forward and backward; delta from
+// P and dP up to there: 245), and dk and dv have those of dS and P in sequences of which no query sees more than 128.  What is decided goes by a sequence's own lengths alone;
+// where these are known here, a kernel for them is taken.
+static uint64_t keys_near(const AttnArgs& a) { return a.window ? (uint64_t)a.window * (a.causal ? 1 : 2) + a.sinks : ~0ull; }
+static int form_dq(const AttnArgs& a) {
+  if (keys_near(a) <= SOME || a.seq_k <= SOME) return FINE;
+  if (a.q_start || a.k_len || (a.window && a.window <= SOME)) return OWN;
+  if (!a.causal) return !a.window || a.seq_q <= a.seq_k ? PLAIN : OWN;
+  return (int64_t)a.seq_k - a.seq_q + 1 > SOME ? PLAIN : OWN;
+}
+static int form_dkdv(const AttnArgs& a) {
+  if (keys_near(a) <= FEWEST || a.seq_k <= FEWEST) return FINE;
+  return a.q_start || a.k_len ? OWN : PLAIN;
 }
 
 template <class T, int DP>
-static void launch_dq(const AttnArgs& a, bool fine, dim3 grid, hipStream_t s) {
-  if (fine) k_attn_dq<T, DP, true><<<grid, 256, 0, s>>>(a);
-  else k_attn_dq<T, DP, false><<<grid, 256, 0, s>>>(a);
+static void launch_dq(const AttnArgs& a, int form, dim3 grid, hipStream_t s) {
+  if (form == FINE) k_attn_dq<T, DP, FINE><<<grid, 256, 0, s>>>(a);
+  else if (form == PLAIN) k_attn_dq<T, DP, PLAIN><<<grid, 256, 0, s>>>(a);
+  else k_attn_dq<T, DP, OWN><<<grid, 256, 0, s>>>(a);
 }
 
+template <class T, int DP, int FORM>
+static void launch_dkdv(const AttnArgs& a, dim3 grid, hipStream_t s) {
+  if (a.shares) k_attn_dkdv<T, DP, FORM, true><<<grid, 256, 0, s>>>(a);
+  else k_attn_dkdv<T, DP, FORM, false><<<grid, 256, 0, s>>>(a);
+}
 template <class T, int DP>
-static void launch_dkdv(const AttnArgs& a, bool fine, dim3 grid, hipStream_t s) {
-  if (fine && a.shares) k_attn_dkdv<T, DP, true, true><<<grid, 256, 0, s>>>(a);
-  else if (fine) k_attn_dkdv<T, DP, true, false><<<grid, 256, 0, s>>>(a);
-  else if (a.shares) k_attn_dkdv<T, DP, false, true><<<grid, 256, 0, s>>>(a);
-  else k_attn_dkdv<T, DP, false, false><<<grid, 256, 0, s>>>(a);
+static void launch_dkdv(const AttnArgs& a, int form, dim3 grid, hipStream_t s) {
+  if (form == FINE) launch_dkdv<T, DP, FINE>(a, grid, s);
+  else if (form == PLAIN) launch_dkdv<T, DP, PLAIN>(a, grid, s);
+  else launch_dkdv<T, DP, OWN>(a, grid, s);
 }
 
 extern "C" int g10_attention_backward_workspace(const g10_attention_args* g, uint64_t* bytes) {
@@ -715,7 +757,6 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < top_bytes(a) + pad256(rows * 8) + share_bytes(a)) return G10_EINVAL;
   const u32 qt = a.q_tiles = query_tiles(a), kt = tiles_in(units, 1, (a.max_k + BW - 1) / BW);
   hipStream_t s = (hipStream_t)hip_stream;
-  const uint64_t seen = keys_seen(a);
   a.amax = (const u32*)workspace;
   a.delta = (const float*)((char*)workspace + top_bytes(a));
   a.lse2 = a.delta + rows;
@@ -723,22 +764,22 @@ extern "C" int g10_attention_backward(const g10_attention_args* g, void* workspa
   a.cuts = (Cut*)(a.part + (uint64_t)a.shares * 4 * BW * (a.dim <= 64 ? 64 : 128));
   const bool narrow = a.dim <= 64, bf = g->type == G10_BF16;
   if (qt) {
-    const bool fine = seen <= SOME;
+    const int form = form_dq(a);
     a.tiles = qt;
     const dim3 grid(with_rest(a, unit_grid(units, a.group * a.tiles)));
-    if (bf && narrow) launch_dq<__bf16, 64>(a, fine, grid, s);
-    else if (bf) launch_dq<__bf16, 128>(a, fine, grid, s);
-    else if (narrow) launch_dq<_Float16, 64>(a, fine, grid, s);
-    else launch_dq<_Float16, 128>(a, fine, grid, s);
+    if (bf && narrow) launch_dq<__bf16, 64>(a, form, grid, s);
+    else if (bf) launch_dq<__bf16, 128>(a, form, grid, s);
+    else if (narrow) launch_dq<_Float16, 64>(a, form, grid, s);
+    else launch_dq<_Float16, 128>(a, form, grid, s);
   }
   if (kt) {
-    const bool fine = seen <= FEWEST;
+    const int form = form_dkdv(a);
     a.tiles = kt;
     const dim3 grid(with_rest(a, a.shares ? a.shares : unit_grid(units, a.tiles)));
-    if (bf && narrow) launch_dkdv<__bf16, 64>(a, fine, grid, s);
-    else if (bf) launch_dkdv<__bf16, 128>(a, fine, grid, s);
-    else if (narrow) launch_dkdv<_Float16, 64>(a, fine, grid, s);
-    else launch_dkdv<_Float16, 128>(a, fine, grid, s);
+    if (bf && narrow) launch_dkdv<__bf16, 64>(a, form, grid, s);
+    else if (bf) launch_dkdv<__bf16, 128>(a, form, grid, s);
+    else if (narrow) launch_dkdv<_Float16, 64>(a, form, grid, s);
+    else launch_dkdv<_Float16, 128>(a, form, grid, s);
   }
   if (kt && a.shares) {
     const dim3 grid(a.shares, 8);
