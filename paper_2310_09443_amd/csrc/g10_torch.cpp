@@ -4,6 +4,7 @@
 #include <torch/extension.h>
 
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 
 #include <math.h>
@@ -440,6 +441,9 @@ class AdamwCore {
       });
       return;
     }
+    // (it allocates, copies from host memory that it then frees, and waits)
+    TORCH_CHECK_VALUE(c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None,
+                      "the first step or norm makes the library's tables, which a graph cannot hold: make one before the capture");
     std::vector<g10_adamw_tensor> ts(params_.size());
     int copy_type = 0;
     for (size_t i = 0; i < ts.size(); ++i) {

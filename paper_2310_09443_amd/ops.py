@@ -200,7 +200,7 @@ class AdamW:
     of 256 (`starts`); saving and loading them and `steps` is all a checkpoint needs.  8-bit moments are rounded to nearest in the first 16 steps
     and then so that their mean over steps is right (to nearest, small changes would be lost in every step).  `copies`: tensors of float16 or bfloat16, one for each
     parameter or None, that receive the updated values in the same pass.  The parameters' memory stays in place until close(); a step that finds it
-    elsewhere raises ValueError.  Steps and norms of one object share a workspace: they must not overlap on two streams."""
+    elsewhere raises ValueError.  The first step or norm makes the library's tables and cannot be captured into a graph, later ones can.  Steps and norms of one object share a workspace: they must not overlap on two streams."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copies=None):
         params = list(params)

@@ -85,3 +85,25 @@ def test_tensors_that_are_replaced_are_refused(ops, bits):
         with pytest.raises(AttributeError):
             setattr(opt, name, torch.zeros(5))
     opt.close()
+
+
+def test_the_first_step_is_not_captured(ops):
+    """It makes the library's tables.  Refused before anything is recorded: what else was captured is whole."""
+    w, g, x = torch.ones(300, device="cuda"), torch.ones(300, device="cuda"), torch.zeros(300, device="cuda")
+    opt = ops.AdamW([w])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1)
+        with pytest.raises(ValueError, match="before the capture"):
+            opt.step([g])
+        with pytest.raises(ValueError, match="before the capture"):
+            opt.grad_norm([g])
+    for n in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (x == n + 1).all() and (w == 1).all() and opt.steps == 0
+    opt.step([g])
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        opt.step([g])
+    opt.close()
