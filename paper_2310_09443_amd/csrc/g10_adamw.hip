@@ -322,9 +322,9 @@ static int check_call(g10_adamw_t* h, const void* const* grads) {
   int now = 0;
   if (hipGetDevice(&now) != hipSuccess) return G10_EDEVICE;
   if (now != h->device) return G10_EINVAL;
-  for (u32 i = 0; i < h->count; ++i)
-    if ((uintptr_t)grads[i] % size_of(h->grad_type)) return G10_EINVAL;
-  return G10_OK;
+  uintptr_t all = 0;
+  for (u32 i = 0; i < h->count; ++i) all |= (uintptr_t)grads[i];
+  return all & (size_of(h->grad_type) - 1) ? G10_EINVAL : G10_OK;
 }
 
 template <class P, class G>

@@ -373,7 +373,6 @@ class AdamwCore {
   at::Device dev_;
   g10_adamw_t* h_ = nullptr;
   at::ScalarType made_for_ = at::kFloat;           // the gradients' type of the handle
-  std::vector<const void*> places_;                // where its tensors lay
   std::vector<const void*> at_;                    // of this call: the gradients' addresses, their type, copies that had to be made
   at::ScalarType type_ = at::kFloat;
   std::vector<at::Tensor> keep_;
@@ -419,7 +418,14 @@ class AdamwCore {
     return found;
   }
 
+  // Where a tensor lies: its memory and its place in it, without data_ptr's checks (a step of 300 small tensors takes as long as they do).
+  typedef std::pair<const void*, int64_t> Place;
+  static Place place_of(const at::Tensor& t) {
+    const c10::TensorImpl* p = t.unsafeGetTensorImpl();
+    return {p->unsafe_storage().unsafeGetStorageImpl()->data(), p->storage_offset()};
+  }
   // what the library's tables point to
+  std::vector<Place> places_;                      // of the handle
   template <class F>
   void each_place(F&& f) const {
     for (size_t i = 0; i < params_.size(); ++i) {
@@ -436,7 +442,7 @@ class AdamwCore {
       TORCH_CHECK_VALUE(type_ == made_for_, "the gradients' type changed");
       size_t k = 0;
       each_place([&](const at::Tensor& t, const char* what, size_t i) {
-        TORCH_CHECK_VALUE(!t.numel() || t.const_data_ptr() == places_[k], what, i, "] has moved: its memory must stay in place until close()");
+        TORCH_CHECK_VALUE(place_of(t) == places_[k], what, i, "] has moved: its memory must stay in place until close()");
         ++k;
       });
       return;
@@ -462,7 +468,7 @@ class AdamwCore {
     check(lib.adamw_create(&d, stream_of(dev_), &h_), "g10_adamw_create");
     made_for_ = type_;
     places_.clear();
-    each_place([&](const at::Tensor& t, const char*, size_t) { places_.push_back(t.numel() ? t.const_data_ptr() : nullptr); });
+    each_place([&](const at::Tensor& t, const char*, size_t) { places_.push_back(place_of(t)); });
   }
 };
 
