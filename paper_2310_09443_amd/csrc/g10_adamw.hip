@@ -104,7 +104,8 @@ __device__ __forceinline__ void read_codes(const void* codes, u64 at, float scal
 // bits of t: over all thresholds the mean is y. A moment is rounded again in every update, and with beta2 = 0.999 an update moves a root by less
 // than 0.05 % where half a step is 3 to 6 %: to nearest it would stay where it is for good (gradients that fall tenfold after 1000 updates: 6.7
 // times the root that they should have 5000 updates later, that grow fivefold: 0.45 times; so 1.01 both). The threshold turns by the golden ratio from update to update, which meets every part of
-// the way in nearly equal numbers: the root's spread about the exact one is 15 % with thresholds that turn and 17 % with random ones.
+// the way in nearly equal numbers: the root's spread about the exact one is 15 % with thresholds that turn and 17 % with random ones. (109
+// million weights: 365 us a step to nearest, 379 so.)
 __device__ __forceinline__ float spread8(float y, u32 t) {
   const float a = fabsf(y), low = a < 0.015625f ? 0.015625f : 0.0f;  // (below 2^-6 neighbours lie 2^-9 apart, as they do from 2^-6 to 2^-5)
   const float up = __uint_as_float((__float_as_uint(a + low) + (t >> 12)) & 0xfff00000u) - low;

@@ -215,7 +215,8 @@ __device__ __forceinline__ int swz(int r) {
 // 64 pieces straight from memory to LDS, lane i's to the place i behind lds (which is the same in every lane).
 // The address is that of the lane's piece: base (the same in every lane) + off bytes.
 // The instruction has no output register and its address is read when it is issued; who reads the tile waits for it first
-// (loads_done) and then meets the others at a barrier.
+// (loads_done) and then meets the others at a barrier.  m0 is not named as written: the compiler reserves it (and warns where a list names it), keeps no
+// value there and sets it right before an instruction of its own that reads it, of which these kernels have none.
 __device__ __forceinline__ void load_piece(const void* base, u32 off, u32 lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }

@@ -118,7 +118,7 @@ class Decoder:
 
 # Microseconds of the operators on an MI355X at the sizes of `decoder48_lean`; the update is bound by its bytes: 16 an element (master
 # 4 + 4, gradient 2, moments 1 + 1 twice, copy 2) and the scales.
-ROPE_US, ROPE_BACK_US, ATTENTION_US, ATTENTION_BACK_US = 210, 331, 680, 2400
+ROPE_US, ROPE_BACK_US, ATTENTION_US, ATTENTION_BACK_US = 210, 327, 677, 2470
 ADAMW_BYTES, ADAMW_BPUS = 16 + 16 / 256, 5.2e6
 
 
