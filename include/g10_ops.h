@@ -107,7 +107,7 @@ int g10_attention_backward(const g10_attention_args *args, void *workspace, uint
  * elements.  state_type G10_F32: m and v themselves.  G10_E4M3: m and sqrt(v) in blocks of G10_ADAMW_BLOCK values, 8-bit
  * floats (3 bits of mantissa) times one 32-bit scale a block, largest magnitude / 448; the update of a step works on
  * the moments before they are rounded.  A root above zero is never held as zero; blocks whose largest magnitude is below
- * 1e-30 are held as zeros.  Steps 1 to G10_ADAMW_NEAREST round to nearest, which is the more exact while the moments come into being (after 16 steps on
+ * 1e-30 are held as zeros.  Tensors and copies must not overlap: they are updated side by side.  Steps 1 to G10_ADAMW_NEAREST round to nearest, which is the more exact while the moments come into being (after 16 steps on
  * normal gradients m and the root are off by 4.9 and 6.0 %, else by 5.7 and 6.9).  Later ones round up or down by a threshold that goes by the
  * value's place and the step's number, so that the mean over steps is right: a step moves a root by far less than half of what separates
  * two 8-bit values, and to nearest it would no longer move.  A step that is captured and replayed has the number, and the thresholds, of its capture. */

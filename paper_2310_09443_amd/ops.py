@@ -193,7 +193,7 @@ def attention(q, k, v, causal=True, window=0, sinks=0, scale=None, q_start=None,
 
 # ---------------------------------------------------------------------------------------------------------------- AdamW
 class AdamW:
-    """AdamW over all of `params` (contiguous tensors of one type: float32, float16 or bfloat16) in one launch a step.
+    """AdamW over all of `params` (contiguous tensors of one type that share no memory: float32, float16 or bfloat16) in one launch a step.
 
     state_bits 32: moments `m` and `v` in float32.  8: `m` and the root of v in float8_e4m3fn, in blocks of 256 values with a float32
     scale each (`m_scale`, `v_scale`): a quarter of the memory.  They are flat tensors, every parameter's part beginning at a multiple
@@ -222,6 +222,10 @@ class AdamW:
             if c is not None:
                 _on_device(c, f"copies[{i}]", dev)
                 _need(c.dtype == ct and c.is_contiguous() and c.shape == p.shape, f"copies[{i}] must be contiguous, of one type and its parameter's shape")
+        written = [(t, f"{n}[{i}]") for n, ts in (("params", params), ("copies", copies)) for i, t in enumerate(ts) if t is not None and t.numel()]
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), n) for t, n in written)
+        for (_, end, a), (begin, _, b) in zip(spans, spans[1:]):        # two updates of one place at once: either may win
+            _need(end <= begin, f"{a} and {b} share memory")
         self.params, self.copies, self.device = params, copies, dev
         self.lr, self.betas, self.eps, self.weight_decay, self.state_bits = lr, betas, eps, weight_decay, state_bits
         self.steps = 0

@@ -107,3 +107,17 @@ def test_the_first_step_is_not_captured(ops):
     with torch.cuda.graph(torch.cuda.CUDAGraph()):
         opt.step([g])
     opt.close()
+
+
+def test_tensors_that_share_memory_are_refused(ops):
+    """They are updated at the same time: which of two updates stays would change from run to run."""
+    w = torch.ones(1000, device="cuda")
+    h = w.bfloat16()
+    for params, copies in (([w, w], None), ([w, w[500:]], None), ([w[:600], w[599:]], None), ([w[:8], w[100:]], [h[:8], h[7:907]]),
+                           ([h, w.bfloat16()], [h, None]), ([w.new_ones(4).bfloat16(), h], [h[:4], None])):
+        with pytest.raises(ValueError, match="share memory"):
+            ops.AdamW(params, copies=copies)
+    opt = ops.AdamW([w[:500], w[500:], w[500:500]], copies=[h[:500], h[500:], None])       # side by side is fine
+    opt.step([torch.ones(500, device="cuda"), torch.ones(500, device="cuda"), None])
+    assert (w < 1).all()
+    opt.close()
