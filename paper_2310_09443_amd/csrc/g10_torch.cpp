@@ -9,6 +9,7 @@
 
 #include <math.h>
 #include <optional>
+#include <unordered_map>
 #include <vector>
 
 #include "g10_ops.h"
@@ -317,7 +318,13 @@ static py::tuple attention_backward(const at::Tensor& d_o, const at::Tensor& q, 
 class AdamwCore {
  public:
   AdamwCore(std::vector<at::Tensor> params, std::vector<Maybe> copies, at::Tensor m, at::Tensor v, Maybe m_scale, Maybe v_scale)
-      : params_(std::move(params)), copies_(std::move(copies)), m_(m), v_(v), ms_(m_scale), vs_(v_scale), dev_(params_.at(0).device()) {}
+      : params_(std::move(params)), copies_(std::move(copies)), m_(m), v_(v), ms_(m_scale), vs_(v_scale), dev_(params_.at(0).device()) {
+    std::unordered_map<const c10::TensorImpl*, uint32_t> of;
+    auto counter = [&](const at::Tensor& t) { return of.emplace((t.is_view() ? t._base() : t).unsafeGetTensorImpl(), (uint32_t)of.size()).first->second; };
+    for (const at::Tensor& t : params_) params_counter_.push_back(counter(t));
+    for (const Maybe& t : copies_) copies_counter_.push_back(t ? counter(*t) : 0);
+    counted_.resize(of.size() + 1);
+  }
   ~AdamwCore() { close(); }
 
   void close() {
@@ -345,11 +352,11 @@ class AdamwCore {
     }
     check(lib.adamw_step(h_, at_.data(), &p, stream_of(dev_)), "g10_adamw_step");
     // (written past autograd: a graph made before that still needs the values of then has to notice)
-    auto written = [](const at::Tensor& t) { if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version(); };
+    ++calls_;
     for (size_t i = 0; i < params_.size(); ++i)
       if (at_[i]) {
-        written(params_[i]);
-        if (copies_[i]) written(*copies_[i]);
+        written(params_[i], params_counter_[i]);
+        if (copies_[i]) written(*copies_[i], copies_counter_[i]);
       }
     keep_.clear();
     return py::make_tuple(true, max_norm ? py::cast(norm.select(0, 0)) : py::object(py::none()));
@@ -376,6 +383,16 @@ class AdamwCore {
   std::vector<const void*> at_;                    // of this call: the gradients' addresses, their type, copies that had to be made
   at::ScalarType type_ = at::kFloat;
   std::vector<at::Tensor> keep_;
+
+  // Version counters: a buffer and its views share one, which is moved once a step (an atomic operation each time).
+  std::vector<uint32_t> params_counter_, copies_counter_;
+  std::vector<uint64_t> counted_;                  // the call that moved it last
+  uint64_t calls_ = 0;
+  void written(const at::Tensor& t, uint32_t counter) {
+    if (counted_[counter] == calls_) return;
+    counted_[counter] = calls_;
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
 
   at::Tensor norms(double max_norm) {
     at::Tensor norm = at::empty({2}, at::TensorOptions().dtype(at::kFloat).device(dev_));

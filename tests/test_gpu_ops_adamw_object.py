@@ -121,3 +121,18 @@ def test_tensors_that_share_memory_are_refused(ops):
     opt.step([torch.ones(500, device="cuda"), torch.ones(500, device="cuda"), None])
     assert (w < 1).all()
     opt.close()
+
+
+def test_views_of_one_buffer_move_its_version(ops):
+    """A buffer and its views have one version: it moves in every step that writes any of them, and other buffers' do not."""
+    flat, other = torch.ones(1000, device="cuda"), torch.ones(50, device="cuda")
+    half = torch.ones(1000, dtype=torch.bfloat16, device="cuda")
+    opt = ops.AdamW([flat[:300], other, flat[300:]], copies=[half[:300], None, half[300:]])
+    one = lambda t: torch.ones(t, device="cuda")                                          # noqa: E731
+    for grads, moved in (([one(300), one(50), one(700)], (1, 1, 1)), ([None, None, one(700)], (1, 0, 1)), ([None, one(50), None], (0, 1, 0)),
+                         ([one(300), None, one(700)], (1, 0, 1))):
+        before = flat._version, other._version, half._version
+        opt.step(grads)
+        for b, a, m in zip(before, (flat._version, other._version, half._version), moved):
+            assert (a > b) == bool(m)
+    opt.close()
