@@ -1,8 +1,10 @@
 /* g10_ops.h - C ABI of the operators of a training step that stand next to the planner (same library, gfx950).
  *
  * The planner of g10.h moves tensors that a step keeps but does not use.  These operators keep fewer: attention whose
- * scores never leave the chip, the norms of queries and keys together with the rotation by position, and one AdamW
- * update over all weights with its moments in 8 bits where wanted.
+ * scores never leave the chip, the norms of queries and keys together with the rotation by position, one AdamW
+ * update over all weights with its moments in 8 bits where wanted, norms of rows and the first half of a gated MLP whose
+ * backward passes are given the inputs alone, log probabilities whose gradient needs one number a row, and the lookup in a table
+ * of embeddings with its gradient.
  *
  * Conventions
  *   - plain C, no exceptions, no state outside the handles of g10_adamw_create; every call but g10_adamw_free returns
@@ -148,6 +150,107 @@ int g10_adamw_step(g10_adamw_t *handle, const void *const *grads, const g10_adam
  * out: device, 2 floats; max_norm > 0.  The handle's own workspace: calls on one handle must not overlap in time. */
 int g10_grad_norm(g10_adamw_t *handle, const void *const *grads, float max_norm, float *out, void *hip_stream);
 void g10_adamw_free(g10_adamw_t *handle); /* after waiting for the device; NULL is allowed */
+
+/* ------------------------------------------------------------------------------------------------------ embeddings
+ * out_t = scale * table[ids_t], and of the table: dtable_v = scale * sum over the tokens t with ids_t = v of dout_t, summed in 32 bits.
+ * Every row of dtable is written, the ones without a token with zeros.  An id outside the table makes its token's out NaN and
+ * has no part in dtable.  The sums' order is that of the tokens, cut into pieces that depend on the sizes and the ids alone. */
+typedef struct {
+  const void *ids;           /* [tokens], int32_t, or int64_t with ids_64                      */
+  const void *table;         /* forward: [vocab][dim]                                          */
+  void *out;                 /* forward: [tokens][dim]                                         */
+  const void *dout;          /* backward: [tokens][dim]                                        */
+  void *dtable;              /* backward: [vocab][dim]                                         */
+  int64_t table_stride, out_stride, dout_stride, dtable_stride; /* of rows                      */
+  uint32_t tokens, vocab, dim; /* tokens below 2^31, vocab 1 .. 2^31 - 1, dim 1 .. 65536         */
+  float scale;
+  uint32_t type;             /* of table, out, dout, dtable: G10_F32, G10_F16, G10_BF16        */
+  uint32_t ids_64;
+} g10_embed_args;
+
+int g10_embed(const g10_embed_args *args, void *hip_stream);
+int g10_embed_backward_workspace(const g10_embed_args *args, uint64_t *bytes);
+int g10_embed_backward(const g10_embed_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------- norms of rows
+ * For every row x of `dim` values:   m = mean(x) with `center`, else 0;   r = 1 / sqrt(mean((x - m)^2) + eps);
+ *   n = (x - m) r;   y = n * weight + bias.
+ * Backward, from x and dy alone, with u = dy * weight:   dx = r (u - n mean(u n) - [center] mean(u)),
+ *   dweight = sum of dy n,  dbias = sum of dy  over the rows.
+ * Row sums in 32 bits (the squares of what is left after the mean is taken off), sums over rows in 32 and joined in 64. */
+typedef struct {
+  const void *x, *dy;        /* [rows][dim]; dy: backward                                      */
+  const void *weight, *bias; /* [dim] of weight_type, or NULL                                  */
+  void *out;                 /* forward: y (may be x); backward: dx (may be x or dy)           */
+  void *dweight, *dbias;     /* backward: [dim] of weight_type, or NULL                        */
+  int64_t x_stride, dy_stride, out_stride; /* of rows                                           */
+  uint32_t rows, dim;        /* rows below 2^31, dim 1 .. 65536                                */
+  float eps;                 /* >= 0                                                           */
+  uint32_t center;
+  uint32_t type, weight_type;/* of x, dy, out: G10_F32, G10_F16, G10_BF16; of the weights: `type` or G10_F32 */
+} g10_norm_args;
+
+int g10_norm(const g10_norm_args *args, void *hip_stream);
+int g10_norm_backward_workspace(const g10_norm_args *args, uint64_t *bytes);
+int g10_norm_backward(const g10_norm_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------------- log probabilities
+ * Of every row z = scale * logits:   lse = log sum_j exp z_j,   p_j = exp(z_j - lse),   logp = z_t - lse for the row's token t,
+ *   entropy = - sum p_j log p_j,   and the `top` largest z_j - lse with their places, ties in order of the places.
+ * dlogits_j = scale * (dlogp ([j = t] - p_j) - dentropy p_j (log p_j + entropy)).
+ * A token equal to `ignore` has logp = 0 and no share in the gradient; any other one outside the row makes logp, and the row's
+ * gradient, NaN.  Places of -infinity have no probability; a row of nothing else has lse = logp = -infinity, entropy 0 and no gradient.
+ * A row with a NaN or +infinity has logp, lse, entropy and the gradient NaN (NaN counts as the largest where the top is sought); a row
+ * with dlogp = 0 or an ignored token, and dentropy = 0, has the gradient 0 whatever it holds. */
+#define G10_LOG_PROBS_TOP 64u
+
+typedef struct {
+  const void *logits;        /* [rows][vocab]                                                  */
+  const int64_t *tokens;     /* [rows], or NULL: no logp (and no share of it in the gradient)  */
+  float *logp, *lse, *entropy; /* forward: [rows]; entropy may be NULL.  Backward reads lse, and entropy with dentropy */
+  float *top_logp;           /* forward: [rows][top], with top > 0                             */
+  int64_t *top_ids;
+  const float *dlogp, *dentropy; /* backward: [rows], or NULL                                  */
+  void *dlogits;             /* backward: [rows][vocab], may be logits                         */
+  int64_t logits_stride, dlogits_stride; /* of rows                                             */
+  uint32_t rows, vocab;      /* vocab 1 .. 2^31 - 1                                            */
+  uint32_t top;              /* 0 .. G10_LOG_PROBS_TOP, at most vocab                          */
+  float scale;               /* > 0                                                            */
+  int64_t ignore;
+  uint32_t type;             /* of logits and dlogits: G10_F32, G10_F16, G10_BF16              */
+} g10_log_probs_args;
+
+int g10_log_probs_workspace(const g10_log_probs_args *args, uint64_t *bytes);
+int g10_log_probs(const g10_log_probs_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);
+int g10_log_probs_backward(const g10_log_probs_args *args, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------------------- gated MLP
+ * Of tokens x and two weights:   g = x gate,   u = x up,   h = act(g) * u.   act: g / (1 + exp(-g)), or g * Phi(g) with the normal
+ * distribution's Phi.  Backward, from x, the weights and dh alone (g and u are computed again):
+ *   dg = dh u act'(g),   du = dh act(g),   dx = dg gate^T + du up^T,   dgate = x^T dg,   dup = x^T du.
+ * Products of 16-bit factors summed in 32 bits; dg and du are rounded to `type` before their products (the matrix unit takes 16-bit
+ * factors), h and the gradients once at their end. */
+#define G10_ACT_SILU 0u
+#define G10_ACT_GELU 1u
+
+typedef struct {
+  const void *x;             /* [tokens][dim]                                                  */
+  const void *gate, *up;     /* [dim][inner], or with out_in [inner][dim]; of one stride       */
+  void *h;                   /* forward: [tokens][inner]                                       */
+  const void *dh;            /* backward: [tokens][inner]                                      */
+  void *dx;                  /* backward: [tokens][dim]                                        */
+  void *dgate, *dup;         /* backward: laid out as the weights                              */
+  int64_t x_stride, w_stride, h_stride, dh_stride, dx_stride, dw_stride; /* of rows              */
+  uint32_t tokens, dim, inner; /* dim and inner multiples of 8 up to 2^20, tokens below 2^31     */
+  uint32_t act, out_in;
+  uint32_t type;             /* G10_F16 or G10_BF16                                            */
+} g10_gated_args;
+/* Pointers and strides are multiples of 16 bytes (of 8 elements), strides from a row's length to 2^22 elements; else G10_EINVAL. */
+
+int g10_gated_workspace(const g10_gated_args *args, uint64_t *bytes);
+int g10_gated(const g10_gated_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);
+int g10_gated_backward_workspace(const g10_gated_args *args, uint64_t *bytes);
+int g10_gated_backward(const g10_gated_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

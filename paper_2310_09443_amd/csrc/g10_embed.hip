@@ -1,0 +1,385 @@
+// Rows of a table by token, and the table's gradient.
+//
+// Both are bound by memory: the lookup reads a row and writes it; the gradient reads every token's row once and writes every row of the
+// table once.  For the sums the tokens are sorted by id (a stable radix sort of ids and places, so that a row's tokens come in their
+// own order), and the sorted list is cut into pieces of one length: a wavefront takes a piece and 16 bytes a lane of its rows,
+// whatever ids the piece holds.  A run of one id inside a piece is a finished row of the table; where a run goes over the ends of
+// pieces its parts go to memory in 32 bits and are added in order by a second kernel.  So a frequent token is no one's long row,
+// and no sum depends on who comes first.
+#include "g10_internal.h"
+#include "g10_ops.h"
+
+#include <math.h>
+
+struct EmbedArgs {
+  const void *ids, *table, *dout;
+  void *out, *dtable;
+  int64_t ts, os, ds, gs;
+  u32 tokens, vocab, dim, slabs, ids64;
+  float scale;
+  // backward
+  u32 *keys[2], *places[2];        // ids and places of tokens, before and after a pass of the sort
+  u32* counts;                     // [digit][tile]
+  u32 tiles, shift, bits;
+  float* parts;                    // [piece][2][dim]: a run that comes from the piece before, one that goes on
+  u32 pieces, per;                 // pieces of `per` tokens
+  u32 sum_groups;                  // workgroups that sum; the others clear rows without tokens
+};
+
+template <class T, int N> struct Pack { typedef T type __attribute__((ext_vector_type(N))); };
+
+__device__ __forceinline__ int64_t id_at(const EmbedArgs& a, u32 t) {
+  return a.ids64 ? ((const int64_t*)a.ids)[t] : (int64_t)((const int*)a.ids)[t];
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// lookup: a wavefront to a token's slab of 64 N values, four tokens at a time
+// ---------------------------------------------------------------------------------------------------------------------
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
+  typedef typename Pack<T, N>::type V;
+  const u64 tasks = (u64)((a.tokens + 3) / 4) * a.slabs, step = (u64)gridDim.x * 4;
+  for (u64 task = (u64)blockIdx.x * 4 + wave_id(); task < tasks; task += step) {
+    const u32 t0 = (u32)(task / a.slabs) * 4, d = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
+    if (d >= a.dim) continue;
+    V v[4];
+    bool fine[4];
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+      const u32 t = t0 + i < a.tokens ? t0 + i : a.tokens - 1;
+      const int64_t id = id_at(a, t);
+      fine[i] = id >= 0 && id < (int64_t)a.vocab;
+      v[i] = *(const V*)((const T*)a.table + (fine[i] ? id : 0) * a.ts + d);
+    }
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+      if (t0 + i >= a.tokens) break;
+      V w;
+#pragma unroll
+      for (int k = 0; k < N; ++k) w[k] = (T)(fine[i] ? (float)v[i][k] * a.scale : __builtin_nanf(""));
+      __builtin_nontemporal_store(w, (V*)((T*)a.out + (int64_t)(t0 + i) * a.os + d));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// the sort: passes of up to 9 bits, each a count by tile, a running sum over digits and tiles, and the move
+// ---------------------------------------------------------------------------------------------------------------------
+#define EMBED_TILE 1024u
+#define EMBED_DIGITS 512u
+
+// (ids outside the table sort behind all others)
+__device__ __forceinline__ u32 key_at(const EmbedArgs& a, u32 t, bool first, const u32* keys) {
+  if (!first) return keys[t];
+  const int64_t id = id_at(a, t);
+  return id >= 0 && id < (int64_t)a.vocab ? (u32)id : a.vocab;
+}
+
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_embed_count(const EmbedArgs a, const u32* keys) {
+  __shared__ u32 n[EMBED_DIGITS];
+  const u32 digits = 1u << a.bits;
+  for (u32 d = threadIdx.x; d < digits; d += 256) n[d] = 0;
+  __syncthreads();
+#pragma unroll
+  for (u32 i = 0; i < EMBED_TILE / 256; ++i) {
+    const u32 t = blockIdx.x * EMBED_TILE + i * 256 + threadIdx.x;
+    if (t < a.tokens) atomicAdd(&n[(key_at(a, t, FIRST, keys) >> a.shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (u32 d = threadIdx.x; d < digits; d += 256) a.counts[(u64)d * a.tiles + blockIdx.x] = n[d];
+}
+
+// Exclusive sums of n counts, in place: one workgroup, 1024 threads with `each` counts running each.
+__global__ __launch_bounds__(1024) void k_embed_scan(u32* counts, u32 n) {
+  __shared__ u32 sums[16];
+  u32 before = 0;
+  for (u32 base = 0; base < n; base += 4096) {
+    const u32 at = base + threadIdx.x * 4;
+    u32 c[4], sum = 0;
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) { c[i] = at + i < n ? counts[at + i] : 0; sum += c[i]; }
+    const u32 upto = wave_scan_dpp<OpAdd>(sum, 0u);
+    __syncthreads();
+    if (lane_id() == 63) sums[wave_id()] = upto;
+    __syncthreads();
+    u32 here = before + upto - sum, all = 0;
+#pragma unroll
+    for (u32 w = 0; w < 16; ++w) { const u32 s = sums[w]; here += w < wave_id() ? s : 0u; all += s; }
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i) {
+      if (at + i < n) counts[at + i] = here;
+      here += c[i];
+    }
+    before += all;
+  }
+}
+
+// A tile's tokens to their places: a wavefront takes 64 tokens running, four times; the rank of a token among its digit's is that of the
+// rounds and wavefronts before it and of the lanes below it with the same digit (found digit bit by digit bit with ballots).
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_embed_move(const EmbedArgs a, const u32* keys, const u32* places, u32* to_keys, u32* to_places) {
+  __shared__ u32 seen[4][EMBED_DIGITS];
+  const u32 digits = 1u << a.bits, w = wave_id(), l = lane_id();
+  for (u32 d = threadIdx.x; d < 4 * EMBED_DIGITS; d += 256) (&seen[0][0])[d] = 0;
+  __syncthreads();
+  u32 key[4], rank[4];
+  const u32 t0 = blockIdx.x * EMBED_TILE + w * 256 + l;                // a wavefront's 256 tokens lie side by side
+#pragma unroll
+  for (u32 i = 0; i < 4; ++i) {
+    const u32 t = t0 + i * 64;
+    const bool on = t < a.tokens;
+    key[i] = on ? key_at(a, t, FIRST, keys) : 0;
+    const u32 d = (key[i] >> a.shift) & (digits - 1);
+    u64 same = ballot(on);
+    for (u32 b = 0; b < a.bits; ++b) {
+      const bool bit = (d >> b) & 1;
+      const u64 m = ballot(bit);
+      same &= bit ? m : ~m;
+    }
+    const u32 below = (u32)__popcll(same & ((1ull << l) - 1));
+    rank[i] = on ? seen[w][d] + below : 0;
+    __builtin_amdgcn_wave_barrier();                                   // (a wavefront's LDS accesses stay in order: all read before one writes)
+    if (on && below == 0) seen[w][d] += (u32)__popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  for (u32 d = threadIdx.x; d < digits; d += 256) {                    // where each wavefront's tokens of a digit begin
+    u32 at = a.counts[(u64)d * a.tiles + blockIdx.x];
+#pragma unroll
+    for (u32 v = 0; v < 4; ++v) { const u32 n = seen[v][d]; seen[v][d] = at; at += n; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (u32 i = 0; i < 4; ++i) {
+    const u32 t = t0 + i * 64;
+    if (t >= a.tokens) continue;
+    const u32 at = seen[w][(key[i] >> a.shift) & (digits - 1)] + rank[i];
+    if (at >= a.tokens) continue;                                      // (ids that change while they are sorted)
+    to_keys[at] = key[i];
+    to_places[at] = FIRST ? t : places[t];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// the sums
+// ---------------------------------------------------------------------------------------------------------------------
+template <class T, int N>
+__device__ __forceinline__ void write_row(const EmbedArgs& a, u32 v, u32 d, const float (&s)[N]) {
+  typedef typename Pack<T, N>::type V;
+  V w;
+#pragma unroll
+  for (int k = 0; k < N; ++k) w[k] = (T)(s[k] * a.scale);
+  __builtin_nontemporal_store(w, (V*)((T*)a.dtable + (int64_t)v * a.gs + d));
+}
+
+// The first place in the sorted keys whose key is not below v.
+__device__ __forceinline__ u32 first_of(const u32* keys, u32 n, u32 v) {
+  u32 lo = 0, hi = n;
+  while (lo < hi) {
+    const u32 mid = lo + (hi - lo) / 2;
+    if (keys[mid] < v) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+#define EMBED_CLEAR 32u            // rows of the table that a wavefront looks after
+
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32* keys, const u32* places) {
+  typedef typename Pack<T, N>::type V;
+  const u32 l = lane_id();
+  if (blockIdx.x < a.sum_groups) {
+    const u64 tasks = (u64)a.pieces * a.slabs, step = (u64)a.sum_groups * 4;
+    for (u64 task = (u64)blockIdx.x * 4 + uniform(wave_id()); task < tasks; task += step) {
+      const u32 piece = (u32)(task / a.slabs), d = ((u32)(task % a.slabs) * 64 + l) * N;
+      const u32 t0 = piece * a.per, n = a.tokens - t0 < a.per ? a.tokens - t0 : a.per;
+      const bool on = d < a.dim;
+      const T* src = (const T*)a.dout + (on ? d : 0);
+      // ids and places of the piece, a lane each (a piece has 64 tokens at most)
+      const u32 mykey = l < n ? keys[t0 + l] : ~0u, myplace = l < n ? places[t0 + l] : 0;
+      const u32 before = t0 ? keys[t0 - 1] : ~0u, behind = t0 + n < a.tokens ? keys[t0 + n] : ~0u;
+      float s[N] = {};
+      u32 key = (u32)__builtin_amdgcn_readlane((int)mykey, 0);
+      bool from = key == before;                                       // the run comes from the piece before
+      auto flush = [&](bool on_from, bool goes_on) {
+        if (on && key < a.vocab) {
+          if (on_from || goes_on) {
+            float* p = a.parts + ((u64)piece * 2 + (on_from ? 0 : 1)) * a.dim + d;
+#pragma unroll
+            for (int k = 0; k < N; ++k) p[k] = s[k];
+          } else {
+            write_row<T, N>(a, key, d, s);
+          }
+        }
+      };
+      for (u32 i = 0; i < n; i += 8) {
+        V v[8];
+#pragma unroll
+        for (u32 j = 0; j < 8; ++j) {
+          const u32 at = i + j < n ? i + j : n - 1;
+          const u32 place = (u32)__builtin_amdgcn_readlane((int)myplace, (int)at);
+          v[j] = *(const V*)(src + (int64_t)(place < a.tokens ? place : 0) * a.ds);
+        }
+#pragma unroll
+        for (u32 j = 0; j < 8; ++j) {
+          if (i + j >= n) break;
+          const u32 k2 = (u32)__builtin_amdgcn_readlane((int)mykey, (int)(i + j));
+          if (k2 != key) {
+            flush(from, false);
+            key = k2;
+            from = false;
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[k] = 0.0f;
+          }
+#pragma unroll
+          for (int k = 0; k < N; ++k) s[k] += (float)v[j][k];
+        }
+      }
+      flush(from, key == behind);
+    }
+    return;
+  }
+  // rows without a token
+  const float zero[N] = {};
+  const u32 waves = (gridDim.x - a.sum_groups) * 4;
+  const u64 rows = ((u64)a.vocab + EMBED_CLEAR - 1) / EMBED_CLEAR;
+  for (u64 r = (u64)(blockIdx.x - a.sum_groups) * 4 + uniform(wave_id()); r < rows; r += waves) {
+    const u32 v0 = (u32)(r * EMBED_CLEAR), v = v0 + l < a.vocab ? v0 + l : a.vocab;
+    const u32 begin = l <= EMBED_CLEAR ? first_of(keys, a.tokens, v) : 0;
+    const u32 end = (u32)__shfl_down((int)begin, 1, 64);
+    u64 empty = ballot(l < EMBED_CLEAR && v0 + l < a.vocab && begin == end);
+    while (empty) {
+      const u32 i = (u32)__builtin_ctzll(empty);
+      empty &= empty - 1;
+      for (u32 d = l * N; d < a.dim; d += 64 * N) write_row<T, N>(a, v0 + i, d, zero);
+    }
+  }
+}
+
+// Runs over the ends of pieces: the piece in which such a run begins adds its parts.
+template <class T, int N>
+__global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32* keys) {
+  const u64 tasks = (u64)a.pieces * a.slabs, step = (u64)gridDim.x * 4;
+  for (u64 task = (u64)blockIdx.x * 4 + uniform(wave_id()); task < tasks; task += step) {
+    const u32 piece = (u32)(task / a.slabs), d = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
+    const u32 t0 = piece * a.per, t1 = t0 + a.per;
+    if (t1 >= a.tokens) continue;
+    const u32 key = uniform(keys[t1 - 1]);
+    if (key >= a.vocab || uniform(keys[t1]) != key) continue;          // nothing goes on from here
+    if (t0 && uniform(keys[t0 - 1]) == key && uniform(keys[t0]) == key) continue;  // nor begins here
+    // its last piece: the one that holds its last token
+    const u32 last = (uniform(first_of(keys, a.tokens, key + 1)) - 1) / a.per;
+    if (d >= a.dim) continue;
+    const float* p = a.parts + ((u64)piece * 2 + 1) * a.dim + d;
+    float s[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) s[k] = p[k];
+    p += a.dim;                                                        // (the next piece's first part)
+    for (u32 q = piece + 1; q <= last; ++q, p += 2 * a.dim) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) s[k] += p[k];
+    }
+    write_row<T, N>(a, key, d, s);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------------
+struct EmbedPlan { u32 lanes_n, grid, passes, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
+
+static u64 up256(u64 x) { return (x + 255) & ~(u64)255; }
+
+static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPlan& p) {
+  if (!g) return G10_EINVAL;
+  if (g->type > G10_BF16 || g->ids_64 > 1 || !(g->scale == g->scale) || isinf(g->scale)) return G10_EINVAL;
+  if (!g->dim || g->dim > 65536 || !g->vocab || g->vocab >= 0x80000000u || g->tokens >= 0x80000000u) return G10_EINVAL;
+  const u32 e = g->type == G10_F32 ? 4 : 2;
+  const void *src = back ? g->dout : g->table, *dst = back ? g->dtable : g->out;
+  const int64_t ss = back ? g->dout_stride : g->table_stride, sd = back ? g->dtable_stride : g->out_stride;
+  if (!dst && (back || g->tokens)) return G10_EINVAL;
+  if (g->tokens && (!src || !g->ids)) return G10_EINVAL;
+  if ((uintptr_t)src % e || (uintptr_t)dst % e || (uintptr_t)g->ids % (g->ids_64 ? 8 : 4)) return G10_EINVAL;
+  a = EmbedArgs{};
+  a.ids = g->ids; a.table = g->table; a.out = g->out; a.dout = g->dout; a.dtable = g->dtable;
+  a.ts = g->table_stride; a.os = g->out_stride; a.ds = g->dout_stride; a.gs = g->dtable_stride;
+  a.tokens = g->tokens; a.vocab = g->vocab; a.dim = g->dim; a.scale = g->scale; a.ids64 = g->ids_64;
+  const u32 n = 16 / e;
+  const bool wide = g->dim % n == 0 && !(((uintptr_t)src | (uintptr_t)dst) & 15) && ss % (int64_t)n == 0 && sd % (int64_t)n == 0;
+  p = EmbedPlan{};
+  p.lanes_n = wide ? n : 1;
+  a.slabs = (g->dim + 64 * p.lanes_n - 1) / (64 * p.lanes_n);
+  auto groups = [](u64 waves, u32 most) { const u64 n = (waves + 3) / 4; return (u32)(n < most ? n : most); };
+  p.grid = groups((u64)((a.tokens + 3) / 4) * a.slabs, 1u << 16);
+  if (!back) return G10_OK;
+  u32 bits = 1;
+  while (bits < 32 && (g->vocab >> bits)) ++bits;                      // ids and one more, for those outside
+  p.passes = (bits + 8) / 9;
+  a.bits = (bits + p.passes - 1) / p.passes;
+  a.tiles = (a.tokens + EMBED_TILE - 1) / EMBED_TILE;
+  a.per = 64;
+  a.pieces = (a.tokens + a.per - 1) / a.per;
+  a.sum_groups = groups((u64)a.pieces * a.slabs, 1u << 16);
+  p.join_groups = a.sum_groups;
+  p.clear_groups = groups(((u64)a.vocab + EMBED_CLEAR - 1) / EMBED_CLEAR, 1u << 14);
+  u64 at = 0;
+  auto take = [&](u64 bytes) { const u64 here = at; at += up256(bytes); return here; };
+  for (int i = 0; i < 2; ++i) { p.at_keys[i] = take((u64)a.tokens * 4); p.at_places[i] = take((u64)a.tokens * 4); }
+  p.at_counts = take((u64)EMBED_DIGITS * a.tiles * 4);
+  p.at_parts = take((u64)a.pieces * 2 * a.dim * 4);
+  p.bytes = at;
+  return G10_OK;
+}
+
+template <class T, int N>
+static void embed_sums(const EmbedArgs& a, const EmbedPlan& p, int last, hipStream_t s) {
+  k_embed_sum<T, N><<<a.sum_groups + p.clear_groups, 256, 0, s>>>(a, a.keys[last], a.places[last]);
+  if (a.pieces > 1) k_embed_join<T, N><<<p.join_groups, 256, 0, s>>>(a, a.keys[last]);
+}
+
+extern "C" int g10_embed(const g10_embed_args* g, void* hip_stream) {
+  EmbedArgs a; EmbedPlan p;
+  G10_TRY(embed_args(g, false, a, p));
+  if (!a.tokens) return G10_OK;
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (g->type == G10_F32) { if (p.lanes_n > 1) k_embed<float, 4><<<p.grid, 256, 0, s>>>(a); else k_embed<float, 1><<<p.grid, 256, 0, s>>>(a); }
+  else if (g->type == G10_F16) { if (p.lanes_n > 1) k_embed<_Float16, 8><<<p.grid, 256, 0, s>>>(a); else k_embed<_Float16, 1><<<p.grid, 256, 0, s>>>(a); }
+  else { if (p.lanes_n > 1) k_embed<__bf16, 8><<<p.grid, 256, 0, s>>>(a); else k_embed<__bf16, 1><<<p.grid, 256, 0, s>>>(a); }
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}
+
+extern "C" int g10_embed_backward_workspace(const g10_embed_args* g, uint64_t* bytes) {
+  if (!bytes) return G10_EINVAL;
+  EmbedArgs a; EmbedPlan p;
+  G10_TRY(embed_args(g, true, a, p));
+  *bytes = p.bytes;
+  return G10_OK;
+}
+
+extern "C" int g10_embed_backward(const g10_embed_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  EmbedArgs a; EmbedPlan p;
+  G10_TRY(embed_args(g, true, a, p));
+  if (p.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < p.bytes)) return G10_EINVAL;
+  hipStream_t s = (hipStream_t)hip_stream;
+  char* ws = (char*)workspace;
+  for (int i = 0; i < 2; ++i) { a.keys[i] = (u32*)(ws + p.at_keys[i]); a.places[i] = (u32*)(ws + p.at_places[i]); }
+  a.counts = (u32*)(ws + p.at_counts);
+  a.parts = (float*)(ws + p.at_parts);
+  int at = 0;
+  for (u32 pass = 0; a.tokens && pass < p.passes; ++pass) {
+    a.shift = pass * a.bits;
+    const int to = (int)(pass & 1), from = to ^ 1;
+    if (!pass) k_embed_count<true><<<a.tiles, 256, 0, s>>>(a, nullptr); else k_embed_count<false><<<a.tiles, 256, 0, s>>>(a, a.keys[from]);
+    k_embed_scan<<<1, 1024, 0, s>>>(a.counts, (1u << a.bits) * a.tiles);
+    if (!pass) k_embed_move<true><<<a.tiles, 256, 0, s>>>(a, nullptr, nullptr, a.keys[to], a.places[to]);
+    else k_embed_move<false><<<a.tiles, 256, 0, s>>>(a, a.keys[from], a.places[from], a.keys[to], a.places[to]);
+    at = to;
+  }
+  if (g->type == G10_F32) { if (p.lanes_n > 1) embed_sums<float, 4>(a, p, at, s); else embed_sums<float, 1>(a, p, at, s); }
+  else if (g->type == G10_F16) { if (p.lanes_n > 1) embed_sums<_Float16, 8>(a, p, at, s); else embed_sums<_Float16, 1>(a, p, at, s); }
+  else { if (p.lanes_n > 1) embed_sums<__bf16, 8>(a, p, at, s); else embed_sums<__bf16, 1>(a, p, at, s); }
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}

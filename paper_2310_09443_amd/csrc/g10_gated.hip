@@ -1,0 +1,290 @@
+// The first half of a gated MLP: act(x gate) * (x up), and its gradients, as products in tiles (g10_tile.h).
+//
+// Bound by the matrix unit with many tokens, by the weights' bytes with few.  Forward both products are one kernel: a tile's two
+// panels are the same columns of both weights, and the activation and the product are taken from the sums in the registers; neither
+// factor goes to memory.  Backward the same kernel makes g and u again and turns dh into dg and du (rounded to 16 bits: the next products take
+// them so), then one kernel makes dx (its sum goes over gate's columns and on over up's) and one the gradients of both weights.
+// Where the tiles are too few to fill the chip the sum over k is cut into shares: these go to memory in 32 bits, and a second kernel
+// adds them in order and does what the tiles' end would have done.
+#include "g10_tile.h"
+
+enum { END_GATED = 0, END_BACK = 1, END_PLAIN = 2 };
+
+struct GatedArgs {
+  const void *a[2], *b[2];         // the first factor's sources; the second one's (gate and up)
+  void* out[2];                    // h | dg, du | the product (the gradients of both weights: one each)
+  const void* dh;
+  int64_t as, bs, os, dhs;         // strides of rows
+  u32 m, n, k, sources;            // rows, columns (of each of two panels where gated), values of k in a source
+  u32 tiles_m, tiles_n, groups, per;  // groups: products of their own (both weights' gradients) or shares of k; per: steps of a share
+  u32 act, shares;
+  float* part;                     // [share][m][columns]
+};
+
+// h's activation and its slope.
+struct Act { float a, slope; };
+__device__ __forceinline__ Act activation(float g, u32 act, bool slope) {
+  if (act == G10_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + exp2_fast(-g * G10_LOG2E));
+    return {g * s, slope ? s * (1.0f + g * (1.0f - s)) : 0.0f};
+  }
+  const float s = 0.5f * erfcf(-0.70710678118654752f * g);
+  return {g * s, slope ? s + g * 0.3989422804014327f * exp2_fast(-0.5f * G10_LOG2E * g * g) : 0.0f};
+}
+
+// What comes of four neighbouring columns of a row: both panels' sums in g and u (END_PLAIN: g alone), to column c.
+template <class T, int END>
+__device__ __forceinline__ void finish(const GatedArgs& a, u32 which, u32 row, u32 c, const f32x4& g, const f32x4& u) {
+  typedef typename Vec<T>::x4 x4;
+  if (row >= a.m || c >= a.n) return;
+  x4 w0, w1;
+  if constexpr (END == END_GATED) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w0[r] = (T)(activation(g[r], a.act, false).a * u[r]);
+  } else if constexpr (END == END_BACK) {
+    const x4 d = *(const x4*)((const T*)a.dh + (int64_t)row * a.dhs + c);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const Act t = activation(g[r], a.act, true);
+      w0[r] = (T)((float)d[r] * u[r] * t.slope);
+      w1[r] = (T)((float)d[r] * t.a);
+    }
+    *(x4*)((T*)a.out[1] + (int64_t)row * a.os + c) = w1;
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w0[r] = (T)g[r];
+  }
+  *(x4*)((T*)(END == END_PLAIN && which ? a.out[1] : a.out[0]) + (int64_t)row * a.os + c) = w0;
+}
+
+template <class T, int LA, int LB, int WM, int TM, int STAGES, int END>
+__global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, STAGES>::LDS <= 80 * 1024 ? 2 : 1)) void k_gated(const GatedArgs a) {
+  typedef Tile<T, LA, LB, WM, TM, STAGES> Tl;
+  typedef typename Tl::PA PA;
+  typedef typename Tl::PB PB;
+  constexpr bool GATED = END != END_PLAIN;
+  __shared__ __attribute__((aligned(256))) char lds[Tl::LDS];
+  // Workgroups go round the 8 XCDs by their number: each XCD gets a run of tiles, eight tiles of rows side by side, so that the panels that its 32
+  // units read at a time lie in its L2.
+  const u32 tiles = a.tiles_m * a.tiles_n, all = tiles * a.groups, each = (all + 7) / 8;
+  const u32 id = (blockIdx.x % 8) * each + blockIdx.x / 8;
+  if (blockIdx.x / 8 >= each || id >= all) return;
+  const u32 group = id / tiles, t = id % tiles, band = t / (8 * a.tiles_n), high = a.tiles_m - band * 8 < 8 ? a.tiles_m - band * 8 : 8;
+  const u32 in = t - band * 8 * a.tiles_n, m0 = (band * 8 + in % high) * Tl::BM, n0 = in / high * (GATED ? 128 : 256);
+  const u32 which = a.shares > 1 ? 0 : group;                          // (shares of one product, or products)
+  const u32 nk = (a.k + TILE_K - 1) / TILE_K, first = a.shares > 1 ? group * a.per : 0;
+  const u32 last = a.shares > 1 ? (first + a.per < nk * a.sources ? first + a.per : nk * a.sources) : nk * a.sources;
+  PA pa[Tl::APANELS];
+  PB pb[2];
+  u32 am[Tl::APANELS], bn[2];
+#pragma unroll
+  for (int i = 0; i < Tl::APANELS; ++i) {
+    am[i] = m0 + i * 128 < a.m ? m0 + i * 128 : 0;                     // (a panel with nothing in it: the first one, which nobody keeps)
+    pa[i].init(threadIdx.x, a.as, am[i], a.m);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    bn[j] = GATED ? n0 : n0 + j * 128 < a.n ? n0 + j * 128 : 0;
+    pb[j].init(threadIdx.x, a.bs, bn[j], a.n);
+  }
+  // (a sum over two sources takes both factors from the second one there; products of their own differ in one factor)
+  typename Tl::Walk w;
+  u32 src = first >= nk;
+  auto place = [&](typename Tl::Walk& w, u32 step) {
+    const void* pa0 = a.a[a.sources > 1 ? src : which];
+#pragma unroll
+    for (int i = 0; i < Tl::APANELS; ++i) w.a[i] = PA::start(pa0, a.as, am[i], step);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) w.b[j] = PB::start(a.b[GATED ? (u32)j : a.sources > 1 ? src : which], a.bs, bn[j], step);
+    w.left = a.k - step * TILE_K;
+  };
+  place(w, first - src * nk);
+  f32x16 acc[2][TM] = {};
+  Tl::run(acc, lds_addr(lds), (int)(last - first), pa, pb, w, PA::bytes(a.as), PB::bytes(a.bs), a.sources == 1 || a.k % TILE_K == 0, [&](typename Tl::Walk& w) {
+    src = 1;
+    if (a.sources > 1) place(w, 0);
+  });
+  const u32 l = lane_id(), wave = uniform(wave_id()), row0 = m0 + (wave / 4) * 32 * TM + (l & 31), c0 = n0 + (wave % 4) * 32 + 4 * (l >> 5);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const u32 row = row0 + 32 * i;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const u32 c = c0 + 8 * q;
+      f32x4 g, u;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) { g[r] = acc[0][i][4 * q + r]; u[r] = acc[1][i][4 * q + r]; }
+      if (a.shares > 1) {
+        const u64 wide = GATED ? 2ull * a.n : a.n;
+        float* to = a.part + ((u64)group * a.m + row) * wide + c;
+        if (row < a.m && c < a.n) *(f32x4*)to = g;
+        if (row < a.m && (GATED ? c : c + 128) < a.n) *(f32x4*)(to + (GATED ? a.n : 128)) = u;
+      } else {
+        finish<T, END>(a, which, row, c, g, u);
+        if (!GATED) finish<T, END>(a, which, row, c + 128, u, g);
+      }
+    }
+  }
+}
+
+// The shares of four columns added in order.
+template <class T, int END>
+__global__ __launch_bounds__(256) void k_gated_join(const GatedArgs a) {
+  const u64 quads = a.n / 4, all = (u64)a.m * quads, wide = END == END_PLAIN ? a.n : 2ull * a.n;
+  for (u64 e = (u64)blockIdx.x * 256 + threadIdx.x; e < all; e += (u64)gridDim.x * 256) {
+    const u32 row = (u32)(e / quads), c = (u32)(e % quads) * 4;
+    f32x4 g = {}, u = {};
+    const float* p = a.part + (u64)row * wide + c;
+#pragma unroll 4
+    for (u32 s = 0; s < a.shares; ++s, p += (u64)a.m * wide) {
+      g += *(const f32x4*)p;
+      if (END != END_PLAIN) u += *(const f32x4*)(p + a.n);
+    }
+    finish<T, END>(a, 0, row, c, g, u);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------------
+// One product: its tiles and the shares of its sum.
+struct ProductPlan { u32 wm, tm, shares, per, groups; u64 part; };
+
+static u32 ceil_div(u64 a, u64 b) { return (u32)((a + b - 1) / b); }
+
+// products: of their own, side by side; wide: columns of a tile that count (128 where gated)
+static ProductPlan product_plan(u64 m, u64 n, u64 k, u32 sources, u32 products, bool gated, bool across) {
+  ProductPlan p{};
+  const u64 tn = ceil_div(n, gated ? 128 : 256);
+  p.wm = 2; p.tm = 4;
+  if (m <= 32 && !across) { p.wm = 1; p.tm = 1; }
+  else if (ceil_div(m, 256) * tn * products < 192) { p.wm = 1; p.tm = across ? 4 : 2; }
+  const u64 tiles = ceil_div(m, 32 * p.tm * p.wm) * tn * products, steps = (u64)ceil_div(k, TILE_K) * sources;
+  const u64 want = p.tm == 2 ? 512 : 256;
+  p.shares = 1;
+  if (products == 1 && tiles && tiles < want * 2 / 3) {
+    u64 s = want / tiles;
+    if (s > steps / 4) s = steps / 4;
+    if (s > 32) s = 32;
+    p.shares = s ? (u32)s : 1;
+  }
+  p.per = ceil_div(steps, p.shares);
+  p.shares = ceil_div(steps, p.per ? p.per : 1);
+  if (!p.shares) p.shares = 1;
+  p.groups = p.shares > 1 ? p.shares : products;
+  p.part = p.shares > 1 ? (u64)p.shares * m * (gated ? 2 * n : n) * 4 : 0;
+  return p;
+}
+
+template <class T, int LA, int LB, int END>
+static int product(GatedArgs a, const ProductPlan& p, void* part, hipStream_t s) {
+  a.tiles_m = ceil_div(a.m, 32 * p.tm * p.wm);
+  a.tiles_n = ceil_div(a.n, END == END_PLAIN ? 256 : 128);
+  a.groups = p.groups; a.per = p.per; a.shares = p.shares; a.part = (float*)part;
+  const u64 all = (u64)a.tiles_m * a.tiles_n * a.groups;
+  if (all > G10_GROUPS_MOST / 2 - 8) return G10_EINVAL;
+  const u32 grid = ceil_div(all, 8) * 8;
+  if (p.wm == 2) k_gated<T, LA, LB, 2, 4, 2, END><<<grid, 512, 0, s>>>(a);
+  else if constexpr (LA == ACROSS) k_gated<T, LA, LB, 1, 4, 2, END><<<grid, 256, 0, s>>>(a);
+  else if (p.tm == 2) k_gated<T, LA, LB, 1, 2, 2, END><<<grid, 256, 0, s>>>(a);
+  else k_gated<T, LA, LB, 1, 1, 4, END><<<grid, 256, 0, s>>>(a);
+  if (p.shares > 1) {
+    const u64 quads = (u64)a.m * (a.n / 4), groups = (quads + 255) / 256;
+    k_gated_join<T, END><<<(u32)(groups < 65536 ? groups : 65536), 256, 0, s>>>(a);
+  }
+  return G10_OK;
+}
+
+static bool lies_well(const void* p, int64_t stride, u32 row) { return p && !((uintptr_t)p & 15) && stride % 8 == 0 && stride >= (int64_t)row && stride <= (1 << 22); }
+
+static int gated_check(const g10_gated_args* g, bool back) {
+  if (!g || (g->type != G10_F16 && g->type != G10_BF16) || g->act > G10_ACT_GELU || g->out_in > 1) return G10_EINVAL;
+  if (!g->dim || !g->inner || g->dim % 8 || g->inner % 8 || g->dim > 1u << 20 || g->inner > 1u << 20 || g->tokens >= 0x80000000u) return G10_EINVAL;
+  const u32 wrow = g->out_in ? g->dim : g->inner;
+  if (!lies_well(g->gate, g->w_stride, wrow) || !lies_well(g->up, g->w_stride, wrow)) return G10_EINVAL;
+  if (g->tokens && !lies_well(g->x, g->x_stride, g->dim)) return G10_EINVAL;
+  if (!back) return !g->tokens || lies_well(g->h, g->h_stride, g->inner) ? G10_OK : G10_EINVAL;
+  if (g->tokens && (!lies_well(g->dh, g->dh_stride, g->inner) || !lies_well(g->dx, g->dx_stride, g->dim))) return G10_EINVAL;
+  return lies_well(g->dgate, g->dw_stride, wrow) && lies_well(g->dup, g->dw_stride, wrow) ? G10_OK : G10_EINVAL;
+}
+
+extern "C" int g10_gated_workspace(const g10_gated_args* g, uint64_t* bytes) {
+  if (!bytes) return G10_EINVAL;
+  G10_TRY(gated_check(g, false));
+  *bytes = g->tokens ? product_plan(g->tokens, g->inner, g->dim, 1, 1, true, false).part : 0;
+  return G10_OK;
+}
+
+template <class T>
+static int gated_forward(const g10_gated_args* g, void* ws, hipStream_t s) {
+  GatedArgs a{};
+  a.a[0] = a.a[1] = g->x; a.b[0] = g->gate; a.b[1] = g->up; a.out[0] = g->h;
+  a.as = g->x_stride; a.bs = g->w_stride; a.os = g->h_stride;
+  a.m = g->tokens; a.n = g->inner; a.k = g->dim; a.sources = 1; a.act = g->act;
+  const ProductPlan p = product_plan(a.m, a.n, a.k, 1, 1, true, false);
+  return g->out_in ? product<T, ALONG, ALONG, END_GATED>(a, p, ws, s) : product<T, ALONG, ACROSS, END_GATED>(a, p, ws, s);
+}
+
+extern "C" int g10_gated(const g10_gated_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  uint64_t n = 0;
+  G10_TRY(g10_gated_workspace(g, &n));
+  if (n && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < n)) return G10_EINVAL;
+  if (!g->tokens) return G10_OK;
+  G10_TRY((g->type == G10_F16 ? gated_forward<_Float16> : gated_forward<__bf16>)(g, workspace, (hipStream_t)hip_stream));
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}
+
+// Backward: dg and du, and behind them room for the shares of one product at a time.
+struct BackPlan { ProductPlan gated, dx, dw; u64 at_part, bytes; };
+static BackPlan back_plan(const g10_gated_args* g) {
+  BackPlan b{};
+  const u32 wm = g->out_in ? g->inner : g->dim, wn = g->out_in ? g->dim : g->inner;
+  b.gated = product_plan(g->tokens, g->inner, g->dim, 1, 1, true, false);
+  b.dx = product_plan(g->tokens, g->dim, g->inner, 2, 1, false, false);
+  b.dw = product_plan(wm, wn, g->tokens, 1, 2, false, true);
+  u64 part = b.gated.part > b.dx.part ? b.gated.part : b.dx.part;
+  b.at_part = 2 * (((u64)g->tokens * g->inner * 2 + 255) & ~255ull);
+  b.bytes = b.at_part + part;
+  return b;
+}
+
+extern "C" int g10_gated_backward_workspace(const g10_gated_args* g, uint64_t* bytes) {
+  if (!bytes) return G10_EINVAL;
+  G10_TRY(gated_check(g, true));
+  *bytes = back_plan(g).bytes;
+  return G10_OK;
+}
+
+template <class T>
+static int gated_back(const g10_gated_args* g, char* ws, hipStream_t s) {
+  const BackPlan b = back_plan(g);
+  void *dg = ws, *du = ws + b.at_part / 2, *part = ws + b.at_part;
+  if (g->tokens) {
+    GatedArgs a{};
+    a.a[0] = a.a[1] = g->x; a.b[0] = g->gate; a.b[1] = g->up; a.out[0] = dg; a.out[1] = du; a.dh = g->dh;
+    a.as = g->x_stride; a.bs = g->w_stride; a.os = g->inner; a.dhs = g->dh_stride;
+    a.m = g->tokens; a.n = g->inner; a.k = g->dim; a.sources = 1; a.act = g->act;
+    G10_TRY((g->out_in ? product<T, ALONG, ALONG, END_BACK> : product<T, ALONG, ACROSS, END_BACK>)(a, b.gated, part, s));
+    a = GatedArgs{};
+    a.a[0] = dg; a.a[1] = du; a.b[0] = g->gate; a.b[1] = g->up; a.out[0] = g->dx;
+    a.as = g->inner; a.bs = g->w_stride; a.os = g->dx_stride;
+    a.m = g->tokens; a.n = g->dim; a.k = g->inner; a.sources = 2;
+    G10_TRY((g->out_in ? product<T, ALONG, ACROSS, END_PLAIN> : product<T, ALONG, ALONG, END_PLAIN>)(a, b.dx, part, s));
+  }
+  GatedArgs a{};                                                       // (without tokens: zeros)
+  a.out[0] = g->dgate; a.out[1] = g->dup; a.os = g->dw_stride;
+  a.k = g->tokens; a.sources = 1;
+  if (g->out_in) { a.a[0] = dg; a.a[1] = du; a.as = g->inner; a.b[0] = a.b[1] = g->x; a.bs = g->x_stride; a.m = g->inner; a.n = g->dim; }
+  else { a.a[0] = a.a[1] = g->x; a.as = g->x_stride; a.b[0] = dg; a.b[1] = du; a.bs = g->inner; a.m = g->dim; a.n = g->inner; }
+  return product<T, ACROSS, ACROSS, END_PLAIN>(a, b.dw, part, s);
+}
+
+extern "C" int g10_gated_backward(const g10_gated_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  uint64_t n = 0;
+  G10_TRY(g10_gated_backward_workspace(g, &n));
+  if (n && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < n)) return G10_EINVAL;
+  G10_TRY((g->type == G10_F16 ? gated_back<_Float16> : gated_back<__bf16>)(g, (char*)workspace, (hipStream_t)hip_stream));
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}

@@ -1,0 +1,338 @@
+// Norms of rows, centred or not, forward and backward.
+//
+// Bound by memory: forward a value is read and written once, backward it is read with its gradient and written once.  A row lies in the
+// registers of a wavefront (up to 1024 values) or of a workgroup, 8 values to a lane and step, so that the statistics are taken from the
+// values themselves: the mean first, then the squares of what is left (the squares' mean less the mean's square would lose what a
+// large mean leaves over).  Backward the statistics are worked out again from x, which has to be read in any case.  The gradients of
+// weight and bias are sums over rows: a lane keeps its columns' over all rows that its group takes, and the groups' sums are joined in
+// one order and 64 bits by a second kernel.
+#include "g10_internal.h"
+#include "g10_ops.h"
+
+#include <math.h>
+
+struct NormArgs {
+  const void *x, *dy, *w, *b;
+  void *out, *dw, *db;
+  int64_t xs, dys, os;
+  u32 rows, dim, w32, center;
+  float eps;
+  float* partial;                  // backward: [groups][2][dim]
+};
+
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_plus(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x = dpp_plus<0xb1>(x);                                            // lanes 1, 0, 3, 2 of a quad
+  x = dpp_plus<0x4e>(x);                                            // lanes 2, 3, 0, 1
+  x = dpp_plus<0x141>(x);                                           // eight lanes mirrored
+  x = dpp_plus<0x140>(x);                                           // sixteen lanes mirrored
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+// Sums over the W wavefronts of a row, in each lane.  `room`: LDS of the call's own (the next call takes another one, so that one barrier a
+// call is enough).
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&x)[N], float* room) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+  if constexpr (W > 1) {
+    if (lane_id() == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) room[i * W + wave_id()] = x[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = room[i * W];
+#pragma unroll
+      for (int w = 1; w < W; ++w) x[i] += room[i * W + w];
+    }
+  }
+}
+
+template <class T> struct Eight {
+  typedef T x8 __attribute__((ext_vector_type(8)));
+  typedef float f4 __attribute__((ext_vector_type(4)));
+};
+
+// W wavefronts to a row, NV steps of 8 values a lane; a workgroup holds 4 / W rows (W = 1) or one (W = 4, 8, 16).
+// VEC: 16-byte accesses; else value by value, any alignment.
+template <class T, bool VEC>
+__device__ __forceinline__ void get8(const T* p, u32 d, u32 dim, float (&v)[8]) {
+  if constexpr (VEC) {
+    typedef typename Eight<T>::x8 x8;
+    const x8 r = *(const x8*)(p + d);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (float)r[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = d + k < dim ? (float)p[d + k] : 0.0f;
+  }
+}
+template <class T, bool VEC>
+__device__ __forceinline__ void put8(T* p, u32 d, u32 dim, const float (&v)[8]) {
+  if constexpr (VEC) {
+    typedef typename Eight<T>::x8 x8;
+    x8 r;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[k] = (T)v[k];
+    __builtin_nontemporal_store(r, (x8*)(p + d));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (d + k < dim) p[d + k] = (T)v[k];
+  }
+}
+template <class T, bool VEC>
+__device__ __forceinline__ void weights8(const void* w, u32 w32, u32 d, u32 dim, float none, float (&v)[8]) {
+  if (!w) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = none;
+  } else if (w32) {
+    get8<float, VEC>((const float*)w, d, dim, v);
+  } else {
+    get8<T, VEC>((const T*)w, d, dim, v);
+  }
+}
+
+template <class T, int W, int NV, bool VEC, bool BACK>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a) {
+  constexpr u32 ROWS = W == 1 ? 4 : 1, LANES = 64 * W;
+  __shared__ float room[4][2 * W];
+  const u32 l = W == 1 ? lane_id() : threadIdx.x, first = blockIdx.x * ROWS + (W == 1 ? wave_id() : 0), step = gridDim.x * ROWS;
+  const float inv = 1.0f / (float)a.dim;
+  float dw[BACK ? NV : 1][8] = {}, db[BACK ? NV : 1][8] = {};
+  u32 turn = 0;
+  for (u64 row = first; row < a.rows; row += step) {
+    const T* x = (const T*)a.x + (int64_t)row * a.xs;
+    const T* y = BACK ? (const T*)a.dy + (int64_t)row * a.dys : nullptr;
+    T* out = (T*)a.out + (int64_t)row * a.os;
+    float v[NV][8], g[BACK ? NV : 1][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const u32 d = (i * LANES + l) * 8;
+      if (d < a.dim) {
+        get8<T, VEC>(x, d, a.dim, v[i]);
+        if constexpr (BACK) get8<T, VEC>(y, d, a.dim, g[i]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { v[i][k] = 0.0f; if constexpr (BACK) g[i][k] = 0.0f; }
+      }
+    }
+    float mean = 0.0f;
+    if (a.center) {
+      float s[1] = {};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[0] += v[i][k];
+      row_sums<W>(s, room[turn]);
+      turn = (turn + 1) & 3;
+      mean = s[0] * inv;
+    }
+    float s[1] = {};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const u32 d = (i * LANES + l) * 8 + k;
+        v[i][k] = d < a.dim ? v[i][k] - mean : 0.0f;
+        s[0] += v[i][k] * v[i][k];
+      }
+    row_sums<W>(s, room[turn]);
+    turn = (turn + 1) & 3;
+    const float r = 1.0f / sqrtf(s[0] * inv + a.eps);
+    if constexpr (!BACK) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const u32 d = (i * LANES + l) * 8;
+        if (d >= a.dim) continue;
+        float w[8], b[8];
+        weights8<T, VEC>(a.w, a.w32, d, a.dim, 1.0f, w);
+        weights8<T, VEC>(a.b, a.w32, d, a.dim, 0.0f, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * r * w[k] + b[k];
+        put8<T, VEC>(out, d, a.dim, v[i]);
+      }
+    } else {
+      float t[2] = {};                                              // sums of u n and of u
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const u32 d = (i * LANES + l) * 8;
+        if (d >= a.dim) continue;
+        float w[8];
+        weights8<T, VEC>(a.w, a.w32, d, a.dim, 1.0f, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          v[i][k] *= r;
+          dw[i][k] += g[i][k] * v[i][k];
+          db[i][k] += g[i][k];
+          g[i][k] *= w[k];
+          t[0] += g[i][k] * v[i][k];
+          t[1] += g[i][k];
+        }
+      }
+      row_sums<W>(t, room[turn]);
+      turn = (turn + 1) & 3;
+      const float dot = t[0] * inv, off = a.center ? t[1] * inv : 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const u32 d = (i * LANES + l) * 8;
+        if (d >= a.dim) continue;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[i][k] = r * (g[i][k] - v[i][k] * dot - off);
+        put8<T, VEC>(out, d, a.dim, g[i]);
+      }
+    }
+  }
+  if constexpr (BACK) {
+    if (!a.partial) return;
+    float* to = a.partial + (u64)blockIdx.x * 2 * a.dim;
+    if constexpr (W == 1) {                                         // the four wavefronts' sums, step by step
+      __shared__ float sums[2][4][512];
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { sums[0][wave_id()][l * 8 + k] = dw[i][k]; sums[1][wave_id()][l * 8 + k] = db[i][k]; }
+        __syncthreads();
+        for (u32 e = threadIdx.x; e < 1024; e += 256) {
+          const u32 which = e / 512, c = e % 512, d = i * 512 + c;
+          if (d < a.dim) to[which * a.dim + d] = (sums[which][0][c] + sums[which][1][c]) + (sums[which][2][c] + sums[which][3][c]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const u32 d = (i * LANES + l) * 8 + k;
+          if (d < a.dim) { to[d] = dw[i][k]; to[a.dim + d] = db[i][k]; }
+        }
+    }
+  }
+}
+
+// The groups' sums of 16 columns to a workgroup, in one order and 64 bits.
+template <class T>
+__global__ __launch_bounds__(1024) void k_norm_weights(const NormArgs a, u32 groups) {
+  __shared__ double sums[64][17];
+  const u32 e = blockIdx.x * 16 + threadIdx.x % 16, w = threadIdx.x / 16;
+  const u64 all = 2ull * a.dim;
+  double t = 0.0;
+  if (e < all) {
+#pragma unroll 8
+    for (u32 i = w; i < groups; i += 64) t += (double)a.partial[i * all + e];
+  }
+  sums[w][threadIdx.x % 16] = t;
+  __syncthreads();
+  if (w || e >= all) return;
+  for (u32 i = 1; i < 64; ++i) t += sums[i][threadIdx.x];
+  const u32 d = e % a.dim;
+  void* to = e / a.dim ? a.db : a.dw;
+  if (!to) return;
+  if (a.w32) ((float*)to)[d] = (float)t;
+  else ((T*)to)[d] = (T)(float)t;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------------------------
+struct NormPlan { u32 grid, waves, steps; bool vec, weights; };
+
+static int norm_args(const g10_norm_args* g, bool back, NormArgs& a, NormPlan& p) {
+  if (!g) return G10_EINVAL;
+  if (g->type > G10_BF16 || (g->weight_type != g->type && g->weight_type != G10_F32) || g->center > 1) return G10_EINVAL;
+  if (!g->dim || g->dim > 65536 || g->rows >= 0x80000000u || !(g->eps >= 0.0f) || isinf(g->eps)) return G10_EINVAL;
+  const u32 e = g->type == G10_F32 ? 4 : 2, we = g->weight_type == G10_F32 ? 4 : 2, n = 16 / e;
+  if (g->rows && (!g->x || !g->out || (back && !g->dy))) return G10_EINVAL;
+  if (back && g->dweight && !g->weight) return G10_EINVAL;
+  for (const void* q : {g->x, (const void*)g->out, back ? g->dy : nullptr})
+    if ((uintptr_t)q % e) return G10_EINVAL;
+  const void* ws[4] = {g->weight, g->bias, back ? g->dweight : nullptr, back ? g->dbias : nullptr};
+  for (const void* q : ws)
+    if ((uintptr_t)q % we) return G10_EINVAL;
+  a = NormArgs{};
+  a.x = g->x; a.dy = g->dy; a.w = g->weight; a.b = g->bias; a.out = g->out;
+  a.dw = back ? g->dweight : nullptr; a.db = back ? g->dbias : nullptr;
+  a.xs = g->x_stride; a.dys = g->dy_stride; a.os = g->out_stride;
+  a.rows = g->rows; a.dim = g->dim; a.w32 = g->weight_type == G10_F32; a.center = g->center; a.eps = g->eps;
+  p.weights = a.dw || a.db;
+  p.vec = g->dim % 8 == 0 && !(((uintptr_t)g->x | (uintptr_t)g->out | (uintptr_t)g->weight | (uintptr_t)g->bias | (back ? (uintptr_t)g->dy : 0)) & 15) &&
+          g->x_stride % n == 0 && g->out_stride % n == 0 && (!back || g->dy_stride % n == 0);
+  const u32 lanes = (g->dim + 7) / 8;
+  p.waves = lanes <= 128 ? 1 : lanes <= 1024 ? 4 : 16;
+  p.steps = (lanes + 64 * p.waves - 1) / (64 * p.waves);
+  if (p.steps == 3) p.steps = 4;
+  if (p.steps > 4) p.steps = 8;
+  const u32 rows_each = p.waves == 1 ? 4 : 1;
+  const u64 groups = ((u64)a.rows + rows_each - 1) / rows_each;
+  const u32 most = back ? (p.waves == 16 ? 256u : 1024u) : 1u << 16;
+  p.grid = (u32)(groups < most ? groups : most);
+  return G10_OK;
+}
+
+template <class T, bool VEC, bool BACK>
+static void norm_launch(const NormArgs& a, const NormPlan& p, hipStream_t s) {
+  auto go = [&](auto w, auto nv) {
+    constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
+    k_norm<T, W, NV, VEC, BACK><<<p.grid, W == 1 ? 256 : 64 * W, 0, s>>>(a);
+  };
+  using std::integral_constant;
+  auto pick = [&](auto w) {
+    if (p.steps == 1) go(w, integral_constant<int, 1>{});
+    else if (p.steps == 2) go(w, integral_constant<int, 2>{});
+    else if (p.steps == 4) go(w, integral_constant<int, 4>{});
+    else go(w, integral_constant<int, 8>{});
+  };
+  if (p.waves == 1) { if (p.steps == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 1>{}, integral_constant<int, 2>{}); }
+  else if (p.waves == 4) { if (p.steps <= 2) { if (p.steps == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 4>{}, integral_constant<int, 2>{}); } else go(integral_constant<int, 4>{}, integral_constant<int, 4>{}); }
+  else pick(integral_constant<int, 16>{});
+}
+
+template <bool BACK>
+static void norm_typed(const g10_norm_args* g, const NormArgs& a, const NormPlan& p, hipStream_t s) {
+  if (g->type == G10_F32) { if (p.vec) norm_launch<float, true, BACK>(a, p, s); else norm_launch<float, false, BACK>(a, p, s); }
+  else if (g->type == G10_F16) { if (p.vec) norm_launch<_Float16, true, BACK>(a, p, s); else norm_launch<_Float16, false, BACK>(a, p, s); }
+  else { if (p.vec) norm_launch<__bf16, true, BACK>(a, p, s); else norm_launch<__bf16, false, BACK>(a, p, s); }
+}
+
+extern "C" int g10_norm(const g10_norm_args* g, void* hip_stream) {
+  NormArgs a; NormPlan p;
+  G10_TRY(norm_args(g, false, a, p));
+  if (!p.grid) return G10_OK;
+  norm_typed<false>(g, a, p, (hipStream_t)hip_stream);
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}
+
+extern "C" int g10_norm_backward_workspace(const g10_norm_args* g, uint64_t* bytes) {
+  if (!bytes) return G10_EINVAL;
+  NormArgs a; NormPlan p;
+  G10_TRY(norm_args(g, true, a, p));
+  *bytes = p.weights ? (uint64_t)p.grid * 2 * a.dim * 4 : 0;
+  return G10_OK;
+}
+
+extern "C" int g10_norm_backward(const g10_norm_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  NormArgs a; NormPlan p;
+  G10_TRY(norm_args(g, true, a, p));
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (p.weights && p.grid) {
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < (uint64_t)p.grid * 2 * a.dim * 4) return G10_EINVAL;
+    a.partial = (float*)workspace;
+  }
+  if (p.grid) norm_typed<true>(g, a, p, s);
+  if (p.weights) {                                                   // (without rows: zeros)
+    const u32 grid = (2 * a.dim + 15) / 16;
+    if (g->type == G10_F32) k_norm_weights<float><<<grid, 1024, 0, s>>>(a, p.grid);
+    else if (g->type == G10_F16) k_norm_weights<_Float16><<<grid, 1024, 0, s>>>(a, p.grid);
+    else k_norm_weights<__bf16><<<grid, 1024, 0, s>>>(a, p.grid);
+  }
+  G10_HIP(hipGetLastError());
+  return G10_OK;
+}

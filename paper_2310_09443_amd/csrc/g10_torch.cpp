@@ -1,21 +1,7 @@
 // Marshalling between torch tensors and the C ABI of include/g10_ops.h: argument checks (ValueError, before anything is
 // launched), outputs and workspaces from torch's allocator, the current stream of the tensors' device.  Host code only; in C++
 // because a step of small tensors is bound by it: the checks of 300 gradients take Python 150 us and this 10.
-#include <torch/extension.h>
-
-#include <c10/core/DeviceGuard.h>
-#include <c10/hip/HIPGraphsC10Utils.h>
-#include <c10/hip/HIPStream.h>
-
-#include <math.h>
-#include <optional>
-#include <unordered_map>
-#include <vector>
-
-#include "g10_ops.h"
-
-namespace py = pybind11;
-typedef std::optional<at::Tensor> Maybe;
+#include "g10_torch.h"
 
 // The library's calls, from the copy of it that paper_2310_09443_amd.binding has loaded.
 static struct {
@@ -39,29 +25,6 @@ static void bind(const std::vector<uintptr_t>& at) {
   next(lib.norm_rope); next(lib.norm_rope_workspace); next(lib.norm_rope_backward);
   next(lib.attention_workspace); next(lib.attention); next(lib.attention_backward_workspace); next(lib.attention_backward);
   next(lib.adamw_create); next(lib.adamw_step); next(lib.grad_norm); next(lib.adamw_free);
-}
-
-static void check(int rc, const char* what) {
-  if (!rc) return;
-  TORCH_CHECK_VALUE(rc != G10_EINVAL, what, " refuses these sizes or numbers");       // (what the checks here leave to the library's)
-  py::object error = py::module_::import("paper_2310_09443_amd.binding").attr("G10Error");
-  PyErr_SetObject(error.ptr(), error(rc, what).ptr());
-  throw py::error_already_set();
-}
-
-static int type_of(at::ScalarType t) {
-  return t == at::kFloat ? G10_F32 : t == at::kHalf ? G10_F16 : t == at::kBFloat16 ? G10_BF16 : -1;
-}
-
-static void on_device(const at::Tensor& t, const char* name, const at::Device* dev) {
-  TORCH_CHECK_VALUE(t.is_cuda(), name, " must lie in GPU memory");
-  TORCH_CHECK_VALUE(!dev || t.device() == *dev, name, " must lie on the device of the other tensors");
-}
-
-static void* stream_of(const at::Device& dev) { return (void*)c10::hip::getCurrentHIPStream(dev.index()).stream(); }
-
-static at::Tensor room(uint64_t bytes, const at::Device& dev) {
-  return at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(dev));
 }
 
 // ---------------------------------------------------------------------------------------------------- norm and rotation
@@ -491,6 +454,7 @@ class AdamwCore {
 
 PYBIND11_MODULE(_g10_torch, m) {
   m.def("bind", &bind);
+  layer_calls(m);
   m.def("norm_rope", &norm_rope);
   m.def("attention", &attention);
   m.def("attention_backward", &attention_backward);

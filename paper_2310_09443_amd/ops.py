@@ -3,8 +3,12 @@
   norm_rope     norms of queries and keys with the rotation by position, one pass over both
   attention     attention with a sliding window and first tokens that stay visible; scores never leave the chip
   AdamW         one update over all weights at once, moments in 32 or 8 bits, and the norm of all gradients
+  embed         rows of a table by token
+  norm          norms of whole rows, centred or not
+  gated         act(x gate) * (x up), the first half of a gated MLP
+  log_probs     logarithms of given tokens' probabilities, entropy, the likeliest tokens
 
-`norm_rope` and `attention` are differentiable; the g10_* functions beside them are the forward and backward calls
+All but AdamW are differentiable; the g10_* functions beside them are the forward and backward calls
 themselves.  Work is enqueued on the current stream of the tensors' device and not waited for; outputs and workspaces are
 torch's, allocated on that stream.  What the library would refuse raises ValueError, before anything is launched.  The
 marshalling is C++ (csrc/g10_torch.cpp): in Python it would take longer than the kernels of a small step.
@@ -20,9 +24,15 @@ from . import binding
 
 EXPORTS = ["g10_norm_rope", "g10_norm_rope_workspace", "g10_norm_rope_backward", "g10_attention_workspace", "g10_attention",
            "g10_attention_backward_workspace", "g10_attention_backward", "g10_adamw_blocks", "g10_adamw_create", "g10_adamw_step",
-           "g10_grad_norm", "g10_adamw_free"]
+           "g10_grad_norm", "g10_adamw_free",
+           "g10_embed", "g10_embed_backward_workspace", "g10_embed_backward", "g10_norm", "g10_norm_backward_workspace", "g10_norm_backward",
+           "g10_log_probs_workspace", "g10_log_probs", "g10_log_probs_backward", "g10_gated_workspace", "g10_gated",
+           "g10_gated_backward_workspace", "g10_gated_backward"]
+LAYER = EXPORTS.index("g10_embed")               # the operators around attention, from here on
 
 F32, F16, BF16, E4M3 = 0, 1, 2, 3
+SILU, GELU = 0, 1
+LOG_PROBS_TOP = 64
 ADAMW_BLOCK = 256
 _TYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _PTR, _I64, _U32, _U64 = C.c_void_p, C.c_int64, C.c_uint32, C.c_uint64
@@ -61,6 +71,30 @@ class _AdamwParams(C.Structure):
                 ("step", _U64), ("coefficient", _PTR)]
 
 
+class _Embed(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("ids", "table", "out", "dout", "dtable")] + \
+               [(n + "_stride", _I64) for n in ("table", "out", "dout", "dtable")] + \
+               [(n, _U32) for n in ("tokens", "vocab", "dim")] + [("scale", C.c_float), ("type", _U32), ("ids_64", _U32)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("x", "dy", "weight", "bias", "out", "dweight", "dbias")] + \
+               [(n + "_stride", _I64) for n in ("x", "dy", "out")] + \
+               [("rows", _U32), ("dim", _U32), ("eps", C.c_float), ("center", _U32), ("type", _U32), ("weight_type", _U32)]
+
+
+class _LogProbs(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("logits", "tokens", "logp", "lse", "entropy", "top_logp", "top_ids", "dlogp", "dentropy", "dlogits")] + \
+               [("logits_stride", _I64), ("dlogits_stride", _I64), ("rows", _U32), ("vocab", _U32), ("top", _U32), ("scale", C.c_float),
+                ("ignore", _I64), ("type", _U32)]
+
+
+class _Gated(C.Structure):
+    _fields_ = [(n, _PTR) for n in ("x", "gate", "up", "h", "dh", "dx", "dgate", "dup")] + \
+               [(n + "_stride", _I64) for n in ("x", "w", "h", "dh", "dx", "dw")] + \
+               [(n, _U32) for n in ("tokens", "dim", "inner", "act", "out_in", "type")]
+
+
 _ready = _torch = None
 
 
@@ -81,6 +115,12 @@ def _load():
         lib.g10_grad_norm.argtypes = [_PTR, C.POINTER(_PTR), C.c_float, _PTR, _PTR]
         lib.g10_adamw_free.argtypes = [_PTR]
         lib.g10_adamw_free.restype = None
+        for n, args, room in (("g10_embed", _Embed, False), ("g10_embed_backward", _Embed, True), ("g10_norm", _Norm, False), ("g10_norm_backward", _Norm, True),
+                              ("g10_log_probs", _LogProbs, True), ("g10_log_probs_backward", _LogProbs, False), ("g10_gated", _Gated, True),
+                              ("g10_gated_backward", _Gated, True)):
+            getattr(lib, n).argtypes = [C.POINTER(args)] + ([_PTR, _U64] if room else []) + [_PTR]
+            if room:
+                getattr(lib, n + "_workspace").argtypes = [C.POINTER(args), ws]
         _ready = lib
     return _ready
 
@@ -94,7 +134,9 @@ def _calls():
             from . import _g10_torch
         except ImportError as e:
             raise ImportError("paper_2310_09443_amd/_g10_torch.so is missing: run `python -m paper_2310_09443_amd.build`") from e
-        _g10_torch.bind([C.cast(getattr(lib, n), _PTR).value for n in EXPORTS if n != "g10_adamw_blocks"])
+        at = [C.cast(getattr(lib, n), _PTR).value for n in EXPORTS]
+        _g10_torch.bind([x for n, x in zip(EXPORTS[:LAYER], at) if n != "g10_adamw_blocks"])
+        _g10_torch.bind_layer(at[LAYER:])
         _torch = _g10_torch
     return _torch
 
@@ -189,6 +231,132 @@ class _AttentionFn(torch.autograd.Function):
 def attention(q, k, v, causal=True, window=0, sinks=0, scale=None, q_start=None, k_start=None, k_len=None, max_q=None, max_k=None):
     """g10_attention's o, differentiable in q, k and v.  What is kept for the backward pass: q, k, v, o and one number a query and head."""
     return _AttentionFn.apply(q, k, v, q_start, k_start, k_len, dict(causal=causal, window=window, sinks=sinks, scale=scale, max_q=max_q, max_k=max_k))
+
+
+# ----------------------------------------------------------------------------------------------------------- embeddings
+def g10_embed(ids, table, scale=1.0):
+    """scale * table[ids]: ids of any shape (int32 or int64), table [rows, dim]; [*ids.shape, dim].  An id outside the table gives NaN."""
+    return _calls().embed(ids, table, scale)
+
+
+def g10_embed_backward(dout, ids, rows, scale=1.0):
+    """The table's gradient, [rows, dim], from that of g10_embed's output: each row the sum over its tokens, in the same order every time, zeros
+    where there are none.  Ids outside the table have no part in it."""
+    return _calls().embed_backward(dout, ids, rows, scale)
+
+
+class _EmbedFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale):
+        ctx.save_for_backward(ids)
+        ctx.args = table.shape[0], scale
+        return g10_embed(ids, table, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        return g10_embed_backward(dout, ctx.saved_tensors[0], *ctx.args), None, None
+
+
+def embed(ids, table, scale=1.0):
+    """g10_embed, differentiable in the table.  What is kept for the backward pass: the ids."""
+    return _EmbedFn.apply(table, ids, float(scale))
+
+
+# -------------------------------------------------------------------------------------------------------- norms of rows
+def g10_norm(x, weight=None, bias=None, eps=1e-6, center=False):
+    """Rows of x ([..., dim]), less their mean with `center` (layer norm), divided by the root of the mean square of what is left, times the
+    weight, plus the bias ([dim], either may be None; of x's type or both float32)."""
+    return _calls().norm(x, weight, bias, eps, center, False, None)[0]
+
+
+def g10_norm_backward(dy, x, weight=None, bias=None, eps=1e-6, center=False):
+    """Gradients of g10_norm's inputs from that of its output: (dx, dweight, dbias), None where there is none."""
+    return _calls().norm(x, weight, bias, eps, center, True, dy)
+
+
+class _NormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, center):
+        ctx.save_for_backward(x, weight, bias)
+        ctx.args = eps, center
+        return g10_norm(x, weight, bias, eps, center)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        return (*g10_norm_backward(dy, *ctx.saved_tensors, *ctx.args), None, None)
+
+
+def norm(x, weight=None, bias=None, eps=1e-6, center=False):
+    """g10_norm, differentiable in x, weight and bias.  The backward pass works the statistics out again from x: nothing else is kept."""
+    return _NormFn.apply(x, weight, bias, float(eps), bool(center))
+
+
+# ----------------------------------------------------------------------------------------------------------- gated MLP
+def g10_gated(x, gate, up, act="silu"):
+    """act(x gate) * (x up): x [..., dim], gate and up [dim, inner], in float16 or bfloat16; act "silu" or "gelu" (with the error
+    function).  Weights kept as [inner, dim] are given transposed (`w.t()`) and read where they lie.  Sums in 32 bits, one rounding."""
+    return _calls().gated(x, gate, up, act)
+
+
+def g10_gated_backward(dh, x, gate, up, act="silu"):
+    """Gradients (dx, dgate, dup) from that of g10_gated's output; the weights' lie as the weights do.  Both products of the forward pass are
+    made again.  Needs room for the gradients of both products, in x's type."""
+    return _calls().gated_backward(dh, x, gate, up, act)
+
+
+class _GatedFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, up, act):
+        ctx.save_for_backward(x, gate, up)
+        ctx.act = act
+        return g10_gated(x, gate, up, act)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        return (*g10_gated_backward(dh, *ctx.saved_tensors, ctx.act), None)
+
+
+def gated(x, gate, up, act="silu"):
+    """g10_gated, differentiable in x and both weights.  What is kept for the backward pass: x and the weights."""
+    return _GatedFn.apply(x, gate, up, act)
+
+
+# ---------------------------------------------------------------------------------------------------- log probabilities
+def g10_log_probs(logits, tokens=None, entropy=False, top=0, scale=1.0, ignore=-100):
+    """Of softmax(scale * logits) over the last dimension: (logp, lse, entropy, top_logp, top_ids), float32 and ids int64, None where not asked for.
+    logp: the logarithm of the given tokens' probabilities (`tokens` [...], int64 or int32; 0 for a token equal to `ignore`, NaN for another one outside the
+    vocabulary); lse: the logarithm of the sum of exponentials; entropy: in nats; top: that many likeliest tokens (up to 64), [..., top], equal
+    ones in their own order.  Places of -inf have no probability; a row of nothing else has lse = logp = -inf and entropy 0."""
+    return _calls().log_probs(logits, tokens, entropy, top, scale, ignore)
+
+
+def g10_log_probs_backward(dlogp, logits, tokens, lse, dentropy=None, entropy=None, scale=1.0, ignore=-100):
+    """The logits' gradient from those of logp and entropy (either may be None), with g10_log_probs's lse and entropy."""
+    return _calls().log_probs_backward(dlogp, logits, tokens, lse, dentropy, entropy, scale, ignore)
+
+
+class _LogProbsFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, entropy, scale, ignore):
+        logp, lse, ent, _, _ = g10_log_probs(logits, tokens, entropy, 0, scale, ignore)
+        ctx.save_for_backward(logits, tokens, lse, ent)
+        ctx.args = scale, ignore
+        return (logp, ent) if entropy else logp
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogp, dentropy=None):
+        logits, tokens, lse, ent = ctx.saved_tensors
+        return (g10_log_probs_backward(dlogp, logits, tokens, lse, dentropy, ent, *ctx.args), None, None, None, None)
+
+
+def log_probs(logits, tokens, entropy=False, scale=1.0, ignore=-100):
+    """g10_log_probs's logp, or (logp, entropy), differentiable in the logits.  What is kept for the backward pass: the logits and a number or two a
+    row; a loss is `-log_probs(logits, tokens).sum() / n`."""
+    return _LogProbsFn.apply(logits, tokens, bool(entropy), float(scale), int(ignore))
 
 
 # ---------------------------------------------------------------------------------------------------------------- AdamW
