@@ -1,15 +1,15 @@
 // Log probabilities of given tokens, entropy, the likeliest tokens of each row, and the gradient of the logits.
 //
 // Bound by memory: forward a logit is read once, backward read and written once.  A workgroup takes a row in one pass: each thread keeps
-// its own running maximum m, sum s of exp(z - m) and sum t of exp(z - m) (z - m), which are scaled when the maximum moves and joined
-// at the end:  lse = m + log s,  entropy = log s - t / s.  Differences are taken before the product with the scale: z - m is then as
-// exact as the logits.
+// its own running maximum m, sum s of exp(z - m) and sum t of exp(z - m) (z - m), which are scaled when the maximum moves and brought to
+// the row's maximum at the end:  lse = m + log s,  entropy = log s - t / s.
 //
-// The `top` likeliest: beside the sums each thread remembers its own largest logit.  The top-th largest of the 64 that a wavefront's lanes
-// remember is no larger than the row's top-th largest, so the largest such bound of all wavefronts leaves few candidates, and they lie with
-// the threads whose own largest passes it: these read theirs again (from the cache), and a candidate's rank is the number of
-// candidates above it.  Keys are the logit's bits in order with the complement of its place below them: no two are equal, and of equal
-// logits the first comes first.  Where there are more candidates than room, or a NaN, the row is read once for each of the top.
+// The `top` likeliest: beside the sums each thread remembers its own largest logit, and 64 groups of threads theirs.  The top-th largest of the
+// 64 is no larger than the row's top-th largest, and little is above it: 32000 logits and a top of 20 leave some 24 candidates.  They lie
+// with the threads whose own largest passes the bound; these go through theirs again, in registers where the row fits into the
+// workgroup's, and a candidate's rank is the number of candidates above it.  Keys are the logit's bits in order with the complement of its place
+// below them: no two are equal, and of equal logits the first comes first.  Where there are more candidates than room (one thread's logits may all be
+// large), or a NaN, the row is read once for each of the top.
 #include "g10_internal.h"
 #include "g10_ops.h"
 
@@ -46,13 +46,38 @@ __device__ __forceinline__ float out_of_order(u32 k) {
 }
 __device__ __forceinline__ u64 key_of(float x, u32 place) { return ((u64)in_order(x) << 32) | (u32)~place; }
 
-struct Sums { float m, s, t; };
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float scale2) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == LOGP_NEG_INF) return {m, a.s + b.s, a.t + b.t};            // (nothing yet, or NaN)
-  const float da = (a.m - m) * scale2, db = (b.m - m) * scale2;
-  const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-  return {m, a.s * fa + b.s * fb, logp_times(fa, a.t + logp_times(a.s, da)) + logp_times(fb, b.t + logp_times(b.s, db))};
+// z - m is taken as one multiply-add of the logit and m in powers of two, which is rounded: what that leaves over is in every exponential and, with
+// the same m, taken out of lse again.  Far from zero it would be more than an exponential holds: m stays within 1e8 (a rounding of 4), and rows
+// beyond that are summed again with their differences taken first.
+#define LOGP_FAR 1e8f
+__device__ __forceinline__ float in_range(float x) { return fminf(fmaxf(x, -LOGP_FAR), LOGP_FAR); }
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, 0xf, 0xf, false)); }
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, dpp<0xb1>(x));                                         // lanes 1, 0, 3, 2 of a quad
+  x = fmaxf(x, dpp<0x4e>(x));                                         // lanes 2, 3, 0, 1
+  x = fmaxf(x, dpp<0x141>(x));                                        // eight lanes mirrored
+  x = fmaxf(x, dpp<0x140>(x));                                        // sixteen lanes mirrored
+  x = fmaxf(x, __shfl_xor(x, 16, 64));
+  return fmaxf(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float wave_add(float x) {
+  x += dpp<0xb1>(x);
+  x += dpp<0x4e>(x);
+  x += dpp<0x141>(x);
+  x += dpp<0x140>(x);
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+template <int CTRL>
+__device__ __forceinline__ u64 dpp_most(u64 x) {
+  const u64 y = ((u64)(u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(x >> 32), CTRL, 0xf, 0xf, false) << 32) |
+                (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)x, CTRL, 0xf, 0xf, false);
+  return y > x ? y : x;
+}
+__device__ __forceinline__ u64 lane_key(u64 x, u32 lane) {
+  return ((u64)(u32)__builtin_amdgcn_readlane((int)(u32)(x >> 32), (int)lane) << 32) | (u32)__builtin_amdgcn_readlane((int)(u32)x, (int)lane);
 }
 
 // A row in pieces of 16 bytes: values up to the first whole piece, the pieces, and what is left.
@@ -93,126 +118,203 @@ struct Row {
   }
 };
 
-template <class T, int NT, bool TOP>
+// NT threads to a row.  P > 0: its pieces stay in registers, P to a thread; 0: they are read as they are needed.
+enum { LOGP_LSE = 0, LOGP_ENTROPY = 1, LOGP_TOP = 2 };                // each with what the one before gives
+template <class T, int NT, int P, int WHAT>
 __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
-  constexpr u32 W = NT / 64, AHEAD = 4, N = Row<T>::N;
+  constexpr u32 W = NT / 64, AHEAD = P ? P : 4, N = Row<T>::N;
+  constexpr bool TOP = WHAT == LOGP_TOP, ENTROPY = WHAT >= LOGP_ENTROPY;
   typedef typename Row<T>::V V;
-  __shared__ Sums sums[W];
-  __shared__ u64 bounds[W];
-  __shared__ u64 list[TOP ? LOGP_ROOM : 1];
-  __shared__ u32 listed;
+  __shared__ float maxima[W], sums[2][W];
+  __shared__ u64 keys[TOP ? 64 : 1], bounds[TOP ? W : 1], list[TOP ? LOGP_ROOM : 1];
+  __shared__ u32 rank[TOP ? 64 : 1], listed;
   const u32 tid = threadIdx.x;
   for (u64 row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const Row<T> r((const T*)a.logits + (int64_t)row * a.ls, a.vocab);
-    Sums me = {LOGP_NEG_INF, 0.0f, 0.0f};
+    float m = LOGP_NEG_INF, m2 = 0.0f, s = 0.0f, t = 0.0f;            // m2: the maximum in powers of two, rounded once and then used as it is
+    // the thread's largest logit, and where the first piece with it begins
+    const bool has = tid < r.head || tid < r.pieces || (tid < N && r.tail() + tid < r.n);
     float best = LOGP_NEG_INF;
-    u64 mine = 0;                                                     // the largest key
-    auto one = [&](float x, u32 place) {
-      const Sums b = {x, x == x && x != LOGP_NEG_INF ? 1.0f : x != x ? x : 0.0f, 0.0f};
-      me = join(me, b, a.scale2);
+    u32 at = tid < r.head ? tid : tid < r.pieces ? r.place(tid) : r.tail() + tid;
+    auto take = [&](const float* x, u32 n, u32 place) {
+      float top = x[0];
+#pragma unroll
+      for (u32 k = 1; k < n; ++k) top = fmaxf(top, x[k]);
       if (TOP) {
-        const u64 k = key_of(x, place);
-        if (k > mine) { mine = k; best = x; }
+        at = top > best ? place : at;
+        best = fmaxf(best, top);
+      }
+      if (top > m) {
+        const float now = in_range(top * a.scale2), d = m2 - now, f = m == LOGP_NEG_INF ? 1.0f : __builtin_amdgcn_exp2f(d);      // (nothing to scale yet, but a NaN stays)
+        if (ENTROPY) t = logp_times(f, t + logp_times(s, d));         // (d may be -infinity: logits apart by more than 32 bits hold)
+        s *= f;
+        m = top;
+        m2 = now;
+      }
+#pragma unroll
+      for (u32 k = 0; k < n; ++k) {
+        const float d = __builtin_fmaf(x[k], a.scale2, -m2), e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        if (ENTROPY) t += logp_times(e, d);
       }
     };
-    auto take = [&](const V& v, u32 place) {
-      float x[N], top = LOGP_NEG_INF;
+    auto one = [&](float x, u32 place) { take(&x, 1, place); };
+    auto piece = [&](const V& v, u32 place) {
+      float x[N];
 #pragma unroll
-      for (u32 k = 0; k < N; ++k) { x[k] = (float)v[k]; top = fmaxf(top, x[k]); }
-      if (TOP && (top > best || mine == 0)) {
-#pragma unroll
-        for (u32 k = 0; k < N; ++k) {
-          const u64 key = key_of(x[k], place + k);
-          if (key > mine) mine = key;
-        }
-        best = top;
-      }
-      if (top > me.m) {
-        const float d = (me.m - top) * a.scale2, f = __builtin_amdgcn_exp2f(d);
-        me.t = logp_times(f, me.t + logp_times(me.s, d));                // (d may be -infinity: logits apart by more than 32 bits hold)
-        me.s *= f;
-        me.m = top;
-      }
-      const float m = me.m == LOGP_NEG_INF ? 0.0f : me.m;
-#pragma unroll
-      for (u32 k = 0; k < N; ++k) {
-        const float d = (x[k] - m) * a.scale2, e = __builtin_amdgcn_exp2f(d);
-        me.s += e;
-        me.t += logp_times(e, d);
-      }
+      for (u32 k = 0; k < N; ++k) x[k] = (float)v[k];
+      take(x, N, place);
     };
     r.first(tid, one);                                                // (places in their order: of equal logits a thread keeps the first)
-    u32 i = tid;
-    for (; i + (AHEAD - 1) * NT < r.pieces; i += AHEAD * NT) {
-      V v[AHEAD];
+    V held[AHEAD];
+    if constexpr (P > 0) {
+      if (r.pieces) {
 #pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) v[u] = r.piece(i + u * NT);
-#pragma unroll
-      for (u32 u = 0; u < AHEAD; ++u) take(v[u], r.place(i + u * NT));
-    }
-    for (; i < r.pieces; i += NT) take(r.piece(i), r.place(i));
-    r.last(tid, one);
-    // the row's sums
-#pragma unroll
-    for (u32 d = 1; d < 64; d *= 2) {
-      const Sums o = {__shfl_xor(me.m, d, 64), __shfl_xor(me.s, d, 64), __shfl_xor(me.t, d, 64)};
-      me = lane_id() & d ? join(o, me, a.scale2) : join(me, o, a.scale2);
-    }
-    if constexpr (TOP) {
-      // the top-th largest of the wavefront's 64, 0 if there are not so many
-      u32 above = 0;
-#pragma unroll
-      for (u32 j = 0; j < 64; ++j) {
-        const u64 o = ((u64)(u32)__builtin_amdgcn_readlane((int)(u32)(mine >> 32), j) << 32) | (u32)__builtin_amdgcn_readlane((int)(u32)mine, j);
-        above += o > mine;
+        for (u32 u = 0; u < P; ++u) held[u] = r.piece(tid + u * NT < r.pieces ? tid + u * NT : 0);
       }
-      const u64 at = ballot(above == a.top - 1 && mine != 0);
-      const u32 who = at ? (u32)__builtin_ctzll(at) : 0;
-      const u64 key = ((u64)(u32)__builtin_amdgcn_readlane((int)(u32)(mine >> 32), who) << 32) | (u32)__builtin_amdgcn_readlane((int)(u32)mine, who);
-      if (lane_id() == 0) bounds[wave_id()] = at ? key : 0;
+#pragma unroll
+      for (u32 u = 0; u < P; ++u)
+        if (tid + u * NT < r.pieces) piece(held[u], r.place(tid + u * NT));
+    } else {
+      u32 i = tid;
+      for (; i + (AHEAD - 1) * NT < r.pieces; i += AHEAD * NT) {
+#pragma unroll
+        for (u32 u = 0; u < AHEAD; ++u) held[u] = r.piece(i + u * NT);
+#pragma unroll
+        for (u32 u = 0; u < AHEAD; ++u) piece(held[u], r.place(i + u * NT));
+      }
+      for (; i < r.pieces; i += NT) piece(r.piece(i), r.place(i));
+    }
+    r.last(tid, one);
+    // the row's maximum; the largest logits of 64 groups of threads, as keys that are not above those of the logits themselves
+    const float wm = wave_max(m);
+    if (lane_id() == 0) maxima[wave_id()] = wm;
+    if constexpr (TOP) {
+      u64 k = has ? key_of(best, at + (N - 1)) : 0;
+      if (NT >= 128) k = dpp_most<0xb1>(k);
+      if (NT >= 256) k = dpp_most<0x4e>(k);
+      if (NT >= 512) k = dpp_most<0x141>(k);
+      if (NT >= 1024) k = dpp_most<0x140>(k);
+      if (tid % (NT / 64) == 0) keys[tid / (NT / 64)] = k;
+      if (tid < 64) rank[tid] = 0;
       if (tid == 0) listed = 0;
     }
-    if (lane_id() == 0) sums[wave_id()] = me;
     __syncthreads();
-    Sums all = sums[0];
+    float top = maxima[0];
 #pragma unroll
-    for (u32 w = 1; w < W; ++w) all = join(all, sums[w], a.scale2);
-    const bool none = all.m == LOGP_NEG_INF && all.s == 0.0f;
-    const float ls = __log2f(all.s) * LOGP_LN2, lse = none ? LOGP_NEG_INF : all.m * a.scale + ls;
+    for (u32 w = 1; w < W; ++w) top = fmaxf(top, maxima[w]);
+    const float top2 = in_range(top * a.scale2);
+    {
+      const float d = m == LOGP_NEG_INF ? 0.0f : m2 - top2, f = __builtin_amdgcn_exp2f(d);
+      if (ENTROPY) t = logp_times(f, t + logp_times(s, d));
+      s *= f;
+    }
+    s = wave_add(s);
+    if (ENTROPY) t = wave_add(t);
+    if (lane_id() == 0) {
+      sums[0][wave_id()] = s;
+      if (ENTROPY) sums[1][wave_id()] = t;
+    }
+    if constexpr (TOP) {                                              // how many groups' are above each: a share of them to each wavefront
+      const u64 k = keys[lane_id()];
+      u32 above = 0;
+#pragma unroll
+      for (u32 j = 0; j < 64 / W; ++j) above += lane_key(k, wave_id() * (64 / W) + j) > k;
+      if (above) atomicAdd(&rank[lane_id()], above);
+    }
+    __syncthreads();
+    s = sums[0][0];
+    t = ENTROPY ? sums[1][0] : 0.0f;
+#pragma unroll
+    for (u32 w = 1; w < W; ++w) {
+      s += sums[0][w];
+      if (ENTROPY) t += sums[1][w];
+    }
+    const bool none = top == LOGP_NEG_INF && s == 0.0f;
+    const bool far = fabsf(top2) >= LOGP_FAR && top != LOGP_NEG_INF;  // (a row masked with the type's lowest value, say)
+    if (far) {
+      s = t = 0.0f;
+      r.template each<NT>(tid, [&](float x, u32) {
+        const float d = (x - top) * a.scale2, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        if (ENTROPY) t += logp_times(e, d);
+      });
+      s = wave_add(s);
+      if (ENTROPY) t = wave_add(t);
+      __syncthreads();
+      if (lane_id() == 0) {
+        sums[0][wave_id()] = s;
+        if (ENTROPY) sums[1][wave_id()] = t;
+      }
+      __syncthreads();
+      s = t = 0.0f;
+      for (u32 w = 0; w < W; ++w) {
+        s += sums[0][w];
+        if (ENTROPY) t += sums[1][w];
+      }
+    }
+    const float ls = __log2f(s), lse = none ? LOGP_NEG_INF : far ? __builtin_fmaf(top, a.scale, ls * LOGP_LN2) : (top2 + ls) * LOGP_LN2;
     if (tid == 0) {
       a.lse[row] = lse;
-      if (a.entropy) a.entropy[row] = none ? 0.0f : ls - all.t / all.s * LOGP_LN2;
+      if (ENTROPY && a.entropy) a.entropy[row] = none ? 0.0f : (ls - t / s) * LOGP_LN2;
       if (a.tokens) {
-        const int64_t t = ((const int64_t*)a.tokens)[row];
+        const int64_t token = ((const int64_t*)a.tokens)[row];
         float lp = __builtin_nanf("");
-        if (t == a.ignore) lp = 0.0f;
-        else if (t >= 0 && t < (int64_t)a.vocab) lp = none ? LOGP_NEG_INF : (float)r.p[t] * a.scale - lse;
+        if (token == a.ignore) lp = 0.0f;
+        else if (token >= 0 && token < (int64_t)a.vocab) lp = none ? LOGP_NEG_INF : __builtin_fmaf((float)r.p[token], a.scale, -lse);
         a.logp[row] = lp;
       }
     }
     if constexpr (TOP) {
-      u64 least = bounds[0];
+      // the top-th largest of the groups' keys (0: there are not so many); above it lie at least as many of the row's
+      const u64 k = keys[lane_id()], is = ballot(rank[lane_id()] == a.top - 1 && k != 0);
+      const u64 least = is ? lane_key(k, (u32)__builtin_ctzll(is)) : 0;
+      const float low = least ? out_of_order((u32)(least >> 32)) : LOGP_NEG_INF;
+      auto list_it = [&](float x, u32 place) {
+        const u64 key = key_of(x, place);
+        if (key >= least) {
+          const u32 to = atomicAdd(&listed, 1u);
+          if (to < LOGP_ROOM) list[to] = key;
+        }
+      };
+      if (has && key_of(best, at) >= least) {
+        r.first(tid, list_it);
+        r.last(tid, list_it);
+        auto some = [&](const V& v, u32 place) {
+          float x[N], most = LOGP_NEG_INF;
 #pragma unroll
-      for (u32 w = 1; w < W; ++w) least = bounds[w] > least ? bounds[w] : least;
-      if (mine >= least && mine) {
-        r.template each<NT>(tid, [&](float x, u32 place) {
-          const u64 key = key_of(x, place);
-          if (key >= least) {
-            const u32 at = atomicAdd(&listed, 1u);
-            if (at < LOGP_ROOM) list[at] = key;
+          for (u32 k = 0; k < N; ++k) { x[k] = (float)v[k]; most = fmaxf(most, x[k]); }
+          if (most >= low) {
+#pragma unroll
+            for (u32 k = 0; k < N; ++k) list_it(x[k], place + k);
           }
-        });
+        };
+        if constexpr (P > 0) {
+#pragma unroll
+          for (u32 u = 0; u < P; ++u)
+            if (tid + u * NT < r.pieces) some(held[u], r.place(tid + u * NT));
+        } else {
+          u32 i = tid;
+          for (; i + (AHEAD - 1) * NT < r.pieces; i += AHEAD * NT) {
+#pragma unroll
+            for (u32 u = 0; u < AHEAD; ++u) held[u] = r.piece(i + u * NT);
+#pragma unroll
+            for (u32 u = 0; u < AHEAD; ++u) some(held[u], r.place(i + u * NT));
+          }
+          for (; i < r.pieces; i += NT) some(r.piece(i), r.place(i));
+        }
       }
       __syncthreads();
       const u32 n = listed;
       auto put = [&](u32 rank, u64 key) {
         a.top_ids[row * a.top + rank] = (int64_t)(u32)~(u32)key;
-        a.top_logp[row * a.top + rank] = none ? LOGP_NEG_INF : key >> 32 == LOGP_NAN ? __builtin_nanf("") : out_of_order((u32)(key >> 32)) * a.scale - lse;
+        a.top_logp[row * a.top + rank] = none ? LOGP_NEG_INF : key >> 32 == LOGP_NAN ? __builtin_nanf("") : __builtin_fmaf(out_of_order((u32)(key >> 32)), a.scale, -lse);
       };
-      if (n <= LOGP_ROOM && all.s == all.s) {
+      if (n <= LOGP_ROOM && s == s) {
         for (u32 c = tid; c < n; c += NT) {
           const u64 key = list[c];
           u32 above = 0;
+#pragma unroll 8
           for (u32 j = 0; j < n; ++j) above += list[j] > key;
           if (above < a.top) put(above, key);
         }
@@ -318,14 +420,28 @@ static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
   return G10_OK;
 }
 
+// Few rows take 1024 threads each, which for a row's top keep it in registers (8 rows of 32000 with a top of 20: 8.6 us; read a second time where
+// needed, 21).  Many rows take 256 and read again the eighth or so of a row in which candidates lie: more workgroups to a unit are worth
+// more than the registers (1500 rows of 30522 in 32 bits, a top of 5: 43 us, in registers of 512 threads 56).  Rows of up to 512 pieces take a
+// wavefront.
+template <class T, int WHAT>
+static void logp_rows(const LogpArgs& a, hipStream_t s) {
+  const u32 grid = a.rows < 1u << 16 ? a.rows : 1u << 16, pieces = a.vocab / (16 / (u32)sizeof(T));
+  if (a.rows <= 512 && pieces > 512) {
+    if (WHAT == LOGP_TOP && pieces <= 4096) k_logp<T, 1024, WHAT == LOGP_TOP ? 4 : 0, WHAT><<<grid, 1024, 0, s>>>(a);
+    else if (WHAT == LOGP_TOP && pieces <= 16384) k_logp<T, 1024, WHAT == LOGP_TOP ? 16 : 0, WHAT><<<grid, 1024, 0, s>>>(a);
+    else k_logp<T, 1024, 0, WHAT><<<grid, 1024, 0, s>>>(a);
+  } else if (pieces > 512) {
+    k_logp<T, 256, 0, WHAT><<<grid, 256, 0, s>>>(a);
+  } else {
+    k_logp<T, 64, 0, WHAT><<<grid, 64, 0, s>>>(a);
+  }
+}
 template <class T>
 static void logp_launch(const LogpArgs& a, hipStream_t s) {
-  const u32 grid = a.rows < 1u << 16 ? a.rows : 1u << 16;
-  if (a.rows <= 512 && a.vocab > 4096) {
-    if (a.top) k_logp<T, 1024, true><<<grid, 1024, 0, s>>>(a); else k_logp<T, 1024, false><<<grid, 1024, 0, s>>>(a);
-  } else {
-    if (a.top) k_logp<T, 256, true><<<grid, 256, 0, s>>>(a); else k_logp<T, 256, false><<<grid, 256, 0, s>>>(a);
-  }
+  if (a.top) logp_rows<T, LOGP_TOP>(a, s);
+  else if (a.entropy) logp_rows<T, LOGP_ENTROPY>(a, s);
+  else logp_rows<T, LOGP_LSE>(a, s);
 }
 
 extern "C" int g10_log_probs_workspace(const g10_log_probs_args* g, uint64_t* bytes) {
