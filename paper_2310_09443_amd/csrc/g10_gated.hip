@@ -32,29 +32,42 @@ __device__ __forceinline__ Act activation(float g, u32 act, bool slope) {
   return {g * s, slope ? s + g * 0.3989422804014327f * exp2_fast(-0.5f * G10_LOG2E * g * g) : 0.0f};
 }
 
-// What comes of four neighbouring columns of a row: both panels' sums in g and u (END_PLAIN: g alone), to column c.
-template <class T, int END>
-__device__ __forceinline__ void finish(const GatedArgs& a, u32 which, u32 row, u32 c, const f32x4& g, const f32x4& u) {
-  typedef typename Vec<T>::x4 x4;
-  if (row >= a.m || c >= a.n) return;
-  x4 w0, w1;
-  if constexpr (END == END_GATED) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) w0[r] = (T)(activation(g[r], a.act, false).a * u[r]);
-  } else if constexpr (END == END_BACK) {
-    const x4 d = *(const x4*)((const T*)a.dh + (int64_t)row * a.dhs + c);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const Act t = activation(g[r], a.act, true);
-      w0[r] = (T)((float)d[r] * u[r] * t.slope);
-      w1[r] = (T)((float)d[r] * t.a);
-    }
-    *(x4*)((T*)a.out[1] + (int64_t)row * a.os + c) = w1;
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) w0[r] = (T)g[r];
+// What comes of N neighbouring columns of a row: both panels' sums in g and u (END_PLAIN: g alone), to column c.  d: dh there.
+template <class T, int END, int N>
+struct Ends {
+  typedef T V __attribute__((ext_vector_type(N)));
+  static __device__ __forceinline__ V dh_at(const GatedArgs& a, u32 row, u32 c) {
+    const bool in = row < a.m && c < a.n;
+    return *(const V*)((const T*)a.dh + (in ? (int64_t)row * a.dhs + c : 0));
   }
-  *(x4*)((T*)(END == END_PLAIN && which ? a.out[1] : a.out[0]) + (int64_t)row * a.os + c) = w0;
+  static __device__ __forceinline__ void put(const GatedArgs& a, u32 which, u32 row, u32 c, const float (&g)[N], const float (&u)[N], const V& d) {
+    if (row >= a.m || c >= a.n) return;
+    V w0, w1;
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      if constexpr (END == END_GATED) {
+        w0[r] = (T)(activation(g[r], a.act, false).a * u[r]);
+      } else if constexpr (END == END_BACK) {
+        const Act t = activation(g[r], a.act, true);
+        w0[r] = (T)((float)d[r] * u[r] * t.slope);
+        w1[r] = (T)((float)d[r] * t.a);
+      } else {
+        w0[r] = (T)g[r];
+      }
+    }
+    *(V*)((T*)(END == END_PLAIN && which ? a.out[1] : a.out[0]) + (int64_t)row * a.os + c) = w0;
+    if constexpr (END == END_BACK) *(V*)((T*)a.out[1] + (int64_t)row * a.os + c) = w1;
+  }
+};
+// A result's registers 8 q .. 8 q + 7 hold a row's columns 16 q + 4 h .. + 3 and 16 q + 8 + 4 h .. + 3 in the halves h of a wavefront; exchanged, eight
+// neighbouring ones from 16 q + 8 h on.
+__device__ __forceinline__ void neighbours(const f32x16& x, int q, float (&y)[8]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const u32x2 s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[8 * q + r]), __float_as_uint(x[8 * q + 4 + r]), false, false);
+    y[r] = __uint_as_float(s[0]);
+    y[4 + r] = __uint_as_float(s[1]);
+  }
 }
 
 template <class T, int LA, int LB, int WM, int TM, int STAGES, int END>
@@ -99,29 +112,43 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, STAGE
     w.left = a.k - step * TILE_K;
   };
   place(w, first - src * nk);
+  const u32 l = lane_id(), wave = uniform(wave_id()), row0 = m0 + (wave / 4) * 32 * TM + (l & 31), c0 = n0 + (wave % 4) * 32 + 8 * (l >> 5);
+  typedef Ends<T, END, 8> E;
+  // (dh is on its way while the tile's first panels are: at the end its latency would be all there is to do)
+  typename E::V dh[END == END_BACK ? TM : 1][2];
+  if constexpr (END == END_BACK) {
+    if (a.shares == 1) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) dh[i][q] = E::dh_at(a, row0 + 32 * i, c0 + 16 * q);
+    }
+  }
   f32x16 acc[2][TM] = {};
   Tl::run(acc, lds_addr(lds), (int)(last - first), pa, pb, w, PA::bytes(a.as), PB::bytes(a.bs), a.sources == 1 || a.k % TILE_K == 0, [&](typename Tl::Walk& w) {
     src = 1;
     if (a.sources > 1) place(w, 0);
   });
-  const u32 l = lane_id(), wave = uniform(wave_id()), row0 = m0 + (wave / 4) * 32 * TM + (l & 31), c0 = n0 + (wave % 4) * 32 + 4 * (l >> 5);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const u32 row = row0 + 32 * i;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const u32 c = c0 + 8 * q;
-      f32x4 g, u;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) { g[r] = acc[0][i][4 * q + r]; u[r] = acc[1][i][4 * q + r]; }
+    for (int q = 0; q < 2; ++q) {
+      const u32 c = c0 + 16 * q;
+      float g[8], u[8];
+      neighbours(acc[0][i], q, g);
+      neighbours(acc[1][i], q, u);
       if (a.shares > 1) {
         const u64 wide = GATED ? 2ull * a.n : a.n;
         float* to = a.part + ((u64)group * a.m + row) * wide + c;
-        if (row < a.m && c < a.n) *(f32x4*)to = g;
-        if (row < a.m && (GATED ? c : c + 128) < a.n) *(f32x4*)(to + (GATED ? a.n : 128)) = u;
+#pragma unroll
+        for (int r = 0; r < 8; r += 4) {
+          if (row < a.m && c < a.n) *(f32x4*)(to + r) = f32x4{g[r], g[r + 1], g[r + 2], g[r + 3]};
+          if (row < a.m && (GATED ? c : c + 128) < a.n) *(f32x4*)(to + (GATED ? a.n : 128) + r) = f32x4{u[r], u[r + 1], u[r + 2], u[r + 3]};
+        }
       } else {
-        finish<T, END>(a, which, row, c, g, u);
-        if (!GATED) finish<T, END>(a, which, row, c + 128, u, g);
+        E::put(a, which, row, c, g, u, dh[END == END_BACK ? i : 0][q]);
+        if (!GATED) E::put(a, which, row, c + 128, u, g, dh[0][q]);
       }
     }
   }
@@ -140,7 +167,11 @@ __global__ __launch_bounds__(256) void k_gated_join(const GatedArgs a) {
       g += *(const f32x4*)p;
       if (END != END_PLAIN) u += *(const f32x4*)(p + a.n);
     }
-    finish<T, END>(a, 0, row, c, g, u);
+    typedef Ends<T, END, 4> E;
+    typename E::V d = {};
+    if constexpr (END == END_BACK) d = E::dh_at(a, row, c);
+    const float gs[4] = {g[0], g[1], g[2], g[3]}, us[4] = {u[0], u[1], u[2], u[3]};
+    E::put(a, 0, row, c, gs, us, d);
   }
 }
 
