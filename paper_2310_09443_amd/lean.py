@@ -2,11 +2,13 @@
 
     python -m paper_2310_09443_amd.lean              # trains a small decoder, lets it continue a text, plans its big sister's step
 
-`Decoder` is the decoder of the benchmark's fourth workload in small: norms of queries and keys with the rotation in one pass,
-attention with a window and sinks, weights in bfloat16 beside 32-bit masters, one AdamW a layer with its moments in 8 bits.
+`Decoder` is the decoder of the benchmark's fourth workload in small: embeddings, norms of rows, norms of queries and keys with the
+rotation in one pass, attention with a window and sinks, a gated MLP whose inner products are made again on the way back, log
+probabilities, weights in bfloat16 beside 32-bit masters, one AdamW a layer with its moments in 8 bits.
 (One a layer and not one for all: a launch needs what it works on in GPU memory at once, and what no launch needs the planner
-may move.)  `decoder48_lean` is that workload's trace with these operators in the place of the ones that keep scores and 32-bit
-moments; planning both says what they save.
+may move.)  `decoder48_lean` is that workload's trace with attention, rotation and AdamW in the place of the ones that keep scores
+and 32-bit moments, and with `layer=True` with the norms and the gated MLP that keep their inputs alone; planning them says what they
+save.
 """
 from __future__ import annotations
 
@@ -48,29 +50,24 @@ class Decoder:
             self.opts.append(ops.AdamW(masters, lr=lr, weight_decay=0.0, state_bits=state_bits, copies=[c.detach() for c in copies]))
         self.table = ops.rope_table(max_len, D, device=device)
 
-    def _norm(self, x, w):
-        f = x.float()
-        return (f * self.torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype) * w
-
     def _qkv(self, w, x):
-        qkv = (self._norm(x, w["norm1"]) @ w["wqkv"]).unflatten(-1, (-1, self.HEAD))
+        qkv = (self.ops.norm(x, w["norm1"]) @ w["wqkv"]).unflatten(-1, (-1, self.HEAD))
         return qkv[:, :, :self.heads], qkv[:, :, self.heads:self.heads + self.kv], qkv[:, :, self.heads + self.kv:]
 
     def _mlp(self, w, x):
-        n = self._norm(x, w["norm2"])
-        return x + (self.torch.nn.functional.silu(n @ w["gate"]) * (n @ w["up"])) @ w["down"]
+        return x + self.ops.gated(self.ops.norm(x, w["norm2"]), w["gate"], w["up"]) @ w["down"]
 
     def logits(self, ids):
         """[batch, token] -> [batch, token, vocab], differentiable."""
         torch, ops, top = self.torch, self.ops, self.layers[0]
         pos = torch.arange(ids.shape[1], device=self.device, dtype=torch.int32).expand(ids.shape)
-        x = top["embed"][ids]
+        x = ops.embed(ids, top["embed"])
         for w in self.layers[1:]:
             q, k, v = self._qkv(w, x)
             q, k = ops.norm_rope(q, k, self.table, pos, w["q_norm"], w["k_norm"])
             o = ops.attention(q, k, v, window=self.window, sinks=self.sinks)
             x = self._mlp(w, x + o.flatten(2) @ w["wo"])
-        return self._norm(x, top["out_norm"]) @ top["head"]
+        return ops.norm(x, top["out_norm"]) @ top["head"]
 
     def step(self, ids, max_norm=1.0):
         """One training step on [batch, token + 1]; returns (loss, norm of the gradients), device tensors."""
@@ -78,7 +75,7 @@ class Decoder:
         for w in self.layers:
             for t in w.values():
                 t.grad = None
-        loss = torch.nn.functional.cross_entropy(self.logits(ids[:, :-1]).float().flatten(0, 1), ids[:, 1:].flatten())
+        loss = -self.ops.log_probs(self.logits(ids[:, :-1]), ids[:, 1:]).mean()
         loss.backward()
         grads = [[t.grad for t in w.values()] for w in self.layers]
         norm = torch.stack([o.grad_norm(g) for o, g in zip(self.opts, grads)]).square().sum().sqrt()
@@ -99,7 +96,7 @@ class Decoder:
                 m = new.shape[1]
                 pos = torch.arange(at, at + m, device=self.device, dtype=torch.int32).expand(b, m)
                 k_len = torch.full((b,), at + m, dtype=torch.int32, device=self.device)
-                x = top["embed"][new]
+                x = ops.embed(new, top["embed"])
                 for w, (ck, cv) in zip(self.layers[1:], caches):
                     q, k, v = self._qkv(w, x)
                     q, k = ops.g10_norm_rope(q, k, self.table, pos, w["q_norm"], w["k_norm"])
@@ -107,7 +104,7 @@ class Decoder:
                     o, _ = ops.g10_attention(q, ck, cv, window=self.window, sinks=self.sinks, k_len=k_len)
                     x = self._mlp(w, x + o.flatten(2) @ w["wo"])
                 at += m
-                new = (self._norm(x[:, -1:], top["out_norm"]) @ top["head"]).argmax(-1)
+                new = ops.g10_log_probs(ops.norm(x[:, -1:], top["out_norm"]) @ top["head"], top=1)[4][..., 0]
                 ids = torch.cat([ids, new], 1)
         return ids
 
@@ -122,15 +119,38 @@ ROPE_US, ROPE_BACK_US, ATTENTION_US, ATTENTION_BACK_US = 210, 327, 677, 2470
 ADAMW_BYTES, ADAMW_BPUS = 16 + 16 / 256, 5.2e6
 
 
-def decoder48_lean(seed: int = 0x67100004) -> traces.Workload:
+class _Graph(traces._Graph):
+    """A graph in which a gated MLP's first half is one operator that keeps its input."""
+
+    def gated(self, x, weights, out):
+        self.op([x], weights, [out], saved=[x])
+        self.fwd[-1]["inner_bytes"] = self.sizes[out]
+
+    def backward(self, split_weight_grads=True):
+        recs = self.fwd
+        for rec in reversed(recs):
+            if "inner_bytes" not in rec:
+                self.fwd = [rec]
+                super().backward(split_weight_grads)
+                continue
+            self.phase = "bwd"
+            (x,), ws, (out,) = rec["ins"], rec["ws"], rec["outs"]
+            inner = [self.tensor(rec["inner_bytes"]) for _ in ws]            # gradients of both products
+            self.kernel([self.grad_of(out), x] + ws + inner)
+            self.kernel(inner + ws + [self.grad_of(x)])
+            self.kernel(inner + [x] + [self.grad_of(w) for w in ws])
+
+
+def decoder48_lean(seed: int = 0x67100004, layer: bool = False) -> traces.Workload:
     """The 48-layer decoder of `traces.decoder48` (same sizes, same weights) with the operators of `ops`: per layer one kernel for the
     norms and the rotation, one for attention (kept for its backward pass: q, k, v, the output and one number a query and head), and
     one AdamW that reads masters, gradients and 8-bit moments and writes the working copies.  The durations of the operators are
-    those measured on an MI355X at these sizes; the others are drawn as there."""
+    those measured on an MI355X at these sizes; the others are drawn as there.  `layer`: norms of rows and the gated MLP's first half are
+    operators that keep their input alone, the MLP's two inner products and their activation one kernel (durations drawn, as those of all products)."""
     Bt, S, H, NH, L, FF, V = 16, 2048, 4096, 32, 48, 16384, 32000
     esz, wsz = 2, 2
     rows = Bt * S
-    g = traces._Graph(tmp_seed=seed, fwd_tmps=2, bwd_tmps=2, opt_tmps=2)
+    g = _Graph(tmp_seed=seed, fwd_tmps=2, bwd_tmps=2, opt_tmps=2)
     us, back_us = {}, {}                      # an operator's kernel -> its duration; the gradient that its backward kernel begins with -> that one's
     ids = g.tensor(rows * 8)
     emb = g.weight(V * H * wsz)
@@ -138,9 +158,16 @@ def decoder48_lean(seed: int = 0x67100004) -> traces.Workload:
     x = g.tensor(rows * H * esz)
     g.op([], [emb], [x], extra=[ids])
     rope = g.tensor(S * (H // NH) * 4, True)
+
+    def norm(x):
+        if not layer:
+            return traces._norm(g, x, H, rows, esz, wsz, affine_bias=False)
+        w, y = g.weight(H * wsz), g.tensor(rows * H * esz)
+        g.op([x], [w], [y])
+        return y
     for _ in range(L):
         first = len(g.weights)
-        h = traces._norm(g, x, H, rows, esz, wsz, affine_bias=False)
+        h = norm(x)
         wq, wk, wv = (g.weight(H * H * wsz) for _ in range(3))
         q, k, v = (g.tensor(rows * H * esz) for _ in range(3))
         for w, o in ((wq, q), (wk, k), (wv, v)):
@@ -159,20 +186,24 @@ def decoder48_lean(seed: int = 0x67100004) -> traces.Workload:
         g.op([ctx], [wo], [o], ws_bytes=32 << 20)
         x1 = g.tensor(rows * H * esz)
         g.op([o, x], [], [x1], saved=[])
-        h2 = traces._norm(g, x1, H, rows, esz, wsz, affine_bias=False)
+        h2 = norm(x1)
         wg, wu, wd = g.weight(H * FF * wsz), g.weight(H * FF * wsz), g.weight(FF * H * wsz)
-        gt, up = g.tensor(rows * FF * esz), g.tensor(rows * FF * esz)
-        g.op([h2], [wg], [gt], ws_bytes=32 << 20)
-        g.op([h2], [wu], [up], ws_bytes=32 << 20)
-        act = g.tensor(rows * FF * esz)
-        g.op([gt, up], [], [act])
+        if layer:
+            act = g.tensor(rows * FF * esz)
+            g.gated(h2, [wg, wu], act)
+        else:
+            gt, up = g.tensor(rows * FF * esz), g.tensor(rows * FF * esz)
+            g.op([h2], [wg], [gt], ws_bytes=32 << 20)
+            g.op([h2], [wu], [up], ws_bytes=32 << 20)
+            act = g.tensor(rows * FF * esz)
+            g.op([gt, up], [], [act])
         dn = g.tensor(rows * H * esz)
         g.op([act], [wd], [dn], ws_bytes=32 << 20)
         x = g.tensor(rows * H * esz)
         g.op([dn, x1], [], [x], saved=[])
         layer_weights.append(g.weights[first:])
     first = len(g.weights)
-    hN = traces._norm(g, x, H, rows, esz, wsz, affine_bias=False)
+    hN = norm(x)
     lm = g.weight(H * V * wsz)
     logits = g.tensor(rows * V * esz)
     g.op([hN], [lm], [logits], ws_bytes=32 << 20)
@@ -196,15 +227,15 @@ def decoder48_lean(seed: int = 0x67100004) -> traces.Workload:
     dur = traces.rand_lognormal_ns(seed, 1, len(g.kernels), 200_000.0, 1.2)
     for i, d in us.items():
         dur[i] = d * 1000
-    return traces.Workload(g.finish("decoder48_lean", np.asarray(dur)), cap_frac=0.30, meta=dict(batch=Bt, seq=S, hidden=H, layers=L))
+    return traces.Workload(g.finish("decoder48_layer" if layer else "decoder48_lean", np.asarray(dur)), cap_frac=0.30, meta=dict(batch=Bt, seq=S, hidden=H, layers=L))
 
 
-def compare_plans(gpu_bytes=288 * 10**9, host_bytes=512 << 30):
-    """Both traces planned for one machine: [(name, peak bytes, peak bytes that the plan leaves, migrations,
+def compare_plans(gpu_bytes=288 * 10**9, host_bytes=512 << 30, layer=False):
+    """Both traces, with `layer` all three, planned for one machine: [(name, peak bytes, peak bytes that the plan leaves, migrations,
     bytes moved out and in, iteration ns, stall ns)]."""
     from . import binding
     out = []
-    for w in (traces.decoder48(), decoder48_lean()):
+    for w in [traces.decoder48(), decoder48_lean()] + ([decoder48_lean(layer=True)] if layer else []):
         h = binding.g10_vitality(binding.DeviceTrace(w.trace))
         r = h.plan(gpu_bytes, host_bytes, w.bw_out_Bpus, w.bw_in_Bpus)
         h.prefetch()
@@ -227,7 +258,7 @@ def main():
     print("continues", int((got[:, 40:] == text[:, 40:60]).sum()), "of", got[:, 40:].numel(), "tokens as it learnt them")
     model.close()
     print("on 288 GB:")
-    for name, peak, left, n, moved, it, stall in compare_plans():
+    for name, peak, left, n, moved, it, stall in compare_plans(layer=True):
         print(f"  {name}: {peak / 2**30:.0f} GiB at its peak, {left / 2**30:.0f} after {n} migrations of {moved / 2**30:.0f} GiB; "
               f"a step of {it / 1e9:.2f} s, {stall / 1e9:.2f} s of it waiting")
 
