@@ -19,8 +19,8 @@ struct EmbedArgs {
   float scale;
   // backward
   u32 *keys[2], *places[2];        // ids and places of tokens, before and after a pass of the sort
-  u32* counts;                     // [digit][tile]
-  u32 tiles, shift, bits;
+  u32* counts;                     // [tile][digit]
+  u32 tiles, tile, bits, passes;   // tiles of `tile` tokens; bits to a pass
   float* parts;                    // [piece][2][dim]: a run that comes from the piece before, one that goes on
   u32 pieces, per;                 // pieces of `per` tokens
   u32 sum_groups;                  // workgroups that sum; the others clear rows without tokens
@@ -63,9 +63,13 @@ __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// the sort: passes of up to 9 bits, each a count by tile, a running sum over digits and tiles, and the move
+// the sort: passes of up to 9 bits, stable, each a count by tile and the move.  Where a tile's digits begin each workgroup works out itself from
+// all tiles' counts, of which there are 128 at most: launches that do little wait for one another (32768 tokens, two passes: with running
+// sums in launches of their own 31 us, so 21.  Counted for the next pass by the move before it, with atomics in memory: 27, they meet at the
+// frequent ids.  All in one workgroup: 85, its unit's accesses to scattered places take as long).
 // ---------------------------------------------------------------------------------------------------------------------
-#define EMBED_TILE 1024u
+#define EMBED_ROUND 1024u          // tokens of a tile that a workgroup takes at a time
+#define EMBED_TILES 128u
 #define EMBED_DIGITS 512u
 
 // (ids outside the table sort behind all others)
@@ -76,88 +80,100 @@ __device__ __forceinline__ u32 key_at(const EmbedArgs& a, u32 t, bool first, con
 }
 
 template <bool FIRST>
-__global__ __launch_bounds__(256) void k_embed_count(const EmbedArgs a, const u32* keys) {
+__global__ __launch_bounds__(256) void k_embed_count(const EmbedArgs a, u32 pass, const u32* keys) {
   __shared__ u32 n[EMBED_DIGITS];
   const u32 digits = 1u << a.bits;
   for (u32 d = threadIdx.x; d < digits; d += 256) n[d] = 0;
   __syncthreads();
-#pragma unroll
-  for (u32 i = 0; i < EMBED_TILE / 256; ++i) {
-    const u32 t = blockIdx.x * EMBED_TILE + i * 256 + threadIdx.x;
-    if (t < a.tokens) atomicAdd(&n[(key_at(a, t, FIRST, keys) >> a.shift) & (digits - 1)], 1u);
-  }
+  const u64 t0 = (u64)blockIdx.x * a.tile, t1 = t0 + a.tile < a.tokens ? t0 + a.tile : a.tokens;
+#pragma unroll 4
+  for (u64 t = t0 + threadIdx.x; t < t1; t += 256) atomicAdd(&n[(key_at(a, (u32)t, FIRST, keys) >> (pass * a.bits)) & (digits - 1)], 1u);
   __syncthreads();
-  for (u32 d = threadIdx.x; d < digits; d += 256) a.counts[(u64)d * a.tiles + blockIdx.x] = n[d];
+  for (u32 d = threadIdx.x; d < digits; d += 256) a.counts[(u64)blockIdx.x * digits + d] = n[d];
 }
 
-// Exclusive sums of n counts, in place: one workgroup, 1024 threads with `each` counts running each.
-__global__ __launch_bounds__(1024) void k_embed_scan(u32* counts, u32 n) {
-  __shared__ u32 sums[16];
-  u32 before = 0;
-  for (u32 base = 0; base < n; base += 4096) {
-    const u32 at = base + threadIdx.x * 4;
-    u32 c[4], sum = 0;
+// The lanes that are on and whose lower `bits` bits are this lane's.
+__device__ __forceinline__ u64 same_digit(bool on, u32 key, u32 bits) {
+  const u64 all = ballot(on);
+  u32 lo = (u32)all, hi = (u32)(all >> 32);
+  for (u32 b = 0; b < bits; ++b) {
+    const u32 mine = (u32)((int)(key << (31 - b)) >> 31);              // all ones where the bit is set
+    const u64 m = ballot((int)mine < 0);
+    lo &= ~((u32)m ^ mine);
+    hi &= ~((u32)(m >> 32) ^ mine);
+  }
+  return ((u64)hi << 32) | lo;
+}
+
+// A wavefront takes 64 tokens running, four times a round; the rank of a token among its digit's is that of the rounds and wavefronts before it and
+// of the lanes below it with the same digit.
+template <bool FIRST>
+__global__ __launch_bounds__(256) void k_embed_move(const EmbedArgs a, u32 pass, const u32* keys, const u32* places, u32* to_keys, u32* to_places) {
+  __shared__ u32 seen[4][EMBED_DIGITS], begin[EMBED_DIGITS], sums[4];
+  const u32 digits = 1u << a.bits, shift = pass * a.bits, w = wave_id(), l = lane_id();
+  const u32* counts = a.counts;
+  // where the tile's tokens of each digit begin: behind all of lower digits, and those of earlier tiles.  Two digits to a thread, side by side
+  u32 before[2] = {}, all[2] = {};
+  const u32 d0 = threadIdx.x * 2;
+  if (d0 < digits) {
+#pragma unroll 8
+    for (u32 t = 0; t < a.tiles; ++t) {
+      const uint2 c = *(const uint2*)(counts + (u64)t * digits + d0);
+      all[0] += c.x; all[1] += c.y;
+      before[0] += t < blockIdx.x ? c.x : 0u; before[1] += t < blockIdx.x ? c.y : 0u;
+    }
+  }
+  const u32 upto = wave_scan_dpp<OpAdd>(all[0] + all[1], 0u);
+  if (l == 63) sums[w] = upto;
+  __syncthreads();
+  if (d0 < digits) {
+    u32 at = upto - all[0] - all[1];
 #pragma unroll
-    for (u32 i = 0; i < 4; ++i) { c[i] = at + i < n ? counts[at + i] : 0; sum += c[i]; }
-    const u32 upto = wave_scan_dpp<OpAdd>(sum, 0u);
-    __syncthreads();
-    if (lane_id() == 63) sums[wave_id()] = upto;
-    __syncthreads();
-    u32 here = before + upto - sum, all = 0;
-#pragma unroll
-    for (u32 w = 0; w < 16; ++w) { const u32 s = sums[w]; here += w < wave_id() ? s : 0u; all += s; }
+    for (u32 v = 0; v < 4; ++v) at += v < w ? sums[v] : 0u;
+    begin[d0] = at + before[0];
+    begin[d0 + 1] = at + all[0] + before[1];
+  }
+  const u64 end = (u64)blockIdx.x * a.tile + a.tile < a.tokens ? (u64)blockIdx.x * a.tile + a.tile : a.tokens;
+  for (u64 round = (u64)blockIdx.x * a.tile; round < end; round += EMBED_ROUND) {
+    u32 key[4], rank[4], from[4];
+    const u64 t0 = round + w * 256 + l;                                // a wavefront's 256 tokens lie side by side
 #pragma unroll
     for (u32 i = 0; i < 4; ++i) {
-      if (at + i < n) counts[at + i] = here;
-      here += c[i];
+      const u64 t = t0 + i * 64;
+      const u32 r = (u32)(t < end ? t : end - 1);
+      key[i] = key_at(a, r, FIRST, keys);
+      from[i] = FIRST ? r : places[r];
     }
-    before += all;
-  }
-}
-
-// A tile's tokens to their places: a wavefront takes 64 tokens running, four times; the rank of a token among its digit's is that of the
-// rounds and wavefronts before it and of the lanes below it with the same digit (found digit bit by digit bit with ballots).
-template <bool FIRST>
-__global__ __launch_bounds__(256) void k_embed_move(const EmbedArgs a, const u32* keys, const u32* places, u32* to_keys, u32* to_places) {
-  __shared__ u32 seen[4][EMBED_DIGITS];
-  const u32 digits = 1u << a.bits, w = wave_id(), l = lane_id();
-  for (u32 d = threadIdx.x; d < 4 * EMBED_DIGITS; d += 256) (&seen[0][0])[d] = 0;
-  __syncthreads();
-  u32 key[4], rank[4];
-  const u32 t0 = blockIdx.x * EMBED_TILE + w * 256 + l;                // a wavefront's 256 tokens lie side by side
+    for (u32 d = threadIdx.x; d < 4 * EMBED_DIGITS; d += 256) (&seen[0][0])[d] = 0;
+    __syncthreads();
 #pragma unroll
-  for (u32 i = 0; i < 4; ++i) {
-    const u32 t = t0 + i * 64;
-    const bool on = t < a.tokens;
-    key[i] = on ? key_at(a, t, FIRST, keys) : 0;
-    const u32 d = (key[i] >> a.shift) & (digits - 1);
-    u64 same = ballot(on);
-    for (u32 b = 0; b < a.bits; ++b) {
-      const bool bit = (d >> b) & 1;
-      const u64 m = ballot(bit);
-      same &= bit ? m : ~m;
+    for (u32 i = 0; i < 4; ++i) {
+      const bool on = t0 + i * 64 < end;
+      const u32 d = (key[i] >> shift) & (digits - 1);
+      const u64 same = same_digit(on, key[i] >> shift, a.bits);
+      const u32 below = (u32)__popcll(same & ((1ull << l) - 1)), before = seen[w][d];
+      rank[i] = before + below;
+      __builtin_amdgcn_wave_barrier();                                 // (a wavefront's LDS accesses stay in order: all read before one writes)
+      if (on && !below) seen[w][d] = before + (u32)__popcll(same);
+      __builtin_amdgcn_wave_barrier();
     }
-    const u32 below = (u32)__popcll(same & ((1ull << l) - 1));
-    rank[i] = on ? seen[w][d] + below : 0;
-    __builtin_amdgcn_wave_barrier();                                   // (a wavefront's LDS accesses stay in order: all read before one writes)
-    if (on && below == 0) seen[w][d] += (u32)__popcll(same);
-    __builtin_amdgcn_wave_barrier();
-  }
-  __syncthreads();
-  for (u32 d = threadIdx.x; d < digits; d += 256) {                    // where each wavefront's tokens of a digit begin
-    u32 at = a.counts[(u64)d * a.tiles + blockIdx.x];
+    __syncthreads();
+    for (u32 d = threadIdx.x; d < digits; d += 256) {                  // where each wavefront's tokens of a digit begin
+      u32 at = begin[d];
 #pragma unroll
-    for (u32 v = 0; v < 4; ++v) { const u32 n = seen[v][d]; seen[v][d] = at; at += n; }
-  }
-  __syncthreads();
+      for (u32 v = 0; v < 4; ++v) { const u32 n = seen[v][d]; seen[v][d] = at; at += n; }
+      begin[d] = at;
+    }
+    __syncthreads();
 #pragma unroll
-  for (u32 i = 0; i < 4; ++i) {
-    const u32 t = t0 + i * 64;
-    if (t >= a.tokens) continue;
-    const u32 at = seen[w][(key[i] >> a.shift) & (digits - 1)] + rank[i];
-    if (at >= a.tokens) continue;                                      // (ids that change while they are sorted)
-    to_keys[at] = key[i];
-    to_places[at] = FIRST ? t : places[t];
+    for (u32 i = 0; i < 4; ++i) {
+      if (t0 + i * 64 >= end) continue;
+      const u32 at = seen[w][(key[i] >> shift) & (digits - 1)] + rank[i];
+      if (at >= a.tokens) continue;                                    // (ids that change while they are sorted)
+      to_keys[at] = key[i];
+      to_places[at] = from[i];
+    }
+    __syncthreads();
   }
 }
 
@@ -265,20 +281,35 @@ __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32
     const u32 piece = (u32)(task / a.slabs), d = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
     const u32 t0 = piece * a.per, t1 = t0 + a.per;
     if (t1 >= a.tokens) continue;
-    const u32 key = uniform(keys[t1 - 1]);
-    if (key >= a.vocab || uniform(keys[t1]) != key) continue;          // nothing goes on from here
-    if (t0 && uniform(keys[t0 - 1]) == key && uniform(keys[t0]) == key) continue;  // nor begins here
-    // its last piece: the one that holds its last token
-    const u32 last = (uniform(first_of(keys, a.tokens, key + 1)) - 1) / a.per;
+    // lane j looks at the first token of the j-th piece behind this one
+    const u64 next = (u64)t1 + (u64)lane_id() * a.per;
+    const u32 key = uniform(keys[t1 - 1]), before = t0 ? uniform(keys[t0 - 1]) : ~0u, theirs = next < a.tokens ? keys[next] : ~0u;
+    u64 on = ballot(theirs == key);
+    if (key >= a.vocab || before == key || !(on & 1)) continue;        // nothing begins here that goes on
+    u32 more = on == ~0ull ? 64u : (u32)__builtin_ctzll(~on);          // pieces that the run goes into
+    while (more % 64 == 0 && on == ~0ull) {
+      const u64 far = (u64)t1 + ((u64)more + lane_id()) * a.per;
+      on = ballot(far < a.tokens && keys[far < a.tokens ? far : 0] == key);
+      more += on == ~0ull ? 64u : (u32)__builtin_ctzll(~on);
+    }
     if (d >= a.dim) continue;
     const float* p = a.parts + ((u64)piece * 2 + 1) * a.dim + d;
     float s[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] = p[k];
     p += a.dim;                                                        // (the next piece's first part)
-    for (u32 q = piece + 1; q <= last; ++q, p += 2 * a.dim) {
+    for (u32 q = 0; q < more; q += 8) {                                // (past the last one it is read again, and not added)
+      float v[8][N];
 #pragma unroll
-      for (int k = 0; k < N; ++k) s[k] += p[k];
+      for (u32 u = 0; u < 8; ++u) {
+        const float* o = p + (u64)(q + u < more ? q + u : more - 1) * 2 * a.dim;
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[u][k] = o[k];
+      }
+#pragma unroll
+      for (u32 u = 0; u < 8; ++u)
+#pragma unroll
+        for (int k = 0; k < N; ++k) s[k] += q + u < more ? v[u][k] : 0.0f;
     }
     write_row<T, N>(a, key, d, s);
   }
@@ -287,7 +318,7 @@ __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-struct EmbedPlan { u32 lanes_n, grid, passes, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
+struct EmbedPlan { u32 lanes_n, grid, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
 
 static u64 up256(u64 x) { return (x + 255) & ~(u64)255; }
 
@@ -315,9 +346,11 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   if (!back) return G10_OK;
   u32 bits = 1;
   while (bits < 32 && (g->vocab >> bits)) ++bits;                      // ids and one more, for those outside
-  p.passes = (bits + 8) / 9;
-  a.bits = (bits + p.passes - 1) / p.passes;
-  a.tiles = (a.tokens + EMBED_TILE - 1) / EMBED_TILE;
+  a.passes = (bits + 8) / 9;
+  a.bits = (bits + a.passes - 1) / a.passes;
+  const u32 rounds = (a.tokens + EMBED_ROUND - 1) / EMBED_ROUND;
+  a.tile = (rounds + EMBED_TILES - 1) / EMBED_TILES * EMBED_ROUND;
+  a.tiles = a.tokens ? (a.tokens + a.tile - 1) / a.tile : 0;
   a.per = 64;
   a.pieces = (a.tokens + a.per - 1) / a.per;
   a.sum_groups = groups((u64)a.pieces * a.slabs, 1u << 16);
@@ -326,7 +359,7 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   u64 at = 0;
   auto take = [&](u64 bytes) { const u64 here = at; at += up256(bytes); return here; };
   for (int i = 0; i < 2; ++i) { p.at_keys[i] = take((u64)a.tokens * 4); p.at_places[i] = take((u64)a.tokens * 4); }
-  p.at_counts = take((u64)EMBED_DIGITS * a.tiles * 4);
+  p.at_counts = take(((u64)a.tiles << a.bits) * 4);
   p.at_parts = take((u64)a.pieces * 2 * a.dim * 4);
   p.bytes = at;
   return G10_OK;
@@ -368,13 +401,15 @@ extern "C" int g10_embed_backward(const g10_embed_args* g, void* workspace, uint
   a.counts = (u32*)(ws + p.at_counts);
   a.parts = (float*)(ws + p.at_parts);
   int at = 0;
-  for (u32 pass = 0; a.tokens && pass < p.passes; ++pass) {
-    a.shift = pass * a.bits;
+  for (u32 pass = 0; a.tokens && pass < a.passes; ++pass) {
     const int to = (int)(pass & 1), from = to ^ 1;
-    if (!pass) k_embed_count<true><<<a.tiles, 256, 0, s>>>(a, nullptr); else k_embed_count<false><<<a.tiles, 256, 0, s>>>(a, a.keys[from]);
-    k_embed_scan<<<1, 1024, 0, s>>>(a.counts, (1u << a.bits) * a.tiles);
-    if (!pass) k_embed_move<true><<<a.tiles, 256, 0, s>>>(a, nullptr, nullptr, a.keys[to], a.places[to]);
-    else k_embed_move<false><<<a.tiles, 256, 0, s>>>(a, a.keys[from], a.places[from], a.keys[to], a.places[to]);
+    if (!pass) {
+      k_embed_count<true><<<a.tiles, 256, 0, s>>>(a, pass, nullptr);
+      k_embed_move<true><<<a.tiles, 256, 0, s>>>(a, pass, nullptr, nullptr, a.keys[to], a.places[to]);
+    } else {
+      k_embed_count<false><<<a.tiles, 256, 0, s>>>(a, pass, a.keys[from]);
+      k_embed_move<false><<<a.tiles, 256, 0, s>>>(a, pass, a.keys[from], a.places[from], a.keys[to], a.places[to]);
+    }
     at = to;
   }
   if (g->type == G10_F32) { if (p.lanes_n > 1) embed_sums<float, 4>(a, p, at, s); else embed_sums<float, 1>(a, p, at, s); }

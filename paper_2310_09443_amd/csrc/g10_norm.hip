@@ -107,20 +107,45 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
   const float inv = 1.0f / (float)a.dim;
   float dw[BACK ? NV : 1][8] = {}, db[BACK ? NV : 1][8] = {};
   u32 turn = 0;
+  // backward with a few steps a row, the next row is on its way while this one is worked on
+  constexpr bool AHEAD = BACK && VEC && NV <= 2;
+  typedef typename Eight<T>::x8 x8;
+  x8 nx[AHEAD ? NV : 1], ny[AHEAD ? NV : 1];
+  auto fetch = [&](u64 row) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const u32 d = (i * LANES + l) * 8, at = d < a.dim ? d : 0;
+      nx[AHEAD ? i : 0] = *(const x8*)((const T*)a.x + (int64_t)row * a.xs + at);
+      ny[AHEAD ? i : 0] = *(const x8*)((const T*)a.dy + (int64_t)row * a.dys + at);
+    }
+  };
+  if constexpr (AHEAD) {
+    if (first < a.rows) fetch(first);
+  }
   for (u64 row = first; row < a.rows; row += step) {
     const T* x = (const T*)a.x + (int64_t)row * a.xs;
     const T* y = BACK ? (const T*)a.dy + (int64_t)row * a.dys : nullptr;
     T* out = (T*)a.out + (int64_t)row * a.os;
     float v[NV][8], g[BACK ? NV : 1][8];
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const u32 d = (i * LANES + l) * 8;
-      if (d < a.dim) {
-        get8<T, VEC>(x, d, a.dim, v[i]);
-        if constexpr (BACK) get8<T, VEC>(y, d, a.dim, g[i]);
-      } else {
+      for (int i = 0; i < NV; ++i) {
+        const bool in = (i * LANES + l) * 8 < a.dim;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { v[i][k] = 0.0f; if constexpr (BACK) g[i][k] = 0.0f; }
+        for (int k = 0; k < 8; ++k) { v[i][k] = in ? (float)nx[i][k] : 0.0f; g[i][k] = in ? (float)ny[i][k] : 0.0f; }
+      }
+      fetch(row + step < a.rows ? row + step : row);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const u32 d = (i * LANES + l) * 8;
+        if (d < a.dim) {
+          get8<T, VEC>(x, d, a.dim, v[i]);
+          if constexpr (BACK) get8<T, VEC>(y, d, a.dim, g[i]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) { v[i][k] = 0.0f; if constexpr (BACK) g[i][k] = 0.0f; }
+        }
       }
     }
     float mean = 0.0f;

@@ -98,3 +98,19 @@ def test_refusals(ops):
                        (lambda: ops.g10_embed_backward(torch.zeros(6, 65537, device="cuda"), ids, 5), "65536")):
         with pytest.raises(ValueError, match=match):
             bad()
+
+
+@pytest.mark.parametrize("tokens", [1023, 1024, 1025, 131072, 131073, 300000])
+def test_sorts(ops, tokens):
+    """Tiles of the sort of one round and of several, with ids of two and three digits."""
+    for vocab in (300, 300000):
+        check(ops, *make(tokens, vocab, 8, torch.float32, seed=vocab, frequent=vocab == 300))
+
+
+def test_a_run_over_many_pieces(ops):
+    """More than 64 pieces of one id, and such a run right behind another one."""
+    ids, table, dout = make(20000, 50, 72, torch.bfloat16)
+    ids[:] = 7
+    ids[::3] = 6
+    ids[:200] = 49
+    check(ops, ids, table, dout)
