@@ -16,9 +16,10 @@ struct GatedArgs {
   const void* dh;
   int64_t as, bs, os, dhs;         // strides of rows
   u32 m, n, k, sources;            // rows, columns (of each of two panels where gated), values of k in a source
-  u32 tiles_m, tiles_n, groups, per;  // groups: products of their own (both weights' gradients) or shares of k; per: steps of a share
-  u32 act, shares;
-  float* part;                     // [share][m][columns]
+  u32 tiles_m, tiles_n;
+  u32 products, shares, per;       // products of their own (both weights' gradients); shares of the sum over k, of `per` steps
+  u32 act;
+  float* part;                     // [product][share][m][columns]
 };
 
 // h's activation and its slope.
@@ -70,23 +71,22 @@ __device__ __forceinline__ void neighbours(const f32x16& x, int q, float (&y)[8]
   }
 }
 
-template <class T, int LA, int LB, int WM, int TM, int STAGES, int END>
-__global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, STAGES>::LDS <= 80 * 1024 ? 2 : 1)) void k_gated(const GatedArgs a) {
-  typedef Tile<T, LA, LB, WM, TM, STAGES> Tl;
+template <class T, int LA, int LB, int WM, int TM, int KS, int STAGES, int END>
+__global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, KS, STAGES>::LDS <= 80 * 1024 ? 2 : 1)) void k_gated(const GatedArgs a) {
+  typedef Tile<T, LA, LB, WM, TM, KS, STAGES> Tl;
   typedef typename Tl::PA PA;
   typedef typename Tl::PB PB;
   constexpr bool GATED = END != END_PLAIN;
   __shared__ __attribute__((aligned(256))) char lds[Tl::LDS];
   // Workgroups go round the 8 XCDs by their number: each XCD gets a run of tiles, eight tiles of rows side by side, so that the panels that its 32
   // units read at a time lie in its L2.
-  const u32 tiles = a.tiles_m * a.tiles_n, all = tiles * a.groups, each = (all + 7) / 8;
+  const u32 tiles = a.tiles_m * a.tiles_n, all = tiles * a.products * a.shares, each = (all + 7) / 8;
   const u32 id = (blockIdx.x % 8) * each + blockIdx.x / 8;
   if (blockIdx.x / 8 >= each || id >= all) return;
   const u32 group = id / tiles, t = id % tiles, band = t / (8 * a.tiles_n), high = a.tiles_m - band * 8 < 8 ? a.tiles_m - band * 8 : 8;
   const u32 in = t - band * 8 * a.tiles_n, m0 = (band * 8 + in % high) * Tl::BM, n0 = in / high * (GATED ? 128 : 256);
-  const u32 which = a.shares > 1 ? 0 : group;                          // (shares of one product, or products)
-  const u32 nk = (a.k + TILE_K - 1) / TILE_K, first = a.shares > 1 ? group * a.per : 0;
-  const u32 last = a.shares > 1 ? (first + a.per < nk * a.sources ? first + a.per : nk * a.sources) : nk * a.sources;
+  const u32 which = group / a.shares, share = group % a.shares;
+  const u32 nk = (a.k + KS - 1) / KS, first = share * a.per, last = first + a.per < nk * a.sources ? first + a.per : nk * a.sources;
   PA pa[Tl::APANELS];
   PB pb[2];
   u32 am[Tl::APANELS], bn[2];
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, STAGE
     for (int i = 0; i < Tl::APANELS; ++i) w.a[i] = PA::start(pa0, a.as, am[i], step);
 #pragma unroll
     for (int j = 0; j < 2; ++j) w.b[j] = PB::start(a.b[GATED ? (u32)j : a.sources > 1 ? src : which], a.bs, bn[j], step);
-    w.left = a.k - step * TILE_K;
+    w.left = a.k - step * KS;
   };
   place(w, first - src * nk);
   const u32 l = lane_id(), wave = uniform(wave_id()), row0 = m0 + (wave / 4) * 32 * TM + (l & 31), c0 = n0 + (wave % 4) * 32 + 8 * (l >> 5);
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, STAGE
     }
   }
   f32x16 acc[2][TM] = {};
-  Tl::run(acc, lds_addr(lds), (int)(last - first), pa, pb, w, PA::bytes(a.as), PB::bytes(a.bs), a.sources == 1 || a.k % TILE_K == 0, [&](typename Tl::Walk& w) {
+  Tl::run(acc, lds_addr(lds), (int)(last - first), pa, pb, w, PA::bytes(a.as), PB::bytes(a.bs), a.sources == 1 || a.k % KS == 0, [&](typename Tl::Walk& w) {
     src = 1;
     if (a.sources > 1) place(w, 0);
   });
@@ -157,11 +157,11 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, STAGE
 // The shares of four columns added in order.
 template <class T, int END>
 __global__ __launch_bounds__(256) void k_gated_join(const GatedArgs a) {
-  const u64 quads = a.n / 4, all = (u64)a.m * quads, wide = END == END_PLAIN ? a.n : 2ull * a.n;
+  const u64 quads = a.n / 4, one = (u64)a.m * quads, all = one * a.products, wide = END == END_PLAIN ? a.n : 2ull * a.n;
   for (u64 e = (u64)blockIdx.x * 256 + threadIdx.x; e < all; e += (u64)gridDim.x * 256) {
-    const u32 row = (u32)(e / quads), c = (u32)(e % quads) * 4;
+    const u32 which = (u32)(e / one), row = (u32)(e % one / quads), c = (u32)(e % quads) * 4;
     f32x4 g = {}, u = {};
-    const float* p = a.part + (u64)row * wide + c;
+    const float* p = a.part + ((u64)which * a.shares * a.m + row) * wide + c;
 #pragma unroll 4
     for (u32 s = 0; s < a.shares; ++s, p += (u64)a.m * wide) {
       g += *(const f32x4*)p;
@@ -171,56 +171,62 @@ __global__ __launch_bounds__(256) void k_gated_join(const GatedArgs a) {
     typename E::V d = {};
     if constexpr (END == END_BACK) d = E::dh_at(a, row, c);
     const float gs[4] = {g[0], g[1], g[2], g[3]}, us[4] = {u[0], u[1], u[2], u[3]};
-    E::put(a, 0, row, c, gs, us, d);
+    E::put(a, which, row, c, gs, us, d);
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-// One product: its tiles and the shares of its sum.
-struct ProductPlan { u32 wm, tm, shares, per, groups; u64 part; };
+// How a product's tiles are cut, by what they cost: us of 64 values of k with every unit full, and of a tile's beginning and end.  Measured in
+// bfloat16: 8192 tokens, 4096 -> 16384 takes 1851 us in tiles of 256 rows, 2031 with the steps of half the length and four stages (more barriers; further
+// ahead does not help), 1988 in tiles of 128; 5001 tokens, 1000 -> 2744 78 and 88; the weights' gradients of 16384 tokens, 768 -> 2048, 376 in 48 tiles of 256
+// rows, 333 in 96 of 128, 165 with the sum of the 256-row ones in three shares.  Few tokens are bound by the weights' bytes: tiles of 32 rows with four
+// stages took as long as these of 64 with two (8 tokens, 4096 -> 16384: 44 us).
+struct TileCut { u32 rows, ks, slots; float step, ends; };
+static const TileCut CUTS[3] = {{256, 64, 256, 1.65f, 9.0f}, {128, 32, 512, 1.85f, 7.0f}, {64, 64, 512, 1.1f, 6.0f}};
+
+// One product, or two of one shape: the cut of its tiles and the shares of its sum.
+struct ProductPlan { u32 cut, shares, per; u64 part; };
 
 static u32 ceil_div(u64 a, u64 b) { return (u32)((a + b - 1) / b); }
 
-// products: of their own, side by side; wide: columns of a tile that count (128 where gated)
 static ProductPlan product_plan(u64 m, u64 n, u64 k, u32 sources, u32 products, bool gated, bool across) {
-  ProductPlan p{};
-  const u64 tn = ceil_div(n, gated ? 128 : 256);
-  p.wm = 2; p.tm = 4;
-  if (m <= 32 && !across) { p.wm = 1; p.tm = 1; }
-  else if (ceil_div(m, 256) * tn * products < 192) { p.wm = 1; p.tm = across ? 4 : 2; }
-  const u64 tiles = ceil_div(m, 32 * p.tm * p.wm) * tn * products, steps = (u64)ceil_div(k, TILE_K) * sources;
-  const u64 want = p.tm == 2 ? 512 : 256;
-  p.shares = 1;
-  if (products == 1 && tiles && tiles < want * 2 / 3) {
-    u64 s = want / tiles;
-    if (s > steps / 4) s = steps / 4;
-    if (s > 32) s = 32;
-    p.shares = s ? (u32)s : 1;
+  ProductPlan best{};
+  float least = 3e38f;
+  const u64 tn = ceil_div(n, gated ? 128 : 256), wide = gated ? 2 * n : n;
+  for (u32 c = 0; c < 3; ++c) {
+    const TileCut& cut = CUTS[c];
+    if (c == 2 && across) continue;                                    // (panels of 128 rows)
+    const u64 tiles = ceil_div(m, cut.rows) * tn * products, steps = (u64)ceil_div(k, cut.ks) * sources;
+    for (u32 want = 1; want <= 32; ++want) {
+      if (want > 1 && want > steps * cut.ks / 256) break;              // (a share has 256 values of k at least)
+      const u32 per = ceil_div(steps, want), shares = per ? ceil_div(steps, per) : 1;
+      const u64 part = shares > 1 ? (u64)products * shares * m * wide * 4 : 0;
+      if (part > 1ull << 30) break;
+      const u64 all = tiles * shares, rounds = all / cut.slots, left = all % cut.slots;
+      // (one workgroup alone on a unit that could hold two takes 0.72 of the time)
+      const float work = (float)rounds + (left ? (cut.slots == 512 && left <= 256 ? 0.72f : 1.0f) : 0.0f);
+      const float t = work * ((float)per * cut.ks / 64 * cut.step + cut.ends) + (shares > 1 ? 4.0f + (float)part * 2 / 5e6f : 0.0f);
+      if (t < least) { least = t; best = {c, shares, per, part}; }
+    }
   }
-  p.per = ceil_div(steps, p.shares);
-  p.shares = ceil_div(steps, p.per ? p.per : 1);
-  if (!p.shares) p.shares = 1;
-  p.groups = p.shares > 1 ? p.shares : products;
-  p.part = p.shares > 1 ? (u64)p.shares * m * (gated ? 2 * n : n) * 4 : 0;
-  return p;
+  return best;
 }
 
 template <class T, int LA, int LB, int END>
-static int product(GatedArgs a, const ProductPlan& p, void* part, hipStream_t s) {
-  a.tiles_m = ceil_div(a.m, 32 * p.tm * p.wm);
+static int product(GatedArgs a, const ProductPlan& p, u32 products, void* part, hipStream_t s) {
+  a.tiles_m = ceil_div(a.m, CUTS[p.cut].rows);
   a.tiles_n = ceil_div(a.n, END == END_PLAIN ? 256 : 128);
-  a.groups = p.groups; a.per = p.per; a.shares = p.shares; a.part = (float*)part;
-  const u64 all = (u64)a.tiles_m * a.tiles_n * a.groups;
+  a.products = products; a.per = p.per; a.shares = p.shares; a.part = (float*)part;
+  const u64 all = (u64)a.tiles_m * a.tiles_n * products * p.shares;
   if (all > G10_GROUPS_MOST / 2 - 8) return G10_EINVAL;
   const u32 grid = ceil_div(all, 8) * 8;
-  if (p.wm == 2) k_gated<T, LA, LB, 2, 4, 2, END><<<grid, 512, 0, s>>>(a);
-  else if constexpr (LA == ACROSS) k_gated<T, LA, LB, 1, 4, 2, END><<<grid, 256, 0, s>>>(a);
-  else if (p.tm == 2) k_gated<T, LA, LB, 1, 2, 2, END><<<grid, 256, 0, s>>>(a);
-  else k_gated<T, LA, LB, 1, 1, 4, END><<<grid, 256, 0, s>>>(a);
+  if (p.cut == 0) k_gated<T, LA, LB, 2, 4, 64, 2, END><<<grid, 512, 0, s>>>(a);
+  else if (p.cut == 1) k_gated<T, LA, LB, 1, 4, 32, 3, END><<<grid, 256, 0, s>>>(a);
+  else if constexpr (LA == ALONG) k_gated<T, LA, LB, 1, 2, 64, 2, END><<<grid, 256, 0, s>>>(a);
   if (p.shares > 1) {
-    const u64 quads = (u64)a.m * (a.n / 4), groups = (quads + 255) / 256;
+    const u64 groups = ((u64)a.m * (a.n / 4) * products + 255) / 256;
     k_gated_join<T, END><<<(u32)(groups < 65536 ? groups : 65536), 256, 0, s>>>(a);
   }
   return G10_OK;
@@ -253,7 +259,7 @@ static int gated_forward(const g10_gated_args* g, void* ws, hipStream_t s) {
   a.as = g->x_stride; a.bs = g->w_stride; a.os = g->h_stride;
   a.m = g->tokens; a.n = g->inner; a.k = g->dim; a.sources = 1; a.act = g->act;
   const ProductPlan p = product_plan(a.m, a.n, a.k, 1, 1, true, false);
-  return g->out_in ? product<T, ALONG, ALONG, END_GATED>(a, p, ws, s) : product<T, ALONG, ACROSS, END_GATED>(a, p, ws, s);
+  return g->out_in ? product<T, ALONG, ALONG, END_GATED>(a, p, 1, ws, s) : product<T, ALONG, ACROSS, END_GATED>(a, p, 1, ws, s);
 }
 
 extern "C" int g10_gated(const g10_gated_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
@@ -275,6 +281,7 @@ static BackPlan back_plan(const g10_gated_args* g) {
   b.dx = product_plan(g->tokens, g->dim, g->inner, 2, 1, false, false);
   b.dw = product_plan(wm, wn, g->tokens, 1, 2, false, true);
   u64 part = b.gated.part > b.dx.part ? b.gated.part : b.dx.part;
+  if (b.dw.part > part) part = b.dw.part;
   b.at_part = 2 * (((u64)g->tokens * g->inner * 2 + 255) & ~255ull);
   b.bytes = b.at_part + part;
   return b;
@@ -296,19 +303,19 @@ static int gated_back(const g10_gated_args* g, char* ws, hipStream_t s) {
     a.a[0] = a.a[1] = g->x; a.b[0] = g->gate; a.b[1] = g->up; a.out[0] = dg; a.out[1] = du; a.dh = g->dh;
     a.as = g->x_stride; a.bs = g->w_stride; a.os = g->inner; a.dhs = g->dh_stride;
     a.m = g->tokens; a.n = g->inner; a.k = g->dim; a.sources = 1; a.act = g->act;
-    G10_TRY((g->out_in ? product<T, ALONG, ALONG, END_BACK> : product<T, ALONG, ACROSS, END_BACK>)(a, b.gated, part, s));
+    G10_TRY((g->out_in ? product<T, ALONG, ALONG, END_BACK> : product<T, ALONG, ACROSS, END_BACK>)(a, b.gated, 1, part, s));
     a = GatedArgs{};
     a.a[0] = dg; a.a[1] = du; a.b[0] = g->gate; a.b[1] = g->up; a.out[0] = g->dx;
     a.as = g->inner; a.bs = g->w_stride; a.os = g->dx_stride;
     a.m = g->tokens; a.n = g->dim; a.k = g->inner; a.sources = 2;
-    G10_TRY((g->out_in ? product<T, ALONG, ACROSS, END_PLAIN> : product<T, ALONG, ALONG, END_PLAIN>)(a, b.dx, part, s));
+    G10_TRY((g->out_in ? product<T, ALONG, ACROSS, END_PLAIN> : product<T, ALONG, ALONG, END_PLAIN>)(a, b.dx, 1, part, s));
   }
   GatedArgs a{};                                                       // (without tokens: zeros)
   a.out[0] = g->dgate; a.out[1] = g->dup; a.os = g->dw_stride;
   a.k = g->tokens; a.sources = 1;
   if (g->out_in) { a.a[0] = dg; a.a[1] = du; a.as = g->inner; a.b[0] = a.b[1] = g->x; a.bs = g->x_stride; a.m = g->inner; a.n = g->dim; }
   else { a.a[0] = a.a[1] = g->x; a.as = g->x_stride; a.b[0] = dg; a.b[1] = du; a.bs = g->inner; a.m = g->dim; a.n = g->inner; }
-  return product<T, ACROSS, ACROSS, END_PLAIN>(a, b.dw, part, s);
+  return product<T, ACROSS, ACROSS, END_PLAIN>(a, b.dw, 2, part, s);
 }
 
 extern "C" int g10_gated_backward(const g10_gated_args* g, void* workspace, uint64_t workspace_bytes, void* hip_stream) {

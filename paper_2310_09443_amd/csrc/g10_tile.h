@@ -4,8 +4,8 @@
 // tile's first panel of 128 columns and the same 32 of its second one.  The panels of B need not lie side by side: a gated product takes
 // one panel of each weight, and a value's two factors come out in one lane's registers.
 //
-// Both factors go through LDS in steps of 64 along k, straight from memory (no registers), in panels of one of two layouts, as they lie in
-// memory: rows of 64 values along k (ALONG), read as fragments of 8 values, or 64 rows of 128 values across (ACROSS), read
+// Both factors go through LDS in steps of KS = 64 or 32 along k, straight from memory (no registers), in panels of one of two layouts, as they
+// lie in memory: rows of KS values along k (ALONG), read as fragments of 8 values, or KS rows of 128 values across (ACROSS), read
 // with the transposing LDS read.  Both orders of k are the same, so any two layouts meet.  The places of 16-byte pieces in a row are exchanged
 // so that each read takes all banks once.
 //
@@ -26,19 +26,19 @@ __device__ __forceinline__ void lds_settled() {
   asm volatile("" ::: "memory");
 }
 
-#define TILE_K 64
-#define TILE_N 256                 // columns of a tile: two panels
-
 enum { ALONG = 0, ACROSS = 1 };
 
-__device__ __forceinline__ u32 swz64(u32 r) { return (r >> 1) & 7; }                     // 8 pieces to a row of 64 values
+// Exchanges of a row's pieces.
+__device__ __forceinline__ u32 swz32(u32 r) { return (r >> 2) & 3; }                     // 4 pieces to a row of 32 values
+__device__ __forceinline__ u32 swz64(u32 r) { return (r >> 1) & 7; }                     // 8 pieces to a row of 64
 __device__ __forceinline__ u32 swz128(u32 r) { return ((r & 3) << 2) | ((r >> 2) & 3); } // 16 pieces to a row of 128
 
-// A panel of ROWS places across (64 values of k each) by NT threads: what each loads, and where it looks.
-template <int LAYOUT, int ROWS, int NT>
+// A panel of ROWS places across (KS values of k each) by NT threads: what each loads, and where it looks.
+template <int LAYOUT, int ROWS, int NT, int KS>
 struct Panel {
-  static constexpr int PIECES = ROWS * 8, IT = (PIECES + NT - 1) / NT, BYTES = PIECES * 16;
-  static constexpr int PER = LAYOUT == ALONG ? 8 : ROWS / 8;                             // pieces to a row in LDS
+  static constexpr int PIECES = ROWS * KS / 8, IT = (PIECES + NT - 1) / NT, BYTES = PIECES * 16;
+  static constexpr int PER = LAYOUT == ALONG ? KS / 8 : ROWS / 8;                        // pieces to a row in LDS
+  static __device__ __forceinline__ u32 swz(u32 row) { return LAYOUT == ACROSS ? swz128(row) : KS == 64 ? swz64(row) : swz32(row); }
   static_assert(LAYOUT == ALONG || ROWS == 128, "rows of 128 across");
   u32 off[IT];
   u32 k[IT];                       // the first value of k of each piece
@@ -49,11 +49,11 @@ struct Panel {
     for (int i = 0; i < IT; ++i) {
       const u32 p = i * NT + t, row = p / PER, place = p % PER;
       if (LAYOUT == ALONG) {
-        const u32 c = place ^ swz64(row), left = n - first, r = row < left ? row : left - 1;
+        const u32 c = place ^ swz(row), left = n - first, r = row < left ? row : left - 1;
         off[i] = (u32)((int64_t)r * stride + c * 8) * 2;
         k[i] = c * 8;
       } else {
-        u32 c = place ^ swz128(row);
+        u32 c = place ^ swz(row);
         if (first + c * 8 >= n) c = 0;
         off[i] = (u32)((int64_t)row * stride + c * 8) * 2;
         k[i] = row;
@@ -64,28 +64,28 @@ struct Panel {
   static __device__ __forceinline__ const char* start(const void* p, int64_t stride, u32 first, u32 step) {
     return (const char*)p + (LAYOUT == ALONG ? (int64_t)first * stride : (int64_t)first) * 2 + step * bytes(stride);
   }
-  static __device__ __forceinline__ int64_t bytes(int64_t stride) { return (LAYOUT == ALONG ? (int64_t)TILE_K : TILE_K * stride) * 2; }
+  static __device__ __forceinline__ int64_t bytes(int64_t stride) { return (LAYOUT == ALONG ? (int64_t)KS : KS * stride) * 2; }
   // lds: the panel + this wavefront's first piece.  left: values of k from the step's first on; pieces past them become zeros.
   __device__ __forceinline__ void load(const char* at, u32 lds, u32 left, u32 t) const {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       if (PIECES % NT && i * NT + (int)t >= PIECES) continue;                            // (whole wavefronts)
-      if (left >= TILE_K || k[i] < left) load_piece(at, off[i], lds + (u32)(i * NT * 16));
+      if (left >= KS || k[i] < left) load_piece(at, off[i], lds + (u32)(i * NT * 16));
       else *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(lds + (u32)(i * NT * 16) + lane_id() * 16) = u32x4{};
     }
   }
   // The base address of a lane's fragments.
   static __device__ __forceinline__ u32 base(u32 panel) {
     const u32 l = lane_id();
-    if (LAYOUT == ALONG) return panel + (l & 31) * 128 + (((l >> 5) ^ swz64(l & 31)) << 4);
+    if (LAYOUT == ALONG) return panel + (l & 31) * (KS * 2) + (((l >> 5) ^ swz(l & 31)) << 4);
     const u32 row = 8 * (l >> 5) + ((l & 15) >> 2), c = 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
-    return panel + row * (ROWS * 2) + ((c ^ swz128(row)) << 4) + (l & 1) * 8;
+    return panel + row * (ROWS * 2) + ((c ^ swz(row)) << 4) + (l & 1) * 8;
   }
   // 32 places from 32 blk on, values 16 kk + 8 (l / 32) + 0..7 of k
   template <class T>
   static __device__ __forceinline__ typename Vec<T>::x8 frag(u32 base, int blk, int kk) {
     if constexpr (LAYOUT == ALONG) {
-      return *(__attribute__((address_space(3))) const typename Vec<T>::x8*)(uintptr_t)((base ^ (u32)(kk << 5)) + (u32)(blk * 32 * 128));
+      return *(__attribute__((address_space(3))) const typename Vec<T>::x8*)(uintptr_t)((base ^ (u32)(kk << 5)) + (u32)(blk * 32 * KS * 2));
     } else {
       const u32 at = base ^ (u32)(blk << 6);
       const typename Vec<T>::x4 a = Vec<T>::read_tr(at + (u32)(kk * 16 * ROWS * 2)), b = Vec<T>::read_tr((at ^ 16) + (u32)((kk * 16 + 4) * ROWS * 2));
@@ -95,12 +95,12 @@ struct Panel {
 };
 
 // The sums of one tile.  acc[j][i]: panel j, rows 32 i of the wavefront; lane l holds row l % 32, columns res_row(r).
-template <class T, int LA, int LB, int WM, int TM, int STAGES>
+template <class T, int LA, int LB, int WM, int TM, int KS, int STAGES>
 struct Tile {
   static constexpr int NT = 256 * WM, BM = 32 * TM * WM;
   static constexpr int AROWS = LA == ALONG ? BM : 128, APANELS = BM / AROWS;
-  typedef Panel<LA, AROWS, NT> PA;
-  typedef Panel<LB, 128, NT> PB;
+  typedef Panel<LA, AROWS, NT, KS> PA;
+  typedef Panel<LB, 128, NT, KS> PB;
   static constexpr int A_BYTES = APANELS * PA::BYTES, STAGE = A_BYTES + 2 * PB::BYTES, LDS = STAGES * STAGE;
   static constexpr int LOADS = APANELS * PA::IT + 2 * PB::IT;                            // of a wavefront and step
   typedef typename Vec<T>::x8 x8;
@@ -126,13 +126,13 @@ struct Tile {
       for (int i = 0; i < APANELS; ++i) { pa[i].load(w.a[i], at + i * PA::BYTES, w.left, t); w.a[i] += sa; }
 #pragma unroll
       for (int j = 0; j < 2; ++j) { pb[j].load(w.b[j], at + A_BYTES + j * PB::BYTES, w.left, t); w.b[j] += sb; }
-      if (w.left > TILE_K) w.left -= TILE_K; else next(w);
+      if (w.left > KS) w.left -= KS; else next(w);
       ++loaded;
       to = to + STAGE < lds0 + LDS ? to + STAGE : lds0;
     };
-    const u32 a_off = LA == ALONG ? wm * (32 * TM * 128) : ((wm * TM * 32) / 128) * (u32)PA::BYTES, a_blk = LA == ALONG ? 0 : (wm * TM) % 4;
+    const u32 a_off = LA == ALONG ? wm * (32 * TM * KS * 2) : ((wm * TM * 32) / 128) * (u32)PA::BYTES, a_blk = LA == ALONG ? 0 : (wm * TM) % 4;
     const u32 ab = PA::base(lds0 + a_off) ^ (a_blk << 6), bb = PB::base(lds0 + A_BYTES) ^ (LB == ALONG ? 0 : wn << 6);
-    const u32 b_off = LB == ALONG ? wn * 32 * 128 : 0;
+    const u32 b_off = LB == ALONG ? wn * (32 * KS * 2) : 0;
     x8 fa[2][TM], fb[2][2];
     auto read = [&](int s, u32 at, int kk) {
 #pragma unroll
@@ -156,7 +156,7 @@ struct Tile {
       read(0, from, 0);
       if (step) { hold(); multiply(1); }
 #pragma unroll
-      for (int kk = 1; kk < 4; ++kk) {
+      for (int kk = 1; kk < KS / 16; ++kk) {
         hold();
         read(kk & 1, from, kk);
         hold();
