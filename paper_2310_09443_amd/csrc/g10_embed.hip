@@ -11,6 +11,8 @@
 
 #include <math.h>
 
+typedef float f4 __attribute__((ext_vector_type(4)));
+
 struct EmbedArgs {
   const void *ids, *table, *dout;
   void *out, *dtable;
@@ -21,12 +23,36 @@ struct EmbedArgs {
   u32 *keys[2], *places[2];        // ids and places of tokens, before and after a pass of the sort
   u32* counts;                     // [tile][digit]
   u32 tiles, tile, bits, passes;   // tiles of `tile` tokens; bits to a pass
-  float* parts;                    // [piece][2][dim]: a run that comes from the piece before, one that goes on
+  float* parts;                    // [piece][2][part_row]: a run that comes from the piece before, one that goes on
+  u32 part_row;
   u32 pieces, per;                 // pieces of `per` tokens
   u32 sum_groups;                  // workgroups that sum; the others clear rows without tokens
 };
 
-template <class T, int N> struct Pack { typedef T type __attribute__((ext_vector_type(N))); };
+// N values side by side, at any address of a value: accesses to memory need not be aligned, only a row's last N may be fewer.  WHOLE: rows of a
+// multiple of N values.
+template <class T, int N> struct Pack { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
+template <class T, int N, bool WHOLE>
+__device__ __forceinline__ typename Pack<T, N>::type get(const T* p, u32 d, u32 dim) {
+  typedef typename Pack<T, N>::type V;
+  if (WHOLE || d + N <= dim) return *(const V*)(p + d);
+  V v = {};
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (d + k < dim) v[k] = p[d + k];
+  return v;
+}
+template <class T, int N, bool WHOLE>
+__device__ __forceinline__ void put(T* p, u32 d, u32 dim, const typename Pack<T, N>::type& v) {
+  typedef typename Pack<T, N>::type V;
+  if (WHOLE || d + N <= dim) {
+    __builtin_nontemporal_store(v, (V*)(p + d));                       // (past the L2: rows of 4095, 71 us, otherwise 117)
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (d + k < dim) p[d + k] = v[k];
+  }
+}
 
 __device__ __forceinline__ int64_t id_at(const EmbedArgs& a, u32 t) {
   return a.ids64 ? ((const int64_t*)a.ids)[t] : (int64_t)((const int*)a.ids)[t];
@@ -35,7 +61,7 @@ __device__ __forceinline__ int64_t id_at(const EmbedArgs& a, u32 t) {
 // ---------------------------------------------------------------------------------------------------------------------
 // lookup: a wavefront to a token's slab of 64 N values, four tokens at a time
 // ---------------------------------------------------------------------------------------------------------------------
-template <class T, int N>
+template <class T, int N, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
   typedef typename Pack<T, N>::type V;
   const u64 tasks = (u64)((a.tokens + 3) / 4) * a.slabs, step = (u64)gridDim.x * 4;
@@ -49,7 +75,7 @@ __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
       const u32 t = t0 + i < a.tokens ? t0 + i : a.tokens - 1;
       const int64_t id = id_at(a, t);
       fine[i] = id >= 0 && id < (int64_t)a.vocab;
-      v[i] = *(const V*)((const T*)a.table + (fine[i] ? id : 0) * a.ts + d);
+      v[i] = get<T, N, WHOLE>((const T*)a.table + (fine[i] ? id : 0) * a.ts, d, a.dim);
     }
 #pragma unroll
     for (u32 i = 0; i < 4; ++i) {
@@ -57,7 +83,7 @@ __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
       V w;
 #pragma unroll
       for (int k = 0; k < N; ++k) w[k] = (T)(fine[i] ? (float)v[i][k] * a.scale : __builtin_nanf(""));
-      __builtin_nontemporal_store(w, (V*)((T*)a.out + (int64_t)(t0 + i) * a.os + d));
+      put<T, N, WHOLE>((T*)a.out + (int64_t)(t0 + i) * a.os, d, a.dim, w);
     }
   }
 }
@@ -180,13 +206,26 @@ __global__ __launch_bounds__(256) void k_embed_move(const EmbedArgs a, u32 pass,
 // ---------------------------------------------------------------------------------------------------------------------
 // the sums
 // ---------------------------------------------------------------------------------------------------------------------
-template <class T, int N>
+template <class T, int N, bool WHOLE>
 __device__ __forceinline__ void write_row(const EmbedArgs& a, u32 v, u32 d, const float (&s)[N]) {
   typedef typename Pack<T, N>::type V;
   V w;
 #pragma unroll
   for (int k = 0; k < N; ++k) w[k] = (T)(s[k] * a.scale);
-  __builtin_nontemporal_store(w, (V*)((T*)a.dtable + (int64_t)v * a.gs + d));
+  put<T, N, WHOLE>((T*)a.dtable + (int64_t)v * a.gs, d, a.dim, w);
+}
+
+// Zeros, by way of the L2.
+template <class T, int N>
+__device__ __forceinline__ void put_near(T* p, u32 d, u32 dim) {
+  typedef typename Pack<T, N>::type V;
+  if (d + N <= dim) {
+    *(V*)(p + d) = V{};
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (d + k < dim) p[d + k] = (T)0.0f;
+  }
 }
 
 // The first place in the sorted keys whose key is not below v.
@@ -201,7 +240,7 @@ __device__ __forceinline__ u32 first_of(const u32* keys, u32 n, u32 v) {
 
 #define EMBED_CLEAR 32u            // rows of the table that a wavefront looks after
 
-template <class T, int N>
+template <class T, int N, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32* keys, const u32* places) {
   typedef typename Pack<T, N>::type V;
   const u32 l = lane_id();
@@ -211,7 +250,8 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
       const u32 piece = (u32)(task / a.slabs), d = ((u32)(task % a.slabs) * 64 + l) * N;
       const u32 t0 = piece * a.per, n = a.tokens - t0 < a.per ? a.tokens - t0 : a.per;
       const bool on = d < a.dim;
-      const T* src = (const T*)a.dout + (on ? d : 0);
+      const T* src = (const T*)a.dout;
+      const u32 at = on ? d : 0;
       // ids and places of the piece, a lane each (a piece has 64 tokens at most)
       const u32 mykey = l < n ? keys[t0 + l] : ~0u, myplace = l < n ? places[t0 + l] : 0;
       const u32 before = t0 ? keys[t0 - 1] : ~0u, behind = t0 + n < a.tokens ? keys[t0 + n] : ~0u;
@@ -221,11 +261,11 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
       auto flush = [&](bool on_from, bool goes_on) {
         if (on && key < a.vocab) {
           if (on_from || goes_on) {
-            float* p = a.parts + ((u64)piece * 2 + (on_from ? 0 : 1)) * a.dim + d;
+            f4* p = (f4*)(a.parts + ((u64)piece * 2 + (on_from ? 0 : 1)) * a.part_row + d);
 #pragma unroll
-            for (int k = 0; k < N; ++k) p[k] = s[k];
+            for (int k = 0; k < N; k += 4) p[k / 4] = f4{s[k], s[k + 1], s[k + 2], s[k + 3]};
           } else {
-            write_row<T, N>(a, key, d, s);
+            write_row<T, N, WHOLE>(a, key, d, s);
           }
         }
       };
@@ -233,9 +273,8 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
         V v[8];
 #pragma unroll
         for (u32 j = 0; j < 8; ++j) {
-          const u32 at = i + j < n ? i + j : n - 1;
-          const u32 place = (u32)__builtin_amdgcn_readlane((int)myplace, (int)at);
-          v[j] = *(const V*)(src + (int64_t)(place < a.tokens ? place : 0) * a.ds);
+          const u32 place = (u32)__builtin_amdgcn_readlane((int)myplace, (int)(i + j < n ? i + j : n - 1));
+          v[j] = get<T, N, WHOLE>(src + (int64_t)(place < a.tokens ? place : 0) * a.ds, at, a.dim);
         }
 #pragma unroll
         for (u32 j = 0; j < 8; ++j) {
@@ -257,7 +296,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
     return;
   }
   // rows without a token
-  const float zero[N] = {};
+  [[maybe_unused]] const float zero[N] = {};
   const u32 waves = (gridDim.x - a.sum_groups) * 4;
   const u64 rows = ((u64)a.vocab + EMBED_CLEAR - 1) / EMBED_CLEAR;
   for (u64 r = (u64)(blockIdx.x - a.sum_groups) * 4 + uniform(wave_id()); r < rows; r += waves) {
@@ -268,13 +307,17 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
     while (empty) {
       const u32 i = (u32)__builtin_ctzll(empty);
       empty &= empty - 1;
-      for (u32 d = l * N; d < a.dim; d += 64 * N) write_row<T, N>(a, v0 + i, d, zero);
+      T* row = (T*)a.dtable + (int64_t)(v0 + i) * a.gs;
+      for (u32 d = l * N; d < a.dim; d += 64 * N) {
+        if (WHOLE) write_row<T, N, WHOLE>(a, v0 + i, d, zero);
+        else put_near<T, N>(row, d, a.dim);                            // (rows of 1001 side by side, that meet inside lines: past the L2 94 us, so 53)
+      }
     }
   }
 }
 
 // Runs over the ends of pieces: the piece in which such a run begins adds its parts.
-template <class T, int N>
+template <class T, int N, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32* keys) {
   const u64 tasks = (u64)a.pieces * a.slabs, step = (u64)gridDim.x * 4;
   for (u64 task = (u64)blockIdx.x * 4 + uniform(wave_id()); task < tasks; task += step) {
@@ -293,32 +336,32 @@ __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32
       more += on == ~0ull ? 64u : (u32)__builtin_ctzll(~on);
     }
     if (d >= a.dim) continue;
-    const float* p = a.parts + ((u64)piece * 2 + 1) * a.dim + d;
+    const float* p = a.parts + ((u64)piece * 2 + 1) * a.part_row + d;
     float s[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] = p[k];
-    p += a.dim;                                                        // (the next piece's first part)
+    p += a.part_row;                                                   // (the next piece's first part)
     for (u32 q = 0; q < more; q += 8) {                                // (past the last one it is read again, and not added)
       float v[8][N];
 #pragma unroll
       for (u32 u = 0; u < 8; ++u) {
-        const float* o = p + (u64)(q + u < more ? q + u : more - 1) * 2 * a.dim;
+        const f4* o = (const f4*)(p + (u64)(q + u < more ? q + u : more - 1) * 2 * a.part_row);
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[u][k] = o[k];
+        for (int k = 0; k < N; ++k) v[u][k] = o[k / 4][k % 4];
       }
 #pragma unroll
       for (u32 u = 0; u < 8; ++u)
 #pragma unroll
         for (int k = 0; k < N; ++k) s[k] += q + u < more ? v[u][k] : 0.0f;
     }
-    write_row<T, N>(a, key, d, s);
+    write_row<T, N, WHOLE>(a, key, d, s);
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-struct EmbedPlan { u32 lanes_n, grid, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
+struct EmbedPlan { bool whole; u32 grid, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
 
 static u64 up256(u64 x) { return (x + 255) & ~(u64)255; }
 
@@ -328,7 +371,6 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   if (!g->dim || g->dim > 65536 || !g->vocab || g->vocab >= 0x80000000u || g->tokens >= 0x80000000u) return G10_EINVAL;
   const u32 e = g->type == G10_F32 ? 4 : 2;
   const void *src = back ? g->dout : g->table, *dst = back ? g->dtable : g->out;
-  const int64_t ss = back ? g->dout_stride : g->table_stride, sd = back ? g->dtable_stride : g->out_stride;
   if (!dst && (back || g->tokens)) return G10_EINVAL;
   if (g->tokens && (!src || !g->ids)) return G10_EINVAL;
   if ((uintptr_t)src % e || (uintptr_t)dst % e || (uintptr_t)g->ids % (g->ids_64 ? 8 : 4)) return G10_EINVAL;
@@ -337,10 +379,10 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   a.ts = g->table_stride; a.os = g->out_stride; a.ds = g->dout_stride; a.gs = g->dtable_stride;
   a.tokens = g->tokens; a.vocab = g->vocab; a.dim = g->dim; a.scale = g->scale; a.ids64 = g->ids_64;
   const u32 n = 16 / e;
-  const bool wide = g->dim % n == 0 && !(((uintptr_t)src | (uintptr_t)dst) & 15) && ss % (int64_t)n == 0 && sd % (int64_t)n == 0;
   p = EmbedPlan{};
-  p.lanes_n = wide ? n : 1;
-  a.slabs = (g->dim + 64 * p.lanes_n - 1) / (64 * p.lanes_n);
+  p.whole = g->dim % n == 0;
+  a.slabs = (g->dim + 64 * n - 1) / (64 * n);
+  a.part_row = (g->dim + 7) & ~7u;
   auto groups = [](u64 waves, u32 most) { const u64 n = (waves + 3) / 4; return (u32)(n < most ? n : most); };
   p.grid = groups((u64)((a.tokens + 3) / 4) * a.slabs, 1u << 16);
   if (!back) return G10_OK;
@@ -351,7 +393,7 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   const u32 rounds = (a.tokens + EMBED_ROUND - 1) / EMBED_ROUND;
   a.tile = (rounds + EMBED_TILES - 1) / EMBED_TILES * EMBED_ROUND;
   a.tiles = a.tokens ? (a.tokens + a.tile - 1) / a.tile : 0;
-  a.per = 64;
+  a.per = 64;                                                          // (16384 tokens of 768 values in pieces of 16: 63 us for 57)
   a.pieces = (a.tokens + a.per - 1) / a.per;
   a.sum_groups = groups((u64)a.pieces * a.slabs, 1u << 16);
   p.join_groups = a.sum_groups;
@@ -360,15 +402,16 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   auto take = [&](u64 bytes) { const u64 here = at; at += up256(bytes); return here; };
   for (int i = 0; i < 2; ++i) { p.at_keys[i] = take((u64)a.tokens * 4); p.at_places[i] = take((u64)a.tokens * 4); }
   p.at_counts = take(((u64)a.tiles << a.bits) * 4);
-  p.at_parts = take((u64)a.pieces * 2 * a.dim * 4);
+  p.at_parts = take((u64)a.pieces * 2 * a.part_row * 4);
   p.bytes = at;
   return G10_OK;
 }
 
-template <class T, int N>
+template <class T, bool WHOLE>
 static void embed_sums(const EmbedArgs& a, const EmbedPlan& p, int last, hipStream_t s) {
-  k_embed_sum<T, N><<<a.sum_groups + p.clear_groups, 256, 0, s>>>(a, a.keys[last], a.places[last]);
-  if (a.pieces > 1) k_embed_join<T, N><<<p.join_groups, 256, 0, s>>>(a, a.keys[last]);
+  constexpr int N = 16 / sizeof(T);
+  k_embed_sum<T, N, WHOLE><<<a.sum_groups + p.clear_groups, 256, 0, s>>>(a, a.keys[last], a.places[last]);
+  if (a.pieces > 1) k_embed_join<T, N, WHOLE><<<p.join_groups, 256, 0, s>>>(a, a.keys[last]);
 }
 
 extern "C" int g10_embed(const g10_embed_args* g, void* hip_stream) {
@@ -376,9 +419,9 @@ extern "C" int g10_embed(const g10_embed_args* g, void* hip_stream) {
   G10_TRY(embed_args(g, false, a, p));
   if (!a.tokens) return G10_OK;
   hipStream_t s = (hipStream_t)hip_stream;
-  if (g->type == G10_F32) { if (p.lanes_n > 1) k_embed<float, 4><<<p.grid, 256, 0, s>>>(a); else k_embed<float, 1><<<p.grid, 256, 0, s>>>(a); }
-  else if (g->type == G10_F16) { if (p.lanes_n > 1) k_embed<_Float16, 8><<<p.grid, 256, 0, s>>>(a); else k_embed<_Float16, 1><<<p.grid, 256, 0, s>>>(a); }
-  else { if (p.lanes_n > 1) k_embed<__bf16, 8><<<p.grid, 256, 0, s>>>(a); else k_embed<__bf16, 1><<<p.grid, 256, 0, s>>>(a); }
+  if (g->type == G10_F32) { if (p.whole) k_embed<float, 4, true><<<p.grid, 256, 0, s>>>(a); else k_embed<float, 4, false><<<p.grid, 256, 0, s>>>(a); }
+  else if (g->type == G10_F16) { if (p.whole) k_embed<_Float16, 8, true><<<p.grid, 256, 0, s>>>(a); else k_embed<_Float16, 8, false><<<p.grid, 256, 0, s>>>(a); }
+  else { if (p.whole) k_embed<__bf16, 8, true><<<p.grid, 256, 0, s>>>(a); else k_embed<__bf16, 8, false><<<p.grid, 256, 0, s>>>(a); }
   G10_HIP(hipGetLastError());
   return G10_OK;
 }
@@ -412,9 +455,9 @@ extern "C" int g10_embed_backward(const g10_embed_args* g, void* workspace, uint
     }
     at = to;
   }
-  if (g->type == G10_F32) { if (p.lanes_n > 1) embed_sums<float, 4>(a, p, at, s); else embed_sums<float, 1>(a, p, at, s); }
-  else if (g->type == G10_F16) { if (p.lanes_n > 1) embed_sums<_Float16, 8>(a, p, at, s); else embed_sums<_Float16, 1>(a, p, at, s); }
-  else { if (p.lanes_n > 1) embed_sums<__bf16, 8>(a, p, at, s); else embed_sums<__bf16, 1>(a, p, at, s); }
+  if (g->type == G10_F32) { if (p.whole) embed_sums<float, true>(a, p, at, s); else embed_sums<float, false>(a, p, at, s); }
+  else if (g->type == G10_F16) { if (p.whole) embed_sums<_Float16, true>(a, p, at, s); else embed_sums<_Float16, false>(a, p, at, s); }
+  else { if (p.whole) embed_sums<__bf16, true>(a, p, at, s); else embed_sums<__bf16, false>(a, p, at, s); }
   G10_HIP(hipGetLastError());
   return G10_OK;
 }

@@ -71,12 +71,13 @@ __device__ __forceinline__ void neighbours(const f32x16& x, int q, float (&y)[8]
   }
 }
 
-template <class T, int LA, int LB, int WM, int TM, int KS, int STAGES, int END>
-__global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, KS, STAGES>::LDS <= 80 * 1024 ? 2 : 1)) void k_gated(const GatedArgs a) {
-  typedef Tile<T, LA, LB, WM, TM, KS, STAGES> Tl;
+template <class T, int LA, int LB, int WM, int WN, int TM, int KS, int STAGES, int END>
+__global__ __launch_bounds__(64 * WM * WN, (WM * WN == 8 || Tile<T, LA, LB, WM, WN, TM, KS, STAGES>::LDS <= 80 * 1024 ? 2 : 1)) void k_gated(const GatedArgs a) {
+  typedef Tile<T, LA, LB, WM, WN, TM, KS, STAGES> Tl;
   typedef typename Tl::PA PA;
   typedef typename Tl::PB PB;
   constexpr bool GATED = END != END_PLAIN;
+  constexpr u32 WIDE = Tl::WIDE;                                       // columns of a panel
   __shared__ __attribute__((aligned(256))) char lds[Tl::LDS];
   // Workgroups go round the 8 XCDs by their number: each XCD gets a run of tiles, eight tiles of rows side by side, so that the panels that its 32
   // units read at a time lie in its L2.
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, KS, S
   const u32 id = (blockIdx.x % 8) * each + blockIdx.x / 8;
   if (blockIdx.x / 8 >= each || id >= all) return;
   const u32 group = id / tiles, t = id % tiles, band = t / (8 * a.tiles_n), high = a.tiles_m - band * 8 < 8 ? a.tiles_m - band * 8 : 8;
-  const u32 in = t - band * 8 * a.tiles_n, m0 = (band * 8 + in % high) * Tl::BM, n0 = in / high * (GATED ? 128 : 256);
+  const u32 in = t - band * 8 * a.tiles_n, m0 = (band * 8 + in % high) * Tl::BM, n0 = in / high * (GATED ? WIDE : 2 * WIDE);
   const u32 which = group / a.shares, share = group % a.shares;
   const u32 nk = (a.k + KS - 1) / KS, first = share * a.per, last = first + a.per < nk * a.sources ? first + a.per : nk * a.sources;
   PA pa[Tl::APANELS];
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, KS, S
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    bn[j] = GATED ? n0 : n0 + j * 128 < a.n ? n0 + j * 128 : 0;
+    bn[j] = GATED ? n0 : n0 + j * WIDE < a.n ? n0 + j * WIDE : 0;
     pb[j].init(threadIdx.x, a.bs, bn[j], a.n);
   }
   // (a sum over two sources takes both factors from the second one there; products of their own differ in one factor)
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, KS, S
     w.left = a.k - step * KS;
   };
   place(w, first - src * nk);
-  const u32 l = lane_id(), wave = uniform(wave_id()), row0 = m0 + (wave / 4) * 32 * TM + (l & 31), c0 = n0 + (wave % 4) * 32 + 8 * (l >> 5);
+  const u32 l = lane_id(), wave = uniform(wave_id()), row0 = m0 + (wave / WN) * 32 * TM + (l & 31), c0 = n0 + (wave % WN) * 32 + 8 * (l >> 5);
   typedef Ends<T, END, 8> E;
   // (dh is on its way while the tile's first panels are: at the end its latency would be all there is to do)
   typename E::V dh[END == END_BACK ? TM : 1][2];
@@ -144,11 +145,11 @@ __global__ __launch_bounds__(256 * WM, (WM == 2 || Tile<T, LA, LB, WM, TM, KS, S
 #pragma unroll
         for (int r = 0; r < 8; r += 4) {
           if (row < a.m && c < a.n) *(f32x4*)(to + r) = f32x4{g[r], g[r + 1], g[r + 2], g[r + 3]};
-          if (row < a.m && (GATED ? c : c + 128) < a.n) *(f32x4*)(to + (GATED ? a.n : 128) + r) = f32x4{u[r], u[r + 1], u[r + 2], u[r + 3]};
+          if (row < a.m && (GATED ? c : c + WIDE) < a.n) *(f32x4*)(to + (GATED ? a.n : WIDE) + r) = f32x4{u[r], u[r + 1], u[r + 2], u[r + 3]};
         }
       } else {
         E::put(a, which, row, c, g, u, dh[END == END_BACK ? i : 0][q]);
-        if (!GATED) E::put(a, which, row, c + 128, u, g, dh[0][q]);
+        if (!GATED) E::put(a, which, row, c + WIDE, u, g, dh[0][q]);
       }
     }
   }
@@ -181,33 +182,42 @@ __global__ __launch_bounds__(256) void k_gated_join(const GatedArgs a) {
 // How a product's tiles are cut, by what they cost: us of 64 values of k with every unit full, and of a tile's beginning and end.  Measured in
 // bfloat16: 8192 tokens, 4096 -> 16384 takes 1851 us in tiles of 256 rows, 2031 with the steps of half the length and four stages (more barriers; further
 // ahead does not help), 1988 in tiles of 128; 5001 tokens, 1000 -> 2744 78 and 88; the weights' gradients of 16384 tokens, 768 -> 2048, 376 in 48 tiles of 256
-// rows, 333 in 96 of 128, 165 with the sum of the 256-row ones in three shares.  Few tokens are bound by the weights' bytes: tiles of 32 rows with four
-// stages took as long as these of 64 with two (8 tokens, 4096 -> 16384: 44 us).
-struct TileCut { u32 rows, ks, slots; float step, ends; };
-static const TileCut CUTS[3] = {{256, 64, 256, 1.65f, 9.0f}, {128, 32, 512, 1.85f, 7.0f}, {64, 64, 512, 1.1f, 6.0f}};
+// rows, 333 in 96 of 128, 165 with the sum of the 256-row ones in three shares.  Few tokens are bound by the weights' bytes and by the way from memory
+// to LDS and back: panels of 64 columns and six stages are more workgroups with more on their way (16 tokens, 512 -> 2048: 8.2 us for 9.7; 64 tokens, 4096 ->
+// 16384: 57 for 63).
+struct TileCut { u32 rows, wide, ks, slots; float step, ends; };      // wide: columns of a panel
+static const TileCut CUTS[4] = {{256, 128, 64, 256, 1.65f, 9.0f}, {128, 128, 32, 512, 1.85f, 7.0f}, {64, 128, 64, 512, 1.1f, 6.0f}, {64, 64, 64, 256, 0.9f, 4.5f}};
 
 // One product, or two of one shape: the cut of its tiles and the shares of its sum.
 struct ProductPlan { u32 cut, shares, per; u64 part; };
 
 static u32 ceil_div(u64 a, u64 b) { return (u32)((a + b - 1) / b); }
 
-static ProductPlan product_plan(u64 m, u64 n, u64 k, u32 sources, u32 products, bool gated, bool across) {
+// across: the first factor lies across k; along: the second one along it
+static ProductPlan product_plan(u64 m, u64 n, u64 k, u32 sources, u32 products, bool gated, bool across, bool along) {
   ProductPlan best{};
   float least = 3e38f;
-  const u64 tn = ceil_div(n, gated ? 128 : 256), wide = gated ? 2 * n : n;
-  for (u32 c = 0; c < 3; ++c) {
+  const u64 wide = gated ? 2 * n : n;
+  const float bytes = (float)(k * sources) * (float)(m + wide) * (float)products * 2 / 5.2e6f;      // us that reading both factors once takes
+  for (u32 c = 0; c < 4; ++c) {
     const TileCut& cut = CUTS[c];
-    if (c == 2 && across) continue;                                    // (panels of 128 rows)
-    const u64 tiles = ceil_div(m, cut.rows) * tn * products, steps = (u64)ceil_div(k, cut.ks) * sources;
+    if (c >= 2 && across) continue;                                    // (panels of 128 rows)
+    if (m <= 64 ? c < 2 && !across : c == 3) continue;                 // (the larger ones are for more rows, the last one for few)
+    const u64 tiles = (u64)ceil_div(m, cut.rows) * ceil_div(n, gated ? cut.wide : 2 * cut.wide) * products, steps = (u64)ceil_div(k, cut.ks) * sources;
     for (u32 want = 1; want <= 32; ++want) {
       if (want > 1 && want > steps * cut.ks / 256) break;              // (a share has 256 values of k at least)
       const u32 per = ceil_div(steps, want), shares = per ? ceil_div(steps, per) : 1;
       const u64 part = shares > 1 ? (u64)products * shares * m * wide * 4 : 0;
       if (part > 1ull << 30) break;
       const u64 all = tiles * shares, rounds = all / cut.slots, left = all % cut.slots;
-      // (one workgroup alone on a unit that could hold two takes 0.72 of the time)
-      const float work = (float)rounds + (left ? (cut.slots == 512 && left <= 256 ? 0.72f : 1.0f) : 0.0f);
-      const float t = work * ((float)per * cut.ks / 64 * cut.step + cut.ends) + (shares > 1 ? 4.0f + (float)part * 2 / 5e6f : 0.0f);
+      // (one workgroup alone on a unit that could hold two of 128 rows takes 0.72 of the time; with six stages a step of few workgroups is short)
+      const float work = (float)rounds + (left ? (c == 1 && left <= 256 ? 0.72f : 1.0f) : 0.0f);
+      const float step = c == 3 && all < 256 ? 0.3f + 0.6f * (float)all / 256 : cut.step;
+      float t = work * ((float)per * cut.ks / 64 * step + cut.ends);
+      // (rows along k are read in pieces of 128 bytes: that takes more workgroups, or longer; 8 tokens, 4096 -> 16384: 50 us with 512, 69 with 256)
+      const float slow = c == 3 ? (along ? 1.15f : 1.05f) : c == 2 && along && all < 512 ? 1.3f : 1.0f;
+      if (t < bytes * slow + cut.ends) t = bytes * slow + cut.ends;
+      if (shares > 1) t += 2.5f + (float)part * 2 / 5e6f;
       if (t < least) { least = t; best = {c, shares, per, part}; }
     }
   }
@@ -217,14 +227,17 @@ static ProductPlan product_plan(u64 m, u64 n, u64 k, u32 sources, u32 products, 
 template <class T, int LA, int LB, int END>
 static int product(GatedArgs a, const ProductPlan& p, u32 products, void* part, hipStream_t s) {
   a.tiles_m = ceil_div(a.m, CUTS[p.cut].rows);
-  a.tiles_n = ceil_div(a.n, END == END_PLAIN ? 256 : 128);
+  a.tiles_n = ceil_div(a.n, CUTS[p.cut].wide * (END == END_PLAIN ? 2 : 1));
   a.products = products; a.per = p.per; a.shares = p.shares; a.part = (float*)part;
   const u64 all = (u64)a.tiles_m * a.tiles_n * products * p.shares;
   if (all > G10_GROUPS_MOST / 2 - 8) return G10_EINVAL;
   const u32 grid = ceil_div(all, 8) * 8;
-  if (p.cut == 0) k_gated<T, LA, LB, 2, 4, 64, 2, END><<<grid, 512, 0, s>>>(a);
-  else if (p.cut == 1) k_gated<T, LA, LB, 1, 4, 32, 3, END><<<grid, 256, 0, s>>>(a);
-  else if constexpr (LA == ALONG) k_gated<T, LA, LB, 1, 2, 64, 2, END><<<grid, 256, 0, s>>>(a);
+  if (p.cut == 0) k_gated<T, LA, LB, 2, 4, 4, 64, 2, END><<<grid, 512, 0, s>>>(a);
+  else if (p.cut == 1) k_gated<T, LA, LB, 1, 4, 4, 32, 3, END><<<grid, 256, 0, s>>>(a);
+  else if constexpr (LA == ALONG) {
+    if (p.cut == 2) k_gated<T, LA, LB, 1, 4, 2, 64, 2, END><<<grid, 256, 0, s>>>(a);
+    else k_gated<T, LA, LB, 2, 2, 1, 64, 6, END><<<grid, 256, 0, s>>>(a);
+  }
   if (p.shares > 1) {
     const u64 groups = ((u64)a.m * (a.n / 4) * products + 255) / 256;
     k_gated_join<T, END><<<(u32)(groups < 65536 ? groups : 65536), 256, 0, s>>>(a);
@@ -248,7 +261,7 @@ static int gated_check(const g10_gated_args* g, bool back) {
 extern "C" int g10_gated_workspace(const g10_gated_args* g, uint64_t* bytes) {
   if (!bytes) return G10_EINVAL;
   G10_TRY(gated_check(g, false));
-  *bytes = g->tokens ? product_plan(g->tokens, g->inner, g->dim, 1, 1, true, false).part : 0;
+  *bytes = g->tokens ? product_plan(g->tokens, g->inner, g->dim, 1, 1, true, false, g->out_in).part : 0;
   return G10_OK;
 }
 
@@ -258,7 +271,7 @@ static int gated_forward(const g10_gated_args* g, void* ws, hipStream_t s) {
   a.a[0] = a.a[1] = g->x; a.b[0] = g->gate; a.b[1] = g->up; a.out[0] = g->h;
   a.as = g->x_stride; a.bs = g->w_stride; a.os = g->h_stride;
   a.m = g->tokens; a.n = g->inner; a.k = g->dim; a.sources = 1; a.act = g->act;
-  const ProductPlan p = product_plan(a.m, a.n, a.k, 1, 1, true, false);
+  const ProductPlan p = product_plan(a.m, a.n, a.k, 1, 1, true, false, g->out_in);
   return g->out_in ? product<T, ALONG, ALONG, END_GATED>(a, p, 1, ws, s) : product<T, ALONG, ACROSS, END_GATED>(a, p, 1, ws, s);
 }
 
@@ -277,9 +290,9 @@ struct BackPlan { ProductPlan gated, dx, dw; u64 at_part, bytes; };
 static BackPlan back_plan(const g10_gated_args* g) {
   BackPlan b{};
   const u32 wm = g->out_in ? g->inner : g->dim, wn = g->out_in ? g->dim : g->inner;
-  b.gated = product_plan(g->tokens, g->inner, g->dim, 1, 1, true, false);
-  b.dx = product_plan(g->tokens, g->dim, g->inner, 2, 1, false, false);
-  b.dw = product_plan(wm, wn, g->tokens, 1, 2, false, true);
+  b.gated = product_plan(g->tokens, g->inner, g->dim, 1, 1, true, false, g->out_in);
+  b.dx = product_plan(g->tokens, g->dim, g->inner, 2, 1, false, false, !g->out_in);
+  b.dw = product_plan(wm, wn, g->tokens, 1, 2, false, true, false);
   u64 part = b.gated.part > b.dx.part ? b.gated.part : b.dx.part;
   if (b.dw.part > part) part = b.dw.part;
   b.at_part = 2 * (((u64)g->tokens * g->inner * 2 + 255) & ~255ull);

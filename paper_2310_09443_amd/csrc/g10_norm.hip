@@ -54,16 +54,14 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float* room) {
   }
 }
 
-template <class T> struct Eight {
-  typedef T x8 __attribute__((ext_vector_type(8)));
-  typedef float f4 __attribute__((ext_vector_type(4)));
-};
+// Eight values side by side, at any address of a value: accesses to memory need not be aligned, only a row's last eight may be fewer.
+template <class T> struct Eight { typedef T x8 __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
 
 // W wavefronts to a row, NV steps of 8 values a lane; a workgroup holds 4 / W rows (W = 1) or one (W = 4, 8, 16).
-// VEC: 16-byte accesses; else value by value, any alignment.
-template <class T, bool VEC>
+// WHOLE: rows of a multiple of 8 values.
+template <class T, bool WHOLE>
 __device__ __forceinline__ void get8(const T* p, u32 d, u32 dim, float (&v)[8]) {
-  if constexpr (VEC) {
+  if (WHOLE || d + 8 <= dim) {
     typedef typename Eight<T>::x8 x8;
     const x8 r = *(const x8*)(p + d);
 #pragma unroll
@@ -73,33 +71,33 @@ __device__ __forceinline__ void get8(const T* p, u32 d, u32 dim, float (&v)[8]) 
     for (int k = 0; k < 8; ++k) v[k] = d + k < dim ? (float)p[d + k] : 0.0f;
   }
 }
-template <class T, bool VEC>
+template <class T, bool WHOLE>
 __device__ __forceinline__ void put8(T* p, u32 d, u32 dim, const float (&v)[8]) {
-  if constexpr (VEC) {
+  if (WHOLE || d + 8 <= dim) {
     typedef typename Eight<T>::x8 x8;
     x8 r;
 #pragma unroll
     for (int k = 0; k < 8; ++k) r[k] = (T)v[k];
-    __builtin_nontemporal_store(r, (x8*)(p + d));
+    __builtin_nontemporal_store(r, (x8*)(p + d));                      // (past the L2)
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
       if (d + k < dim) p[d + k] = (T)v[k];
   }
 }
-template <class T, bool VEC>
+template <class T, bool WHOLE>
 __device__ __forceinline__ void weights8(const void* w, u32 w32, u32 d, u32 dim, float none, float (&v)[8]) {
   if (!w) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = none;
   } else if (w32) {
-    get8<float, VEC>((const float*)w, d, dim, v);
+    get8<float, WHOLE>((const float*)w, d, dim, v);
   } else {
-    get8<T, VEC>((const T*)w, d, dim, v);
+    get8<T, WHOLE>((const T*)w, d, dim, v);
   }
 }
 
-template <class T, int W, int NV, bool VEC, bool BACK>
+template <class T, int W, int NV, bool WHOLE, bool BACK>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a) {
   constexpr u32 ROWS = W == 1 ? 4 : 1, LANES = 64 * W;
   __shared__ float room[4][2 * W];
@@ -108,7 +106,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
   float dw[BACK ? NV : 1][8] = {}, db[BACK ? NV : 1][8] = {};
   u32 turn = 0;
   // backward with a few steps a row, the next row is on its way while this one is worked on
-  constexpr bool AHEAD = BACK && VEC && NV <= 2;
+  constexpr bool AHEAD = BACK && WHOLE && NV <= 2;
   typedef typename Eight<T>::x8 x8;
   x8 nx[AHEAD ? NV : 1], ny[AHEAD ? NV : 1];
   auto fetch = [&](u64 row) {
@@ -122,6 +120,27 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
   if constexpr (AHEAD) {
     if (first < a.rows) fetch(first);
   }
+  // A lane's columns are the same in every row: with a few steps their weights stay in registers (16384 rows of 768 forward 11.5 -> 9.8 us; not where
+  // a workgroup has one row: 32768 of 4096 89 -> 96, fewer wavefronts fit).
+  constexpr bool KEPT = NV <= 2 && (BACK || W == 1);
+  float kw[KEPT ? NV : 1][8], kb[KEPT && !BACK ? NV : 1][8];
+  if constexpr (KEPT) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const u32 d = (i * LANES + l) * 8;
+      if (d >= a.dim) continue;
+      weights8<T, WHOLE>(a.w, a.w32, d, a.dim, 1.0f, kw[i]);
+      if constexpr (!BACK) weights8<T, WHOLE>(a.b, a.w32, d, a.dim, 0.0f, kb[i]);
+    }
+  }
+  auto weights = [&](int i, u32 d, float (&w)[8]) {
+    if constexpr (KEPT) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = kw[i][k];
+    } else {
+      weights8<T, WHOLE>(a.w, a.w32, d, a.dim, 1.0f, w);
+    }
+  };
   for (u64 row = first; row < a.rows; row += step) {
     const T* x = (const T*)a.x + (int64_t)row * a.xs;
     const T* y = BACK ? (const T*)a.dy + (int64_t)row * a.dys : nullptr;
@@ -140,8 +159,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
       for (int i = 0; i < NV; ++i) {
         const u32 d = (i * LANES + l) * 8;
         if (d < a.dim) {
-          get8<T, VEC>(x, d, a.dim, v[i]);
-          if constexpr (BACK) get8<T, VEC>(y, d, a.dim, g[i]);
+          get8<T, WHOLE>(x, d, a.dim, v[i]);
+          if constexpr (BACK) get8<T, WHOLE>(y, d, a.dim, g[i]);
         } else {
 #pragma unroll
           for (int k = 0; k < 8; ++k) { v[i][k] = 0.0f; if constexpr (BACK) g[i][k] = 0.0f; }
@@ -177,11 +196,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
         const u32 d = (i * LANES + l) * 8;
         if (d >= a.dim) continue;
         float w[8], b[8];
-        weights8<T, VEC>(a.w, a.w32, d, a.dim, 1.0f, w);
-        weights8<T, VEC>(a.b, a.w32, d, a.dim, 0.0f, b);
+        weights(i, d, w);
+        if constexpr (!KEPT) weights8<T, WHOLE>(a.b, a.w32, d, a.dim, 0.0f, b);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * r * w[k] + b[k];
-        put8<T, VEC>(out, d, a.dim, v[i]);
+        for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * r * w[k] + (KEPT ? kb[KEPT ? i : 0][k] : b[k]);
+        put8<T, WHOLE>(out, d, a.dim, v[i]);
       }
     } else {
       float t[2] = {};                                              // sums of u n and of u
@@ -190,7 +209,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
         const u32 d = (i * LANES + l) * 8;
         if (d >= a.dim) continue;
         float w[8];
-        weights8<T, VEC>(a.w, a.w32, d, a.dim, 1.0f, w);
+        weights(i, d, w);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           v[i][k] *= r;
@@ -210,7 +229,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
         if (d >= a.dim) continue;
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[i][k] = r * (g[i][k] - v[i][k] * dot - off);
-        put8<T, VEC>(out, d, a.dim, g[i]);
+        put8<T, WHOLE>(out, d, a.dim, g[i]);
       }
     }
   }
@@ -267,13 +286,13 @@ __global__ __launch_bounds__(1024) void k_norm_weights(const NormArgs a, u32 gro
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-struct NormPlan { u32 grid, waves, steps; bool vec, weights; };
+struct NormPlan { u32 grid, waves, steps; bool whole, weights; };
 
 static int norm_args(const g10_norm_args* g, bool back, NormArgs& a, NormPlan& p) {
   if (!g) return G10_EINVAL;
   if (g->type > G10_BF16 || (g->weight_type != g->type && g->weight_type != G10_F32) || g->center > 1) return G10_EINVAL;
   if (!g->dim || g->dim > 65536 || g->rows >= 0x80000000u || !(g->eps >= 0.0f) || isinf(g->eps)) return G10_EINVAL;
-  const u32 e = g->type == G10_F32 ? 4 : 2, we = g->weight_type == G10_F32 ? 4 : 2, n = 16 / e;
+  const u32 e = g->type == G10_F32 ? 4 : 2, we = g->weight_type == G10_F32 ? 4 : 2;
   if (g->rows && (!g->x || !g->out || (back && !g->dy))) return G10_EINVAL;
   if (back && g->dweight && !g->weight) return G10_EINVAL;
   for (const void* q : {g->x, (const void*)g->out, back ? g->dy : nullptr})
@@ -287,43 +306,42 @@ static int norm_args(const g10_norm_args* g, bool back, NormArgs& a, NormPlan& p
   a.xs = g->x_stride; a.dys = g->dy_stride; a.os = g->out_stride;
   a.rows = g->rows; a.dim = g->dim; a.w32 = g->weight_type == G10_F32; a.center = g->center; a.eps = g->eps;
   p.weights = a.dw || a.db;
-  p.vec = g->dim % 8 == 0 && !(((uintptr_t)g->x | (uintptr_t)g->out | (uintptr_t)g->weight | (uintptr_t)g->bias | (back ? (uintptr_t)g->dy : 0)) & 15) &&
-          g->x_stride % n == 0 && g->out_stride % n == 0 && (!back || g->dy_stride % n == 0);
+  p.whole = g->dim % 8 == 0;
   const u32 lanes = (g->dim + 7) / 8;
-  p.waves = lanes <= 128 ? 1 : lanes <= 1024 ? 4 : 16;
+  p.waves = lanes <= 128 ? 1 : lanes <= 512 ? 4 : lanes <= 1024 ? 8 : 16;
   p.steps = (lanes + 64 * p.waves - 1) / (64 * p.waves);
   if (p.steps == 3) p.steps = 4;
   if (p.steps > 4) p.steps = 8;
   const u32 rows_each = p.waves == 1 ? 4 : 1;
   const u64 groups = ((u64)a.rows + rows_each - 1) / rows_each;
-  const u32 most = back ? (p.waves == 16 ? 256u : 1024u) : 1u << 16;
+  const u32 most = back ? (p.waves == 16 ? 256u : 512u) : 1u << 16;
   p.grid = (u32)(groups < most ? groups : most);
   return G10_OK;
 }
 
-template <class T, bool VEC, bool BACK>
+template <class T, bool WHOLE, bool BACK>
 static void norm_launch(const NormArgs& a, const NormPlan& p, hipStream_t s) {
   auto go = [&](auto w, auto nv) {
     constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-    k_norm<T, W, NV, VEC, BACK><<<p.grid, W == 1 ? 256 : 64 * W, 0, s>>>(a);
+    k_norm<T, W, NV, WHOLE, BACK><<<p.grid, W == 1 ? 256 : 64 * W, 0, s>>>(a);
   };
   using std::integral_constant;
   auto pick = [&](auto w) {
-    if (p.steps == 1) go(w, integral_constant<int, 1>{});
-    else if (p.steps == 2) go(w, integral_constant<int, 2>{});
+    if (p.steps == 2) go(w, integral_constant<int, 2>{});
     else if (p.steps == 4) go(w, integral_constant<int, 4>{});
     else go(w, integral_constant<int, 8>{});
   };
   if (p.waves == 1) { if (p.steps == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 1>{}, integral_constant<int, 2>{}); }
-  else if (p.waves == 4) { if (p.steps <= 2) { if (p.steps == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 4>{}, integral_constant<int, 2>{}); } else go(integral_constant<int, 4>{}, integral_constant<int, 4>{}); }
+  else if (p.waves == 4) { if (p.steps == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 4>{}, integral_constant<int, 2>{}); }
+  else if (p.waves == 8) go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
   else pick(integral_constant<int, 16>{});
 }
 
 template <bool BACK>
 static void norm_typed(const g10_norm_args* g, const NormArgs& a, const NormPlan& p, hipStream_t s) {
-  if (g->type == G10_F32) { if (p.vec) norm_launch<float, true, BACK>(a, p, s); else norm_launch<float, false, BACK>(a, p, s); }
-  else if (g->type == G10_F16) { if (p.vec) norm_launch<_Float16, true, BACK>(a, p, s); else norm_launch<_Float16, false, BACK>(a, p, s); }
-  else { if (p.vec) norm_launch<__bf16, true, BACK>(a, p, s); else norm_launch<__bf16, false, BACK>(a, p, s); }
+  if (g->type == G10_F32) { if (p.whole) norm_launch<float, true, BACK>(a, p, s); else norm_launch<float, false, BACK>(a, p, s); }
+  else if (g->type == G10_F16) { if (p.whole) norm_launch<_Float16, true, BACK>(a, p, s); else norm_launch<_Float16, false, BACK>(a, p, s); }
+  else { if (p.whole) norm_launch<__bf16, true, BACK>(a, p, s); else norm_launch<__bf16, false, BACK>(a, p, s); }
 }
 
 extern "C" int g10_norm(const g10_norm_args* g, void* hip_stream) {

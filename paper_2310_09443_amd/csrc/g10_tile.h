@@ -1,11 +1,11 @@
 // Matrix products of 16-bit factors in tiles: C[m][n] = sum over k of A[m][k] B[k][n], summed in 32 bits.
 //
-// A workgroup of WM x 4 wavefronts makes a tile of 32 TM WM rows by 256 columns, a wavefront 32 TM rows by twice 32 columns: 32 of the
-// tile's first panel of 128 columns and the same 32 of its second one.  The panels of B need not lie side by side: a gated product takes
+// A workgroup of WM x WN wavefronts makes a tile of 32 TM WM rows by 64 WN columns, a wavefront 32 TM rows by twice 32 columns: 32 of the
+// tile's first panel of 32 WN columns and the same 32 of its second one.  The panels of B need not lie side by side: a gated product takes
 // one panel of each weight, and a value's two factors come out in one lane's registers.
 //
 // Both factors go through LDS in steps of KS = 64 or 32 along k, straight from memory (no registers), in panels of one of two layouts, as they
-// lie in memory: rows of KS values along k (ALONG), read as fragments of 8 values, or KS rows of 128 values across (ACROSS), read
+// lie in memory: rows of KS values along k (ALONG), read as fragments of 8 values, or KS rows of 128 or 64 values across (ACROSS), read
 // with the transposing LDS read.  Both orders of k are the same, so any two layouts meet.  The places of 16-byte pieces in a row are exchanged
 // so that each read takes all banks once.
 //
@@ -31,6 +31,7 @@ enum { ALONG = 0, ACROSS = 1 };
 // Exchanges of a row's pieces.
 __device__ __forceinline__ u32 swz32(u32 r) { return (r >> 2) & 3; }                     // 4 pieces to a row of 32 values
 __device__ __forceinline__ u32 swz64(u32 r) { return (r >> 1) & 7; }                     // 8 pieces to a row of 64
+__device__ __forceinline__ u32 swz64a(u32 r) { return ((r & 2) << 1) | ((r >> 2) & 3); } // 8 pieces to a row of 64 across, read transposed
 __device__ __forceinline__ u32 swz128(u32 r) { return ((r & 3) << 2) | ((r >> 2) & 3); } // 16 pieces to a row of 128
 
 // A panel of ROWS places across (KS values of k each) by NT threads: what each loads, and where it looks.
@@ -38,8 +39,8 @@ template <int LAYOUT, int ROWS, int NT, int KS>
 struct Panel {
   static constexpr int PIECES = ROWS * KS / 8, IT = (PIECES + NT - 1) / NT, BYTES = PIECES * 16;
   static constexpr int PER = LAYOUT == ALONG ? KS / 8 : ROWS / 8;                        // pieces to a row in LDS
-  static __device__ __forceinline__ u32 swz(u32 row) { return LAYOUT == ACROSS ? swz128(row) : KS == 64 ? swz64(row) : swz32(row); }
-  static_assert(LAYOUT == ALONG || ROWS == 128, "rows of 128 across");
+  static __device__ __forceinline__ u32 swz(u32 row) { return LAYOUT == ACROSS ? (ROWS == 128 ? swz128(row) : swz64a(row)) : KS == 64 ? swz64(row) : swz32(row); }
+  static_assert(LAYOUT == ALONG || ROWS == 128 || ROWS == 64, "rows of 128 or 64 across");
   u32 off[IT];
   u32 k[IT];                       // the first value of k of each piece
   // first, n: the panel's first place across, and how many there are in all (places past them repeat the last row or piece: who uses them
@@ -95,12 +96,12 @@ struct Panel {
 };
 
 // The sums of one tile.  acc[j][i]: panel j, rows 32 i of the wavefront; lane l holds row l % 32, columns res_row(r).
-template <class T, int LA, int LB, int WM, int TM, int KS, int STAGES>
+template <class T, int LA, int LB, int WM, int WN, int TM, int KS, int STAGES>
 struct Tile {
-  static constexpr int NT = 256 * WM, BM = 32 * TM * WM;
+  static constexpr int NT = 64 * WM * WN, BM = 32 * TM * WM, WIDE = 32 * WN;
   static constexpr int AROWS = LA == ALONG ? BM : 128, APANELS = BM / AROWS;
   typedef Panel<LA, AROWS, NT, KS> PA;
-  typedef Panel<LB, 128, NT, KS> PB;
+  typedef Panel<LB, WIDE, NT, KS> PB;
   static constexpr int A_BYTES = APANELS * PA::BYTES, STAGE = A_BYTES + 2 * PB::BYTES, LDS = STAGES * STAGE;
   static constexpr int LOADS = APANELS * PA::IT + 2 * PB::IT;                            // of a wavefront and step
   typedef typename Vec<T>::x8 x8;
@@ -116,7 +117,7 @@ struct Tile {
   template <class NEXT>
   static __device__ __forceinline__ void run(f32x16 (&acc)[2][TM], u32 lds0, int steps, const PA (&pa)[APANELS], const PB (&pb)[2], Walk w, int64_t sa, int64_t sb,
                                              bool whole, NEXT&& next) {
-    const u32 t = threadIdx.x, wave = uniform(wave_id()), wm = wave / 4, wn = wave % 4;
+    const u32 t = threadIdx.x, wave = uniform(wave_id()), wm = wave / WN, wn = wave % WN;
     int loaded = 0;
     u32 to = lds0;
     auto load = [&]() {

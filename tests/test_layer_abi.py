@@ -202,5 +202,20 @@ def test_every_tile_has_a_workgroup(launches):
             assert rc == 0 and "k_gated" in ran[0][0], (m, k, n)
             shares = room // (m * 2 * n * 4) or 1
             assert len(ran) == (2 if shares > 1 else 1) and room == (shares * m * 2 * n * 4 if shares > 1 else 0)
-            fits = [rows for rows in (32, 64, 128, 256) if -(-m // rows) * -(-n // 128) * shares <= ran[0][1] < -(-m // rows) * -(-n // 128) * shares + 8]
-            assert fits, (m, k, n, ran)
+            tiles = [-(-m // rows) * -(-n // wide) * shares for rows, wide in ((256, 128), (128, 128), (64, 128), (64, 64))]
+            assert any(t <= ran[0][1] < t + 8 for t in tiles), (m, k, n, ran)
+
+
+def test_every_cut_of_tiles_is_reached(launches):
+    """Large products, middling ones, few tokens on large weights and on small ones; sums in shares and whole."""
+    sizes = [(8192, 4096, 16384), (16384, 768, 2048), (2048, 1024, 2816), (300, 512, 2048), (64, 4096, 16384), (8, 4096, 16384), (16, 512, 2048), (100, 4096, 4096)]
+    seen = set()
+    for out_in in (0, 1):
+        for name, more in (("g10_gated", {}), ("g10_gated_backward", {})):
+            calls = [(name, dict(tokens=m, dim=k, inner=n, out_in=out_in, x_stride=k, dx_stride=k, w_stride=k if out_in else n, dw_stride=k if out_in else n, h_stride=n, dh_stride=n))
+                     for m, k, n in sizes]
+            for rc, ran, _ in launches(*calls):
+                assert rc == 0
+                seen |= {x[0] for x in ran}
+    cuts = {tuple(part for part in ("Li2ELi4ELi4ELi64ELi2", "Li1ELi4ELi4ELi32ELi3", "Li1ELi4ELi2ELi64ELi2", "Li2ELi2ELi1ELi64ELi6") if part in x) for x in seen if "join" not in x}
+    assert cuts == {("Li2ELi4ELi4ELi64ELi2",), ("Li1ELi4ELi4ELi32ELi3",), ("Li1ELi4ELi2ELi64ELi2",), ("Li2ELi2ELi1ELi64ELi6",)} and any("join" in x for x in seen), seen
