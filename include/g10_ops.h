@@ -235,17 +235,18 @@ int g10_log_probs_backward(const g10_log_probs_args *args, void *hip_stream);
 
 typedef struct {
   const void *x;             /* [tokens][dim]                                                  */
-  const void *gate, *up;     /* [dim][inner], or with out_in [inner][dim]; of one stride       */
+  const void *gate, *up;     /* [dim][inner], or with out_in [inner][dim]                      */
   void *h;                   /* forward: [tokens][inner]                                       */
   const void *dh;            /* backward: [tokens][inner]                                      */
   void *dx;                  /* backward: [tokens][dim]                                        */
   void *dgate, *dup;         /* backward: laid out as the weights                              */
-  int64_t x_stride, w_stride, h_stride, dh_stride, dx_stride, dw_stride; /* of rows              */
-  uint32_t tokens, dim, inner; /* dim and inner multiples of 8 up to 2^20, tokens below 2^31     */
+  int64_t x_stride, gate_stride, up_stride, h_stride, dh_stride, dx_stride, dw_stride; /* of rows, not shorter than they are */
+  uint32_t tokens, dim, inner; /* dim and inner 1 .. 2^20, tokens below 2^31                     */
   uint32_t act, out_in;
   uint32_t type;             /* G10_F16 or G10_BF16                                            */
 } g10_gated_args;
-/* Pointers and strides are multiples of 16 bytes (of 8 elements), strides from a row's length to 2^22 elements; else G10_EINVAL. */
+/* Inputs whose pointers and strides are multiples of 16 bytes (of 8 elements) and whose rows are multiples of 8 elements, with strides up to 2^22 and
+ * one stride for both weights, are read where they lie; others are laid out in the workspace first.  Outputs may lie anywhere. */
 
 int g10_gated_workspace(const g10_gated_args *args, uint64_t *bytes);
 int g10_gated(const g10_gated_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);

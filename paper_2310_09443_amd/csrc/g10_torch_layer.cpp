@@ -248,27 +248,11 @@ static at::Tensor log_probs_backward(const Maybe& dlogp, const at::Tensor& logit
 }
 
 // ----------------------------------------------------------------------------------------------------------- gated MLP
-static int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
-static bool lies_well(const at::Tensor& t) {                                       // as the kernels read a [rows, columns]
-  return !((uintptr_t)t.const_data_ptr() & 15) && t.size(1) % 8 == 0 && t.stride(1) == 1 && row_stride(t) % 8 == 0 && row_stride(t) >= t.size(1) && row_stride(t) <= (1 << 22);
-}
-// The same with zeros up to multiples of 8 where that is asked for, in memory of its own.
-static at::Tensor laid_out(const at::Tensor& t, int64_t rows, int64_t columns) {
-  at::Tensor r = at::zeros({rows, columns}, t.options());
-  r.narrow(0, 0, t.size(0)).narrow(1, 0, t.size(1)).copy_(t);
-  return r;
-}
-
 struct GatedCall {
   g10_gated_args a{};
   at::Tensor x, w[2];
   at::Device dev{at::kCPU};
-  int64_t tokens, dim, inner;      // as given
 };
-static at::Tensor gated_rows(const at::Tensor& t, int64_t width) {
-  const at::Tensor r = rows_of(t);
-  return !r.numel() || lies_well(r) ? r : laid_out(r, r.size(0), up8(width));
-}
 static void gated_args(GatedCall& c, const at::Tensor& x, const at::Tensor& gate, const at::Tensor& up, const std::string& act) {
   const at::ScalarType dt = float_type(x, "x");
   c.dev = x.device();
@@ -278,24 +262,20 @@ static void gated_args(GatedCall& c, const at::Tensor& x, const at::Tensor& gate
   TORCH_CHECK_VALUE(gate.dim() == 2 && gate.size(0) == x.size(-1) && gate.size(1) > 0 && gate.scalar_type() == dt, "gate must be [dim, inner], of the type of x");
   TORCH_CHECK_VALUE(up.sizes() == gate.sizes() && up.scalar_type() == dt, "up must have the shape and type of gate");
   TORCH_CHECK_VALUE(act == "silu" || act == "gelu", "act must be silu or gelu");
-  c.dim = x.size(-1); c.inner = gate.size(1); c.tokens = x.numel() / c.dim;
-  TORCH_CHECK_VALUE(c.dim <= 1 << 20 && c.inner <= 1 << 20 && c.tokens < 0x80000000ll, "dim and inner must be up to 2^20, tokens below 2^31");
+  const int64_t dim = x.size(-1), inner = gate.size(1), tokens = x.numel() / dim;
+  TORCH_CHECK_VALUE(dim <= 1 << 20 && inner <= 1 << 20 && tokens < 0x80000000ll, "dim and inner must be up to 2^20, tokens below 2^31");
   const bool out_in = gate.stride(1) != 1 && gate.stride(0) == 1;                  // a linear layer's weight, transposed
-  const at::Tensor given[2] = {out_in ? gate.t() : gate, out_in ? up.t() : up};
-  const bool alike = row_stride(given[0]) == row_stride(given[1]);
-  for (int i = 0; i < 2; ++i) c.w[i] = alike && lies_well(given[i]) && given[i].size(0) % 8 == 0 ? given[i] : laid_out(given[i], up8(given[i].size(0)), up8(given[i].size(1)));
-  if (row_stride(c.w[0]) != row_stride(c.w[1])) c.w[0] = laid_out(c.w[0], c.w[0].size(0), c.w[0].size(1)), c.w[1] = laid_out(c.w[1], c.w[1].size(0), c.w[1].size(1));
-  c.x = gated_rows(x, c.dim);
+  auto rows = [](const at::Tensor& t) { return (t.stride(1) == 1 || t.size(1) == 1) && row_stride(t) >= t.size(1) ? t : t.contiguous(); };
+  c.w[0] = rows(out_in ? gate.t() : gate);
+  c.w[1] = rows(out_in ? up.t() : up);
+  c.x = rows(rows_of(x));
   g10_gated_args& a = c.a;
   a.x = in_of(c.x); a.gate = c.w[0].const_data_ptr(); a.up = c.w[1].const_data_ptr();
-  a.x_stride = row_stride(c.x); a.w_stride = row_stride(c.w[0]);
-  a.tokens = (uint32_t)c.tokens; a.dim = (uint32_t)up8(c.dim); a.inner = (uint32_t)up8(c.inner);
+  a.x_stride = row_stride(c.x); a.gate_stride = row_stride(c.w[0]); a.up_stride = row_stride(c.w[1]);
+  a.tokens = (uint32_t)tokens; a.dim = (uint32_t)dim; a.inner = (uint32_t)inner;
   a.act = act == "silu" ? G10_ACT_SILU : G10_ACT_GELU;
   a.out_in = out_in;
   a.type = (uint32_t)type_of(dt);
-}
-static at::Tensor as_given(const at::Tensor& t, int64_t rows, int64_t columns) {
-  return t.size(0) == rows && t.size(1) == columns ? t : t.narrow(0, 0, rows).narrow(1, 0, columns).contiguous();
 }
 static std::vector<int64_t> with_last(const at::Tensor& x, int64_t n) {
   std::vector<int64_t> s = x.sizes().vec();
@@ -307,7 +287,7 @@ static at::Tensor gated(const at::Tensor& x, const at::Tensor& gate, const at::T
   GatedCall c;
   gated_args(c, x, gate, up, act);
   g10_gated_args& a = c.a;
-  at::Tensor h = empty({c.tokens, (int64_t)a.inner}, x.scalar_type(), c.dev);
+  at::Tensor h = empty(with_last(x, a.inner), x.scalar_type(), c.dev);
   a.h = h.numel() ? h.mutable_data_ptr() : nullptr;
   a.h_stride = a.inner;
   const c10::DeviceGuard guard(c.dev);
@@ -315,7 +295,7 @@ static at::Tensor gated(const at::Tensor& x, const at::Tensor& gate, const at::T
   check(lib.gated_workspace(&a, &n), "g10_gated_workspace");
   const at::Tensor ws = workspace(n, c.dev);
   check(lib.gated(&a, at_of(ws), n, stream_of(c.dev)), "g10_gated");
-  return as_given(h, c.tokens, c.inner).view(with_last(x, c.inner));
+  return h;
 }
 
 static py::tuple gated_backward(const at::Tensor& dh_in, const at::Tensor& x, const at::Tensor& gate, const at::Tensor& up, const std::string& act) {
@@ -323,21 +303,20 @@ static py::tuple gated_backward(const at::Tensor& dh_in, const at::Tensor& x, co
   gated_args(c, x, gate, up, act);
   g10_gated_args& a = c.a;
   on_device(dh_in, "dh", &c.dev);
-  TORCH_CHECK_VALUE(dh_in.sizes() == at::IntArrayRef(with_last(x, c.inner)) && dh_in.scalar_type() == x.scalar_type(), "dh must have the shape and type of h");
-  const at::Tensor dh = gated_rows(dh_in, c.inner);
-  const int64_t rows = c.w[0].size(0), columns = c.w[0].size(1);
-  at::Tensor dx = empty({c.tokens, (int64_t)a.dim}, x.scalar_type(), c.dev), dw[2];
-  for (at::Tensor& t : dw) t = empty({rows, columns}, x.scalar_type(), c.dev);
+  TORCH_CHECK_VALUE(dh_in.sizes() == at::IntArrayRef(with_last(x, a.inner)) && dh_in.scalar_type() == x.scalar_type(), "dh must have the shape and type of h");
+  at::Tensor dh = rows_of(dh_in);
+  if (row_stride(dh) < dh.size(1)) dh = dh.contiguous();                           // (a row for all tokens)
+  at::Tensor dx = empty(x.sizes(), x.scalar_type(), c.dev), dw[2];
+  for (at::Tensor& t : dw) t = empty(c.w[0].sizes(), x.scalar_type(), c.dev);
   a.dh = in_of(dh); a.dx = dx.numel() ? dx.mutable_data_ptr() : nullptr;
   a.dgate = dw[0].mutable_data_ptr(); a.dup = dw[1].mutable_data_ptr();
-  a.dh_stride = row_stride(dh); a.dx_stride = a.dim; a.dw_stride = columns;
+  a.dh_stride = row_stride(dh); a.dx_stride = a.dim; a.dw_stride = c.w[0].size(1);
   const c10::DeviceGuard guard(c.dev);
   uint64_t n = 0;
   check(lib.gated_backward_workspace(&a, &n), "g10_gated_backward_workspace");
   const at::Tensor ws = workspace(n, c.dev);
   check(lib.gated_backward(&a, at_of(ws), n, stream_of(c.dev)), "g10_gated_backward");
-  for (at::Tensor& t : dw) t = a.out_in ? as_given(t, c.inner, c.dim).t() : as_given(t, c.dim, c.inner);
-  return py::make_tuple(as_given(dx, c.tokens, c.dim).view(x.sizes()), dw[0], dw[1]);
+  return py::make_tuple(dx, a.out_in ? dw[0].t() : dw[0], a.out_in ? dw[1].t() : dw[1]);
 }
 
 void layer_calls(py::module_& m) {

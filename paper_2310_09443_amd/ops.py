@@ -91,7 +91,7 @@ class _LogProbs(C.Structure):
 
 class _Gated(C.Structure):
     _fields_ = [(n, _PTR) for n in ("x", "gate", "up", "h", "dh", "dx", "dgate", "dup")] + \
-               [(n + "_stride", _I64) for n in ("x", "w", "h", "dh", "dx", "dw")] + \
+               [(n + "_stride", _I64) for n in ("x", "gate", "up", "h", "dh", "dx", "dw")] + \
                [(n, _U32) for n in ("tokens", "dim", "inner", "act", "out_in", "type")]
 
 

@@ -100,10 +100,10 @@ def test_refusals(ops):
             bad()
 
 
-@pytest.mark.parametrize("tokens", [1023, 1024, 1025, 131072, 131073, 300000])
+@pytest.mark.parametrize("tokens", [1, 64, 255, 4096, 4097, 5121, 131072, 131073, 300000])
 def test_sorts(ops, tokens):
-    """Tiles of the sort of one round and of several, with ids of two and three digits."""
-    for vocab in (300, 300000):
+    """Sorted in one workgroup, in tiles of one round and of several, with ids of one, two and three digits."""
+    for vocab in (300, 30000, 300000):
         check(ops, *make(tokens, vocab, 8, torch.float32, seed=vocab, frequent=vocab == 300))
 
 

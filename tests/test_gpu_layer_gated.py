@@ -57,10 +57,13 @@ def test_activations(ops, act):
     check(ops, x, gate, up, dh * 0.01, act)
 
 
-def test_odd_sizes_and_layouts(ops):
-    for tokens, dim, inner in ((5, 1, 1), (9, 7, 13), (33, 65, 100), (2, 1001, 3)):
-        for out_in in (False, True):
-            check(ops, *make(tokens, dim, inner, torch.bfloat16, out_in, seed=dim))
+@pytest.mark.parametrize("out_in", [False, True])
+@pytest.mark.parametrize("tokens, dim, inner", [(5, 1, 1), (9, 7, 13), (33, 65, 100), (2, 1001, 3), (70, 129, 259), (1, 2500, 70), (300, 517, 1030), (1100, 333, 1717)])
+def test_odd_sizes(ops, tokens, dim, inner, out_in):
+    check(ops, *make(tokens, dim, inner, torch.bfloat16 if dim % 2 else torch.float16, out_in, seed=dim))
+
+
+def test_layouts(ops):
     x, gate, up, dh = make(24, 64, 128, torch.bfloat16)
     check(ops, x.view(2, 3, 4, 64), gate, up, dh.view(2, 3, 4, 128))
     check(ops, x.view(4, 6, 64).transpose(0, 1), gate, up, dh.view(6, 4, 128))

@@ -157,7 +157,7 @@ def test_rows_behind_the_last_are_left_as_they_were(ops):
     dh = torch.randn(rows, inner, device="cuda").to(BF)
     p = lambda t: t.data_ptr()                                                                          # noqa: E731
     room = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
-    a = ops._Gated(x=p(x), gate=p(wg), up=p(wu), h=p(h), dh=p(dh), dx=p(dx), dgate=p(dg), dup=p(du), x_stride=dim, w_stride=inner, h_stride=h.stride(0), dh_stride=inner,
+    a = ops._Gated(x=p(x), gate=p(wg), up=p(wu), h=p(h), dh=p(dh), dx=p(dx), dgate=p(dg), dup=p(du), x_stride=dim, gate_stride=inner, up_stride=inner, h_stride=h.stride(0), dh_stride=inner,
                    dx_stride=dx.stride(0), dw_stride=dg.stride(0), tokens=rows, dim=dim, inner=inner, act=0, type=ops.BF16)
     assert lib.g10_gated(C.byref(a), p(room), room.numel(), stream) == 0 and lib.g10_gated_backward(C.byref(a), p(room), room.numel(), stream) == 0
     assert torch.equal(h[:rows, :inner], ops.g10_gated(x, wg, wu))

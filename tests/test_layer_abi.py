@@ -54,7 +54,7 @@ def log_probs_args(**kw):
 
 
 def gated_args(**kw):
-    return fill(ops._Gated, **dict(dict(x=4096, gate=4096, up=4096, h=4096, dh=4096, dx=4096, dgate=4096, dup=4096, x_stride=64, w_stride=128, h_stride=128, dh_stride=128,
+    return fill(ops._Gated, **dict(dict(x=4096, gate=4096, up=4096, h=4096, dh=4096, dx=4096, dgate=4096, dup=4096, x_stride=64, gate_stride=128, up_stride=128, h_stride=128, dh_stride=128,
                                         dx_stride=64, dw_stride=128, tokens=10, dim=64, inner=128, act=ops.SILU, type=ops.BF16), **kw))
 
 
@@ -85,9 +85,8 @@ BOTH = [("embed", dict(type=3)), ("embed", dict(dim=0)), ("embed", dict(dim=6553
         ("log_probs", dict(type=3)), ("log_probs", dict(scale=0.0)), ("log_probs", dict(scale=float("nan"))), ("log_probs", dict(scale=float("inf"))),
         ("log_probs", dict(vocab=0)), ("log_probs", dict(vocab=1 << 31)), ("log_probs", dict(rows=1 << 31)), ("log_probs", dict(logits=None)), ("log_probs", dict(lse=None)),
         ("log_probs", dict(logits=4097)), ("log_probs", dict(tokens=4100)),
-        ("gated", dict(type=ops.F32)), ("gated", dict(act=2)), ("gated", dict(out_in=2)), ("gated", dict(dim=0)), ("gated", dict(dim=60)), ("gated", dict(inner=132)),
-        ("gated", dict(dim=(1 << 20) + 8)), ("gated", dict(tokens=1 << 31)), ("gated", dict(x=None)), ("gated", dict(gate=4104)), ("gated", dict(up=None)),
-        ("gated", dict(x_stride=56)), ("gated", dict(w_stride=132)), ("gated", dict(w_stride=(1 << 22) + 8)), ("gated", dict(out_in=1, w_stride=56))]
+        ("gated", dict(type=ops.F32)), ("gated", dict(act=2)), ("gated", dict(out_in=2)), ("gated", dict(dim=0)), ("gated", dict(dim=(1 << 20) + 8)), ("gated", dict(tokens=1 << 31)), ("gated", dict(x=None)), ("gated", dict(gate=4097)), ("gated", dict(up=None)),
+        ("gated", dict(x_stride=56)), ("gated", dict(up_stride=127)), ("gated", dict(gate_stride=-128)), ("gated", dict(out_in=1, gate_stride=56))]
 
 
 @pytest.mark.parametrize("op, bad", BOTH)
@@ -103,8 +102,8 @@ def test_both_passes_refuse(op, bad):
                                        ("norm_backward", dict(dweight=4097)), ("log_probs", dict(top=65)), ("log_probs", dict(top=5, vocab=4)),
                                        ("log_probs", dict(logp=None)), ("log_probs", dict(top_ids=None)), ("log_probs", dict(top_logp=None)),
                                        ("log_probs_backward", dict(dlogits=None)), ("log_probs_backward", dict(tokens=None)), ("log_probs_backward", dict(entropy=None)),
-                                       ("log_probs_backward", dict(dlogits=4097)), ("gated", dict(h=None)), ("gated", dict(h_stride=120)), ("gated_backward", dict(dh=4104)),
-                                       ("gated_backward", dict(dx=None)), ("gated_backward", dict(dgate=None)), ("gated_backward", dict(dup=4100)),
+                                       ("log_probs_backward", dict(dlogits=4097)), ("gated", dict(h=None)), ("gated", dict(h_stride=120)), ("gated_backward", dict(dh=4097)),
+                                       ("gated_backward", dict(dx=None)), ("gated_backward", dict(dgate=None)), ("gated_backward", dict(dup=4101)),
                                        ("gated_backward", dict(dw_stride=120)), ("gated_backward", dict(dx_stride=60))])
 def test_one_pass_refuses(name, bad):
     assert call(ops._load(), "g10_" + name, C.byref(MAKE["g10_" + name](**bad))) == binding.EINVAL
@@ -172,8 +171,8 @@ def test_largest_sizes_fit_into_their_grids(launches):
     calls = [("g10_embed", dict(tokens=BIG, dim=8)), ("g10_embed", dict(tokens=BIG, dim=65535)), ("g10_embed_backward", dict(tokens=BIG, vocab=BIG, dim=8)),
              ("g10_embed_backward", dict(tokens=0, vocab=BIG)), ("g10_norm", dict(rows=BIG, dim=8)), ("g10_norm_backward", dict(rows=BIG, dim=65536)),
              ("g10_log_probs", dict(rows=BIG, vocab=100)), ("g10_log_probs", dict(rows=3, vocab=BIG)), ("g10_log_probs_backward", dict(rows=BIG)),
-             ("g10_gated", dict(tokens=1 << 24, inner=1 << 10, w_stride=1 << 10, h_stride=1 << 10)),
-             ("g10_gated_backward", dict(tokens=1 << 22, inner=1 << 10, w_stride=1 << 10, dh_stride=1 << 10, dw_stride=1 << 10))]
+             ("g10_gated", dict(tokens=1 << 24, inner=1 << 10, gate_stride=1 << 10, up_stride=1 << 10, h_stride=1 << 10)),
+             ("g10_gated_backward", dict(tokens=1 << 22, inner=1 << 10, gate_stride=1 << 10, up_stride=1 << 10, dh_stride=1 << 10, dw_stride=1 << 10))]
     for c, (rc, ran, n) in zip(calls, launches(*calls)):
         assert rc == 0 and ran, c
         for name, groups, threads in ran:
@@ -181,7 +180,7 @@ def test_largest_sizes_fit_into_their_grids(launches):
 
 
 def test_more_tiles_than_a_grid_holds_are_refused(launches):
-    kw = dict(dim=8, inner=1 << 20, w_stride=1 << 20, h_stride=1 << 20, x_stride=8)
+    kw = dict(dim=8, inner=1 << 20, gate_stride=1 << 20, up_stride=1 << 20, h_stride=1 << 20, x_stride=8)
     (rc, ran, _), (rc1, ran1, _) = launches(("g10_gated", dict(tokens=BIG, **kw)), ("g10_gated", dict(tokens=4096, **kw)))
     assert rc == binding.EINVAL and not ran and rc1 == 0 and len(ran1) == 1
 
@@ -197,7 +196,7 @@ def test_every_tile_has_a_workgroup(launches):
     """Of a product's tiles, their rows by their columns by the shares of the sum (or the products side by side)."""
     sizes = [(1, 64, 128), (32, 4096, 16384), (33, 4096, 16384), (5001, 1000, 2744), (8192, 4096, 16384), (100, 8, 8), (300, 12000, 64)]
     for out_in in (0, 1):
-        calls = [("g10_gated", dict(tokens=m, dim=k, inner=n, out_in=out_in, x_stride=k, w_stride=k if out_in else n, h_stride=n)) for m, k, n in sizes]
+        calls = [("g10_gated", dict(tokens=m, dim=k, inner=n, out_in=out_in, x_stride=k, gate_stride=k if out_in else n, up_stride=k if out_in else n, h_stride=n)) for m, k, n in sizes]
         for (m, k, n), (rc, ran, room) in zip(sizes, launches(*calls)):
             assert rc == 0 and "k_gated" in ran[0][0], (m, k, n)
             shares = room // (m * 2 * n * 4) or 1
@@ -212,7 +211,7 @@ def test_every_cut_of_tiles_is_reached(launches):
     seen = set()
     for out_in in (0, 1):
         for name, more in (("g10_gated", {}), ("g10_gated_backward", {})):
-            calls = [(name, dict(tokens=m, dim=k, inner=n, out_in=out_in, x_stride=k, dx_stride=k, w_stride=k if out_in else n, dw_stride=k if out_in else n, h_stride=n, dh_stride=n))
+            calls = [(name, dict(tokens=m, dim=k, inner=n, out_in=out_in, x_stride=k, dx_stride=k, gate_stride=k if out_in else n, up_stride=k if out_in else n, dw_stride=k if out_in else n, h_stride=n, dh_stride=n))
                      for m, k, n in sizes]
             for rc, ran, _ in launches(*calls):
                 assert rc == 0
