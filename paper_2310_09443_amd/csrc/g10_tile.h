@@ -37,7 +37,8 @@ __device__ __forceinline__ u32 swz128(u32 r) { return ((r & 3) << 2) | ((r >> 2)
 // A panel of ROWS places across (KS values of k each) by NT threads: what each loads, and where it looks.
 template <int LAYOUT, int ROWS, int NT, int KS>
 struct Panel {
-  static constexpr int PIECES = ROWS * KS / 8, IT = (PIECES + NT - 1) / NT, BYTES = PIECES * 16;
+  static constexpr int PIECES = ROWS * KS / 8, IT = PIECES / NT, BYTES = PIECES * 16;
+  static_assert(PIECES % NT == 0, "whole rounds");
   static constexpr int PER = LAYOUT == ALONG ? KS / 8 : ROWS / 8;                        // pieces to a row in LDS
   static __device__ __forceinline__ u32 swz(u32 row) { return LAYOUT == ACROSS ? (ROWS == 128 ? swz128(row) : swz64a(row)) : KS == 64 ? swz64(row) : swz32(row); }
   static_assert(LAYOUT == ALONG || ROWS == 128 || ROWS == 64, "rows of 128 or 64 across");
@@ -66,14 +67,12 @@ struct Panel {
     return (const char*)p + (LAYOUT == ALONG ? (int64_t)first * stride : (int64_t)first) * 2 + step * bytes(stride);
   }
   static __device__ __forceinline__ int64_t bytes(int64_t stride) { return (LAYOUT == ALONG ? (int64_t)KS : KS * stride) * 2; }
-  // lds: the panel + this wavefront's first piece.  left: values of k from the step's first on; pieces past them become zeros.
-  __device__ __forceinline__ void load(const char* at, u32 lds, u32 left, u32 t) const {
-#pragma unroll
-    for (int i = 0; i < IT; ++i) {
-      if (PIECES % NT && i * NT + (int)t >= PIECES) continue;                            // (whole wavefronts)
-      if (left >= KS || k[i] < left) load_piece(at, off[i], lds + (u32)(i * NT * 16));
-      else *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(lds + (u32)(i * NT * 16) + lane_id() * 16) = u32x4{};
-    }
+  // lds: the panel + this wavefront's first piece
+  __device__ __forceinline__ void load(int i, const char* at, u32 lds) const { load_piece(at, off[i], lds + (u32)(i * NT * 16)); }
+  // left: values of k from the step's first on; pieces past them become zeros
+  __device__ __forceinline__ void load_short(int i, const char* at, u32 lds, u32 left) const {
+    if (k[i] < left) load_piece(at, off[i], lds + (u32)(i * NT * 16));
+    else *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(lds + (u32)(i * NT * 16) + lane_id() * 16) = u32x4{};
   }
   // The base address of a lane's fragments.
   static __device__ __forceinline__ u32 base(u32 panel) {
@@ -117,16 +116,35 @@ struct Tile {
   template <class NEXT>
   static __device__ __forceinline__ void run(f32x16 (&acc)[2][TM], u32 lds0, int steps, const PA (&pa)[APANELS], const PB (&pb)[2], Walk w, int64_t sa, int64_t sb,
                                              bool whole, NEXT&& next) {
-    const u32 t = threadIdx.x, wave = uniform(wave_id()), wm = wave / WN, wn = wave % WN;
+    const u32 wave = uniform(wave_id()), wm = wave / WN, wn = wave % WN;
     int loaded = 0;
     u32 to = lds0;
-    auto load = [&]() {
-      if (loaded >= steps) return;
+    // one load of a step's LOADS; the last one goes on to the next step
+    auto load = [&](int n) {
       const u32 at = to + wave * 1024;
 #pragma unroll
-      for (int i = 0; i < APANELS; ++i) { pa[i].load(w.a[i], at + i * PA::BYTES, w.left, t); w.a[i] += sa; }
+      for (int i = 0; i < APANELS; ++i)
+        if (n / PA::IT == i && n < APANELS * PA::IT) pa[i].load(n % PA::IT, w.a[i], at + i * PA::BYTES);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) { pb[j].load(w.b[j], at + A_BYTES + j * PB::BYTES, w.left, t); w.b[j] += sb; }
+      for (int j = 0; j < 2; ++j)
+        if (n >= APANELS * PA::IT && (n - APANELS * PA::IT) / PB::IT == j) pb[j].load((n - APANELS * PA::IT) % PB::IT, w.b[j], at + A_BYTES + j * PB::BYTES);
+    };
+    auto load_short = [&]() {
+      const u32 at = to + wave * 1024;
+#pragma unroll
+      for (int i = 0; i < APANELS; ++i)
+#pragma unroll
+        for (int n = 0; n < PA::IT; ++n) pa[i].load_short(n, w.a[i], at + i * PA::BYTES, w.left);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int n = 0; n < PB::IT; ++n) pb[j].load_short(n, w.b[j], at + A_BYTES + j * PB::BYTES, w.left);
+    };
+    auto loaded_one = [&]() {
+#pragma unroll
+      for (int i = 0; i < APANELS; ++i) w.a[i] += sa;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) w.b[j] += sb;
       if (w.left > KS) w.left -= KS; else next(w);
       ++loaded;
       to = to + STAGE < lds0 + LDS ? to + STAGE : lds0;
@@ -134,7 +152,7 @@ struct Tile {
     const u32 a_off = LA == ALONG ? wm * (32 * TM * KS * 2) : ((wm * TM * 32) / 128) * (u32)PA::BYTES, a_blk = LA == ALONG ? 0 : (wm * TM) % 4;
     const u32 ab = PA::base(lds0 + a_off) ^ (a_blk << 6), bb = PB::base(lds0 + A_BYTES) ^ (LB == ALONG ? 0 : wn << 6);
     const u32 b_off = LB == ALONG ? wn * (32 * KS * 2) : 0;
-    x8 fa[2][TM], fb[2][2];
+    x8 fa[2][TM] = {}, fb[2][2] = {};
     auto read = [&](int s, u32 at, int kk) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) fb[s][j] = PB::template frag<T>(bb + at + b_off + j * PB::BYTES, 0, kk);
@@ -147,15 +165,38 @@ struct Tile {
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[j][i] = Vec<T>::mfma(fb[s][j], fa[s][i], acc[j][i]);
     };
-    for (int i = 0; i < STAGES - 1; ++i) load();
+    for (int i = 0; i < STAGES - 1 && loaded < steps; ++i) {
+      if (w.left >= KS) {
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) load(n);
+      } else {
+        load_short();
+      }
+      loaded_one();
+    }
     u32 from = 0;
     for (int step = 0; step < steps; ++step) {
       // (fewer loads are on their way at the end: all are waited for there)
       if (STAGES > 2 && whole && loaded < steps) lds_settled<LOADS * (STAGES - 2)>(); else lds_settled<0>();
       __syncthreads();
-      load();
       read(0, from, 0);
-      if (step) { hold(); multiply(1); }
+      hold();
+      // the last products of the step before (at first of zeros), with the next loads between them: a wavefront that issues all loads at a stretch
+      // leaves the matrix unit without work
+      const bool more = loaded < steps, full = more && w.left >= KS;
+      if (more && !full) load_short();
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (full) {
+#pragma unroll
+          for (int n = i * LOADS / TM; n < (i + 1) * LOADS / TM; ++n) load(n);
+        }
+        hold();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[j][i] = Vec<T>::mfma(fb[1][j], fa[1][i], acc[j][i]);
+        hold();
+      }
+      if (more) loaded_one();
 #pragma unroll
       for (int kk = 1; kk < KS / 16; ++kk) {
         hold();
