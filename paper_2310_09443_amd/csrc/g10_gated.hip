@@ -191,12 +191,12 @@ __global__ __launch_bounds__(256) void k_gated_join(const GatedArgs a) {
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-// How a product's tiles are cut, by what they cost: us of 64 values of k with every unit full, and of a tile's beginning and end.  Measured in
-// bfloat16: 8192 tokens, 4096 -> 16384 takes 1851 us in tiles of 256 rows, 2031 with the steps of half the length and four stages (more barriers; further
-// ahead does not help), 1988 in tiles of 128; 5001 tokens, 1000 -> 2744 78 and 88; the weights' gradients of 16384 tokens, 768 -> 2048, 376 in 48 tiles of 256
-// rows, 333 in 96 of 128, 165 with the sum of the 256-row ones in three shares.  Few tokens are bound by the weights' bytes and by the way from memory
-// to LDS and back: panels of 64 columns and six stages are more workgroups with more on their way (16 tokens, 512 -> 2048: 8.2 us for 9.7; 64 tokens, 4096 ->
-// 16384: 57 for 63).
+// How a product's tiles are cut, by what they cost: us of 64 values of k with every unit full, and of a tile's beginning and end.  Measured in bfloat16:
+// 2048 tokens, 4096 -> 16384, forward 464 us in tiles of 256 rows, 497 of 128, 501 of 256 with steps half as long and twice the stages (more barriers; loads
+// further ahead do not help); 5001 tokens, 1000 -> 2744, 78 and 88; the weights' gradients of 16384 tokens, 768 -> 2048, 376 in 48 tiles of 256 rows, 333 in
+// 96 of 128, 165 with the sum of the former in three shares, 121 in five.  Few tokens are bound by the weights' bytes and by the way from memory to LDS and
+// back: panels of 64 columns and six stages are more workgroups with more on their way (16 tokens, 512 -> 2048: 8 us for 9.7; 64 tokens, 4096 -> 16384:
+// 56 for 63).
 struct TileCut { u32 rows, wide, ks, slots; float step, ends; };      // wide: columns of a panel
 static const TileCut CUTS[4] = {{256, 128, 64, 256, 1.65f, 9.0f}, {128, 128, 32, 512, 1.85f, 7.0f}, {64, 128, 64, 512, 1.1f, 6.0f}, {64, 64, 64, 256, 0.9f, 4.5f}};
 
