@@ -11,8 +11,6 @@
 
 #include <math.h>
 
-typedef float f4 __attribute__((ext_vector_type(4)));
-
 struct EmbedArgs {
   const void *ids, *table, *dout;
   void *out, *dtable;
@@ -29,24 +27,28 @@ struct EmbedArgs {
   u32 sum_groups;                  // workgroups that sum; the others clear rows without tokens
 };
 
-// N values side by side, at any address of a value: accesses to memory need not be aligned, only a row's last N may be fewer.  WHOLE: rows of a
-// multiple of N values.
+// N values side by side, at any address of a value: accesses to memory need not be aligned.  A row's last lane takes the row's last N values, whatever
+// it shares with the lane before it: both work out and write the same.  (Value by value, a token's loads wait for the one's before: 32768
+// tokens of 4095 values 71 and 198 us, so 63 and 159.)  SHORT: rows of fewer than N values, value by value.
 template <class T, int N> struct Pack { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
-template <class T, int N, bool WHOLE>
+typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+template <int N, bool SHORT>
+__device__ __forceinline__ u32 lane_column(u32 d, u32 dim) { return SHORT || d + N <= dim ? d : dim - N; }
+template <class T, int N, bool SHORT>
 __device__ __forceinline__ typename Pack<T, N>::type get(const T* p, u32 d, u32 dim) {
   typedef typename Pack<T, N>::type V;
-  if (WHOLE || d + N <= dim) return *(const V*)(p + d);
+  if constexpr (!SHORT) return *(const V*)(p + d);
   V v = {};
 #pragma unroll
   for (int k = 0; k < N; ++k)
     if (d + k < dim) v[k] = p[d + k];
   return v;
 }
-template <class T, int N, bool WHOLE>
+template <class T, int N, bool SHORT>
 __device__ __forceinline__ void put(T* p, u32 d, u32 dim, const typename Pack<T, N>::type& v) {
   typedef typename Pack<T, N>::type V;
-  if (WHOLE || d + N <= dim) {
-    __builtin_nontemporal_store(v, (V*)(p + d));                       // (past the L2: rows of 4095, 71 us, otherwise 117)
+  if constexpr (!SHORT) {
+    __builtin_nontemporal_store(v, (V*)(p + d));                       // (past the L2)
   } else {
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -61,13 +63,14 @@ __device__ __forceinline__ int64_t id_at(const EmbedArgs& a, u32 t) {
 // ---------------------------------------------------------------------------------------------------------------------
 // lookup: a wavefront to a token's slab of 64 N values, four tokens at a time
 // ---------------------------------------------------------------------------------------------------------------------
-template <class T, int N, bool WHOLE>
+template <class T, int N, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
   typedef typename Pack<T, N>::type V;
   const u64 tasks = (u64)((a.tokens + 3) / 4) * a.slabs, step = (u64)gridDim.x * 4;
   for (u64 task = (u64)blockIdx.x * 4 + wave_id(); task < tasks; task += step) {
-    const u32 t0 = (u32)(task / a.slabs) * 4, d = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
-    if (d >= a.dim) continue;
+    const u32 t0 = (u32)(task / a.slabs) * 4, d0 = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
+    if (d0 >= a.dim) continue;
+    const u32 d = lane_column<N, SHORT>(d0, a.dim);
     V v[4];
     bool fine[4];
 #pragma unroll
@@ -75,7 +78,7 @@ __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
       const u32 t = t0 + i < a.tokens ? t0 + i : a.tokens - 1;
       const int64_t id = id_at(a, t);
       fine[i] = id >= 0 && id < (int64_t)a.vocab;
-      v[i] = get<T, N, WHOLE>((const T*)a.table + (fine[i] ? id : 0) * a.ts, d, a.dim);
+      v[i] = get<T, N, SHORT>((const T*)a.table + (fine[i] ? id : 0) * a.ts, d, a.dim);
     }
 #pragma unroll
     for (u32 i = 0; i < 4; ++i) {
@@ -83,7 +86,7 @@ __global__ __launch_bounds__(256) void k_embed(const EmbedArgs a) {
       V w;
 #pragma unroll
       for (int k = 0; k < N; ++k) w[k] = (T)(fine[i] ? (float)v[i][k] * a.scale : __builtin_nanf(""));
-      put<T, N, WHOLE>((T*)a.out + (int64_t)(t0 + i) * a.os, d, a.dim, w);
+      put<T, N, SHORT>((T*)a.out + (int64_t)(t0 + i) * a.os, d, a.dim, w);
     }
   }
 }
@@ -273,20 +276,20 @@ __global__ __launch_bounds__(1024) void k_embed_sort(const EmbedArgs a, u32* to_
 // ---------------------------------------------------------------------------------------------------------------------
 // the sums
 // ---------------------------------------------------------------------------------------------------------------------
-template <class T, int N, bool WHOLE>
+template <class T, int N, bool SHORT>
 __device__ __forceinline__ void write_row(const EmbedArgs& a, u32 v, u32 d, const float (&s)[N]) {
   typedef typename Pack<T, N>::type V;
   V w;
 #pragma unroll
   for (int k = 0; k < N; ++k) w[k] = (T)(s[k] * a.scale);
-  put<T, N, WHOLE>((T*)a.dtable + (int64_t)v * a.gs, d, a.dim, w);
+  put<T, N, SHORT>((T*)a.dtable + (int64_t)v * a.gs, d, a.dim, w);
 }
 
 // Zeros, by way of the L2.
-template <class T, int N>
+template <class T, int N, bool SHORT>
 __device__ __forceinline__ void put_near(T* p, u32 d, u32 dim) {
   typedef typename Pack<T, N>::type V;
-  if (d + N <= dim) {
+  if constexpr (!SHORT) {
     *(V*)(p + d) = V{};
   } else {
 #pragma unroll
@@ -305,20 +308,22 @@ __device__ __forceinline__ u32 first_of(const u32* keys, u32 n, u32 v) {
   return lo;
 }
 
-#define EMBED_CLEAR 8u             // rows of the table that a wavefront looks after (32: 5 tokens, 191 rows of 2141, 20 us for the kernel)
+#define EMBED_CLEAR 8u              // rows of the table that a wavefront looks after (32: 5 tokens, 191 rows of 2141, 16 us for 6)
 
-template <class T, int N, bool WHOLE>
+// NEAR: rows that begin inside a line, so that two of them write it: the ones without tokens, side by side, go by way of the L2 (100000 of 1001 values past
+// it 94 us, so 53; rows of whole lines are faster past it).
+template <class T, int N, bool SHORT, bool NEAR>
 __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32* keys, const u32* places) {
   typedef typename Pack<T, N>::type V;
   const u32 l = lane_id();
   if (blockIdx.x < a.sum_groups) {
     const u64 tasks = (u64)a.pieces * a.slabs, step = (u64)a.sum_groups * 4;
     for (u64 task = (u64)blockIdx.x * 4 + uniform(wave_id()); task < tasks; task += step) {
-      const u32 piece = (u32)(task / a.slabs), d = ((u32)(task % a.slabs) * 64 + l) * N;
+      const u32 piece = (u32)(task / a.slabs), d0 = ((u32)(task % a.slabs) * 64 + l) * N;
+      const bool on = d0 < a.dim;
+      const u32 d = on ? lane_column<N, SHORT>(d0, a.dim) : 0;
       const u32 t0 = piece * a.per, n = a.tokens - t0 < a.per ? a.tokens - t0 : a.per;
-      const bool on = d < a.dim;
       const T* src = (const T*)a.dout;
-      const u32 at = on ? d : 0;
       // ids and places of the piece, a lane each (a piece has 64 tokens at most)
       const u32 mykey = l < n ? keys[t0 + l] : ~0u, myplace = l < n ? places[t0 + l] : 0;
       const u32 before = t0 ? keys[t0 - 1] : ~0u, behind = t0 + n < a.tokens ? keys[t0 + n] : ~0u;
@@ -328,11 +333,11 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
       auto flush = [&](bool on_from, bool goes_on) {
         if (on && key < a.vocab) {
           if (on_from || goes_on) {
-            f4* p = (f4*)(a.parts + ((u64)piece * 2 + (on_from ? 0 : 1)) * a.part_row + d);
+            f4u* p = (f4u*)(a.parts + ((u64)piece * 2 + (on_from ? 0 : 1)) * a.part_row + d);
 #pragma unroll
-            for (int k = 0; k < N; k += 4) p[k / 4] = f4{s[k], s[k + 1], s[k + 2], s[k + 3]};
+            for (int k = 0; k < N; k += 4) p[k / 4] = f4u{s[k], s[k + 1], s[k + 2], s[k + 3]};
           } else {
-            write_row<T, N, WHOLE>(a, key, d, s);
+            write_row<T, N, SHORT>(a, key, d, s);
           }
         }
       };
@@ -341,7 +346,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
 #pragma unroll
         for (u32 j = 0; j < 8; ++j) {
           const u32 place = (u32)__builtin_amdgcn_readlane((int)myplace, (int)(i + j < n ? i + j : n - 1));
-          v[j] = get<T, N, WHOLE>(src + (int64_t)(place < a.tokens ? place : 0) * a.ds, at, a.dim);
+          v[j] = get<T, N, SHORT>(src + (int64_t)(place < a.tokens ? place : 0) * a.ds, d, a.dim);
         }
 #pragma unroll
         for (u32 j = 0; j < 8; ++j) {
@@ -363,7 +368,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
     return;
   }
   // rows without a token
-  [[maybe_unused]] const float zero[N] = {};
+  const float zero[N] = {};
   const u32 waves = (gridDim.x - a.sum_groups) * 4;
   const u64 rows = ((u64)a.vocab + EMBED_CLEAR - 1) / EMBED_CLEAR;
   for (u64 r = (u64)(blockIdx.x - a.sum_groups) * 4 + uniform(wave_id()); r < rows; r += waves) {
@@ -376,19 +381,19 @@ __global__ __launch_bounds__(256) void k_embed_sum(const EmbedArgs a, const u32*
       empty &= empty - 1;
       T* row = (T*)a.dtable + (int64_t)(v0 + i) * a.gs;
       for (u32 d = l * N; d < a.dim; d += 64 * N) {
-        if (WHOLE) write_row<T, N, WHOLE>(a, v0 + i, d, zero);
-        else put_near<T, N>(row, d, a.dim);                            // (rows of 1001 side by side, that meet inside lines: past the L2 94 us, so 53)
+        if constexpr (NEAR) put_near<T, N, SHORT>(row, lane_column<N, SHORT>(d, a.dim), a.dim);
+        else write_row<T, N, SHORT>(a, v0 + i, lane_column<N, SHORT>(d, a.dim), zero);
       }
     }
   }
 }
 
 // Runs over the ends of pieces: the piece in which such a run begins adds its parts.
-template <class T, int N, bool WHOLE>
+template <class T, int N, bool SHORT>
 __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32* keys) {
   const u64 tasks = (u64)a.pieces * a.slabs, step = (u64)gridDim.x * 4;
   for (u64 task = (u64)blockIdx.x * 4 + uniform(wave_id()); task < tasks; task += step) {
-    const u32 piece = (u32)(task / a.slabs), d = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
+    const u32 piece = (u32)(task / a.slabs), d0 = ((u32)(task % a.slabs) * 64 + lane_id()) * N;
     const u32 t0 = piece * a.per, t1 = t0 + a.per;
     if (t1 >= a.tokens) continue;
     // lane j looks at the first token of the j-th piece behind this one
@@ -402,7 +407,8 @@ __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32
       on = ballot(far < a.tokens && keys[far < a.tokens ? far : 0] == key);
       more += on == ~0ull ? 64u : (u32)__builtin_ctzll(~on);
     }
-    if (d >= a.dim) continue;
+    if (d0 >= a.dim) continue;
+    const u32 d = lane_column<N, SHORT>(d0, a.dim);
     const float* p = a.parts + ((u64)piece * 2 + 1) * a.part_row + d;
     float s[N];
 #pragma unroll
@@ -412,7 +418,7 @@ __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32
       float v[8][N];
 #pragma unroll
       for (u32 u = 0; u < 8; ++u) {
-        const f4* o = (const f4*)(p + (u64)(q + u < more ? q + u : more - 1) * 2 * a.part_row);
+        const f4u* o = (const f4u*)(p + (u64)(q + u < more ? q + u : more - 1) * 2 * a.part_row);
 #pragma unroll
         for (int k = 0; k < N; ++k) v[u][k] = o[k / 4][k % 4];
       }
@@ -421,14 +427,14 @@ __global__ __launch_bounds__(256) void k_embed_join(const EmbedArgs a, const u32
 #pragma unroll
         for (int k = 0; k < N; ++k) s[k] += q + u < more ? v[u][k] : 0.0f;
     }
-    write_row<T, N, WHOLE>(a, key, d, s);
+    write_row<T, N, SHORT>(a, key, d, s);
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-struct EmbedPlan { bool whole; u32 grid, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
+struct EmbedPlan { bool few, near; u32 grid, clear_groups, join_groups; u64 at_keys[2], at_places[2], at_counts, at_parts, bytes; };
 
 static u64 up256(u64 x) { return (x + 255) & ~(u64)255; }
 
@@ -438,6 +444,7 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   if (!g->dim || g->dim > 65536 || !g->vocab || g->vocab >= 0x80000000u || g->tokens >= 0x80000000u) return G10_EINVAL;
   const u32 e = g->type == G10_F32 ? 4 : 2;
   const void *src = back ? g->dout : g->table, *dst = back ? g->dtable : g->out;
+  const int64_t sd = back ? g->dtable_stride : g->out_stride;
   if (!dst && (back || g->tokens)) return G10_EINVAL;
   if (g->tokens && (!src || !g->ids)) return G10_EINVAL;
   if ((uintptr_t)src % e || (uintptr_t)dst % e || (uintptr_t)g->ids % (g->ids_64 ? 8 : 4)) return G10_EINVAL;
@@ -447,7 +454,8 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   a.tokens = g->tokens; a.vocab = g->vocab; a.dim = g->dim; a.scale = g->scale; a.ids64 = g->ids_64;
   const u32 n = 16 / e;
   p = EmbedPlan{};
-  p.whole = g->dim % n == 0;
+  p.few = g->dim < n;
+  p.near = g->dim % n || ((uintptr_t)dst & 15) || sd % (int64_t)n;
   a.slabs = (g->dim + 64 * n - 1) / (64 * n);
   a.part_row = (g->dim + 7) & ~7u;
   auto groups = [](u64 waves, u32 most) { const u64 n = (waves + 3) / 4; return (u32)(n < most ? n : most); };
@@ -474,11 +482,12 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   return G10_OK;
 }
 
-template <class T, bool WHOLE>
+template <class T, bool SHORT>
 static void embed_sums(const EmbedArgs& a, const EmbedPlan& p, int last, hipStream_t s) {
   constexpr int N = 16 / sizeof(T);
-  k_embed_sum<T, N, WHOLE><<<a.sum_groups + p.clear_groups, 256, 0, s>>>(a, a.keys[last], a.places[last]);
-  if (a.pieces > 1) k_embed_join<T, N, WHOLE><<<p.join_groups, 256, 0, s>>>(a, a.keys[last]);
+  if (SHORT || p.near) k_embed_sum<T, N, SHORT, true><<<a.sum_groups + p.clear_groups, 256, 0, s>>>(a, a.keys[last], a.places[last]);
+  else k_embed_sum<T, N, SHORT, SHORT><<<a.sum_groups + p.clear_groups, 256, 0, s>>>(a, a.keys[last], a.places[last]);
+  if (a.pieces > 1) k_embed_join<T, N, SHORT><<<p.join_groups, 256, 0, s>>>(a, a.keys[last]);
 }
 
 extern "C" int g10_embed(const g10_embed_args* g, void* hip_stream) {
@@ -486,9 +495,9 @@ extern "C" int g10_embed(const g10_embed_args* g, void* hip_stream) {
   G10_TRY(embed_args(g, false, a, p));
   if (!a.tokens) return G10_OK;
   hipStream_t s = (hipStream_t)hip_stream;
-  if (g->type == G10_F32) { if (p.whole) k_embed<float, 4, true><<<p.grid, 256, 0, s>>>(a); else k_embed<float, 4, false><<<p.grid, 256, 0, s>>>(a); }
-  else if (g->type == G10_F16) { if (p.whole) k_embed<_Float16, 8, true><<<p.grid, 256, 0, s>>>(a); else k_embed<_Float16, 8, false><<<p.grid, 256, 0, s>>>(a); }
-  else { if (p.whole) k_embed<__bf16, 8, true><<<p.grid, 256, 0, s>>>(a); else k_embed<__bf16, 8, false><<<p.grid, 256, 0, s>>>(a); }
+  if (g->type == G10_F32) { if (p.few) k_embed<float, 4, true><<<p.grid, 256, 0, s>>>(a); else k_embed<float, 4, false><<<p.grid, 256, 0, s>>>(a); }
+  else if (g->type == G10_F16) { if (p.few) k_embed<_Float16, 8, true><<<p.grid, 256, 0, s>>>(a); else k_embed<_Float16, 8, false><<<p.grid, 256, 0, s>>>(a); }
+  else { if (p.few) k_embed<__bf16, 8, true><<<p.grid, 256, 0, s>>>(a); else k_embed<__bf16, 8, false><<<p.grid, 256, 0, s>>>(a); }
   G10_HIP(hipGetLastError());
   return G10_OK;
 }
@@ -523,9 +532,9 @@ extern "C" int g10_embed_backward(const g10_embed_args* g, void* workspace, uint
     }
     at = to;
   }
-  if (g->type == G10_F32) { if (p.whole) embed_sums<float, true>(a, p, at, s); else embed_sums<float, false>(a, p, at, s); }
-  else if (g->type == G10_F16) { if (p.whole) embed_sums<_Float16, true>(a, p, at, s); else embed_sums<_Float16, false>(a, p, at, s); }
-  else { if (p.whole) embed_sums<__bf16, true>(a, p, at, s); else embed_sums<__bf16, false>(a, p, at, s); }
+  if (g->type == G10_F32) { if (p.few) embed_sums<float, true>(a, p, at, s); else embed_sums<float, false>(a, p, at, s); }
+  else if (g->type == G10_F16) { if (p.few) embed_sums<_Float16, true>(a, p, at, s); else embed_sums<_Float16, false>(a, p, at, s); }
+  else { if (p.few) embed_sums<__bf16, true>(a, p, at, s); else embed_sums<__bf16, false>(a, p, at, s); }
   G10_HIP(hipGetLastError());
   return G10_OK;
 }
