@@ -468,7 +468,9 @@ static int embed_args(const g10_embed_args* g, bool back, EmbedArgs& a, EmbedPla
   const u32 rounds = (a.tokens + EMBED_ROUND - 1) / EMBED_ROUND;
   a.tile = (rounds + EMBED_TILES - 1) / EMBED_TILES * EMBED_ROUND;
   a.tiles = a.tokens ? (a.tokens + a.tile - 1) / a.tile : 0;
-  a.per = 64;                                                          // (16384 tokens of 768 values in pieces of 16: 63 us for 57)
+  // pieces of 64 tokens; of 16 where that leaves few wavefronts, each of which waits eight times for its tokens (326 tokens: 15 us for the kernel, so 6; 16384 of
+  // 768 values in pieces of 16 63 us altogether for 57, more runs are joined)
+  a.per = a.tokens > 64 && (u64)a.tokens / 64 * a.slabs < 512 ? 16 : 64;
   a.pieces = (a.tokens + a.per - 1) / a.per;
   a.sum_groups = groups((u64)a.pieces * a.slabs, 1u << 16);
   p.join_groups = a.sum_groups;
