@@ -24,7 +24,12 @@ struct LogpArgs {
   int64_t ls, ds, ignore;
   u32 rows, vocab, top;
   float scale, scale2;             // scale2: in powers of two
+  // few long rows: `parts` workgroups to a row, `each` logits to one; what they find
+  u32 parts, each;
+  struct Part* part;               // [row][part]
+  u64* part_top;                   // [row][part][top]: keys, 0 where there are no more
 };
+struct Part { float top, top2, s, t; };   // the largest logit, the same in powers of two as it was taken off; far beyond the range top2 is cut, the sums are not
 
 #define LOGP_LOG2E 1.4426950408889634f
 #define LOGP_LN2 0.6931471805599453f
@@ -118,7 +123,20 @@ struct Row {
   }
 };
 
-// NT threads to a row.  P > 0: its pieces stay in registers, P to a thread; 0: they are read as they are needed.
+template <class T>
+__device__ __forceinline__ void put_logp(const LogpArgs& a, u64 row, bool none, float lse) {
+  const int64_t token = ((const int64_t*)a.tokens)[row];
+  float lp = __builtin_nanf("");
+  if (token == a.ignore) lp = 0.0f;
+  else if (token >= 0 && token < (int64_t)a.vocab) lp = none ? LOGP_NEG_INF : __builtin_fmaf((float)((const T*)a.logits)[(int64_t)row * a.ls + token], a.scale, -lse);
+  a.logp[row] = lp;
+}
+__device__ __forceinline__ void put_top(const LogpArgs& a, u64 row, u32 rank, u64 key, bool none, float lse) {
+  a.top_ids[row * a.top + rank] = (int64_t)(u32)~(u32)key;
+  a.top_logp[row * a.top + rank] = none ? LOGP_NEG_INF : key >> 32 == LOGP_NAN ? __builtin_nanf("") : __builtin_fmaf(out_of_order((u32)(key >> 32)), a.scale, -lse);
+}
+
+// NT threads to a row or a part of one.  P > 0: its pieces stay in registers, P to a thread; 0: they are read as they are needed.
 enum { LOGP_LSE = 0, LOGP_ENTROPY = 1, LOGP_TOP = 2 };                // each with what the one before gives
 template <class T, int NT, int P, int WHAT>
 __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
@@ -129,8 +147,11 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
   __shared__ u64 keys[TOP ? 64 : 1], bounds[TOP ? W : 1], list[TOP ? LOGP_ROOM : 1];
   __shared__ u32 rank[TOP ? 64 : 1], listed;
   const u32 tid = threadIdx.x;
-  for (u64 row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const Row<T> r((const T*)a.logits + (int64_t)row * a.ls, a.vocab);
+  for (u64 b = blockIdx.x; b < (u64)a.rows * a.parts; b += gridDim.x) {
+    const u64 row = b / a.parts;
+    const u32 first = (u32)(b % a.parts) * a.each, count = a.vocab - first < a.each ? a.vocab - first : a.each;
+    const u32 wanted = a.top < count ? a.top : count;                 // of this part
+    const Row<T> r((const T*)a.logits + (int64_t)row * a.ls + first, count);
     float m = LOGP_NEG_INF, m2 = 0.0f, s = 0.0f, t = 0.0f;            // m2: the maximum in powers of two, rounded once and then used as it is
     // the thread's largest logit, and where the first piece with it begins
     const bool has = tid < r.head || tid < r.pieces || (tid < N && r.tail() + tid < r.n);
@@ -190,7 +211,7 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
     const float wm = wave_max(m);
     if (lane_id() == 0) maxima[wave_id()] = wm;
     if constexpr (TOP) {
-      u64 k = has ? key_of(best, at + (N - 1)) : 0;
+      u64 k = has ? key_of(best, first + at + (N - 1)) : 0;
       if (NT >= 128) k = dpp_most<0xb1>(k);
       if (NT >= 256) k = dpp_most<0x4e>(k);
       if (NT >= 512) k = dpp_most<0x141>(k);
@@ -253,31 +274,28 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
         if (ENTROPY) t += sums[1][w];
       }
     }
+    if (a.parts > 1) {
+      if (tid == 0) a.part[b] = {top, top2, s, t};
+    }
     const float ls = __log2f(s), lse = none ? LOGP_NEG_INF : far ? __builtin_fmaf(top, a.scale, ls * LOGP_LN2) : (top2 + ls) * LOGP_LN2;
-    if (tid == 0) {
+    if (tid == 0 && a.parts == 1) {
       a.lse[row] = lse;
       if (ENTROPY && a.entropy) a.entropy[row] = none ? 0.0f : (ls - t / s) * LOGP_LN2;
-      if (a.tokens) {
-        const int64_t token = ((const int64_t*)a.tokens)[row];
-        float lp = __builtin_nanf("");
-        if (token == a.ignore) lp = 0.0f;
-        else if (token >= 0 && token < (int64_t)a.vocab) lp = none ? LOGP_NEG_INF : __builtin_fmaf((float)r.p[token], a.scale, -lse);
-        a.logp[row] = lp;
-      }
+      if (a.tokens) put_logp<T>(a, row, none, lse);
     }
     if constexpr (TOP) {
       // the top-th largest of the groups' keys (0: there are not so many); above it lie at least as many of the row's
-      const u64 k = keys[lane_id()], is = ballot(rank[lane_id()] == a.top - 1 && k != 0);
+      const u64 k = keys[lane_id()], is = ballot(rank[lane_id()] == wanted - 1 && k != 0);
       const u64 least = is ? lane_key(k, (u32)__builtin_ctzll(is)) : 0;
       const float low = least ? out_of_order((u32)(least >> 32)) : LOGP_NEG_INF;
       auto list_it = [&](float x, u32 place) {
-        const u64 key = key_of(x, place);
+        const u64 key = key_of(x, first + place);
         if (key >= least) {
           const u32 to = atomicAdd(&listed, 1u);
           if (to < LOGP_ROOM) list[to] = key;
         }
       };
-      if (has && key_of(best, at) >= least) {
+      if (has && key_of(best, first + at) >= least) {
         r.first(tid, list_it);
         r.last(tid, list_it);
         auto some = [&](const V& v, u32 place) {
@@ -307,23 +325,24 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
       __syncthreads();
       const u32 n = listed;
       auto put = [&](u32 rank, u64 key) {
-        a.top_ids[row * a.top + rank] = (int64_t)(u32)~(u32)key;
-        a.top_logp[row * a.top + rank] = none ? LOGP_NEG_INF : key >> 32 == LOGP_NAN ? __builtin_nanf("") : __builtin_fmaf(out_of_order((u32)(key >> 32)), a.scale, -lse);
+        if (a.parts > 1) a.part_top[b * a.top + rank] = key;
+        else put_top(a, row, rank, key, none, lse);
       };
+      if (a.parts > 1 && tid >= wanted && tid < a.top) a.part_top[b * a.top + tid] = 0;
       if (n <= LOGP_ROOM && s == s) {
         for (u32 c = tid; c < n; c += NT) {
           const u64 key = list[c];
           u32 above = 0;
 #pragma unroll 8
           for (u32 j = 0; j < n; ++j) above += list[j] > key;
-          if (above < a.top) put(above, key);
+          if (above < wanted) put(above, key);
         }
       } else {
         u64 last = ~0ull;                                             // (above every key)
-        for (u32 k = 0; k < a.top; ++k) {
+        for (u32 k = 0; k < wanted; ++k) {
           u64 next = 0;
           r.template each<NT>(tid, [&](float x, u32 place) {
-            const u64 key = key_of(x, place);
+            const u64 key = key_of(x, first + place);
             if (key < last && key > next) next = key;
           });
 #pragma unroll
@@ -342,6 +361,44 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
       }
     }
     __syncthreads();                                                  // (the next row's sums go where these lie)
+  }
+}
+
+// Rows in parts: their sums brought to the row's maximum, and the top of the parts' tops.
+#define LOGP_PARTS 16u
+template <class T>
+__global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
+  __shared__ u64 list[LOGP_PARTS * G10_LOG_PROBS_TOP];
+  for (u64 row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const Part* p = a.part + row * a.parts;
+    float top = LOGP_NEG_INF, top2 = -LOGP_FAR;
+    for (u32 i = 0; i < a.parts; ++i) { top = fmaxf(top, p[i].top); top2 = fmaxf(top2, p[i].top2); }
+    const bool far = fabsf(top2) >= LOGP_FAR && top != LOGP_NEG_INF;
+    float s = 0.0f, t = 0.0f;
+    for (u32 i = 0; i < a.parts; ++i) {
+      const Part q = p[i];
+      const float d = q.top == LOGP_NEG_INF ? LOGP_NEG_INF : far ? (q.top - top) * a.scale2 : q.top2 - top2, f = __builtin_amdgcn_exp2f(d);
+      s += q.s * f;
+      t += logp_times(f, q.t + logp_times(q.s, d));
+    }
+    const bool none = top == LOGP_NEG_INF && s == 0.0f;
+    const float ls = __log2f(s), lse = none ? LOGP_NEG_INF : far ? __builtin_fmaf(top, a.scale, ls * LOGP_LN2) : (top2 + ls) * LOGP_LN2;
+    if (threadIdx.x == 0) {
+      a.lse[row] = lse;
+      if (a.entropy) a.entropy[row] = none ? 0.0f : (ls - t / s) * LOGP_LN2;
+      if (a.tokens) put_logp<T>(a, row, none, lse);
+    }
+    const u32 n = a.parts * a.top;
+    for (u32 i = threadIdx.x; i < n; i += 256) list[i] = a.part_top[row * n + i];
+    __syncthreads();
+    for (u32 i = threadIdx.x; i < n; i += 256) {
+      const u64 key = list[i];
+      u32 above = 0;
+#pragma unroll 8
+      for (u32 j = 0; j < n; ++j) above += list[j] > key;
+      if (above < a.top && key) put_top(a, row, above, key, none, lse);
+    }
+    __syncthreads();
   }
 }
 
@@ -417,6 +474,16 @@ static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
   a.ls = g->logits_stride; a.ds = g->dlogits_stride; a.ignore = g->ignore;
   a.rows = g->rows; a.vocab = g->vocab; a.top = back ? 0 : g->top;
   a.scale = g->scale; a.scale2 = g->scale * LOGP_LOG2E;
+  a.parts = 1; a.each = a.vocab;
+  // Few long rows are cut into parts of 16384 logits or more, and joined: a unit's issue is what a row waits for (200000 in 16 bits, entropy 15 us, so 9; a top
+  // of 20 24, so 15).
+  if (!back && a.rows && a.rows <= 64 && a.vocab >= 65536) {
+    const u32 most = a.vocab / 16384, room = 512 / a.rows;
+    a.parts = most < LOGP_PARTS ? most : LOGP_PARTS;
+    a.parts = a.parts < room ? a.parts : room;
+    a.each = ((a.vocab + a.parts - 1) / a.parts + 63) / 64 * 64;
+    a.parts = (a.vocab + a.each - 1) / a.each;
+  }
   return G10_OK;
 }
 
@@ -426,8 +493,9 @@ static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
 // wavefront.
 template <class T, int WHAT>
 static void logp_rows(const LogpArgs& a, hipStream_t s) {
-  const u32 grid = a.rows < 1u << 16 ? a.rows : 1u << 16, pieces = a.vocab / (16 / (u32)sizeof(T));
-  if (a.rows <= 512 && pieces > 512) {
+  const u64 rows = (u64)a.rows * a.parts;
+  const u32 grid = (u32)(rows < 1u << 16 ? rows : 1u << 16), pieces = a.each / (16 / (u32)sizeof(T));
+  if (rows <= 512 && pieces > 512) {
     if (WHAT == LOGP_TOP && pieces <= 4096) k_logp<T, 1024, WHAT == LOGP_TOP ? 4 : 0, WHAT><<<grid, 1024, 0, s>>>(a);
     else if (WHAT == LOGP_TOP && pieces <= 16384) k_logp<T, 1024, WHAT == LOGP_TOP ? 16 : 0, WHAT><<<grid, 1024, 0, s>>>(a);
     else k_logp<T, 1024, 0, WHAT><<<grid, 1024, 0, s>>>(a);
@@ -442,13 +510,16 @@ static void logp_launch(const LogpArgs& a, hipStream_t s) {
   if (a.top) logp_rows<T, LOGP_TOP>(a, s);
   else if (a.entropy) logp_rows<T, LOGP_ENTROPY>(a, s);
   else logp_rows<T, LOGP_LSE>(a, s);
+  if (a.parts > 1) k_logp_join<T><<<a.rows, 256, 0, s>>>(a);
 }
+
+static u64 logp_room(const LogpArgs& a) { return a.parts > 1 ? (u64)a.rows * a.parts * (sizeof(Part) + a.top * 8) : 0; }
 
 extern "C" int g10_log_probs_workspace(const g10_log_probs_args* g, uint64_t* bytes) {
   if (!bytes) return G10_EINVAL;
   LogpArgs a;
   G10_TRY(logp_args(g, false, a));
-  *bytes = 0;
+  *bytes = logp_room(a);
   return G10_OK;
 }
 
@@ -456,6 +527,11 @@ extern "C" int g10_log_probs(const g10_log_probs_args* g, void* workspace, uint6
   LogpArgs a;
   G10_TRY(logp_args(g, false, a));
   if (!a.rows) return G10_OK;
+  if (const u64 n = logp_room(a)) {
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < n) return G10_EINVAL;
+    a.part = (Part*)workspace;
+    a.part_top = (u64*)(a.part + (u64)a.rows * a.parts);
+  }
   hipStream_t s = (hipStream_t)hip_stream;
   if (g->type == G10_F32) logp_launch<float>(a, s);
   else if (g->type == G10_F16) logp_launch<_Float16>(a, s);

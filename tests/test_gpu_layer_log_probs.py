@@ -51,6 +51,30 @@ def test_rows(ops, rows, vocab):
     check(ops, x, t, dl, de, top=5)
 
 
+@pytest.mark.parametrize("rows, vocab", [(1, 65536), (1, 400000), (3, 100001), (64, 70000), (65, 70000), (17, 131072)])
+def test_rows_in_parts(ops, rows, vocab):
+    """Few long rows are cut and joined: each kind of row that can go wrong in one part alone or in all."""
+    for dtype in (torch.bfloat16, torch.float32):
+        x, t, dl, de = make(rows, vocab, dtype, seed=vocab)
+        low = torch.finfo(dtype).min
+        if rows >= 17:
+            x[0], x[1] = -math.inf, low
+            x[2, :-5], x[3, 5:], x[4] = -math.inf, -math.inf, 0.25                                # one part has something, all are alike
+            x[5, : vocab // 2] = low
+            x[6, ::2] = low
+            x[7] = torch.arange(vocab, device="cuda").div(vocab // 8, rounding_mode="floor").to(dtype)
+        check(ops, x, t, dl, de, top=20)
+        check(ops, x, t, dl, None, top=64, scale=0.6)
+        check(ops, x, None, None, de, top=1)
+        check(ops, x, t, dl, de)
+        if rows >= 17:
+            x[9, vocab - 2], x[10, 3], x[11] = math.nan, math.inf, math.nan
+            logp, lse, ent, top_logp, ids = ops.g10_log_probs(x, t, entropy=True, top=5)
+            for y in (logp, lse, ent, top_logp):
+                assert y[9:12].isnan().all() and not y[12:].isnan().any()
+            assert ids[9, 0] == vocab - 2 and ids[10, 0] == 3 and ids[11].tolist() == [0, 1, 2, 3, 4]
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_equal_logits_come_in_their_own_order(ops, dtype):
     x, t, _, _ = make(6, 9000, dtype)
