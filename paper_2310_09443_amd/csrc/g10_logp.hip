@@ -402,14 +402,16 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
   }
 }
 
-// The gradient of a row: p (c0 + c1 log p), c0 = - (dlogp + dentropy entropy), c1 = - dentropy, and dlogp at the token.
+// The gradient of a row: p (c0 + c1 log p), c0 = - (dlogp + dentropy entropy), c1 = - dentropy, and dlogp at the token.  Few rows are cut into parts.
 template <class T>
 __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
   constexpr u32 N = Row<T>::N;
   typedef typename Row<T>::V V;
-  for (u64 row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const Row<T> r((const T*)a.logits + (int64_t)row * a.ls, a.vocab);
-    T* out = (T*)a.dlogits + (int64_t)row * a.ds;
+  for (u64 b = blockIdx.x; b < (u64)a.rows * a.parts; b += gridDim.x) {
+    const u64 row = b / a.parts;
+    const u32 first = (u32)(b % a.parts) * a.each, count = a.vocab - first < a.each ? a.vocab - first : a.each;
+    const Row<T> r((const T*)a.logits + (int64_t)row * a.ls + first, count);
+    T* out = (T*)a.dlogits + (int64_t)row * a.ds + first;
     const float lse = a.lse[row];
     float dl = a.tokens && a.dlogp ? a.dlogp[row] : 0.0f;
     const float de = a.dentropy ? a.dentropy[row] : 0.0f;
@@ -418,6 +420,7 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
       if (t == a.ignore) { dl = 0.0f; t = -1; }
       else if (t < 0 || t >= (int64_t)a.vocab) { dl = __builtin_nanf(""); t = -1; }
     }
+    t -= first;                                                       // (its place in this part, or outside it)
     const bool none = lse == LOGP_NEG_INF;
     const float c0 = none ? 0.0f : -(dl + (a.dentropy ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = none ? 0.0f : -de * a.scale, hit = none ? 0.0f : dl * a.scale;
     const bool zero = c0 == 0.0f && c1 == 0.0f && hit == 0.0f;        // (nothing of the row counts: it is not read)
@@ -426,16 +429,16 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
       const float p = __builtin_amdgcn_exp2f(lp * LOGP_LOG2E);
       float g = p * c0;
       if (a.dentropy) g += logp_times(p, lp) * c1;
-      return (place == (u32)t && t >= 0 ? g + hit : g);
+      return (int64_t)place == t ? g + hit : g;
     };
     if (zero) {
       auto nothing = [&](u32 at) { out[at] = (T)0.0f; };
-      const u32 head = (u32)((0 - (uintptr_t)out) & 15) / (u32)sizeof(T), h = head < a.vocab ? head : a.vocab, pieces = (a.vocab - h) / N;
+      const u32 head = (u32)((0 - (uintptr_t)out) & 15) / (u32)sizeof(T), h = head < count ? head : count, pieces = (count - h) / N;
       const V z = {};
       if (threadIdx.x < h) nothing(threadIdx.x);
       for (u32 i = threadIdx.x; i < pieces; i += 256) __builtin_nontemporal_store(z, (V*)(out + h + (u64)i * N));
       const u32 at = h + pieces * N + threadIdx.x;
-      if (threadIdx.x < N && at < a.vocab) nothing(at);
+      if (threadIdx.x < N && at < count) nothing(at);
     } else if (vec) {
       auto one = [&](float x, u32 place) { out[place] = (T)grad(x, place); };
       r.first(threadIdx.x, one);
@@ -448,7 +451,7 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
         __builtin_nontemporal_store(w, (V*)(out + r.place(i)));
       }
     } else {
-      for (u32 i = threadIdx.x; i < a.vocab; i += 256) out[i] = (T)grad((float)r.p[i], i);
+      for (u32 i = threadIdx.x; i < count; i += 256) out[i] = (T)grad((float)r.p[i], i);
     }
   }
 }
@@ -482,6 +485,10 @@ static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
     a.parts = most < LOGP_PARTS ? most : LOGP_PARTS;
     a.parts = a.parts < room ? a.parts : room;
     a.each = ((a.vocab + a.parts - 1) / a.parts + 63) / 64 * 64;
+    a.parts = (a.vocab + a.each - 1) / a.each;
+  }
+  if (back && a.rows && a.rows < 2048 && a.vocab > 8192) {             // (2 rows of 194004: 32 us on a unit each, so 4)
+    a.each = 8192;
     a.parts = (a.vocab + a.each - 1) / a.each;
   }
   return G10_OK;
@@ -545,7 +552,8 @@ extern "C" int g10_log_probs_backward(const g10_log_probs_args* g, void* hip_str
   G10_TRY(logp_args(g, true, a));
   if (!a.rows) return G10_OK;
   hipStream_t s = (hipStream_t)hip_stream;
-  const u32 grid = a.rows < 1u << 16 ? a.rows : 1u << 16, e = g->type == G10_F32 ? 4 : 2;
+  const u64 groups = (u64)a.rows * a.parts;
+  const u32 grid = (u32)(groups < 1u << 16 ? groups : 1u << 16), e = g->type == G10_F32 ? 4 : 2;
   // (rows of both tensors lie alike within 16 bytes)
   const u32 vec = !(((uintptr_t)g->logits ^ (uintptr_t)g->dlogits) & 15) && ((g->logits_stride - g->dlogits_stride) * (int64_t)e) % 16 == 0;
   if (g->type == G10_F32) k_logp_back<float><<<grid, 256, 0, s>>>(a, vec);
