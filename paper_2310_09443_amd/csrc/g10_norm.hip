@@ -1,11 +1,11 @@
 // Norms of rows, centred or not, forward and backward.
 //
 // Bound by memory: forward a value is read and written once, backward it is read with its gradient and written once.  A row lies in the
-// registers of a wavefront (up to 1024 values) or of a workgroup, 8 values to a lane and step, so that the statistics are taken from the
-// values themselves: the mean first, then the squares of what is left (the squares' mean less the mean's square would lose what a
-// large mean leaves over).  Backward the statistics are worked out again from x, which has to be read in any case.  The gradients of
-// weight and bias are sums over rows: a lane keeps its columns' over all rows that its group takes, and the groups' sums are joined in
-// one order and 64 bits by a second kernel.
+// registers of a part of a wavefront (up to 256 values), of a wavefront (up to 1024) or of a workgroup, 8 values to a lane and step, so
+// that the statistics are taken from the values themselves: the mean first, then the squares of what is left (the squares' mean less the
+// mean's square would lose what a large mean leaves over).  Backward the statistics are worked out again from x, which has to be read in
+// any case.  The gradients of weight and bias are sums over rows: a lane keeps its columns' over all rows that its group takes, and the
+// groups' sums are joined in one order and 64 bits by a second kernel.
 #include "g10_internal.h"
 #include "g10_ops.h"
 
@@ -25,20 +25,23 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_plus(float x) {
   return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float wave_sum(float x) {
+// sum over an aligned group of L lanes, in each of them
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
   x = dpp_plus<0xb1>(x);                                            // lanes 1, 0, 3, 2 of a quad
   x = dpp_plus<0x4e>(x);                                            // lanes 2, 3, 0, 1
   x = dpp_plus<0x141>(x);                                           // eight lanes mirrored
-  x = dpp_plus<0x140>(x);                                           // sixteen lanes mirrored
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
+  if (L >= 16) x = dpp_plus<0x140>(x);                              // sixteen lanes mirrored
+  if (L >= 32) x += __shfl_xor(x, 16, 64);
+  if (L >= 64) x += __shfl_xor(x, 32, 64);
+  return x;
 }
-// Sums over the W wavefronts of a row, in each lane.  `room`: LDS of the call's own (the next call takes another one, so that one barrier a
-// call is enough).
-template <int W, int N>
+// Sums over the L lanes or W wavefronts of a row, in each lane.  `room`: LDS of the call's own (the next call takes another one, so that
+// one barrier a call is enough).
+template <int W, int L, int N>
 __device__ __forceinline__ void row_sums(float (&x)[N], float* room) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+  for (int i = 0; i < N; ++i) x[i] = lanes_sum<L>(x[i]);
   if constexpr (W > 1) {
     if (lane_id() == 0) {
 #pragma unroll
@@ -57,7 +60,6 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float* room) {
 // Eight values side by side, at any address of a value: accesses to memory need not be aligned, only a row's last eight may be fewer.
 template <class T> struct Eight { typedef T x8 __attribute__((ext_vector_type(8), aligned(sizeof(T)))); };
 
-// W wavefronts to a row, NV steps of 8 values a lane; a workgroup holds 4 / W rows (W = 1) or one (W = 4, 8, 16).
 // WHOLE: rows of a multiple of 8 values.
 template <class T, bool WHOLE>
 __device__ __forceinline__ void get8(const T* p, u32 d, u32 dim, float (&v)[8]) {
@@ -97,11 +99,16 @@ __device__ __forceinline__ void weights8(const void* w, u32 w32, u32 d, u32 dim,
   }
 }
 
-template <class T, int W, int NV, bool WHOLE, bool BACK>
+// W wavefronts to a row, NV steps of 8 values a lane; a workgroup holds one row (W = 4, 8, 16) or four wavefronts' (W = 1), of which each has
+// 64 / L: rows of up to 256 values lie side by side in a wavefront (100000 x 128 in bf16: 7.3 us forward and 19 backward, with a wavefront to
+// each row 24 and 47; 14021 x 69: 4.1 and 10.6 for 7.1 and 18.5).
+template <class T, int W, int L, int NV, bool WHOLE, bool BACK>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a) {
-  constexpr u32 ROWS = W == 1 ? 4 : 1, LANES = 64 * W;
+  constexpr u32 BESIDE = 64 / L, ROWS = W == 1 ? 4 * BESIDE : 1, LANES = L * W;
   __shared__ float room[4][2 * W];
-  const u32 l = W == 1 ? lane_id() : threadIdx.x, first = blockIdx.x * ROWS + (W == 1 ? wave_id() : 0), step = gridDim.x * ROWS;
+  const u32 l = W == 1 ? lane_id() % L : threadIdx.x, mine = L < 64 ? lane_id() / L : 0;
+  const u64 first = (u64)blockIdx.x * ROWS + (W == 1 ? wave_id() * BESIDE : 0), step = (u64)gridDim.x * ROWS;      // (the same in all lanes)
+  auto row_of = [&](u64 base) { return L == 64 || base + mine < a.rows ? base + mine : (u64)a.rows - 1; };
   const float inv = 1.0f / (float)a.dim;
   float dw[BACK ? NV : 1][8] = {}, db[BACK ? NV : 1][8] = {};
   u32 turn = 0;
@@ -118,7 +125,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
     }
   };
   if constexpr (AHEAD) {
-    if (first < a.rows) fetch(first);
+    if (first < a.rows) fetch(row_of(first));
   }
   // A lane's columns are the same in every row: with a few steps their weights stay in registers (16384 rows of 768 forward 11.5 -> 9.8 us; not where
   // a workgroup has one row: 32768 of 4096 89 -> 96, fewer wavefronts fit).
@@ -141,7 +148,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
       weights8<T, WHOLE>(a.w, a.w32, d, a.dim, 1.0f, w);
     }
   };
-  for (u64 row = first; row < a.rows; row += step) {
+  for (u64 base = first; base < a.rows; base += step) {
+    const u64 row = row_of(base);
+    const bool on = L == 64 || base + mine < a.rows;                // (lanes of rows past the last one repeat it, and neither write nor add)
     const T* x = (const T*)a.x + (int64_t)row * a.xs;
     const T* y = BACK ? (const T*)a.dy + (int64_t)row * a.dys : nullptr;
     T* out = (T*)a.out + (int64_t)row * a.os;
@@ -153,7 +162,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
 #pragma unroll
         for (int k = 0; k < 8; ++k) { v[i][k] = in ? (float)nx[i][k] : 0.0f; g[i][k] = in ? (float)ny[i][k] : 0.0f; }
       }
-      fetch(row + step < a.rows ? row + step : row);
+      fetch(base + step < a.rows ? row_of(base + step) : row);
     } else {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
       for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[0] += v[i][k];
-      row_sums<W>(s, room[turn]);
+      row_sums<W, L>(s, room[turn]);
       turn = (turn + 1) & 3;
       mean = s[0] * inv;
     }
@@ -187,7 +196,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
         v[i][k] = d < a.dim ? v[i][k] - mean : 0.0f;
         s[0] += v[i][k] * v[i][k];
       }
-    row_sums<W>(s, room[turn]);
+    row_sums<W, L>(s, room[turn]);
     turn = (turn + 1) & 3;
     const float r = 1.0f / sqrtf(s[0] * inv + a.eps);
     if constexpr (!BACK) {
@@ -200,7 +209,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
         if constexpr (!KEPT) weights8<T, WHOLE>(a.b, a.w32, d, a.dim, 0.0f, b);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * r * w[k] + (KEPT ? kb[KEPT ? i : 0][k] : b[k]);
-        put8<T, WHOLE>(out, d, a.dim, v[i]);
+        if (on) put8<T, WHOLE>(out, d, a.dim, v[i]);
       }
     } else {
       float t[2] = {};                                              // sums of u n and of u
@@ -213,14 +222,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           v[i][k] *= r;
-          dw[i][k] += g[i][k] * v[i][k];
-          db[i][k] += g[i][k];
+          dw[i][k] += on ? g[i][k] * v[i][k] : 0.0f;
+          db[i][k] += on ? g[i][k] : 0.0f;
           g[i][k] *= w[k];
           t[0] += g[i][k] * v[i][k];
           t[1] += g[i][k];
         }
       }
-      row_sums<W>(t, room[turn]);
+      row_sums<W, L>(t, room[turn]);
       turn = (turn + 1) & 3;
       const float dot = t[0] * inv, off = a.center ? t[1] * inv : 0.0f;
 #pragma unroll
@@ -229,7 +238,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
         if (d >= a.dim) continue;
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[i][k] = r * (g[i][k] - v[i][k] * dot - off);
-        put8<T, WHOLE>(out, d, a.dim, g[i]);
+        if (on) put8<T, WHOLE>(out, d, a.dim, g[i]);
       }
     }
   }
@@ -237,15 +246,21 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm(const NormArgs a
     if (!a.partial) return;
     float* to = a.partial + (u64)blockIdx.x * 2 * a.dim;
     if constexpr (W == 1) {                                         // the four wavefronts' sums, step by step
-      __shared__ float sums[2][4][512];
+      constexpr u32 WIDE = 8 * L;
+      __shared__ float sums[2][4][WIDE];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { sums[0][wave_id()][l * 8 + k] = dw[i][k]; sums[1][wave_id()][l * 8 + k] = db[i][k]; }
+        for (int k = 0; k < 8; ++k) {
+          float w = dw[i][k], b = db[i][k];
+#pragma unroll
+          for (int d = L; d < 64; d *= 2) { w += __shfl_xor(w, d, 64); b += __shfl_xor(b, d, 64); }
+          if (mine == 0) { sums[0][wave_id()][l * 8 + k] = w; sums[1][wave_id()][l * 8 + k] = b; }
+        }
         __syncthreads();
-        for (u32 e = threadIdx.x; e < 1024; e += 256) {
-          const u32 which = e / 512, c = e % 512, d = i * 512 + c;
+        for (u32 e = threadIdx.x; e < 2 * WIDE; e += 256) {
+          const u32 which = e / WIDE, c = e % WIDE, d = i * WIDE + c;
           if (d < a.dim) to[which * a.dim + d] = (sums[which][0][c] + sums[which][1][c]) + (sums[which][2][c] + sums[which][3][c]);
         }
       }
@@ -286,7 +301,7 @@ __global__ __launch_bounds__(1024) void k_norm_weights(const NormArgs a, u32 gro
 // ---------------------------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------------------------
-struct NormPlan { u32 grid, waves, steps; bool whole, weights; };
+struct NormPlan { u32 grid, waves, lanes, steps; bool whole, weights; };
 
 static int norm_args(const g10_norm_args* g, bool back, NormArgs& a, NormPlan& p) {
   if (!g) return G10_EINVAL;
@@ -309,10 +324,11 @@ static int norm_args(const g10_norm_args* g, bool back, NormArgs& a, NormPlan& p
   p.whole = g->dim % 8 == 0;
   const u32 lanes = (g->dim + 7) / 8;
   p.waves = lanes <= 128 ? 1 : lanes <= 512 ? 4 : lanes <= 1024 ? 8 : 16;
+  p.lanes = lanes <= 8 ? 8 : lanes <= 16 ? 16 : lanes <= 32 ? 32 : 64;
   p.steps = (lanes + 64 * p.waves - 1) / (64 * p.waves);
   if (p.steps == 3) p.steps = 4;
   if (p.steps > 4) p.steps = 8;
-  const u32 rows_each = p.waves == 1 ? 4 : 1;
+  const u32 rows_each = p.waves == 1 ? 4 * (64 / p.lanes) : 1;
   const u64 groups = ((u64)a.rows + rows_each - 1) / rows_each;
   const u32 most = back ? (p.waves == 16 ? 256u : 512u) : 1u << 16;
   p.grid = (u32)(groups < most ? groups : most);
@@ -323,7 +339,7 @@ template <class T, bool WHOLE, bool BACK>
 static void norm_launch(const NormArgs& a, const NormPlan& p, hipStream_t s) {
   auto go = [&](auto w, auto nv) {
     constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-    k_norm<T, W, NV, WHOLE, BACK><<<p.grid, W == 1 ? 256 : 64 * W, 0, s>>>(a);
+    k_norm<T, W, 64, NV, WHOLE, BACK><<<p.grid, W == 1 ? 256 : 64 * W, 0, s>>>(a);
   };
   using std::integral_constant;
   auto pick = [&](auto w) {
@@ -331,7 +347,10 @@ static void norm_launch(const NormArgs& a, const NormPlan& p, hipStream_t s) {
     else if (p.steps == 4) go(w, integral_constant<int, 4>{});
     else go(w, integral_constant<int, 8>{});
   };
-  if (p.waves == 1) { if (p.steps == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 1>{}, integral_constant<int, 2>{}); }
+  if (p.lanes == 8) k_norm<T, 1, 8, 1, WHOLE, BACK><<<p.grid, 256, 0, s>>>(a);
+  else if (p.lanes == 16) k_norm<T, 1, 16, 1, WHOLE, BACK><<<p.grid, 256, 0, s>>>(a);
+  else if (p.lanes == 32) k_norm<T, 1, 32, 1, WHOLE, BACK><<<p.grid, 256, 0, s>>>(a);
+  else if (p.waves == 1) { if (p.steps == 1) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 1>{}, integral_constant<int, 2>{}); }
   else if (p.waves == 4) { if (p.steps == 1) go(integral_constant<int, 4>{}, integral_constant<int, 1>{}); else go(integral_constant<int, 4>{}, integral_constant<int, 2>{}); }
   else if (p.waves == 8) go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
   else pick(integral_constant<int, 16>{});

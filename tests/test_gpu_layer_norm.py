@@ -121,3 +121,10 @@ def test_refusals(ops):
                        (lambda: ops.g10_norm(torch.zeros(1, 65537, device="cuda")), "65536")):
         with pytest.raises(ValueError, match=match):
             bad()
+
+
+@pytest.mark.parametrize("dim", [3, 64, 65, 120, 128, 130, 250, 256, 264])
+@pytest.mark.parametrize("rows", [1, 7, 8, 31, 33, 1025, 20001])
+def test_narrow_rows(ops, rows, dim):
+    """Rows side by side in a wavefront, the last one with some of them; more of them than a backward pass has places."""
+    check(ops, *make(rows, dim, torch.bfloat16, wtype=torch.float32, seed=rows + dim))
