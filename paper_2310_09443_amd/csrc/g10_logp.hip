@@ -2,7 +2,7 @@
 //
 // Bound by memory: forward a logit is read once, backward read and written once.  A workgroup takes a row in one pass: each thread keeps
 // its own running maximum m, sum s of exp(z - m) and sum t of exp(z - m) (z - m), which are scaled when the maximum moves and brought to
-// the row's maximum at the end:  lse = m + log s,  entropy = log s - t / s.
+// the row's maximum at the end:  lse = m + log s,  entropy = log s - t / s,  and of a logit  log p = (z - m) - log s.
 //
 // The `top` likeliest: beside the sums each thread remembers its own largest logit, and 64 groups of threads theirs.  The top-th largest of the
 // 64 is no larger than the row's top-th largest, and little is above it: 32000 logits and a top of 20 leave some 24 candidates.  They lie
@@ -123,17 +123,34 @@ struct Row {
   }
 };
 
+// What a row's sum was taken from: its largest logit, the same in powers of two as it was taken off, and the sum's logarithm in powers of two.
+struct Found { float top, top2, log; };
+// The row's lse is a place, which 32 bits round where it lies: a row of 32000 times -1e9 has the lse -1e9.  A logarithm of a probability is a distance,
+// and is taken from the row's largest logit: what of top2 is rounding is in the sum as well.
+__device__ __forceinline__ bool is_none(const Found& r, float s) { return r.top == LOGP_NEG_INF && s == 0.0f; }
+__device__ __forceinline__ bool is_far(const Found& r) { return fabsf(r.top2) >= LOGP_FAR && r.top != LOGP_NEG_INF; }
+__device__ __forceinline__ float lse_of(const LogpArgs& a, const Found& r, bool none) {
+  return none ? LOGP_NEG_INF : is_far(r) ? __builtin_fmaf(r.top, a.scale, r.log * LOGP_LN2) : (r.top2 + r.log) * LOGP_LN2;
+}
+__device__ __forceinline__ float log_of(const LogpArgs& a, const Found& r, bool none, float x) {
+  if (none) return LOGP_NEG_INF;
+  // (halves: logits at both ends of the type lie further apart than it holds; what they lose of a small logit is nothing beside the top)
+  if (is_far(r)) return __builtin_fmaf((0.5f * x - 0.5f * r.top) * a.scale, 2.0f, -r.log * LOGP_LN2);
+  const float d = __builtin_fmaf(x, a.scale2, -r.top2);
+  return d < -LOGP_FAR ? __builtin_fmaf(x, a.scale, -lse_of(a, r, none)) : (d - r.log) * LOGP_LN2;      // (a distance may end 32 bits in powers of two alone)
+}
+
 template <class T>
-__device__ __forceinline__ void put_logp(const LogpArgs& a, u64 row, bool none, float lse) {
+__device__ __forceinline__ void put_logp(const LogpArgs& a, u64 row, const Found& r, bool none) {
   const int64_t token = ((const int64_t*)a.tokens)[row];
   float lp = __builtin_nanf("");
   if (token == a.ignore) lp = 0.0f;
-  else if (token >= 0 && token < (int64_t)a.vocab) lp = none ? LOGP_NEG_INF : __builtin_fmaf((float)((const T*)a.logits)[(int64_t)row * a.ls + token], a.scale, -lse);
+  else if (token >= 0 && token < (int64_t)a.vocab) lp = log_of(a, r, none, (float)((const T*)a.logits)[(int64_t)row * a.ls + token]);
   a.logp[row] = lp;
 }
-__device__ __forceinline__ void put_top(const LogpArgs& a, u64 row, u32 rank, u64 key, bool none, float lse) {
+__device__ __forceinline__ void put_top(const LogpArgs& a, u64 row, u32 rank, u64 key, const Found& r, bool none) {
   a.top_ids[row * a.top + rank] = (int64_t)(u32)~(u32)key;
-  a.top_logp[row * a.top + rank] = none ? LOGP_NEG_INF : key >> 32 == LOGP_NAN ? __builtin_nanf("") : __builtin_fmaf(out_of_order((u32)(key >> 32)), a.scale, -lse);
+  a.top_logp[row * a.top + rank] = key >> 32 == LOGP_NAN ? __builtin_nanf("") : log_of(a, r, none, out_of_order((u32)(key >> 32)));
 }
 
 // NT threads to a row or a part of one.  P > 0: its pieces stay in registers, P to a thread; 0: they are read as they are needed.
@@ -251,9 +268,9 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
       s += sums[0][w];
       if (ENTROPY) t += sums[1][w];
     }
-    const bool none = top == LOGP_NEG_INF && s == 0.0f;
-    const bool far = fabsf(top2) >= LOGP_FAR && top != LOGP_NEG_INF;  // (a row masked with the type's lowest value, say)
-    if (far) {
+    Found found = {top, top2, 0.0f};
+    const bool none = is_none(found, s);
+    if (is_far(found)) {                                              // (a row masked with the type's lowest value, say)
       s = t = 0.0f;
       r.template each<NT>(tid, [&](float x, u32) {
         const float d = (x - top) * a.scale2, e = __builtin_amdgcn_exp2f(d);
@@ -277,11 +294,11 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
     if (a.parts > 1) {
       if (tid == 0) a.part[b] = {top, top2, s, t};
     }
-    const float ls = __log2f(s), lse = none ? LOGP_NEG_INF : far ? __builtin_fmaf(top, a.scale, ls * LOGP_LN2) : (top2 + ls) * LOGP_LN2;
+    found.log = __log2f(s);
     if (tid == 0 && a.parts == 1) {
-      a.lse[row] = lse;
-      if (ENTROPY && a.entropy) a.entropy[row] = none ? 0.0f : (ls - t / s) * LOGP_LN2;
-      if (a.tokens) put_logp<T>(a, row, none, lse);
+      a.lse[row] = lse_of(a, found, none);
+      if (ENTROPY && a.entropy) a.entropy[row] = none ? 0.0f : (found.log - t / s) * LOGP_LN2;
+      if (a.tokens) put_logp<T>(a, row, found, none);
     }
     if constexpr (TOP) {
       // the top-th largest of the groups' keys (0: there are not so many); above it lie at least as many of the row's
@@ -326,7 +343,7 @@ __global__ __launch_bounds__(NT) void k_logp(const LogpArgs a) {
       const u32 n = listed;
       auto put = [&](u32 rank, u64 key) {
         if (a.parts > 1) a.part_top[b * a.top + rank] = key;
-        else put_top(a, row, rank, key, none, lse);
+        else put_top(a, row, rank, key, found, none);
       };
       if (a.parts > 1 && tid >= wanted && tid < a.top) a.part_top[b * a.top + tid] = 0;
       if (n <= LOGP_ROOM && s == s) {
@@ -373,7 +390,8 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
     const Part* p = a.part + row * a.parts;
     float top = LOGP_NEG_INF, top2 = -LOGP_FAR;
     for (u32 i = 0; i < a.parts; ++i) { top = fmaxf(top, p[i].top); top2 = fmaxf(top2, p[i].top2); }
-    const bool far = fabsf(top2) >= LOGP_FAR && top != LOGP_NEG_INF;
+    Found found = {top, top2, 0.0f};
+    const bool far = is_far(found);
     float s = 0.0f, t = 0.0f;
     for (u32 i = 0; i < a.parts; ++i) {
       const Part q = p[i];
@@ -381,12 +399,12 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
       s += q.s * f;
       t += logp_times(f, q.t + logp_times(q.s, d));
     }
-    const bool none = top == LOGP_NEG_INF && s == 0.0f;
-    const float ls = __log2f(s), lse = none ? LOGP_NEG_INF : far ? __builtin_fmaf(top, a.scale, ls * LOGP_LN2) : (top2 + ls) * LOGP_LN2;
+    const bool none = is_none(found, s);
+    found.log = __log2f(s);
     if (threadIdx.x == 0) {
-      a.lse[row] = lse;
-      if (a.entropy) a.entropy[row] = none ? 0.0f : (ls - t / s) * LOGP_LN2;
-      if (a.tokens) put_logp<T>(a, row, none, lse);
+      a.lse[row] = lse_of(a, found, none);
+      if (a.entropy) a.entropy[row] = none ? 0.0f : (found.log - t / s) * LOGP_LN2;
+      if (a.tokens) put_logp<T>(a, row, found, none);
     }
     const u32 n = a.parts * a.top;
     for (u32 i = threadIdx.x; i < n; i += 256) list[i] = a.part_top[row * n + i];
@@ -396,7 +414,7 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
       u32 above = 0;
 #pragma unroll 8
       for (u32 j = 0; j < n; ++j) above += list[j] > key;
-      if (above < a.top && key) put_top(a, row, above, key, none, lse);
+      if (above < a.top && key) put_top(a, row, above, key, found, none);
     }
     __syncthreads();
   }
