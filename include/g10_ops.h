@@ -200,8 +200,9 @@ int g10_norm_backward(const g10_norm_args *args, void *workspace, uint64_t works
  * dlogits_j = scale * (dlogp ([j = t] - p_j) - dentropy p_j (log p_j + entropy)).
  * A token equal to `ignore` has logp = 0 and no share in the gradient; any other one outside the row makes logp, and the row's
  * gradient, NaN.  Places of -infinity have no probability; a row of nothing else has lse = logp = -infinity, entropy 0 and no gradient.
- * Sums, logp, top_logp and entropy go by distances from the row's largest logit and are as exact for a row with a large offset, or at the type's end, as for one
- * around zero; lse is rounded to 32 bits where it lies, and infinite where scale * logits are beyond them.
+ * Sums, logp, top_logp, entropy and the gradient go by distances from the row's largest logit and are as exact for a row with a large offset, or at the type's end,
+ * as for one around zero; lse is rounded to 32 bits where it lies, and infinite where scale * logits are beyond them.  Where it is 64 or more (16-bit logits: 256),
+ * either side of zero, the backward pass sums the row again.
  * A row with a NaN or +infinity has logp, lse, entropy and the gradient NaN (NaN counts as the largest where the top is sought); a row
  * with dlogp = 0 or an ignored token, and dentropy = 0, has the gradient 0 whatever it holds. */
 #define G10_LOG_PROBS_TOP 64u

@@ -420,9 +420,62 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
   }
 }
 
+// How far from zero lse may lie for p to be taken from it.  Its roundings are in every p: at 64 up to 6e-6 of p, a hundred half steps of 32 bits (the
+// roundings of a product with `scale` are as large); at 256 3e-5, an eighth of half a step of 16 bits of 5 exponent bits.
+template <class T> struct Near { static constexpr float LSE = sizeof(T) == 4 ? 64.0f : 256.0f; };
+
+// A whole row's largest logit and the logarithm of its sum once more, in all threads (rows without NaN and +infinity).
+template <class T, int NT>
+__device__ __forceinline__ Found again(const LogpArgs& a, u64 row) {
+  constexpr u32 W = NT / 64, N = Row<T>::N;
+  __shared__ float room[2][W];
+  const Row<T> r((const T*)a.logits + (int64_t)row * a.ls, a.vocab);
+  float m = LOGP_NEG_INF, s = 0.0f;
+  auto take = [&](const float* x, u32 n) {
+    float top = x[0];
+#pragma unroll
+    for (u32 k = 1; k < n; ++k) top = fmaxf(top, x[k]);
+    if (top > m) {
+      s *= m == LOGP_NEG_INF ? 0.0f : __builtin_amdgcn_exp2f((m - top) * a.scale2);
+      m = top;
+    }
+    const float from = m == LOGP_NEG_INF ? 0.0f : m;
+#pragma unroll
+    for (u32 k = 0; k < n; ++k) s += __builtin_amdgcn_exp2f((x[k] - from) * a.scale2);
+  };
+  auto one = [&](float x, u32) { take(&x, 1); };
+  r.first(threadIdx.x, one);
+  r.last(threadIdx.x, one);
+#pragma unroll 4
+  for (u32 i = threadIdx.x; i < r.pieces; i += NT) {
+    const typename Row<T>::V v = r.piece(i);
+    float x[N];
+#pragma unroll
+    for (u32 k = 0; k < N; ++k) x[k] = (float)v[k];
+    take(x, N);
+  }
+  const float wm = wave_max(m);
+  if (lane_id() == 0) room[0][wave_id()] = wm;
+  __syncthreads();
+  float top = room[0][0];
+#pragma unroll
+  for (u32 w = 1; w < W; ++w) top = fmaxf(top, room[0][w]);
+  s = wave_add(m == LOGP_NEG_INF ? 0.0f : s * __builtin_amdgcn_exp2f((m - top) * a.scale2));
+  if (lane_id() == 0) room[1][wave_id()] = s;
+  __syncthreads();
+  s = room[1][0];
+#pragma unroll
+  for (u32 w = 1; w < W; ++w) s += room[1][w];
+  __syncthreads();                                                    // (a next row's go where these lie)
+  return {top, 0.0f, __log2f(s)};
+}
+
 // The gradient of a row: p (c0 + c1 log p), c0 = - (dlogp + dentropy entropy), c1 = - dentropy, and dlogp at the token.  Few rows are cut into parts.
-template <class T>
-__global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
+// log p = scale (x - from) - off: from lse, or where that lies too far from zero from the row's largest logit and its sum, for which each workgroup reads the
+// row (32768 x 32000 in bf16: 0.80 ms, 0.87 where all rows are such; in parts 2 x 194004 4 us and 18, 2047 x 152064 in fp32 0.48 ms and 1.74: each part
+// reads it).
+template <class T, int NT>
+__global__ __launch_bounds__(NT) void k_logp_back(const LogpArgs a, u32 vec) {
   constexpr u32 N = Row<T>::N;
   typedef typename Row<T>::V V;
   for (u64 b = blockIdx.x; b < (u64)a.rows * a.parts; b += gridDim.x) {
@@ -439,11 +492,17 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
       else if (t < 0 || t >= (int64_t)a.vocab) { dl = __builtin_nanf(""); t = -1; }
     }
     t -= first;                                                       // (its place in this part, or outside it)
-    const bool none = lse == LOGP_NEG_INF;
-    const float c0 = none ? 0.0f : -(dl + (a.dentropy ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = none ? 0.0f : -de * a.scale, hit = none ? 0.0f : dl * a.scale;
-    const bool zero = c0 == 0.0f && c1 == 0.0f && hit == 0.0f;        // (nothing of the row counts: it is not read)
+    const float c0 = -(dl + (a.dentropy ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = -de * a.scale, hit = dl * a.scale;
+    bool zero = c0 == 0.0f && c1 == 0.0f && hit == 0.0f;              // (nothing of the row counts: it is not read)
+    float from = 0.0f, off = lse;
+    if (!zero && fabsf(lse) >= Near<T>::LSE) {
+      const Found found = again<T, NT>(a, row);
+      zero = found.top == LOGP_NEG_INF;                               // (a row without any probability)
+      from = found.top;
+      off = found.log * LOGP_LN2;
+    }
     auto grad = [&](float x, u32 place) {
-      const float lp = __builtin_fmaf(x, a.scale, -lse);              // -infinity where there is no probability
+      const float lp = __builtin_fmaf(x - from, a.scale, -off);       // -infinity where there is no probability
       const float p = __builtin_amdgcn_exp2f(lp * LOGP_LOG2E);
       float g = p * c0;
       if (a.dentropy) g += logp_times(p, lp) * c1;
@@ -454,14 +513,14 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
       const u32 head = (u32)((0 - (uintptr_t)out) & 15) / (u32)sizeof(T), h = head < count ? head : count, pieces = (count - h) / N;
       const V z = {};
       if (threadIdx.x < h) nothing(threadIdx.x);
-      for (u32 i = threadIdx.x; i < pieces; i += 256) __builtin_nontemporal_store(z, (V*)(out + h + (u64)i * N));
+      for (u32 i = threadIdx.x; i < pieces; i += NT) __builtin_nontemporal_store(z, (V*)(out + h + (u64)i * N));
       const u32 at = h + pieces * N + threadIdx.x;
       if (threadIdx.x < N && at < count) nothing(at);
     } else if (vec) {
       auto one = [&](float x, u32 place) { out[place] = (T)grad(x, place); };
       r.first(threadIdx.x, one);
       r.last(threadIdx.x, one);
-      for (u32 i = threadIdx.x; i < r.pieces; i += 256) {
+      for (u32 i = threadIdx.x; i < r.pieces; i += NT) {
         const V v = r.piece(i);
         V w;
 #pragma unroll
@@ -469,7 +528,7 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec) {
         __builtin_nontemporal_store(w, (V*)(out + r.place(i)));
       }
     } else {
-      for (u32 i = threadIdx.x; i < count; i += 256) out[i] = (T)grad((float)r.p[i], i);
+      for (u32 i = threadIdx.x; i < count; i += NT) out[i] = (T)grad((float)r.p[i], i);
     }
   }
 }
@@ -505,8 +564,13 @@ static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
     a.each = ((a.vocab + a.parts - 1) / a.parts + 63) / 64 * 64;
     a.parts = (a.vocab + a.each - 1) / a.each;
   }
-  if (back && a.rows && a.rows < 2048 && a.vocab > 8192) {             // (2 rows of 194004: 32 us on a unit each, so 4)
-    a.each = 8192;
+  // Gradients of few long rows: parts of 8192 logits (2 rows of 194004: 32 us on a unit each, so 4).  Each part may have to read its whole row, so there are no more
+  // than 16384 in all (2047 rows of 152064 in 32 bits: 478 us with 19 parts to a row or with 8, with 2 500), nor than read 2^34 logits.  Written over the
+  // logits a row stays whole: a part would read what another has written.
+  if (back && a.rows && a.rows < 2048 && a.vocab > 8192 && a.logits != a.dlogits) {
+    const u64 room = (1ull << 34) / a.vocab;
+    const u32 all = (u32)(room < 16384 ? room : 16384), most = all / a.rows ? all / a.rows : 1, parts = (a.vocab + 8191) / 8192;
+    a.each = parts <= most ? 8192 : ((a.vocab + most - 1) / most + 63) / 64 * 64;
     a.parts = (a.vocab + a.each - 1) / a.each;
   }
   return G10_OK;
@@ -574,9 +638,10 @@ extern "C" int g10_log_probs_backward(const g10_log_probs_args* g, void* hip_str
   const u32 grid = (u32)(groups < 1u << 16 ? groups : 1u << 16), e = g->type == G10_F32 ? 4 : 2;
   // (rows of both tensors lie alike within 16 bytes)
   const u32 vec = !(((uintptr_t)g->logits ^ (uintptr_t)g->dlogits) & 15) && ((g->logits_stride - g->dlogits_stride) * (int64_t)e) % 16 == 0;
-  if (g->type == G10_F32) k_logp_back<float><<<grid, 256, 0, s>>>(a, vec);
-  else if (g->type == G10_F16) k_logp_back<_Float16><<<grid, 256, 0, s>>>(a, vec);
-  else k_logp_back<__bf16><<<grid, 256, 0, s>>>(a, vec);
+  const bool wide = a.parts == 1 && a.rows <= 512 && a.vocab > 8192;   // (few long rows over their logits: 1024 threads each)
+  if (g->type == G10_F32) { if (wide) k_logp_back<float, 1024><<<grid, 1024, 0, s>>>(a, vec); else k_logp_back<float, 256><<<grid, 256, 0, s>>>(a, vec); }
+  else if (g->type == G10_F16) { if (wide) k_logp_back<_Float16, 1024><<<grid, 1024, 0, s>>>(a, vec); else k_logp_back<_Float16, 256><<<grid, 256, 0, s>>>(a, vec); }
+  else { if (wide) k_logp_back<__bf16, 1024><<<grid, 1024, 0, s>>>(a, vec); else k_logp_back<__bf16, 256><<<grid, 256, 0, s>>>(a, vec); }
   G10_HIP(hipGetLastError());
   return G10_OK;
 }

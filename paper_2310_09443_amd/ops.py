@@ -328,13 +328,15 @@ def gated(x, gate, up, act="silu"):
 def g10_log_probs(logits, tokens=None, entropy=False, top=0, scale=1.0, ignore=-100):
     """Of softmax(scale * logits) over the last dimension: (logp, lse, entropy, top_logp, top_ids), float32 and ids int64, None where not asked for.
     logp: the logarithm of the given tokens' probabilities (`tokens` [...], int64 or int32; 0 for a token equal to `ignore`, NaN for another one outside the
-    vocabulary); lse: the logarithm of the sum of exponentials; entropy: in nats; top: that many likeliest tokens (up to 64), [..., top], equal
+    vocabulary); lse: the logarithm of the sum of exponentials (rounded where it lies: of a row of -1e9 it is -1e9, while logp goes by distances from the
+    largest logit); entropy: in nats; top: that many likeliest tokens (up to 64), [..., top], equal
     ones in their own order.  Places of -inf have no probability; a row of nothing else has lse = logp = -inf and entropy 0."""
     return _calls().log_probs(logits, tokens, entropy, top, scale, ignore)
 
 
 def g10_log_probs_backward(dlogp, logits, tokens, lse, dentropy=None, entropy=None, scale=1.0, ignore=-100):
-    """The logits' gradient from those of logp and entropy (either may be None), with g10_log_probs's lse and entropy."""
+    """The logits' gradient from those of logp and entropy (either may be None), with g10_log_probs's lse and entropy.  Rows whose lse is 64 or more, of
+    16-bit logits 256, either side of zero, are summed again: their lse is rounded too much to take probabilities from."""
     return _calls().log_probs_backward(dlogp, logits, tokens, lse, dentropy, entropy, scale, ignore)
 
 

@@ -95,3 +95,90 @@ def test_no_logit_is_lost_from_the_sums(ops, rows, vocab, dtype):
     t = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(1)).cuda()
     got, _ = forward(ops, x, t, 3, 1.0)
     K.check(got, K.log_probs(x, t, 1.0, top=3)[0])
+
+
+# -------------------------------------------------------------------------------------------------------------- gradients
+NEAR = {torch.float32: 64.0, torch.float16: 256.0, torch.bfloat16: 256.0}                   # lse up to which p is taken from it
+
+
+def both(ops, x, t, dl, de, scale):
+    _, lse, ent, _, _ = ops.g10_log_probs(x, t, entropy=True, scale=scale)
+    K.check(dict(dlogits=ops.g10_log_probs_backward(dl, x, t, lse, de, ent, scale)), K.log_probs(x, t, scale, dlogp=dl, dentropy=de, near=NEAR[x.dtype])[0])
+
+
+def shares(rows):
+    g = torch.Generator().manual_seed(rows)
+    return [torch.randn(rows, generator=g).cuda() for _ in range(2)]
+
+
+@pytest.mark.parametrize("scale", [0.5, 1.0, 1.25])
+@pytest.mark.parametrize("vocab", [5, 1003, 32000, 70000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_rows_all_alike(ops, dtype, vocab, scale):
+    """scale dlogp ([j = t] - 1 / V), and nothing of the entropy, which is as large as it can be.  A probability is off by the sum's additions and by
+    some twenty roundings of log V (of lse, of its two products, of the argument) and of 1; then the result's own."""
+    values = ends(dtype)
+    x = torch.tensor(values, dtype=dtype, device="cuda")[:, None].repeat(1, vocab)
+    t = torch.arange(len(values), device="cuda") % vocab
+    dl, de = shares(len(values))
+    _, lse, _, _, _ = ops.g10_log_probs(x, t, scale=scale)
+    got = ops.g10_log_probs_backward(dl, x, t, lse, scale=scale).double()
+    want = -dl.double()[:, None].expand(-1, vocab) / vocab * scale
+    want = want.scatter_add(1, t[:, None], dl.double()[:, None] * scale)
+    off = (K.additions(vocab) + 20 * math.log(vocab) + 60) * K.U32
+    assert ((got - want).abs() <= K.rounding(want.cpu(), dtype).cuda() + off * want.abs()).all()
+    both(ops, x, t, dl, None, scale)
+    both(ops, x, t, dl, de, scale)
+
+
+@pytest.mark.parametrize("offset", [0.0, 40.0, 70.0, -3e3, 1e4, 1e6, -3e7])
+@pytest.mark.parametrize("vocab", [300, 5003, 30522, 100001])
+def test_gradients_with_a_common_offset(ops, vocab, offset):
+    x = (torch.randn(6, vocab, generator=torch.Generator().manual_seed(vocab)) * 3 + offset).cuda()
+    t = torch.randint(0, vocab, (6,), generator=torch.Generator().manual_seed(1)).cuda()
+    for scale in (1.0, 0.7):
+        both(ops, x, t, *shares(6), scale)
+    if abs(offset) < 1e5:
+        both(ops, x.half(), t, *shares(6), 1.0)
+        both(ops, x.bfloat16(), t, *shares(6), 1.0)
+
+
+@pytest.mark.parametrize("scale", [0.25, 1.0, 1.25])
+@pytest.mark.parametrize("vocab", [40, 2050, 9000, 70000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradients_of_far_and_near_in_a_row(ops, dtype, vocab, scale):
+    x = mixed(dtype, vocab)
+    for at in (0, vocab // 2, vocab - 1):
+        t = torch.full((17,), at, device="cuda")
+        both(ops, x, t, shares(17)[0], None, scale)
+        both(ops, x, t, *shares(17), scale)
+
+
+@pytest.mark.parametrize("rows, vocab", [(1, 400000), (300, 70000), (2047, 16400), (2048, 16400)])
+def test_gradients_of_far_rows_in_parts_and_whole(ops, rows, vocab):
+    x = (torch.randn(rows, vocab, generator=torch.Generator().manual_seed(rows)) * 2).cuda()
+    x[::2] += 1e5
+    t = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(1)).cuda()
+    dl, de = shares(rows)
+    _, lse, ent, _, _ = ops.g10_log_probs(x, t, entropy=True)
+    got = ops.g10_log_probs_backward(dl, x, t, lse, de, ent)
+    for a in range(0, rows, 64):                                                             # (64 bits of them all are 1 GB)
+        at = slice(a, min(a + 8, rows))
+        K.check(dict(dlogits=got[at]), K.log_probs(x[at], t[at], 1.0, dlogp=dl[at], dentropy=de[at], near=64.0)[0])
+
+
+@pytest.mark.parametrize("rows, vocab", [(3, 40), (2, 100000), (40, 20001), (600, 9000)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_over_the_logits(ops, rows, vocab, dtype):
+    """Far rows and near ones, written where the logits lay: a row is summed again from logits, not from gradients."""
+    import ctypes as C
+    x = (torch.randn(rows, vocab, generator=torch.Generator().manual_seed(rows)) * 2).to(dtype).cuda()
+    x[::2] += 3e4
+    t = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(1)).cuda()
+    dl, de = shares(rows)
+    _, lse, ent, _, _ = ops.g10_log_probs(x, t, entropy=True)
+    want, z = K.log_probs(x, t, 1.0, dlogp=dl, dentropy=de, near=NEAR[dtype])[0], x.clone()
+    q = ops._LogProbs(logits=z.data_ptr(), tokens=t.data_ptr(), lse=lse.data_ptr(), entropy=ent.data_ptr(), dlogp=dl.data_ptr(), dentropy=de.data_ptr(), dlogits=z.data_ptr(),
+                      logits_stride=vocab, dlogits_stride=vocab, rows=rows, vocab=vocab, scale=1.0, ignore=-100, type=ops._TYPE[dtype])
+    assert ops._load().g10_log_probs_backward(C.byref(q), torch.cuda.current_stream().cuda_stream) == 0
+    K.check(dict(dlogits=z), want)
