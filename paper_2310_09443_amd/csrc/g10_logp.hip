@@ -425,9 +425,9 @@ __global__ __launch_bounds__(256) void k_logp_join(const LogpArgs a) {
 template <class T> struct Near { static constexpr float LSE = sizeof(T) == 4 ? 64.0f : 256.0f; };
 
 // A whole row's largest logit and the logarithm of its sum once more, in all threads (rows without NaN and +infinity).
-template <class T, int NT>
+template <class T>
 __device__ __forceinline__ Found again(const LogpArgs& a, u64 row) {
-  constexpr u32 W = NT / 64, N = Row<T>::N;
+  constexpr u32 NT = 256, W = NT / 64, N = Row<T>::N;
   __shared__ float room[2][W];
   const Row<T> r((const T*)a.logits + (int64_t)row * a.ls, a.vocab);
   float m = LOGP_NEG_INF, s = 0.0f;
@@ -471,18 +471,16 @@ __device__ __forceinline__ Found again(const LogpArgs& a, u64 row) {
 }
 
 // The gradient of a row: p (c0 + c1 log p), c0 = - (dlogp + dentropy entropy), c1 = - dentropy, and dlogp at the token.  Few rows are cut into parts.
-// log p = scale (x - from) - off: from lse, or where that lies too far from zero from the row's largest logit and its sum, for which each workgroup reads the
-// row (32768 x 32000 in bf16: 0.80 ms, 0.87 where all rows are such; in parts 2 x 194004 4 us and 18, 2047 x 152064 in fp32 0.48 ms and 1.74: each part
-// reads it).
-template <class T, int NT>
-__global__ __launch_bounds__(NT) void k_logp_back(const LogpArgs a, u32 vec) {
-  constexpr u32 N = Row<T>::N;
+// log p = scale (x - from) - off: from lse, or where that lies too far from zero from the row's largest logit and its sum, for which the row is read once more
+// (32768 x 32000 in bf16: 0.80 ms, 0.87 where all rows are such).  Each of a row's parts reads it, or with `whole` the first part does the row's work alone.
+template <class T>
+__global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec, u32 whole) {
+  constexpr u32 NT = 256, N = Row<T>::N;
   typedef typename Row<T>::V V;
   for (u64 b = blockIdx.x; b < (u64)a.rows * a.parts; b += gridDim.x) {
-    const u64 row = b / a.parts;
-    const u32 first = (u32)(b % a.parts) * a.each, count = a.vocab - first < a.each ? a.vocab - first : a.each;
-    const Row<T> r((const T*)a.logits + (int64_t)row * a.ls + first, count);
-    T* out = (T*)a.dlogits + (int64_t)row * a.ds + first;
+    const u64 row = b % a.rows;                                       // (all rows' first parts go ahead, and are on all XCDs)
+    const u32 first = (u32)(b / a.rows) * a.each;
+    u32 count = a.vocab - first < a.each ? a.vocab - first : a.each;
     const float lse = a.lse[row];
     float dl = a.tokens && a.dlogp ? a.dlogp[row] : 0.0f;
     const float de = a.dentropy ? a.dentropy[row] : 0.0f;
@@ -491,16 +489,22 @@ __global__ __launch_bounds__(NT) void k_logp_back(const LogpArgs a, u32 vec) {
       if (t == a.ignore) { dl = 0.0f; t = -1; }
       else if (t < 0 || t >= (int64_t)a.vocab) { dl = __builtin_nanf(""); t = -1; }
     }
-    t -= first;                                                       // (its place in this part, or outside it)
     const float c0 = -(dl + (a.dentropy ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = -de * a.scale, hit = dl * a.scale;
     bool zero = c0 == 0.0f && c1 == 0.0f && hit == 0.0f;              // (nothing of the row counts: it is not read)
     float from = 0.0f, off = lse;
     if (!zero && fabsf(lse) >= Near<T>::LSE) {
-      const Found found = again<T, NT>(a, row);
+      if (whole) {
+        if (first) continue;
+        count = a.vocab;
+      }
+      const Found found = again<T>(a, row);
       zero = found.top == LOGP_NEG_INF;                               // (a row without any probability)
       from = found.top;
       off = found.log * LOGP_LN2;
     }
+    t -= first;                                                       // (its place in this part, or outside it)
+    const Row<T> r((const T*)a.logits + (int64_t)row * a.ls + first, count);
+    T* out = (T*)a.dlogits + (int64_t)row * a.ds + first;
     auto grad = [&](float x, u32 place) {
       const float lp = __builtin_fmaf(x - from, a.scale, -off);       // -infinity where there is no probability
       const float p = __builtin_amdgcn_exp2f(lp * LOGP_LOG2E);
@@ -564,13 +568,8 @@ static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
     a.each = ((a.vocab + a.parts - 1) / a.parts + 63) / 64 * 64;
     a.parts = (a.vocab + a.each - 1) / a.each;
   }
-  // Gradients of few long rows: parts of 8192 logits (2 rows of 194004: 32 us on a unit each, so 4).  Each part may have to read its whole row, so there are no more
-  // than 16384 in all (2047 rows of 152064 in 32 bits: 478 us with 19 parts to a row or with 8, with 2 500), nor than read 2^34 logits.  Written over the
-  // logits a row stays whole: a part would read what another has written.
-  if (back && a.rows && a.rows < 2048 && a.vocab > 8192 && a.logits != a.dlogits) {
-    const u64 room = (1ull << 34) / a.vocab;
-    const u32 all = (u32)(room < 16384 ? room : 16384), most = all / a.rows ? all / a.rows : 1, parts = (a.vocab + 8191) / 8192;
-    a.each = parts <= most ? 8192 : ((a.vocab + most - 1) / most + 63) / 64 * 64;
+  if (back && a.rows && a.rows < 2048 && a.vocab > 8192) {             // (2 rows of 194004: 32 us on a unit each, so 4)
+    a.each = 8192;
     a.parts = (a.vocab + a.each - 1) / a.each;
   }
   return G10_OK;
@@ -638,10 +637,12 @@ extern "C" int g10_log_probs_backward(const g10_log_probs_args* g, void* hip_str
   const u32 grid = (u32)(groups < 1u << 16 ? groups : 1u << 16), e = g->type == G10_F32 ? 4 : 2;
   // (rows of both tensors lie alike within 16 bytes)
   const u32 vec = !(((uintptr_t)g->logits ^ (uintptr_t)g->dlogits) & 15) && ((g->logits_stride - g->dlogits_stride) * (int64_t)e) % 16 == 0;
-  const bool wide = a.parts == 1 && a.rows <= 512 && a.vocab > 8192;   // (few long rows over their logits: 1024 threads each)
-  if (g->type == G10_F32) { if (wide) k_logp_back<float, 1024><<<grid, 1024, 0, s>>>(a, vec); else k_logp_back<float, 256><<<grid, 256, 0, s>>>(a, vec); }
-  else if (g->type == G10_F16) { if (wide) k_logp_back<_Float16, 1024><<<grid, 1024, 0, s>>>(a, vec); else k_logp_back<_Float16, 256><<<grid, 256, 0, s>>>(a, vec); }
-  else { if (wide) k_logp_back<__bf16, 1024><<<grid, 1024, 0, s>>>(a, vec); else k_logp_back<__bf16, 256><<<grid, 256, 0, s>>>(a, vec); }
+  // Written over the logits a row that is summed again stays with one workgroup: a part would read what another has written.  So it does where there are
+  // workgroups enough (all rows such, read by each part and by one: 2 x 194004 18 us and 49, 32 x 100000 19 and 28, 64 x 200000 85 and 55, 2047 x 32000 113 and 63).
+  const u32 whole = a.parts > 1 && (g->logits == g->dlogits || groups > 1024);
+  if (g->type == G10_F32) k_logp_back<float><<<grid, 256, 0, s>>>(a, vec, whole);
+  else if (g->type == G10_F16) k_logp_back<_Float16><<<grid, 256, 0, s>>>(a, vec, whole);
+  else k_logp_back<__bf16><<<grid, 256, 0, s>>>(a, vec, whole);
   G10_HIP(hipGetLastError());
   return G10_OK;
 }
