@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec, u3
       if (t == a.ignore) { dl = 0.0f; t = -1; }
       else if (t < 0 || t >= (int64_t)a.vocab) { dl = __builtin_nanf(""); t = -1; }
     }
-    const float c0 = -(dl + (a.dentropy ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = -de * a.scale, hit = dl * a.scale;
+    const float c0 = -(dl + (de != 0.0f ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = -de * a.scale, hit = dl * a.scale;
     bool zero = c0 == 0.0f && c1 == 0.0f && hit == 0.0f;              // (nothing of the row counts: it is not read)
     float from = 0.0f, off = lse;
     if (!zero && fabsf(lse) >= Near<T>::LSE) {
