@@ -198,8 +198,8 @@ int g10_norm_backward(const g10_norm_args *args, void *workspace, uint64_t works
  * Of every row z = scale * logits:   lse = log sum_j exp z_j,   p_j = exp(z_j - lse),   logp = z_t - lse for the row's token t,
  *   entropy = - sum p_j log p_j,   and the `top` largest z_j - lse with their places, ties in order of the places.
  * dlogits_j = scale * (dlogp ([j = t] - p_j) - dentropy p_j (log p_j + entropy)).
- * A token equal to `ignore` has logp = 0 and no share in the gradient; any other one outside the row makes logp, and the row's
- * gradient, NaN.  Places of -infinity have no probability; a row of nothing else has lse = logp = -infinity, entropy 0 and no gradient.
+ * A token equal to `ignore` has logp = 0 and no share in the gradient; any other one outside the row makes logp NaN, and the row's
+ * gradient too where dlogp is given and not 0.  Places of -infinity have no probability; a row of nothing else has lse = logp = -infinity, entropy 0 and no gradient.
  * Sums, logp, top_logp, entropy and the gradient go by distances from the row's largest logit and are as exact for a row with a large offset, or at the type's end,
  * as for one around zero; lse is rounded to 32 bits where it lies, and infinite where scale * logits are beyond them.  Where it is 64 or more (16-bit logits: 256),
  * either side of zero, the backward pass sums the row again.

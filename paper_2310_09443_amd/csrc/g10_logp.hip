@@ -487,7 +487,7 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec, u3
     int64_t t = a.tokens ? ((const int64_t*)a.tokens)[row] : -1;
     if (a.tokens) {
       if (t == a.ignore) { dl = 0.0f; t = -1; }
-      else if (t < 0 || t >= (int64_t)a.vocab) { dl = __builtin_nanf(""); t = -1; }
+      else if (t < 0 || t >= (int64_t)a.vocab) { dl = dl != 0.0f ? __builtin_nanf("") : 0.0f; t = -1; }
     }
     const float c0 = -(dl + (de != 0.0f ? de * a.entropy[row] : 0.0f)) * a.scale, c1 = -de * a.scale, hit = dl * a.scale;
     bool zero = c0 == 0.0f && c1 == 0.0f && hit == 0.0f;              // (nothing of the row counts: it is not read)

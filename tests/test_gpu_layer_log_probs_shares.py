@@ -42,3 +42,24 @@ def test_no_share_of_entropy_in_rows_that_have_none(ops, dtype, vocab):
     logp, ent = ops.log_probs(leaf, t, entropy=True)
     logp[1:2].sum().backward()                                                               # a loss of one row, whose token does not count
     assert not leaf.grad.any()
+
+
+@pytest.mark.parametrize("vocab", [60, 3001, 70000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tokens_outside_the_row_that_have_no_share(ops, dtype, vocab):
+    """Such a token's logp is NaN, and so is its row's gradient, but not where logp has no share in the loss."""
+    x, t, dl, de = make(6, vocab, dtype)
+    t[0], t[1], t[2], t[3] = vocab, -1, 2 ** 40, -(2 ** 40)
+    dl[0], de[0], dl[1], dl[4] = 0.0, 0.0, 0.0, 0.0                                          # no share at all; none of logp; (the last: nor a token outside)
+    _, lse, ent, _, _ = ops.g10_log_probs(x, t, entropy=True)
+    for d2 in (de, None):
+        g = ops.g10_log_probs_backward(dl, x, t, lse, d2, ent)
+        assert not g[0].any() and g[2:4].isnan().all()
+        K.check(dict(dlogits=g), K.log_probs(x, t, 1.0, dlogp=dl, dentropy=d2, near=64.0)[0])
+    with_tokens, without = (ops.g10_log_probs_backward(None, x, t1, lse, de, ent) for t1 in (t, None))
+    assert torch.equal(with_tokens, without)                                                 # nothing of logp: the tokens do not matter
+    K.check(dict(dlogits=without), K.log_probs(x, None, 1.0, dentropy=de, near=64.0)[0])
+    leaf = x.clone().requires_grad_()
+    logp, ent = ops.log_probs(leaf, t, entropy=True)
+    (ent * de).sum().backward()
+    assert torch.equal(leaf.grad, without)
