@@ -218,7 +218,7 @@ typedef struct {
   int64_t logits_stride, dlogits_stride; /* of rows                                             */
   uint32_t rows, vocab;      /* vocab 1 .. 2^31 - 1                                            */
   uint32_t top;              /* 0 .. G10_LOG_PROBS_TOP, at most vocab                          */
-  float scale;               /* > 0                                                            */
+  float scale;               /* above 0, up to 2e38                                            */
   int64_t ignore;
   uint32_t type;             /* of logits and dlogits: G10_F32, G10_F16, G10_BF16              */
 } g10_log_probs_args;

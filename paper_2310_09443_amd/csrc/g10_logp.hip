@@ -35,6 +35,7 @@ struct Part { float top, top2, s, t; };   // the largest logit, the same in powe
 #define LOGP_LN2 0.6931471805599453f
 #define LOGP_NEG_INF (-__builtin_inff())
 #define LOGP_ROOM 1024u            // candidates of a row
+#define LOGP_SCALE 2e38f           // (in powers of two still a number)
 #define LOGP_NAN 0xfffffffeu
 
 // A product that is 0 where p is, whatever x is (v_mul_legacy_f32, which the compiler knows by this name only).
@@ -542,7 +543,7 @@ __global__ __launch_bounds__(256) void k_logp_back(const LogpArgs a, u32 vec, u3
 // ---------------------------------------------------------------------------------------------------------------------
 static int logp_args(const g10_log_probs_args* g, bool back, LogpArgs& a) {
   if (!g) return G10_EINVAL;
-  if (g->type > G10_BF16 || !(g->scale > 0.0f) || isinf(g->scale) || !g->vocab || g->vocab >= 0x80000000u || g->rows >= 0x80000000u) return G10_EINVAL;
+  if (g->type > G10_BF16 || !(g->scale > 0.0f) || !(g->scale <= LOGP_SCALE) || !g->vocab || g->vocab >= 0x80000000u || g->rows >= 0x80000000u) return G10_EINVAL;
   const u32 e = g->type == G10_F32 ? 4 : 2;
   if ((uintptr_t)g->logits % e || (uintptr_t)g->dlogits % e || (uintptr_t)g->tokens % 8) return G10_EINVAL;
   if (g->rows && (!g->logits || !g->lse)) return G10_EINVAL;

@@ -168,7 +168,7 @@ static void log_probs_args(LogProbsCall& c, const at::Tensor& logits, const Mayb
   const at::ScalarType dt = float_type(logits, "logits");
   c.dev = logits.device();
   c.lead = logits.sizes().slice(0, logits.dim() - 1).vec();
-  TORCH_CHECK_VALUE(scale > 0 && scale < 3e38, "scale must be above zero");
+  TORCH_CHECK_VALUE(scale > 0 && scale <= 2e38, "scale must be above zero, up to 2e38");
   TORCH_CHECK_VALUE(logits.size(-1) < 0x80000000ll && logits.numel() / logits.size(-1) < 0x80000000ll, "too many rows or logits in one");
   c.logits = rows_of(logits);
   g10_log_probs_args& a = c.a;
