@@ -70,12 +70,14 @@ class Decoder:
         return ops.norm(x, top["out_norm"]) @ top["head"]
 
     def step(self, ids, max_norm=1.0):
-        """One training step on [batch, token + 1]; returns (loss, norm of the gradients), device tensors."""
+        """One training step on [batch, token + 1]; returns (loss, norm of the gradients), device tensors.  The loss is the mean over the targets that are
+        not -100."""
         torch = self.torch
         for w in self.layers:
             for t in w.values():
                 t.grad = None
-        loss = -self.ops.log_probs(self.logits(ids[:, :-1]), ids[:, 1:]).mean()
+        targets = ids[:, 1:]
+        loss = -(self.ops.log_probs(self.logits(ids[:, :-1]), targets).sum() / (targets != -100).sum())
         loss.backward()
         grads = [[t.grad for t in w.values()] for w in self.layers]
         norm = torch.stack([o.grad_norm(g) for o, g in zip(self.opts, grads)]).square().sum().sqrt()
