@@ -29,7 +29,7 @@ class Decoder:
         import torch
         from . import ops
         self.ops, self.torch = ops, torch
-        self.dim, self.heads, self.kv, self.window, self.sinks, self.device = dim, heads, kv_heads, window, sinks, device
+        self.vocab, self.dim, self.heads, self.kv, self.window, self.sinks, self.device = vocab, dim, heads, kv_heads, window, sinks, device
         gen = torch.Generator().manual_seed(seed)
         D = self.HEAD
 
@@ -57,8 +57,23 @@ class Decoder:
     def _mlp(self, w, x):
         return x + self.ops.gated(self.ops.norm(x, w["norm2"]), w["gate"], w["up"]) @ w["down"]
 
+    def _rows(self, ids, targets=None):
+        """The ids as rows of the table: from -vocab on they count from its end, as indices do.  Others raise, as do targets that are neither rows nor -100;
+        the host waits for them.  Under capture nothing can be waited for: there an id outside the table makes its token's outputs NaN."""
+        torch, n = self.torch, self.vocab
+        if not ids.numel() or (ids.is_cuda and torch.cuda.is_current_stream_capturing()):
+            return ids
+        ends = ids.aminmax() if targets is None else ids.aminmax() + torch.where(targets == -100, 0, targets).aminmax()
+        least, most, *rest = torch.stack(ends).tolist()
+        if least < -n or most >= n or (rest and (rest[0] < 0 or rest[1] >= n)):
+            raise ValueError(f"ids or targets outside the vocabulary of {n}")
+        return ids % n if least < 0 else ids
+
     def logits(self, ids):
-        """[batch, token] -> [batch, token, vocab], differentiable."""
+        """[batch, token] -> [batch, token, vocab], differentiable.  An id outside the vocabulary raises ValueError."""
+        return self._logits(self._rows(ids))
+
+    def _logits(self, ids):
         torch, ops, top = self.torch, self.ops, self.layers[0]
         pos = torch.arange(ids.shape[1], device=self.device, dtype=torch.int32).expand(ids.shape)
         x = ops.embed(ids, top["embed"])
@@ -72,12 +87,12 @@ class Decoder:
     def step(self, ids, max_norm=1.0):
         """One training step on [batch, token + 1]; returns (loss, norm of the gradients), device tensors.  The loss is the mean over the targets that are
         not -100."""
-        torch = self.torch
+        torch, targets = self.torch, ids[:, 1:]
+        rows = self._rows(ids[:, :-1], targets)
         for w in self.layers:
             for t in w.values():
                 t.grad = None
-        targets = ids[:, 1:]
-        loss = -(self.ops.log_probs(self.logits(ids[:, :-1]), targets).sum() / (targets != -100).sum())
+        loss = -(self.ops.log_probs(self._logits(rows), targets).sum() / (targets != -100).sum())
         loss.backward()
         grads = [[t.grad for t in w.values()] for w in self.layers]
         norm = torch.stack([o.grad_norm(g) for o, g in zip(self.opts, grads)]).square().sum().sqrt()
@@ -93,7 +108,7 @@ class Decoder:
             b, s = ids.shape
             room = s + n
             caches = [[torch.zeros(b, room, self.kv, self.HEAD, dtype=torch.bfloat16, device=self.device) for _ in range(2)] for _ in self.layers[1:]]
-            at, new = 0, ids
+            at, new = 0, self._rows(ids)
             for _ in range(n):
                 m = new.shape[1]
                 pos = torch.arange(at, at + m, device=self.device, dtype=torch.int32).expand(b, m)
