@@ -61,6 +61,7 @@ class Decoder:
         """The ids as rows of the table: from -vocab on they count from its end, as indices do.  Others raise, as do targets that are neither rows nor -100;
         the host waits for them.  Under capture nothing can be waited for: there an id outside the table makes its token's outputs NaN."""
         torch, n = self.torch, self.vocab
+        ids = ids.to(self.device)
         if not ids.numel() or (ids.is_cuda and torch.cuda.is_current_stream_capturing()):
             return ids
         ends = ids.aminmax() if targets is None else ids.aminmax() + torch.where(targets == -100, 0, targets).aminmax()

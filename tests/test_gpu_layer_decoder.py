@@ -77,3 +77,8 @@ def test_logits_in_a_graph(model):
             assert torch.equal(out, w)
             model.logits(ids(7))
             torch.cuda.synchronize()
+
+
+def test_logits_of_ids_in_host_memory(model):
+    x = ids(8)
+    assert torch.equal(model.logits(x.cpu()), model.logits(x))
