@@ -358,6 +358,7 @@ class _LogProbsFn(torch.autograd.Function):
 def log_probs(logits, tokens, entropy=False, scale=1.0, ignore=-100):
     """g10_log_probs's logp, or (logp, entropy), differentiable in the logits.  What is kept for the backward pass: the logits and a number or two a
     row; a loss is `-log_probs(logits, tokens).sum() / n`."""
+    _need(tokens is not None or entropy, "tokens or entropy is needed")
     return _LogProbsFn.apply(logits, tokens, bool(entropy), float(scale), int(ignore))
 
 
