@@ -177,7 +177,8 @@ int g10_embed_backward(const g10_embed_args *args, void *workspace, uint64_t wor
  *   n = (x - m) r;   y = n * weight + bias.
  * Backward, from x and dy alone, with u = dy * weight:   dx = r (u - n mean(u n) - [center] mean(u)),
  *   dweight = sum of dy n,  dbias = sum of dy  over the rows.
- * Row sums in 32 bits (the squares of what is left after the mean is taken off), sums over rows in 32 and joined in 64. */
+ * Row sums in 32 bits (the squares of what is left after the mean is taken off), sums over rows in 32 and joined in 64.  Squares that add up
+ * beyond 32 bits (values of 1.8e19) make a row's n zero. */
 typedef struct {
   const void *x, *dy;        /* [rows][dim]; dy: backward                                      */
   const void *weight, *bias; /* [dim] of weight_type, or NULL                                  */
@@ -232,7 +233,8 @@ int g10_log_probs_backward(const g10_log_probs_args *args, void *hip_stream);
  * distribution's Phi.  Backward, from x, the weights and dh alone (g and u are computed again):
  *   dg = dh u act'(g),   du = dh act(g),   dx = dg gate^T + du up^T,   dgate = x^T dg,   dup = x^T du.
  * Products of 16-bit factors summed in 32 bits; dg and du are rounded to `type` before their products (the matrix unit takes 16-bit
- * factors), h and the gradients once at their end. */
+ * factors), h and the gradients once at their end.  In G10_F16 a dg or du above 65504 is infinite from there on, and one below 6e-5 has fewer bits:
+ * dh is scaled so that they lie between. */
 #define G10_ACT_SILU 0u
 #define G10_ACT_GELU 1u
 
@@ -249,7 +251,9 @@ typedef struct {
   uint32_t type;             /* G10_F16 or G10_BF16                                            */
 } g10_gated_args;
 /* Inputs whose pointers and strides are multiples of 16 bytes (of 8 elements) and whose rows are multiples of 8 elements, with strides up to 2^22 and
- * one stride for both weights, are read where they lie; others are laid out in the workspace first.  Outputs may lie anywhere. */
+ * one stride for both weights, are read where they lie; others are laid out in the workspace first.  Outputs may lie anywhere.
+ * A product is cut into tiles of 64 to 256 rows by 64 to 256 columns, and its sum into up to 32 shares; one of more than 2^23 tiles and shares
+ * altogether is refused (2^20 inner values: from some 2^18 tokens on), by the call, not by the workspace's. */
 
 int g10_gated_workspace(const g10_gated_args *args, uint64_t *bytes);
 int g10_gated(const g10_gated_args *args, void *workspace, uint64_t workspace_bytes, void *hip_stream);

@@ -5,7 +5,9 @@
 // that the statistics are taken from the values themselves: the mean first, then the squares of what is left (the squares' mean less the
 // mean's square would lose what a large mean leaves over).  Backward the statistics are worked out again from x, which has to be read in
 // any case.  The gradients of weight and bias are sums over rows: a lane keeps its columns' over all rows that its group takes, and the
-// groups' sums are joined in one order and 64 bits by a second kernel.
+// groups' sums are joined in one order and 64 bits by a second kernel.  Backward a row's four arrays of values do not fit the 128 registers that 1024 threads have
+// from 8193 values on (36 to 96 bytes of scratch a lane in whole rows of up to 16384 values in bf16 and fp32, 0.15 to 1.4 KB above; forward from 16385 in
+// rows that are no multiple of 8, from 32769 in all): 8192 rows of 12288 in bf16 62 us forward and 131 backward, 5033 of 20000 79 and 306.
 #include "g10_internal.h"
 #include "g10_ops.h"
 

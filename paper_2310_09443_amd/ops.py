@@ -10,8 +10,9 @@
 
 All but AdamW are differentiable; the g10_* functions beside them are the forward and backward calls
 themselves.  Work is enqueued on the current stream of the tensors' device and not waited for; outputs and workspaces are
-torch's, allocated on that stream.  What the library would refuse raises ValueError, before anything is launched.  The
-marshalling is C++ (csrc/g10_torch.cpp): in Python it would take longer than the kernels of a small step.
+torch's, allocated on that stream.  What the library would refuse raises ValueError, before anything is launched.  Rows that no one
+stride describes are copied first: `logits[:, :-1]` of [batch, token, vocab] is (shift the tokens instead, or leave the last one out before the
+logits are made).  The marshalling is C++ (csrc/g10_torch.cpp): in Python it would take longer than the kernels of a small step.
 """
 from __future__ import annotations
 
@@ -302,7 +303,8 @@ def g10_gated(x, gate, up, act="silu"):
 
 def g10_gated_backward(dh, x, gate, up, act="silu"):
     """Gradients (dx, dgate, dup) from that of g10_gated's output; the weights' lie as the weights do.  Both products of the forward pass are
-    made again.  Needs room for the gradients of both products, in x's type."""
+    made again.  Needs room for the gradients of both products, in x's type: in float16 one of them above 65504 is infinite from there on, and one below
+    6e-5 has fewer bits.  All three gradients are made, whichever of the inputs need one."""
     return _calls().gated_backward(dh, x, gate, up, act)
 
 
